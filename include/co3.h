@@ -347,6 +347,76 @@ int co3_decode(const uint8_t* stream_in, size_t stream_bytes,
                void* workspace, size_t workspace_bytes, co3_result* res, void* stream);
 
 /*
+ * Orthogonalised updates (no counterpart in the paper, whose server step is w <- w - lr * avg: this is the step of the
+ * Muon optimiser for the weight matrices of a model).  A gradient G of a layer with `rows` outputs and `cols` inputs (a
+ * convolution: cols = input channels x kernel size) is replaced by the nearest semi-orthogonal matrix, approximated
+ * by Newton-Schulz steps with an odd quintic: with m = min(rows, cols), G transposed first if rows > cols,
+ *     X_0 = G / (||G||_F + eps);   A = X X^T,  X <- a X + (b A + c A A) X  for every step;   result = scale * X.
+ * A singular value s of X becomes a s + b s^3 + c s^5 in each step.  All matrices of a call are worked on together.
+ */
+#define CO3_F32 0 /* element types of buffers that may be other than fp32 */
+#define CO3_F16 1
+#define CO3_BF16 2
+
+#define CO3_MAT_PLAIN 1u /* co3_muon_update: no orthogonalisation, the momentum itself is the update (vectors, biases) */
+
+/* Where a matrix lies: entry (r, c) is element offset + r * row_stride + c of its buffer.  Matrices of one call must
+ * not overlap.  rows == 0 or cols == 0: nothing to do for this one. */
+typedef struct {
+    uint64_t offset;
+    uint64_t row_stride; /* >= cols */
+    uint32_t rows, cols; /* each < 2^31, rows * cols < 2^40 */
+    float scale;         /* factor of the result */
+    uint32_t flags;      /* 0 or CO3_MAT_PLAIN */
+} co3_mat;
+
+#define CO3_NS_MAX_STEPS 16
+
+/* Steps of the iteration; coef[k] = {a, b, c} of step k.  Refused (CO3_ERR_INVALID_ARG) if steps is not in
+ * 1..CO3_NS_MAX_STEPS, eps is negative or not finite, or some singular value in [0, 1] leaves [-2, 2] on the way or
+ * meets |b s^2 + c s^4| > 4 (the products are formed from scaled half-precision pairs, which hold that range). */
+typedef struct {
+    uint32_t steps;
+    float eps;
+    float coef[CO3_NS_MAX_STEPS][3];
+} co3_ns;
+
+/* The iteration used where `ns` is NULL: 5 steps of (3.4445, -4.7750, 2.0315), eps 1e-7.  It takes singular values
+ * from about 0.002 up to within [0.68, 1.14]. */
+int co3_ns_default(co3_ns* out /* [host] */);
+
+/* Device workspace of the two calls below for these matrices. */
+int co3_orthogonalize_workspace_bytes(const co3_mat* mats /* [host] */, uint32_t n_mats, size_t* out /* [host] */);
+
+/*
+ * out <- scale * orthogonalised in, matrix by matrix.
+ *   in, out [device]    buffers of in_type / out_type (CO3_F32, CO3_F16, CO3_BF16), aligned to their element size;
+ *                       they may be the same buffer with the same layout and type
+ *   in_mats, out_mats   [host] n_mats layouts, read before the call returns; rows and cols have to agree; out_mats'
+ *                       scale and flags (0) count; out_mats may be NULL (same layout)
+ *   res [device]        one co3_result: CO3_ERR_NONFINITE if a matrix holds a NaN or an infinity (its result is NaN;
+ *                       n_nonfinite counts such matrices, first_bad_chunk is the first); CO3_ERR_CUDA as elsewhere
+ * Inputs of any magnitude are handled (the norm is formed in fp64).  Products run on the tensor cores from pairs of
+ * fp16 values that hold 22 significant bits, accumulated in fp32.
+ */
+int co3_orthogonalize(const void* in, int in_type, const co3_mat* in_mats, void* out, int out_type,
+                      const co3_mat* out_mats, uint32_t n_mats, const co3_ns* ns /* [host], nullable */, co3_result* res,
+                      void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The server's whole step on an averaged gradient (co3_decode_aggregate's avg_out), per listed layer:
+ *     buf <- mu * buf + g;   u = nesterov ? g + mu * buf : buf;
+ *     w <- (1 - lr * weight_decay) * w - lr * scale * (CO3_MAT_PLAIN ? u : orthogonalised u)
+ *   grad [device] fp32, read only;  momentum, params [device] fp32, updated in place; one layout for the three
+ * Elements outside the listed layers stay as they are.  res as above; a layer that holds a NaN or an infinity gets
+ * NaN parameters, as the formula has it.
+ */
+int co3_muon_update(const float* grad, float* momentum, float* params, const co3_mat* mats /* [host] */,
+                    uint32_t n_mats, float mu, int nesterov, float lr, float weight_decay,
+                    const co3_ns* ns /* [host], nullable */, co3_result* res, void* workspace, size_t workspace_bytes,
+                    void* stream);
+
+/*
  * Diagnostics (no counterpart in the paper).  With profiling enabled every kernel launched by the
  * entry points above is bracketed by a CUDA event pair on the caller's stream; co3_profile_read
  * waits for those events, adds up the elapsed time and the number of launches per kernel kind

@@ -22,6 +22,13 @@ RESULT_DTYPE = np.dtype([("status", np.int32), ("first_bad_chunk", np.uint32), (
                          ("container_bytes", np.uint64), ("n_saturated", np.uint64), ("n_nonfinite", np.uint64)])
 assert FMT_DTYPE.itemsize == 12 and CODE_DTYPE.itemsize == 768 and SEG_DTYPE.itemsize == 16
 assert RESULT_DTYPE.itemsize == 40
+MAT_DTYPE = np.dtype([("offset", np.uint64), ("row_stride", np.uint64), ("rows", np.uint32), ("cols", np.uint32),
+                      ("scale", np.float32), ("flags", np.uint32)])
+MAT_PLAIN = 1
+NS_MAX_STEPS = 16
+NS_DTYPE = np.dtype([("steps", np.uint32), ("eps", np.float32), ("coef", np.float32, (NS_MAX_STEPS, 3))])
+assert MAT_DTYPE.itemsize == 32 and NS_DTYPE.itemsize == 8 + 12 * NS_MAX_STEPS
+_TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 
 _lib = None
 
@@ -59,9 +66,13 @@ def _load():
     L.co3_decode_aggregate.argtypes = [vp, sz, u32, vp, vp, vp, u32, u64, u32, vp, vp, sz, vp, vp]
     L.co3_decode_aggregate_update.argtypes = [vp, sz, u32, vp, vp, vp, u32, u64, u32, f32, vp, vp, vp, sz, vp, vp]
     L.co3_decode.argtypes = [vp, sz, vp, vp, vp, u32, u64, u32, vp, vp, vp, sz, vp, vp]
+    L.co3_ns_default.argtypes = [vp]
+    L.co3_orthogonalize_workspace_bytes.argtypes = [vp, u32, C.POINTER(sz)]
+    L.co3_orthogonalize.argtypes = [vp, C.c_int, vp, vp, C.c_int, vp, u32, vp, vp, vp, sz, vp]
+    L.co3_muon_update.argtypes = [vp, vp, vp, vp, u32, f32, C.c_int, f32, f32, vp, vp, vp, sz, vp]
     L.co3_profile_enable.argtypes = [C.c_int]
     L.co3_profile_read.argtypes = [vp, vp]
-    for name in ("co3_histogram", "co3_convert_dither", "co3_histogram_dither", "co3_encode_dither", "co3_error_magnitude", "co3_model_weights", "co3_fit_scale", "co3_profile_enable", "co3_profile_read", "co3_convert_static", "co3_workspace_bytes", "co3_stream_capacity_bytes", "co3_convert", "co3_code_build", "co3_code_build_device", "co3_encode",
+    for name in ("co3_ns_default", "co3_orthogonalize_workspace_bytes", "co3_orthogonalize", "co3_muon_update", "co3_histogram", "co3_convert_dither", "co3_histogram_dither", "co3_encode_dither", "co3_error_magnitude", "co3_model_weights", "co3_fit_scale", "co3_profile_enable", "co3_profile_read", "co3_convert_static", "co3_workspace_bytes", "co3_stream_capacity_bytes", "co3_convert", "co3_code_build", "co3_code_build_device", "co3_encode",
                  "co3_encode_symbols", "co3_decode_aggregate", "co3_decode_aggregate_update", "co3_decode"):
         getattr(L, name).restype = C.c_int
     _lib = L
@@ -101,6 +112,26 @@ def make_segs(sizes) -> np.ndarray:
     for k, n in enumerate(sizes):
         a[k] = (off, int(n))
         off += int(n)
+    return a
+
+
+def make_mats(mats) -> np.ndarray:
+    """co3_mat[n] from (offset, rows, cols[, row_stride[, scale[, flags]]]) tuples; row_stride defaults to cols,
+    scale to 1, flags to 0."""
+    a = np.zeros(len(mats), dtype=MAT_DTYPE)
+    for k, m in enumerate(mats):
+        offset, rows, cols, row_stride, scale, flags = (*m, *((m[2], 1.0, 0)[len(m) - 3:]))
+        a[k] = (offset, row_stride, rows, cols, scale, flags)
+    return a
+
+
+def make_ns(coef=None, steps: int = 5, eps: float = 1e-7) -> np.ndarray:
+    """co3_ns: coef is one (a, b, c) for every step or a list with one per step; None: the default coefficients."""
+    a = np.zeros(1, dtype=NS_DTYPE)
+    c = np.asarray((3.4445, -4.7750, 2.0315) if coef is None else coef, dtype=np.float32)
+    n = steps if c.ndim == 1 else len(c)
+    a["steps"], a["eps"] = n, eps
+    a["coef"][0, :min(n, NS_MAX_STEPS)] = c[:NS_MAX_STEPS] if c.ndim == 2 else c
     return a
 
 
@@ -270,6 +301,66 @@ def co3_decode(stream_in, stream_bytes, fmts, codes, segs, n_seg, n_elem, ghat_o
     return _load().co3_decode(_dev(stream_in), stream_bytes, _dev(fmts), _dev(codes), _dev(segs), n_seg, n_elem,
                               chunk_syms, _dev(ghat_out, True), _dev(sym_out, True), _dev(workspace),
                               workspace.numel() * workspace.element_size(), _dev(res), _stream(stream))
+
+
+def _mats(mats):
+    if not (isinstance(mats, np.ndarray) and mats.dtype == MAT_DTYPE and mats.flags.c_contiguous):
+        raise ValueError("expected the array make_mats returns")
+    return mats.ctypes.data, mats.size
+
+
+def _ns(ns):
+    if ns is None:
+        return None
+    if not (isinstance(ns, np.ndarray) and ns.dtype == NS_DTYPE and ns.size == 1):
+        raise ValueError("expected the array make_ns returns")
+    return ns.ctypes.data
+
+
+def _fits(mats, t, what) -> None:
+    """The library cannot see a buffer's length: every listed matrix has to end inside the tensor."""
+    used = mats[(mats["rows"] > 0) & (mats["cols"] > 0)]
+    if used.size:
+        ends = used["offset"].astype(object) + (used["rows"].astype(object) - 1) * used["row_stride"].astype(object) + used["cols"].astype(object)
+        if ends.max() > t.numel():
+            raise ValueError("%s: a matrix ends beyond the tensor" % what)
+
+
+def co3_orthogonalize_workspace_bytes(mats: np.ndarray) -> int:
+    """Device workspace of co3_orthogonalize / co3_muon_update for these matrices (as make_mats returns them)."""
+    out = C.c_size_t(0)
+    p, n = _mats(mats)
+    st = _load().co3_orthogonalize_workspace_bytes(p, n, C.byref(out))
+    if st != OK:
+        raise ValueError("co3_orthogonalize_workspace_bytes: " + co3_status_string(st))
+    return out.value
+
+
+def co3_orthogonalize(inp, in_mats, out, out_mats, workspace, res, ns=None, stream=None) -> int:
+    """out <- scale * orthogonalised inp for every listed matrix; contiguous fp32, fp16 or bf16 tensors of any shape
+    whose elements the layouts index (out_mats None: as in_mats)."""
+    p, n = _mats(in_mats)
+    q, nq = (None, n) if out_mats is None or out_mats is in_mats else _mats(out_mats)
+    if nq != n or inp.dtype not in _TYPES or out.dtype not in _TYPES:
+        raise ValueError("co3_orthogonalize: fp32, fp16 or bf16 tensors and as many layouts for out as for in")
+    _fits(in_mats, inp, "co3_orthogonalize")
+    _fits(in_mats if q is None else out_mats, out, "co3_orthogonalize")
+    return _load().co3_orthogonalize(_dev(inp), _TYPES[inp.dtype], p, _dev(out), _TYPES[out.dtype], q, n, _ns(ns),
+                                     _dev(res), _dev(workspace), workspace.numel() * workspace.element_size(),
+                                     _stream(stream))
+
+
+def co3_muon_update(grad, momentum, params, mats, mu, nesterov, lr, weight_decay, workspace, res, ns=None,
+                    stream=None) -> int:
+    """One server step on fp32 vectors: momentum, orthogonalisation of the matrices, weight decay and parameters."""
+    p, n = _mats(mats)
+    for t in (grad, momentum, params):
+        if t.dtype != torch.float32:
+            raise ValueError("co3_muon_update: fp32 tensors")
+        _fits(mats, t, "co3_muon_update")
+    return _load().co3_muon_update(_dev(grad), _dev(momentum), _dev(params), p, n, float(mu), 1 if nesterov else 0,
+                                   float(lr), float(weight_decay), _ns(ns), _dev(res), _dev(workspace),
+                                   workspace.numel() * workspace.element_size(), _stream(stream))
 
 
 KERNEL_NAMES = ("prepare", "convert", "pack", "scan", "compact", "code_build", "decode", "fit", "clear")

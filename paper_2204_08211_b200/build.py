@@ -6,14 +6,14 @@ import subprocess
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_PKG)
-SOURCES = [os.path.join(_PKG, "csrc", "co3_kernels.cu"), os.path.join(_PKG, "csrc", "co3_code_build.cc")]
-HEADERS = [os.path.join(_PKG, "csrc", "co3_device.cuh"), os.path.join(_ROOT, "include", "co3.h")]
+SOURCES = [os.path.join(_PKG, "csrc", f) for f in ("co3_kernels.cu", "co3_orth.cu", "co3_code_build.cc")]
+HEADERS = [os.path.join(_PKG, "csrc", f) for f in ("co3_device.cuh", "co3_launch.cuh")] + [os.path.join(_ROOT, "include", "co3.h")]
 LIB = os.path.join(_PKG, "libco3.so")
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
     "-fmad=false",            # products and sums are written with explicit intrinsics; never contract
-    "-Xcompiler", "-fPIC", "-shared",
+    "-Xcompiler", "-fPIC", "-shared", "--threads", "0",
 ]
 
 

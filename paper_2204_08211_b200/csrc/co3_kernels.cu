@@ -16,6 +16,7 @@
 
 #include "co3.h"
 #include "co3_device.cuh"
+#include "co3_launch.cuh"
 
 namespace co3 {
 
@@ -2508,11 +2509,6 @@ uint64_t fixed_part_bound(uint32_t n_seg, uint64_t n_chunks_max) {
     return o;
 }
 
-#define CO3_CUDA(call)                                  \
-    do {                                                \
-        if ((call) != cudaSuccess) return CO3_ERR_CUDA; \
-    } while (0)
-
 // Blocks of a persistent kernel: enough to fill every SM at the kernel's occupancy, never more than the work.
 // grouped: items are handed out four consecutive ones at a time when that still leaves every block many groups
 // (the kernels with private histograms, which flush them when the layer changes; the others balance better one by one).
@@ -2532,8 +2528,6 @@ int persistent_grid(Kernel kernel, int threads, size_t smem, uint64_t items, boo
     *grid = (uint32_t)(groups < want ? groups : want);
     return CO3_OK;
 }
-
-bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
 // Optional per-kernel timing (off by default): an event pair around every launch, read back by
 // co3_profile_read.  Used by benchmarks to time the kernels inside the entry points.
@@ -2560,23 +2554,6 @@ struct Profiler {
     }
 };
 Profiler g_prof;
-
-// Launch of a kernel that follows another kernel of the same call: programmatic stream serialization lets its launch
-// overlap the tail of that kernel; the kernel itself starts with wait_for_previous_kernel().
-template <typename... Params, typename... Args>
-cudaError_t launch_behind(void (*kernel)(Params...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args&&... args) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = grid;
-    cfg.blockDim = block;
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kernel, std::forward<Args>(args)...);
-}
 
 #define CO3_LAUNCH(id, st, ...)        \
     do {                               \
