@@ -346,6 +346,46 @@ int co3_decode(const uint8_t* stream_in, size_t stream_bytes,
                float* ghat_out, uint8_t* sym_out,
                void* workspace, size_t workspace_bytes, co3_result* res, void* stream);
 
+/* Element types of the buffers of the calls below that may be other than fp32. */
+#define CO3_F32 0
+#define CO3_F16 1
+#define CO3_BF16 2
+
+/*
+ * Layer norm (no counterpart in the paper, whose clients train networks with batch norm; clients whose data differ
+ * cannot share batch statistics, and layer norm needs none).  Per row of `cols` elements:
+ *     mean = sum x / cols;   rstd = 1 / sqrt(sum (x - mean)^2 / cols + eps);   y = (x - mean) * rstd * weight + bias
+ *   x, y [device]             `type` elements, aligned to their size; row r starts r * row_stride elements after the
+ *                             base; y may be x (same stride).  16-byte aligned bases and strides are read and written
+ *                             16 bytes at a time
+ *   weight, bias [device]     fp32[cols], each nullable (1, 0): a layer of the parameter vector
+ *   mean, rstd [device]       fp32[rows], each nullable: what the backward pass needs
+ * Statistics and sums are fp32; results are rounded to `type` once.  rows == 0 or cols == 0: nothing is done.
+ */
+int co3_layer_norm(const void* x, int type, const float* weight, const float* bias, void* y, uint64_t rows,
+                   uint32_t cols, uint64_t x_row_stride, uint64_t y_row_stride, float eps, float* mean, float* rstd,
+                   void* stream);
+
+/* Device workspace of co3_layer_norm_backward. */
+int co3_layer_norm_workspace_bytes(uint64_t rows, uint32_t cols, uint32_t n_clients, size_t* out /* [host] */);
+
+/*
+ * Its gradients, for n_clients batches of `rows` rows each (rows of client u are u * rows .. u * rows + rows - 1):
+ *     xh = (x - mean) * rstd;   g = dy * weight;   dx = rstd * (g - sum g / cols - xh * sum(g * xh) / cols)
+ *     dweight_u = sum over the client's rows of dy * xh;   dbias_u = sum over the client's rows of dy
+ *   dy, x, dx [device]        as above; dx nullable, and may be dy or x (same stride)
+ *   mean, rstd [device]       fp32[n_clients * rows] as co3_layer_norm wrote them;  weight nullable (1)
+ *   dweight, dbias [device]   fp32, each nullable: client u's cols sums go to dweight + u * client_stride_elems, so that
+ *                             they can be layers of the gradient vectors that co3_encode reads; added to what is
+ *                             there if `accumulate` is not 0.  No rows: zeros (or nothing, if accumulating)
+ * Sums are fp32 in an order that depends on the sizes alone: the same call gives the same bits.
+ */
+int co3_layer_norm_backward(const void* dy, const void* x, int type, const float* weight, const float* mean,
+                            const float* rstd, void* dx, float* dweight, float* dbias, uint64_t rows, uint32_t cols,
+                            uint64_t dy_row_stride, uint64_t x_row_stride, uint64_t dx_row_stride, uint32_t n_clients,
+                            uint64_t client_stride_elems, int accumulate, void* workspace, size_t workspace_bytes,
+                            void* stream);
+
 /*
  * Orthogonalised updates (no counterpart in the paper, whose server step is w <- w - lr * avg: this is the step of the
  * Muon optimiser for the weight matrices of a model).  A gradient G of a layer with `rows` outputs and `cols` inputs (a
@@ -354,10 +394,6 @@ int co3_decode(const uint8_t* stream_in, size_t stream_bytes,
  *     X_0 = G / (||G||_F + eps);   A = X X^T,  X <- a X + (b A + c A A) X  for every step;   result = scale * X.
  * A singular value s of X becomes a s + b s^3 + c s^5 in each step.  All matrices of a call are worked on together.
  */
-#define CO3_F32 0 /* element types of buffers that may be other than fp32 */
-#define CO3_F16 1
-#define CO3_BF16 2
-
 #define CO3_MAT_PLAIN 1u /* co3_muon_update: no orthogonalisation, the momentum itself is the update (vectors, biases) */
 
 /* Where a matrix lies: entry (r, c) is element offset + r * row_stride + c of its buffer.  Matrices of one call must

@@ -66,13 +66,17 @@ def _load():
     L.co3_decode_aggregate.argtypes = [vp, sz, u32, vp, vp, vp, u32, u64, u32, vp, vp, sz, vp, vp]
     L.co3_decode_aggregate_update.argtypes = [vp, sz, u32, vp, vp, vp, u32, u64, u32, f32, vp, vp, vp, sz, vp, vp]
     L.co3_decode.argtypes = [vp, sz, vp, vp, vp, u32, u64, u32, vp, vp, vp, sz, vp, vp]
+    L.co3_layer_norm.argtypes = [vp, C.c_int, vp, vp, vp, u64, u32, u64, u64, f32, vp, vp, vp]
+    L.co3_layer_norm_workspace_bytes.argtypes = [u64, u32, u32, C.POINTER(sz)]
+    L.co3_layer_norm_backward.argtypes = [vp, vp, C.c_int, vp, vp, vp, vp, vp, vp, u64, u32, u64, u64, u64, u32, u64,
+                                          C.c_int, vp, sz, vp]
     L.co3_ns_default.argtypes = [vp]
     L.co3_orthogonalize_workspace_bytes.argtypes = [vp, u32, C.POINTER(sz)]
     L.co3_orthogonalize.argtypes = [vp, C.c_int, vp, vp, C.c_int, vp, u32, vp, vp, vp, sz, vp]
     L.co3_muon_update.argtypes = [vp, vp, vp, vp, u32, f32, C.c_int, f32, f32, vp, vp, vp, sz, vp]
     L.co3_profile_enable.argtypes = [C.c_int]
     L.co3_profile_read.argtypes = [vp, vp]
-    for name in ("co3_ns_default", "co3_orthogonalize_workspace_bytes", "co3_orthogonalize", "co3_muon_update", "co3_histogram", "co3_convert_dither", "co3_histogram_dither", "co3_encode_dither", "co3_error_magnitude", "co3_model_weights", "co3_fit_scale", "co3_profile_enable", "co3_profile_read", "co3_convert_static", "co3_workspace_bytes", "co3_stream_capacity_bytes", "co3_convert", "co3_code_build", "co3_code_build_device", "co3_encode",
+    for name in ("co3_layer_norm", "co3_layer_norm_workspace_bytes", "co3_layer_norm_backward", "co3_ns_default", "co3_orthogonalize_workspace_bytes", "co3_orthogonalize", "co3_muon_update", "co3_histogram", "co3_convert_dither", "co3_histogram_dither", "co3_encode_dither", "co3_error_magnitude", "co3_model_weights", "co3_fit_scale", "co3_profile_enable", "co3_profile_read", "co3_convert_static", "co3_workspace_bytes", "co3_stream_capacity_bytes", "co3_convert", "co3_code_build", "co3_code_build_device", "co3_encode",
                  "co3_encode_symbols", "co3_decode_aggregate", "co3_decode_aggregate_update", "co3_decode"):
         getattr(L, name).restype = C.c_int
     _lib = L
@@ -92,7 +96,7 @@ def _dev(t, allow_none: bool = False):
 
 def _stream(stream):
     if stream is None:
-        return torch.cuda.current_stream().cuda_stream
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
@@ -301,6 +305,61 @@ def co3_decode(stream_in, stream_bytes, fmts, codes, segs, n_seg, n_elem, ghat_o
     return _load().co3_decode(_dev(stream_in), stream_bytes, _dev(fmts), _dev(codes), _dev(segs), n_seg, n_elem,
                               chunk_syms, _dev(ghat_out, True), _dev(sym_out, True), _dev(workspace),
                               workspace.numel() * workspace.element_size(), _dev(res), _stream(stream))
+
+
+def _rows(t, like=None):
+    """(pointer, rows, cols, row stride) of a 2-D CUDA tensor whose rows are contiguous."""
+    if not t.is_cuda or t.dim() != 2 or t.dtype not in _TYPES:
+        raise ValueError("expected a 2-D CUDA tensor of fp32, fp16 or bf16")
+    rows, cols = t.shape
+    rs, cs = t.stride()
+    if (cs != 1 and cols > 1) or (rs < cols and rows > 1):
+        raise ValueError("expected contiguous rows that do not overlap")
+    if like is not None and (t.dtype != like.dtype or t.shape != like.shape):
+        raise ValueError("expected tensors of one shape and type")
+    return t.data_ptr(), rows, cols, rs if rows > 1 else max(rs, cols)
+
+
+def _vec(t, n):
+    """Device pointer of n fp32 values (or None)."""
+    if t is None:
+        return None
+    if t.dtype != torch.float32 or t.numel() < n or not t.is_cuda or not t.is_contiguous():
+        raise ValueError("expected a contiguous fp32 CUDA tensor of at least %d elements" % n)
+    return t.data_ptr()
+
+
+def co3_layer_norm(x, weight, bias, y, mean=None, rstd=None, eps=1e-5, stream=None) -> int:
+    """y <- layer norm of the rows of x; weight, bias (fp32) and the statistics mean, rstd (fp32, out) may be None."""
+    px, rows, cols, xs = _rows(x)
+    py, _, _, ys = _rows(y, x)
+    return (_lib or _load()).co3_layer_norm(px, _TYPES[x.dtype], _vec(weight, cols), _vec(bias, cols), py, rows, cols, xs,
+                                            ys, eps, _vec(mean, rows), _vec(rstd, rows), _stream(stream))
+
+
+def co3_layer_norm_workspace_bytes(rows: int, cols: int, n_clients: int = 1) -> int:
+    """Device workspace of co3_layer_norm_backward for n_clients batches of `rows` rows each."""
+    out = C.c_size_t(0)
+    st = _load().co3_layer_norm_workspace_bytes(rows, cols, n_clients, C.byref(out))
+    if st != OK:
+        raise ValueError("co3_layer_norm_workspace_bytes: " + co3_status_string(st))
+    return out.value
+
+
+def co3_layer_norm_backward(dy, x, weight, mean, rstd, dx, dweight, dbias, n_clients, client_stride_elems, workspace,
+                            accumulate: bool = False, stream=None) -> int:
+    """Gradients of co3_layer_norm; the rows are n_clients equal batches.  dweight and dbias are fp32 tensors that start
+    at client 0's gradient of that layer (a slice of the clients' gradient buffer); dx, dweight, dbias may be None."""
+    pd, rows, cols, ds = _rows(dy)
+    px, _, _, xs = _rows(x, dy)
+    po, _, _, os_ = (None, 0, 0, 0) if dx is None else _rows(dx, dy)
+    if n_clients < 1 or rows % n_clients:
+        raise ValueError("co3_layer_norm_backward: the rows do not divide into n_clients batches")
+    reach = (n_clients - 1) * client_stride_elems + cols
+    return _load().co3_layer_norm_backward(pd, px, _TYPES[dy.dtype], _vec(weight, cols), _vec(mean, rows), _vec(rstd, rows), po,
+                                           _vec(dweight, reach), _vec(dbias, reach), rows // n_clients, cols, ds, xs, os_,
+                                           n_clients, client_stride_elems, 1 if accumulate else 0, _dev(workspace),
+                                           workspace.numel() * workspace.element_size(), _stream(stream))
 
 
 def _mats(mats):

@@ -11,8 +11,6 @@
 // the tensor core wants it in shared memory (128-byte rows, 16-byte pieces XORed with the row number modulo 8), so
 // that a tile is fetched by one plain bulk copy, and padding of the matrix to whole blocks is stored as zeros.  A
 // product is hi*hi + 2^-11 (hi*lo + lo*hi): the part left out, lo*lo, is below 2^-22 of the whole.
-#include <cuda_bf16.h>
-#include <cuda_fp16.h>
 #include <cuda_runtime.h>
 #include <math.h>
 #include <stddef.h>
@@ -23,6 +21,7 @@
 #include "co3.h"
 #include "co3_device.cuh"
 #include "co3_launch.cuh"
+#include "co3_types.cuh"
 
 namespace co3 {
 
@@ -114,23 +113,6 @@ __host__ __device__ inline float orth_s(const OrthShape& s) {
     while (k < kMaxLogS && (1ull << (2 * (k + 1))) <= p) ++k;
     return (float)(1u << k);
 }
-
-template <typename T>
-__device__ __forceinline__ float to_float(T v);
-template <>
-__device__ __forceinline__ float to_float(float v) { return v; }
-template <>
-__device__ __forceinline__ float to_float(__half v) { return __half2float(v); }
-template <>
-__device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
-template <typename T>
-__device__ __forceinline__ T from_float(float v);
-template <>
-__device__ __forceinline__ float from_float(float v) { return v; }
-template <>
-__device__ __forceinline__ __half from_float(float v) { return __float2half_rn(v); }
-template <>
-__device__ __forceinline__ __nv_bfloat16 from_float(float v) { return __float2bfloat16_rn(v); }
 
 // Index of the matrix that owns item `x`: largest k with first(k) <= x.  Matrices without items are skipped because
 // the next one starts at the same item.
@@ -936,8 +918,6 @@ bool valid_ns(const co3_ns& ns) {
     }
     return true;
 }
-
-size_t type_size(int type) { return type == CO3_F32 ? 4u : 2u; }
 
 struct OrthCall {
     const void* in;
