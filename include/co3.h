@@ -410,7 +410,8 @@ typedef struct {
 
 /* Steps of the iteration; coef[k] = {a, b, c} of step k.  Refused (CO3_ERR_INVALID_ARG) if steps is not in
  * 1..CO3_NS_MAX_STEPS, eps is negative or not finite, or some singular value in [0, 1] leaves [-2, 2] on the way or
- * meets |b s^2 + c s^4| > 4 (the products are formed from scaled half-precision pairs, which hold that range). */
+ * meets |b s^2 + c s^4| > 4 or |a + b s^2 + c s^4| > 4 (the products are formed from scaled half-precision pairs, which
+ * hold that range). */
 typedef struct {
     uint32_t steps;
     float eps;

@@ -2,21 +2,24 @@
 // fifth-generation tensor cores.
 //
 //   orth_begin_kernel   (momentum update +) sum of squares of every matrix
-//   orth_load_kernel    X_0 = G / (norm + eps) as operand blocks, as it is and transposed
+//   orth_load_kernel    X_0 = G / (norm + eps) as operand blocks
 //   orth_steps_kernel   all products of all steps in one cooperative launch: per step A = X X^T; B = b A + c A A;
 //                       X <- a X + B X; the last product writes the result (or steps the parameters) instead of X
 //
 // Operands live in the workspace as blocks of 128 rows x 64 columns, each a pair of fp16 planes of 16 KB: hi = the
 // value rounded, lo = 2^11 times the remainder rounded, together 22 significant bits.  A plane is stored exactly as
 // the tensor core wants it in shared memory (128-byte rows, 16-byte pieces XORed with the row number modulo 8), so
-// that a tile is fetched by one plain bulk copy, and padding of the matrix to whole blocks is stored as zeros.  A
-// product is hi*hi + 2^-11 (hi*lo + lo*hi): the part left out, lo*lo, is below 2^-22 of the whole.
+// that a tile is fetched by plain bulk copies, and padding of the matrix to whole blocks is stored as zeros.  The same
+// bytes serve as the transposed operand (a row of the block runs along the operand's rows instead of along the sum): X is
+// not stored transposed, and of the symmetric A and B only the tiles on and below the diagonal are computed and stored.
+// A product is hi*hi + 2^-11 (hi*lo + lo*hi): the part left out, lo*lo, is below 2^-22 of the whole.
 #include <cuda_runtime.h>
 #include <math.h>
 #include <stddef.h>
 #include <stdint.h>
 
 #include <algorithm>
+#include <atomic>
 
 #include "co3.h"
 #include "co3_device.cuh"
@@ -28,9 +31,11 @@ namespace co3 {
 constexpr uint32_t kOrthMats = 96;                  // matrices of one batch of launches
 constexpr uint32_t kPlane = 128 * 64 * 2;           // bytes of a plane of a block
 constexpr uint32_t kBlock = 2 * kPlane;             // hi, then lo
+constexpr uint32_t kHalfPlane = kPlane / 2;         // 64 rows
 constexpr uint32_t kBeginElems = 8192;              // elements per block of orth_begin_kernel
 constexpr int kBeginThreads = 256;
 constexpr int kLoadThreads = 256;
+constexpr int kLoBits = 11;
 constexpr float kLoScale = 2048.0f;
 constexpr int kMaxLogS = 13;                        // values are held times S = 2^min(13, log2 sqrt(m n)): entries about 1
 
@@ -57,7 +62,7 @@ struct OrthBatch {
     uint32_t n_tasks[3];
     uint32_t index0;  // index of mat[0] in the caller's list
     uint32_t first;   // 1: the call's first batch, which clears the result
-    uint32_t pad;
+    uint32_t ctas;    // blocks per tile: 1 or 2
 };
 
 struct OrthCtrl {
@@ -75,34 +80,38 @@ struct OrthWs {
 };
 
 struct OrthShape {
-    uint32_t m, n, mb, nb;  // small side, long side, and both in blocks of 128
-    bool tall;              // rows > cols: X is the transposed matrix
+    uint32_t m, n;    // small side, long side
+    uint32_t mt, nt;  // both in tiles (of ctas * 128)
+    uint32_t mb, nb;  // both in blocks of 128, filled up to whole tiles
+    bool tall;        // rows > cols: X is the transposed matrix
 };
 
-__host__ __device__ inline OrthShape orth_shape(uint32_t rows, uint32_t cols) {
+// ctas: blocks that work on a tile together, each on 128 rows of it: a tile is 128 x 128 or 256 x 256.
+__host__ __device__ inline OrthShape orth_shape(uint32_t rows, uint32_t cols, uint32_t ctas) {
     OrthShape s;
     s.tall = rows > cols;
     s.m = s.tall ? cols : rows;
     s.n = s.tall ? rows : cols;
-    s.mb = (s.m + 127u) / 128u;
-    s.nb = (s.n + 127u) / 128u;
+    s.mt = (s.m + 128u * ctas - 1u) / (128u * ctas);
+    s.nt = (s.n + 128u * ctas - 1u) / (128u * ctas);
+    s.mb = s.mt * ctas;
+    s.nb = s.nt * ctas;
     return s;
 }
 
-// Operand blocks of one matrix: X [mb][2 nb], X^T twice [nb][2 mb], A and B [mb][2 mb].
+// Operand blocks of one matrix: X twice [mb][2 nb], A and B [mb][2 mb] (their lower triangles of tiles are used).
 __host__ __device__ inline uint64_t orth_blocks(const OrthShape& s) {
-    return 6ull * s.mb * s.nb + 4ull * s.mb * s.mb;
+    return 4ull * s.mb * s.nb + 4ull * s.mb * s.mb;
 }
 struct OrthOperands {
-    unsigned char *x, *xt[2], *a, *b;
+    unsigned char *x[2], *a, *b;
 };
 __device__ inline OrthOperands orth_operands(const OrthWs& ws, const OrthMat& t, const OrthShape& s) {
     OrthOperands o;
     const uint64_t xs = 2ull * s.mb * s.nb * kBlock;
-    o.x = ws.blocks + (uint64_t)t.block0 * kBlock;
-    o.xt[0] = o.x + xs;
-    o.xt[1] = o.xt[0] + xs;
-    o.a = o.xt[1] + xs;
+    o.x[0] = ws.blocks + (uint64_t)t.block0 * kBlock;
+    o.x[1] = o.x[0] + xs;
+    o.a = o.x[1] + xs;
     o.b = o.a + 2ull * s.mb * s.mb * kBlock;
     return o;
 }
@@ -203,7 +212,7 @@ __global__ void __launch_bounds__(kBeginThreads) orth_begin_kernel(const __grid_
 }
 
 // ------------------------------------------------------------------------------------------------
-// load: one block per 64 x 64 piece of X (padding included): both operand layouts of S * G / (norm + eps).
+// load: one block per 64 x 64 piece of X (padding included): S * G / (norm + eps).
 // ------------------------------------------------------------------------------------------------
 struct LoadArgs {
     const void* in;
@@ -216,29 +225,28 @@ struct LoadArgs {
 
 __device__ __forceinline__ uint32_t swizzled(uint32_t row, uint32_t piece) { return row * 128u + ((piece ^ (row & 7u)) << 4); }
 
-__device__ __forceinline__ uint32_t pack_halves(__half a, __half b) {
-    return (uint32_t)__half_as_ushort(a) | ((uint32_t)__half_as_ushort(b) << 16);
-}
-
 // hi and lo of eight values, as 16-byte pieces.
-__device__ __forceinline__ void split8(const float (&v)[8], uint4& hi, uint4& lo) {
-    __half h[8], l[8];
+__device__ __forceinline__ void split8(const float* v, uint4& hi, uint4& lo) {
+    uint32_t h[4], l[4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        h[i] = __float2half_rn(v[i]);
-        l[i] = __float2half_rn(__fmul_rn(__fsub_rn(v[i], __half2float(h[i])), kLoScale));
+    for (int i = 0; i < 4; ++i) {
+        const __half2 a = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
+        const float2 f = __half22float2(a);
+        const __half2 b = __floats2half2_rn(__fmul_rn(__fsub_rn(v[2 * i], f.x), kLoScale), __fmul_rn(__fsub_rn(v[2 * i + 1], f.y), kLoScale));
+        h[i] = *reinterpret_cast<const uint32_t*>(&a);
+        l[i] = *reinterpret_cast<const uint32_t*>(&b);
     }
-    hi = make_uint4(pack_halves(h[0], h[1]), pack_halves(h[2], h[3]), pack_halves(h[4], h[5]), pack_halves(h[6], h[7]));
-    lo = make_uint4(pack_halves(l[0], l[1]), pack_halves(l[2], l[3]), pack_halves(l[4], l[5]), pack_halves(l[6], l[7]));
+    hi = make_uint4(h[0], h[1], h[2], h[3]);
+    lo = make_uint4(l[0], l[1], l[2], l[3]);
 }
 
 __device__ __forceinline__ void join8(const uint4& hi, const uint4& lo, float (&v)[8]) {
     const uint32_t h[4] = {hi.x, hi.y, hi.z, hi.w}, l[4] = {lo.x, lo.y, lo.z, lo.w};
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float a = __half2float(__ushort_as_half((unsigned short)(h[i / 2] >> (16 * (i & 1)))));
-        const float b = __half2float(__ushort_as_half((unsigned short)(l[i / 2] >> (16 * (i & 1)))));
-        v[i] = __fmaf_rn(b, 1.0f / kLoScale, a);
+    for (int i = 0; i < 4; ++i) {
+        const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&h[i])), b = __half22float2(*reinterpret_cast<const __half2*>(&l[i]));
+        v[2 * i] = __fmaf_rn(b.x, 1.0f / kLoScale, a.x);
+        v[2 * i + 1] = __fmaf_rn(b.y, 1.0f / kLoScale, a.y);
     }
 }
 
@@ -252,7 +260,7 @@ __global__ void __launch_bounds__(kLoadThreads) orth_load_kernel(LoadArgs a) {
     const uint32_t tile = blockIdx.x >> 2;  // tile of 128 x 128, quarter blockIdx.x & 3
     const uint32_t k = orth_find(batch.n_mats, tile, [&](uint32_t i) { return batch.mat[i].full0; });
     const OrthMat t = batch.mat[k];
-    const OrthShape s = orth_shape(t.rows, t.cols);
+    const OrthShape s = orth_shape(t.rows, t.cols, batch.ctas);
     // the norm: this matrix' partial sums in order
     const uint32_t n_part = (uint32_t)(((uint64_t)t.rows * t.cols + kBeginElems - 1) / kBeginElems);
     double sum = 0.0;
@@ -298,18 +306,15 @@ __global__ void __launch_bounds__(kLoadThreads) orth_load_kernel(LoadArgs a) {
     }
     __syncthreads();
     const OrthOperands op = orth_operands(a.ws, t, s);
-    unsigned char* xb = op.x + ((uint64_t)(x_row0 >> 7) * (2 * s.nb) + (x_col0 >> 6)) * kBlock;
-    unsigned char* tb = op.xt[0] + ((uint64_t)(x_col0 >> 7) * (2 * s.mb) + (x_row0 >> 6)) * kBlock;
-    const uint32_t xr = x_row0 & 64u, tr = x_col0 & 64u;
-    for (uint32_t i = threadIdx.x; i < 2 * 64 * 8; i += kLoadThreads) {
-        const bool tr_part = i >= 64 * 8;
-        const uint32_t row = (i >> 3) & 63u, piece = i & 7u;
+    unsigned char* xb = op.x[0] + ((uint64_t)(x_row0 >> 7) * (2 * s.nb) + (x_col0 >> 6)) * kBlock;
+    for (uint32_t i = threadIdx.x; i < 64 * 8; i += kLoadThreads) {
+        const uint32_t row = i >> 3, piece = i & 7u;
         float v[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = tr_part ? s_v[piece * 8 + e][row] : s_v[row][piece * 8 + e];
+        for (int e = 0; e < 8; ++e) v[e] = s_v[row][piece * 8 + e];
         uint4 hi, lo;
         split8(v, hi, lo);
-        unsigned char* p = (tr_part ? tb : xb) + swizzled(row + (tr_part ? tr : xr), piece);
+        unsigned char* p = xb + swizzled((x_row0 & 64u) + row, piece);
         *reinterpret_cast<uint4*>(p) = hi;
         *reinterpret_cast<uint4*>(p + kPlane) = lo;
     }
@@ -318,29 +323,81 @@ __global__ void __launch_bounds__(kLoadThreads) orth_load_kernel(LoadArgs a) {
 // ------------------------------------------------------------------------------------------------
 // tcgen05: operands in shared memory (K-major, 128-byte swizzle), fp32 accumulators in tensor memory.
 // ------------------------------------------------------------------------------------------------
-__device__ __forceinline__ uint64_t smem_desc(uint32_t addr) {
-    // start address, leading offset 16 (unused with this swizzle), 1024 bytes between groups of eight rows, the
-    // fixed version bit of this architecture, 128-byte swizzle
-    return (uint64_t)((addr >> 4) & 0x3fffu) | (1ull << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
+// An operand of 128 rows and 64 columns of the sum in shared memory.  As it lies in memory: rows of 128 bytes along the
+// sum, 1024 bytes between groups of eight.  Transposed: two halves of 64 operand rows, 8 KB apart, each with a row of
+// 128 bytes per column of the sum, 1024 bytes between groups of eight columns.  Both swizzled.
+__device__ __forceinline__ uint64_t smem_desc(uint32_t addr, bool transposed) {
+    return (uint64_t)((addr >> 4) & 0x3fffu) | ((uint64_t)(transposed ? kHalfPlane >> 4 : 1u) << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
 }
-// D fp32, A and B fp16, both K-major, M = 128, N = 128
-constexpr uint32_t kInstrDesc = (1u << 4) | ((128u / 8u) << 17) | ((128u / 16u) << 24);
+// 16 columns of the sum further
+__device__ __forceinline__ uint64_t desc_step(bool transposed) { return transposed ? 2048u >> 4 : 32u >> 4; }
+// D fp32, A and B fp16; one block: 128 x 128, a pair of blocks: 256 x 256
+template <int kCtas>
+__device__ __forceinline__ uint32_t instr_desc(bool a_transposed, bool b_transposed) {
+    return (1u << 4) | ((uint32_t)a_transposed << 15) | ((uint32_t)b_transposed << 16) | ((128u * kCtas / 8u) << 17) | ((128u * kCtas / 16u) << 24);
+}
 
-__device__ __forceinline__ void tc_mma(uint32_t d, uint64_t a, uint64_t b, bool accumulate) {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(kInstrDesc),
-        "r"((uint32_t)accumulate)
-        : "memory");
+// kScale: what is there already counts 2^-kScale.
+template <int kCtas, int kScale = 0>
+__device__ __forceinline__ void tc_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t instr, bool accumulate) {
+    if constexpr (kCtas == 1) {
+        if constexpr (kScale == 0)
+            asm volatile(
+                "{\n\t.reg .pred p;\n\t"
+                "setp.ne.b32 p, %4, 0;\n\t"
+                "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(instr),
+                "r"((uint32_t)accumulate)
+                : "memory");
+        else
+            asm volatile(
+                "{\n\t.reg .pred p;\n\t"
+                "setp.ne.b32 p, %4, 0;\n\t"
+                "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p, %5;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(instr),
+                "r"((uint32_t)accumulate), "n"(kScale)
+                : "memory");
+    } else {
+        if constexpr (kScale == 0)
+            asm volatile(
+                "{\n\t.reg .pred p;\n\t"
+                "setp.ne.b32 p, %4, 0;\n\t"
+                "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(instr),
+                "r"((uint32_t)accumulate)
+                : "memory");
+        else
+            asm volatile(
+                "{\n\t.reg .pred p;\n\t"
+                "setp.ne.b32 p, %4, 0;\n\t"
+                "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p, %5;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(instr),
+                "r"((uint32_t)accumulate), "n"(kScale)
+                : "memory");
+    }
 }
+// The products issued so far arrive on this barrier when they are done; of a pair, on both blocks' barrier.
+template <int kCtas>
 __device__ __forceinline__ void tc_commit(uint64_t* bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(bar)) : "memory");
+    if constexpr (kCtas == 1)
+        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(bar)) : "memory");
+    else
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(smem_addr(bar)), "h"((uint16_t)3)
+                     : "memory");
 }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(bar)) : "memory");
+}
+// The same on the barrier of the pair's first block.
+template <int kCtas>
+__device__ __forceinline__ void mbar_arrive_first(uint64_t* bar) {
+    if constexpr (kCtas == 1) {
+        mbar_arrive(bar);
+    } else {
+        asm volatile(
+            "{\n\t.reg .b32 r;\n\t"
+            "mapa.shared::cluster.u32 r, %0, 0;\n\t"
+            "mbarrier.arrive.release.cluster.shared::cluster.b64 _, [r];\n\t}" ::"r"(smem_addr(bar))
+            : "memory");
+    }
 }
 // 32 columns of this warp's 32 lanes
 __device__ __forceinline__ void tc_load32(uint32_t addr, float (&v)[32]) {
@@ -362,58 +419,40 @@ __device__ __forceinline__ void tc_load32(uint32_t addr, float (&v)[32]) {
 
 // ------------------------------------------------------------------------------------------------
 // steps: persistent blocks (all resident: a cooperative launch).  The products of all steps form one list of tasks,
-// phase by phase; a task is a 128 x 128 tile, or a part of its sum where there are fewer tiles than SMs.  Block b takes
-// tasks b, b + gridDim.x, ... in order, and before a task's operands are fetched it waits until the matrix' tiles of
-// the phases before it are finished (a counter per matrix): the tasks waited for stand earlier in the list, so that
+// phase by phase; a task is a tile, or a part of its sum where there are fewer tiles than SMs.  Block (or pair) b takes
+// tasks b, b + number of blocks, ... in order, and before a task's operands are fetched it waits until the matrix' tiles
+// of the phases before it are finished (a counter per matrix): the tasks waited for stand earlier in the list, so that
 // waiting always ends, and one matrix' tail is filled with other matrices' work.
 //
-// Warp 0 copies operand blocks into a ring, warp 1 issues the products, warps 2..9 take the accumulators: each of them
-// 32 rows x 64 columns of the tile in registers.
+// Warp 0 copies operand blocks into a ring, warp 1 issues the products, warps 2..9 take the sums: each of them 32 rows x
+// half of the tile's columns in registers, and from there on each works on its own.  Behind a task's operands the ring
+// carries its linear term (b A or a X, the tile's own blocks); the warps put the finished values in its place, from where
+// bulk copies take them to memory.
+//
+// kCtas == 1: a tile of 128 x 128.  A stage (64 columns of the sum) is 64 KB for 3 x 2 x 128 x 128 x 64 operations, which
+// a GPU full of such blocks fetches from L2 at about 10 TB/s: 0.9 us where the products take 0.4.  kCtas == 2: two
+// blocks multiply one tile of 256 x 256 (each fetches 128 rows of either operand, the tensor cores read both blocks'
+// shared memory): the same 64 KB and twice the operations per block.
 // ------------------------------------------------------------------------------------------------
 constexpr int kEpiThreads = 256;
 constexpr int kStepThreads = 64 + kEpiThreads;
 constexpr int kStages = 3;
 // The tensor core cuts what it adds to 26 bits below the largest term, always towards zero: sums of one sign (the
-// diagonal of A) drift.  Sums of this many stages (64 columns each) are therefore added up in registers, where fp32
-// rounds to nearest.  1000 x 513, five steps, error against 64 bits: 1.3e-5 if never, 6.1e-6 every 4 stages, 2.1e-6
-// every stage (2.9e-6 with all sums in fp32 arithmetic).
-constexpr uint32_t kDrain = 1;
+// diagonal of A) drift.  The sum of each stage is therefore taken out and added up in registers, where fp32 rounds to
+// nearest.  1000 x 513, five steps, error against 64 bits: 1.3e-5 if the tensor core adds up all stages, 6.1e-6 if
+// four, 2.1e-6 if one (2.9e-6 with all sums in fp32 arithmetic).  Steps that multiply the hi planes alone leave all
+// sums to the tensor core.
 constexpr uint32_t kStageBytes = 2 * kBlock;
-constexpr uint32_t kPitch = 129;  // floats between columns of the staged half tile
-
-struct StepSmem {
-    uint64_t full[kStages], empty[kStages];
-    uint64_t main_full[2], main_empty[2], corr_full[2], corr_empty[2];
-    uint64_t done;
-    uint32_t tmem, failed, last;
-    uint32_t task0[3][kOrthMats];
-};
-constexpr size_t kStageOff = (size_t)kStages * kStageBytes;
-constexpr size_t kSmemOff = kStageOff + 64 * kPitch * 4;
-constexpr size_t kStepSmem = 1024 + kSmemOff + sizeof(StepSmem);
-static_assert(kStepSmem <= 227 * 1024 && kSmemOff % 8 == 0, "shared memory of a block");
-
-enum OrthOut { kOutF32 = 0, kOutF16 = 1, kOutBf16 = 2, kOutParams = 3 };
-
-struct StepArgs {
-    OrthWs ws;
-    co3_ns ns;
-    uint32_t pairs;  // bit k: step k multiplies pairs (three products), otherwise the hi planes alone
-    int out_kind;
-    void* out;
-    float lr, shrink;
-    uint64_t limit_ns;  // longest wait
-    co3_result* res;
-};
 
 struct Task {
     uint32_t step, phase, mat;
-    uint32_t i, j;           // block row and column of the tile (kApply: i of the small side, j of the long side)
+    uint32_t rb, cb;      // block row and first block column of this block's part of the tile
+    uint32_t k0, k1;      // operand blocks of the summed dimension
     uint32_t part, parts;
-    uint32_t k0, k1;         // operand blocks of the summed dimension
-    uint32_t tile;           // index within the matrix and phase
-    uint32_t before;         // tiles of this matrix that have to be finished
-    bool swap;               // kApply: the tile's rows are the long side
+    uint32_t tile;        // index within the matrix and phase
+    uint32_t before;      // warps' parts of this matrix' tiles that have to be finished
+    bool swap;            // kApply: the tile's rows are the long side
+    bool diagonal;        // both operands are the same blocks
 };
 
 struct MatView {
@@ -422,7 +461,37 @@ struct MatView {
     OrthOperands op;
 };
 
-__device__ __forceinline__ Task find_task(const StepArgs& a, const StepSmem& sm, const uint32_t* n_tasks, uint32_t n_mats, uint32_t g, MatView& v) {
+struct StepSmem {
+    uint64_t full[kStages];
+    uint64_t empty[kStages];      // a stage of operands has been multiplied
+    uint64_t out_empty[kStages];  // a stage of the tile's own blocks has been stored
+    uint64_t peer_full[kStages];  // first block of a pair: the other block's stage is full
+    uint64_t sum_full[4], sum_empty[4];
+    uint64_t done;
+    uint32_t tmem, failed;
+    uint32_t task0[3][kOrthMats];
+    Task task[8];  // what warps 2..9 work on: in shared memory, the sums need the registers
+    MatView view[8];
+};
+constexpr size_t kSmemOff = (size_t)kStages * kStageBytes;
+constexpr size_t kStepSmem = 1024 + kSmemOff + sizeof(StepSmem);
+static_assert(kStepSmem <= 227 * 1024 && kSmemOff % 8 == 0, "shared memory of a block");
+
+enum OrthOut { kOutF32 = 0, kOutF16 = 1, kOutBf16 = 2, kOutParams = 3 };
+
+struct StepArgs {
+    OrthWs ws;
+    co3_ns ns;
+    uint32_t pairs;  // bit k: step k multiplies pairs of halves (three products), otherwise the hi planes alone
+    int out_kind;
+    void* out;
+    float lr, shrink;
+    uint64_t limit_ns;  // longest wait
+    co3_result* res;
+};
+
+template <int kCtas>
+__device__ __forceinline__ Task find_task(const StepArgs& a, const StepSmem& sm, const uint32_t* n_tasks, uint32_t n_mats, uint32_t g, uint32_t rank, MatView& v) {
     Task k;
     const uint32_t per_step = n_tasks[0] + n_tasks[1] + n_tasks[2];
     k.step = g / per_step;
@@ -432,34 +501,86 @@ __device__ __forceinline__ Task find_task(const StepArgs& a, const StepSmem& sm,
     const uint32_t* first = sm.task0[k.phase];
     k.mat = orth_find(n_mats, x, [&](uint32_t i) { return first[i]; });
     v.t = a.ws.batch->mat[k.mat];
-    v.s = orth_shape(v.t.rows, v.t.cols);
+    v.s = orth_shape(v.t.rows, v.t.cols, kCtas);
     v.op = orth_operands(a.ws, v.t, v.s);
     x -= first[k.mat];
     k.parts = v.t.splits[k.phase];
     k.tile = x / k.parts;
     k.part = x - k.tile * k.parts;
-    const uint32_t sym = v.s.mb * (v.s.mb + 1) / 2;
-    k.before = k.step * (2 * sym + v.s.mb * v.s.nb) + k.phase * sym;
-    k.swap = false;
-    uint32_t blocks;
+    const uint32_t sym = v.s.mt * (v.s.mt + 1) / 2;
+    k.before = 8 * kCtas * (k.step * (2 * sym + v.s.mt * v.s.nt) + k.phase * sym);
+    k.swap = k.diagonal = false;
+    uint32_t i, j, blocks;
     if (k.phase == kApply) {
-        k.i = k.tile / v.s.nb;
-        k.j = k.tile - k.i * v.s.nb;
+        i = k.tile / v.s.nt;  // small side
+        j = k.tile - i * v.s.nt;
         // in the last product of a matrix that is not tall the tile's rows are the long side, so that a warp's rows
         // are neighbours in the caller's memory
         k.swap = k.step + 1 == a.ns.steps && !v.s.tall;
+        if (k.swap) { const uint32_t h = i; i = j; j = h; }
         blocks = (v.s.m + 63u) / 64u;
     } else {  // the triangle i >= j
-        uint32_t i = (uint32_t)((sqrtf(8.0f * (float)k.tile + 1.0f) - 1.0f) * 0.5f);
+        i = (uint32_t)((sqrtf(8.0f * (float)k.tile + 1.0f) - 1.0f) * 0.5f);
         while (i * (i + 1) / 2 > k.tile) --i;
         while ((i + 1) * (i + 2) / 2 <= k.tile) ++i;
-        k.i = i;
-        k.j = k.tile - i * (i + 1) / 2;
+        j = k.tile - i * (i + 1) / 2;
+        k.diagonal = i == j;
         blocks = ((k.phase == kGram ? v.s.n : v.s.m) + 63u) / 64u;
     }
+    k.rb = i * kCtas + rank;
+    k.cb = j * kCtas;
     k.k0 = (uint32_t)((uint64_t)blocks * k.part / k.parts);
     k.k1 = (uint32_t)((uint64_t)blocks * (k.part + 1) / k.parts);
     return k;
+}
+
+// Whether the apply product of a step adds a X in fp32.  In the last step a I is part of B instead: the result's tiles may
+// lie the other way round there, where X has no blocks to add.  In the steps before, the rounding of B + a I to pairs
+// would grow with the small singular values (130 x 70: error 2.5e-6 instead of 1.5e-6), and where the hi planes alone
+// are multiplied they would carry the rounding of X to 11 bits along.
+__device__ __forceinline__ bool adds_x(const StepArgs& a, uint32_t step) { return step + 1 < a.ns.steps; }
+
+// The tile's own blocks of the linear term, 2 kCtas of them in a row; null if there is none.
+__device__ __forceinline__ const unsigned char* linear_term(const StepArgs& a, const Task& k, const MatView& v) {
+    if (k.phase == kPoly) return v.op.a + ((uint64_t)k.rb * (2 * v.s.mb) + 2 * k.cb) * kBlock;
+    if (k.phase == kApply && adds_x(a, k.step)) return v.op.x[k.step & 1u] + ((uint64_t)k.rb * (2 * v.s.nb) + 2 * k.cb) * kBlock;
+    return nullptr;
+}
+
+// How one of a task's operands is fetched: for 128 rows from block r on, columns 64 q .. 64 q + 63 of the sum.
+struct Operand {
+    const unsigned char* base;
+    uint64_t row;      // bytes between block rows
+    uint32_t r;        // block row of the operand
+    uint32_t from;     // stages from this one on are fetched transposed
+    __device__ __forceinline__ void fetch(unsigned char* dst, uint32_t q, bool pairs, uint64_t* bar) const {
+        if (q < from) {
+            bulk_copy_g2s(dst, base + r * row + (uint64_t)q * kBlock, pairs ? kBlock : kPlane, bar);
+        } else {  // rows 64 q .. of block row q / 2, columns of blocks 2 r and 2 r + 1
+            const unsigned char* p = base + (q >> 1) * row + (uint64_t)(2 * r) * kBlock + (q & 1u) * kHalfPlane;
+            bulk_copy_g2s(dst, p, kHalfPlane, bar);
+            bulk_copy_g2s(dst + kHalfPlane, p + kBlock, kHalfPlane, bar);
+            if (pairs) {
+                bulk_copy_g2s(dst + kPlane, p + kPlane, kHalfPlane, bar);
+                bulk_copy_g2s(dst + kPlane + kHalfPlane, p + kBlock + kPlane, kHalfPlane, bar);
+            }
+        }
+    }
+};
+// The operand of the tile's rows (which == 0) or columns (1), this block's 128 of them.
+template <int kCtas>
+__device__ __forceinline__ Operand operand(const Task& k, const MatView& v, uint32_t rank, int which) {
+    Operand o;
+    o.r = which == 0 ? k.rb : k.cb + rank;
+    const uint64_t row_x = (uint64_t)(2 * v.s.nb) * kBlock, row_m = (uint64_t)(2 * v.s.mb) * kBlock;
+    if (k.phase == kGram) {
+        o = {v.op.x[k.step & 1u], row_x, o.r, 0xffffffffu};
+    } else if (k.phase == kApply && (which == 1) != k.swap) {
+        o = {v.op.x[k.step & 1u], row_x, o.r, 0u};
+    } else {  // a symmetric matrix: stored up to and including the tile on the diagonal
+        o = {k.phase == kPoly ? v.op.a : v.op.b, row_m, o.r, (o.r / kCtas + 1) * (2 * kCtas)};
+    }
+    return o;
 }
 
 __device__ __forceinline__ uint32_t load_acquire(const uint32_t* p) {
@@ -469,17 +590,31 @@ __device__ __forceinline__ uint32_t load_acquire(const uint32_t* p) {
 }
 __device__ __forceinline__ void fence_async_all() { asm volatile("fence.proxy.async;" ::: "memory"); }
 
+__device__ __forceinline__ bool try_wait_cluster(uint64_t* bar, uint32_t parity) {
+    uint32_t done;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(done)
+        : "r"(smem_addr(bar)), "r"(parity)
+        : "memory");
+    return done != 0;
+}
+
+template <int kCtas>
 __device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity, uint64_t limit_ns) {
-    if (mbar_try_wait(bar, parity)) return true;
+    auto test = [&]() { return kCtas == 1 ? mbar_try_wait(bar, parity) : try_wait_cluster(bar, parity); };
+    if (test()) return true;
     const uint64_t t0 = global_timer_ns();
     for (;;) {
         for (int i = 0; i < 64; ++i)
-            if (mbar_try_wait(bar, parity)) return true;
+            if (test()) return true;
         if (global_timer_ns() - t0 > limit_ns) return false;
     }
 }
 
-// Waits until at least `need` tiles of a matrix are finished.
+// Waits until at least `need` parts of a matrix' tiles are finished.
 __device__ __forceinline__ bool wait_tiles(const OrthCtrl* ctrl, uint32_t mat, uint32_t need, uint64_t limit_ns) {
     if (load_acquire(&ctrl->done[mat]) >= need) return true;
     const uint64_t t0 = global_timer_ns();
@@ -489,307 +624,331 @@ __device__ __forceinline__ bool wait_tiles(const OrthCtrl* ctrl, uint32_t mat, u
     }
 }
 
-__device__ __forceinline__ void epi_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
-// The same, and whether any of the threads says so.
-__device__ __forceinline__ bool epi_any(bool x) {
-    uint32_t any;
-    asm volatile(
-        "{\n\t.reg .pred p, q;\n\t"
-        "setp.ne.b32 q, %1, 0;\n\t"
-        "bar.red.or.pred p, 1, 256, q;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(any)
-        : "r"((uint32_t)x)
-        : "memory");
-    return any != 0u;
+__device__ __forceinline__ void bulk_copy_s2g(void* dst_gmem, const void* src_smem, uint32_t bytes) {
+    asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst_gmem), "r"(smem_addr(src_smem)), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void bulk_stores_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void bulk_stores_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+__device__ __forceinline__ void bulk_stores_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+
+template <int kCtas>
+__device__ __forceinline__ void tile_sync() {  // all threads of the blocks that share a tile
+    if constexpr (kCtas == 1) {
+        __syncthreads();
+    } else {
+        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    }
 }
 
+template <int kCtas>
 __global__ void __launch_bounds__(kStepThreads, 1) orth_steps_kernel(const __grid_constant__ StepArgs a) {
     extern __shared__ unsigned char smem_raw[];
+    constexpr uint32_t kCols = 128 * kCtas, kSums = 512 / kCols;  // columns of a tile, sums that tensor memory holds
     unsigned char* ring = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
-    float* stage = reinterpret_cast<float*>(ring + kStageOff);
     StepSmem& sm = *reinterpret_cast<StepSmem*>(ring + kSmemOff);
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
+    const uint32_t rank = blockIdx.x % kCtas, group = blockIdx.x / kCtas, groups = gridDim.x / kCtas;
     const uint32_t n_mats = a.ws.batch->n_mats;
     const uint32_t n_tasks[3] = {a.ws.batch->n_tasks[0], a.ws.batch->n_tasks[1], a.ws.batch->n_tasks[2]};
     const uint32_t total = a.ns.steps * (n_tasks[0] + n_tasks[1] + n_tasks[2]);
     for (uint32_t i = threadIdx.x; i < n_mats; i += kStepThreads)
         for (int p = 0; p < 3; ++p) sm.task0[p][i] = a.ws.batch->mat[i].task0[p];
     if (threadIdx.x == 0) {
-        for (int i = 0; i < kStages; ++i) { mbar_init(&sm.full[i], 1); mbar_init(&sm.empty[i], 1); }
-        for (int i = 0; i < 2; ++i) {
-            mbar_init(&sm.main_full[i], 1);
-            mbar_init(&sm.main_empty[i], kEpiThreads);
-            mbar_init(&sm.corr_full[i], 1);
-            mbar_init(&sm.corr_empty[i], kEpiThreads);
-        }
+        for (int i = 0; i < kStages; ++i) { mbar_init(&sm.full[i], 1); mbar_init(&sm.empty[i], 1); mbar_init(&sm.out_empty[i], 8 / kCtas); mbar_init(&sm.peer_full[i], 1); }
+        for (uint32_t i = 0; i < kSums; ++i) { mbar_init(&sm.sum_full[i], 1); mbar_init(&sm.sum_empty[i], 8 * kCtas); }
         mbar_init(&sm.done, 1);
         sm.failed = 0;
     }
     if (warp == 1) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(&sm.tmem)) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        if constexpr (kCtas == 1) {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(&sm.tmem)) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(&sm.tmem)) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        }
     }
+    __syncwarp();
     tc_fence_before();
-    __syncthreads();
+    tile_sync<kCtas>();
     tc_fence_after();
-    const uint32_t tmem = sm.tmem;  // columns: main 0..127, 128..255; corrections 256..383, 384..511
+    const uint32_t tmem = sm.tmem;
     volatile uint32_t* failed = &sm.failed;
     MatView v;
 
     if (warp == 0 && lane == 0) {
-        uint32_t it = 0;
-        for (uint32_t g = blockIdx.x; g < total && !*failed; g += gridDim.x) {
-            const Task k = find_task(a, sm, n_tasks, n_mats, g, v);
-            const unsigned char *pa, *pb;
-            if (k.phase == kGram) {
-                pa = v.op.x + (uint64_t)k.i * (2 * v.s.nb) * kBlock;
-                pb = v.op.x + (uint64_t)k.j * (2 * v.s.nb) * kBlock;
-            } else if (k.phase == kPoly) {
-                pa = v.op.a + (uint64_t)k.i * (2 * v.s.mb) * kBlock;
-                pb = v.op.a + (uint64_t)k.j * (2 * v.s.mb) * kBlock;
-            } else {
-                const unsigned char* b = v.op.b + (uint64_t)k.i * (2 * v.s.mb) * kBlock;
-                const unsigned char* x = v.op.xt[k.step & 1u] + (uint64_t)k.j * (2 * v.s.mb) * kBlock;
-                pa = k.swap ? x : b;
-                pb = k.swap ? b : x;
-            }
-            const uint32_t bytes = (a.pairs >> k.step) & 1u ? kBlock : kPlane;
+        uint32_t it = 0, held[kStages] = {}, uses[2][kStages] = {};  // held: 1 operands, 2 the tile's own blocks
+        for (uint32_t g = group; g < total && !*failed; g += groups) {
+            const Task k = find_task<kCtas>(a, sm, n_tasks, n_mats, g, rank, v);
+            const Operand oa = operand<kCtas>(k, v, rank, 0), ob = operand<kCtas>(k, v, rank, 1);
+            const bool pairs = (a.pairs >> k.step) & 1u;
+            const uint32_t bytes = pairs ? kBlock : kPlane;
             if (!wait_tiles(a.ws.ctrl, k.mat, k.before, a.limit_ns)) { *failed = 1; break; }
-            fence_async_all();  // the blocks were written by ordinary stores of other SMs
-            for (uint32_t q = k.k0; q < k.k1; ++q, ++it) {
+            fence_async_all();  // orders what the counter says after the copies that follow
+            auto begin = [&](bool out) {
                 const uint32_t st = it % kStages;
-                if (it >= (uint32_t)kStages && !wait_for(&sm.empty[st], (it / kStages - 1) & 1u, a.limit_ns)) { *failed = 1; break; }
-                unsigned char* dst = ring + (size_t)st * kStageBytes;
-                mbar_arrive_expect_tx(&sm.full[st], 2 * bytes);
-                bulk_copy_g2s(dst, pa + (uint64_t)q * kBlock, bytes, &sm.full[st]);
-                bulk_copy_g2s(dst + kBlock, pb + (uint64_t)q * kBlock, bytes, &sm.full[st]);
+                bool free = true;
+                if (held[st] == 1) free = wait_for<kCtas>(&sm.empty[st], (uses[0][st] - 1) & 1u, a.limit_ns);
+                if (held[st] == 2) free = wait_for<kCtas>(&sm.out_empty[st], (uses[1][st] - 1) & 1u, a.limit_ns);
+                if (!free) { *failed = 1; return false; }
+                held[st] = out ? 2 : 1;
+                ++uses[out ? 1 : 0][st];
+                return true;
+            };
+            for (uint32_t q = k.k0; q < k.k1 && begin(false); ++q, ++it) {
+                unsigned char* dst = ring + (size_t)(it % kStages) * kStageBytes;
+                uint64_t* bar = &sm.full[it % kStages];
+                mbar_arrive_expect_tx(bar, k.diagonal ? bytes : 2 * bytes);
+                oa.fetch(dst, q, pairs, bar);
+                if (!k.diagonal) ob.fetch(dst + kBlock, q, pairs, bar);
+            }
+            const unsigned char* lin = linear_term(a, k, v);
+            for (uint32_t q = 0; q < kCtas && begin(true); ++q, ++it) {
+                uint64_t* bar = &sm.full[it % kStages];
+                if (lin) {
+                    mbar_arrive_expect_tx(bar, kStageBytes);
+                    bulk_copy_g2s(ring + (size_t)(it % kStages) * kStageBytes, lin + (uint64_t)q * kStageBytes, kStageBytes, bar);
+                } else {
+                    mbar_arrive(bar);  // nothing to fetch: the stage is there for the results
+                }
             }
         }
         // copies in flight end before the block does, whoever else has given up
         for (uint32_t q = it > (uint32_t)kStages ? it - kStages : 0; q < it; ++q) mbar_wait(&sm.full[q % kStages], (q / kStages) & 1u);
-    } else if (warp == 1 && lane == 0) {
-        uint32_t it = 0, chunk = 0, tile = 0;
-        for (uint32_t g = blockIdx.x; g < total && !*failed; g += gridDim.x) {
-            const Task k = find_task(a, sm, n_tasks, n_mats, g, v);
+    } else if (warp == 1 && lane == 0 && rank == 0) {
+        uint32_t it = 0, chunk = 0;
+        for (uint32_t g = group; g < total && !*failed; g += groups) {
+            const Task k = find_task<kCtas>(a, sm, n_tasks, n_mats, g, rank, v);
             const bool pairs = (a.pairs >> k.step) & 1u;
-            const uint32_t drain = pairs ? kDrain : k.k1 - k.k0;
-            const uint32_t tb = tile & 1u, corr = tmem + 256u + tb * 128u;
-            if (pairs && tile >= 2 && !wait_for(&sm.corr_empty[tb], (tile / 2 - 1) & 1u, a.limit_ns)) { *failed = 1; break; }
+            const uint32_t from_a = operand<kCtas>(k, v, rank, 0).from, from_b = operand<kCtas>(k, v, rank, 1).from;
             bool ok = true;
             for (uint32_t q = k.k0; q < k.k1; ++q, ++it) {
-                const uint32_t st = it % kStages, n = q - k.k0, in_chunk = n % drain;
-                const uint32_t cb = chunk & 1u, main = tmem + cb * 128u;
-                if (in_chunk == 0 && chunk >= 2 && !wait_for(&sm.main_empty[cb], (chunk / 2 - 1) & 1u, a.limit_ns)) { ok = false; break; }
-                if (!wait_for(&sm.full[st], (it / kStages) & 1u, a.limit_ns)) { ok = false; break; }
+                const uint32_t st = it % kStages, buf = chunk % kSums, d = tmem + buf * kCols;
+                const bool opens = pairs || q == k.k0, closes = pairs || q + 1 == k.k1;
+                if (opens && chunk >= kSums && !wait_for<kCtas>(&sm.sum_empty[buf], (chunk / kSums - 1) & 1u, a.limit_ns)) { ok = false; break; }
+                if (!wait_for<kCtas>(&sm.full[st], (it / kStages) & 1u, a.limit_ns)) { ok = false; break; }
+                if (kCtas == 2 && !wait_for<kCtas>(&sm.peer_full[st], (it / kStages) & 1u, a.limit_ns)) { ok = false; break; }
                 tc_fence_after();
-                const uint32_t at = smem_addr(ring + (size_t)st * kStageBytes);
-                const uint64_t ah = smem_desc(at), al = smem_desc(at + kPlane);
-                const uint64_t bh = smem_desc(at + kBlock), bl = smem_desc(at + kBlock + kPlane);
-#pragma unroll
-                for (uint32_t e = 0; e < 4; ++e) tc_mma(main, ah + 2 * e, bh + 2 * e, in_chunk + e > 0);
-                if (in_chunk == drain - 1 || q + 1 == k.k1) { tc_commit(&sm.main_full[cb]); ++chunk; }
+                const uint32_t at = smem_addr(ring + (size_t)st * kStageBytes), bt = k.diagonal ? at : at + kBlock;
+                const bool ta = q >= from_a, tb = q >= from_b;
+                const uint32_t instr = instr_desc<kCtas>(ta, tb);
+                const uint64_t ah = smem_desc(at, ta), bh = smem_desc(bt, tb), da = desc_step(ta), db = desc_step(tb);
+                const uint64_t al = ah + (kPlane >> 4), bl = bh + (kPlane >> 4);
                 if (pairs) {
+                    // the corrections first, 2^11 times too large; the first product of the hi planes scales them down
 #pragma unroll
-                    for (uint32_t e = 0; e < 4; ++e) tc_mma(corr, ah + 2 * e, bl + 2 * e, n + e > 0);
+                    for (uint32_t e = 0; e < 4; ++e) tc_mma<kCtas>(d, ah + e * da, bl + e * db, instr, e > 0);
 #pragma unroll
-                    for (uint32_t e = 0; e < 4; ++e) tc_mma(corr, al + 2 * e, bh + 2 * e, true);
+                    for (uint32_t e = 0; e < 4; ++e) tc_mma<kCtas>(d, al + e * da, bh + e * db, instr, true);
+                    tc_mma<kCtas, kLoBits>(d, ah, bh, instr, true);
+#pragma unroll
+                    for (uint32_t e = 1; e < 4; ++e) tc_mma<kCtas>(d, ah + e * da, bh + e * db, instr, true);
+                } else {
+#pragma unroll
+                    for (uint32_t e = 0; e < 4; ++e) tc_mma<kCtas>(d, ah + e * da, bh + e * db, instr, !opens || e > 0);
                 }
-                tc_commit(&sm.empty[st]);
+                if (closes) { tc_commit<kCtas>(&sm.sum_full[buf]); ++chunk; }
+                tc_commit<kCtas>(&sm.empty[st]);
             }
             if (!ok) { *failed = 1; break; }
-            if (pairs) { tc_commit(&sm.corr_full[tb]); ++tile; }
+            // the stages of the tile's own blocks pass from the copies to warps 2..9
+            for (uint32_t q = 0; q < kCtas; ++q, ++it)
+                if (kCtas == 2 && !wait_for<kCtas>(&sm.peer_full[it % kStages], (it / kStages) & 1u, a.limit_ns)) { *failed = 1; break; }
         }
-        tc_commit(&sm.done);
+        tc_commit<kCtas>(&sm.done);
         mbar_wait(&sm.done, 0);
+    } else if (kCtas == 2 && warp == 1 && lane == 0) {
+        // the pair's second block tells the first which of its stages are full
+        uint32_t it = 0;
+        for (uint32_t g = group; g < total && !*failed; g += groups) {
+            const Task k = find_task<kCtas>(a, sm, n_tasks, n_mats, g, rank, v);
+            const uint32_t n = k.k1 - k.k0 + kCtas;
+            for (uint32_t q = 0; q < n; ++q, ++it) {
+                if (!wait_for<kCtas>(&sm.full[it % kStages], (it / kStages) & 1u, a.limit_ns)) { *failed = 1; break; }
+                mbar_arrive_first<kCtas>(&sm.peer_full[it % kStages]);
+            }
+        }
     } else if (warp >= 2) {
-        const uint32_t et = threadIdx.x - 64u, quad = warp & 3u, half = (warp - 2u) >> 2;
-        const uint32_t row = quad * 32u + lane;
-        const uint32_t lane_base = tmem + ((quad * 32u) << 16) + half * 64u;
-        uint32_t chunk = 0, tile = 0;
-        for (uint32_t g = blockIdx.x; g < total; g += gridDim.x) {
-            const Task k = find_task(a, sm, n_tasks, n_mats, g, v);
-            const bool pairs = (a.pairs >> k.step) & 1u;
-            const uint32_t drain = pairs ? kDrain : k.k1 - k.k0;
-            float acc[64];
+        constexpr int kAcc = 64 * kCtas;  // columns of this warp
+        const uint32_t quad = warp & 3u, half = (warp - 2u) >> 2, row = quad * 32u + lane;
+        const uint32_t lane_base = tmem + ((quad * 32u) << 16) + half * kAcc;
+        uint32_t it = 0, chunk = 0;
+        for (uint32_t g = group; g < total; g += groups) {
+            if (lane == 0) sm.task[warp - 2] = find_task<kCtas>(a, sm, n_tasks, n_mats, g, rank, sm.view[warp - 2]);
+            __syncwarp();
+            const Task& k = sm.task[warp - 2];
+            const MatView& v = sm.view[warp - 2];
+            const uint32_t chunks = (a.pairs >> k.step) & 1u ? k.k1 - k.k0 : 1u;
+            float acc[kAcc];
 #pragma unroll
-            for (int i = 0; i < 64; ++i) acc[i] = 0.0f;
+            for (int i = 0; i < kAcc; ++i) acc[i] = 0.0f;
             bool ok = true;
-            for (uint32_t q = k.k0; q < k.k1; q += drain, ++chunk) {
-                const uint32_t cb = chunk & 1u;
-                ok = wait_for(&sm.main_full[cb], (chunk / 2) & 1u, a.limit_ns);
+            for (uint32_t q = 0; q < chunks; ++q, ++chunk) {
+                const uint32_t buf = chunk % kSums;
+                ok = wait_for<kCtas>(&sm.sum_full[buf], (chunk / kSums) & 1u, a.limit_ns);
                 if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
                 tc_fence_after();
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
+                for (int h = 0; h < kAcc / 32; ++h) {
                     float w[32];
-                    tc_load32(lane_base + cb * 128u + h * 32u, w);
+                    tc_load32(lane_base + buf * kCols + h * 32u, w);
 #pragma unroll
                     for (int i = 0; i < 32; ++i) acc[h * 32 + i] = __fadd_rn(acc[h * 32 + i], w[i]);
                 }
                 tc_fence_before();
-                mbar_arrive(&sm.main_empty[cb]);
+                __syncwarp();
+                if (lane == 0) mbar_arrive_first<kCtas>(&sm.sum_empty[buf]);
             }
-            if (ok && pairs) {
-                const uint32_t tb = tile & 1u;
-                ok = __all_sync(0xffffffffu, wait_for(&sm.corr_full[tb], (tile / 2) & 1u, a.limit_ns));
-                if (ok) {
-                    tc_fence_after();
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        float w[32];
-                        tc_load32(lane_base + 256u + tb * 128u + h * 32u, w);
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) acc[h * 32 + i] = __fmaf_rn(w[i], 1.0f / kLoScale, acc[h * 32 + i]);
-                    }
-                    tc_fence_before();
-                    mbar_arrive(&sm.corr_empty[tb]);
-                    ++tile;
-                }
-            }
-            if (epi_any(!ok)) { *failed = 1; break; }
+            // the stage with this warp's columns of the tile's own blocks
+            const uint32_t out_it = it + (k.k1 - k.k0) + (kCtas == 1 ? 0u : half), out_st = out_it % kStages;
+            it += k.k1 - k.k0 + kCtas;
+            ok = ok && wait_for<kCtas>(&sm.full[out_st], (out_it / kStages) & 1u, a.limit_ns);
+            if (!__all_sync(0xffffffffu, ok)) { *failed = 1; break; }
 
+            bool mine = true;  // this warp finishes its part of the tile
             if (k.parts > 1) {
-                // this part's sums into its slot; the part that arrives last adds all of them in order
-                float* mine = a.ws.slots + ((uint64_t)v.t.slot0 + k.tile * k.parts + k.part) * (128 * 128);
+                // the sums of this part of the summed dimension into its slot; whoever arrives last adds all of them
+                // in order
+                const uint64_t slot0 = v.t.slot0 + ((uint64_t)k.tile * kCtas + rank) * k.parts;
+                float* to = a.ws.slots + (slot0 + k.part) * (128 * kCols);
 #pragma unroll
-                for (int i = 0; i < 64; ++i) __stcg(mine + (half * 64 + i) * 128 + row, acc[i]);
+                for (int i = 0; i < kAcc; ++i) __stcg(to + (half * kAcc + i) * 128 + row, acc[i]);
                 __threadfence();
-                epi_sync();
-                if (et == 0) {
-                    const uint32_t sym = v.s.mb * (v.s.mb + 1) / 2;
-                    const uint32_t old = atomicAdd(a.ws.arrive + v.t.arrive0 + k.phase * sym + k.tile, 1u);
+                __syncwarp();
+                uint32_t old = 0;
+                if (lane == 0) {
+                    const uint32_t sym = v.s.mt * (v.s.mt + 1) / 2;
+                    old = atomicAdd(a.ws.arrive + v.t.arrive0 + ((k.phase * sym + k.tile) * kCtas + rank) * 8 + warp - 2, 1u);
                     __threadfence();
-                    sm.last = old == k.step * k.parts + k.parts - 1 ? 1u : 0u;
                 }
-                epi_sync();
-                if (!sm.last) continue;
+                old = __shfl_sync(0xffffffffu, old, 0);
+                mine = old == k.step * k.parts + k.parts - 1;
+                if (mine) {
 #pragma unroll
-                for (int i = 0; i < 64; ++i) acc[i] = 0.0f;
-                for (uint32_t p = 0; p < k.parts; ++p) {
-                    const float* from = a.ws.slots + ((uint64_t)v.t.slot0 + k.tile * k.parts + p) * (128 * 128);
+                    for (int i = 0; i < kAcc; ++i) acc[i] = 0.0f;
+                    for (uint32_t p = 0; p < k.parts; ++p) {
+                        const float* from = a.ws.slots + (slot0 + p) * (128 * kCols);
 #pragma unroll
-                    for (int i = 0; i < 64; ++i) acc[i] = __fadd_rn(acc[i], __ldcg(from + (half * 64 + i) * 128 + row));
+                        for (int i = 0; i < kAcc; ++i) acc[i] = __fadd_rn(acc[i], __ldcg(from + (half * kAcc + i) * 128 + row));
+                    }
                 }
             }
 
-            const float s_val = orth_s(v.s), inv_s = 1.0f / s_val;
-            const bool last = k.phase == kApply && k.step + 1 == a.ns.steps;
-            const float ca = a.ns.coef[k.step][0], cb = a.ns.coef[k.step][1], cc = a.ns.coef[k.step][2];
-            const uint32_t row_blk = k.swap ? k.j : k.i, col_blk = k.swap ? k.i : k.j;
-            const uint32_t n_rows = k.phase == kApply ? (k.swap ? v.s.n : v.s.m) : v.s.m;
-            const uint32_t n_cols = k.phase == kApply ? (k.swap ? v.s.m : v.s.n) : v.s.m;
-            // rows and columns up to a multiple of 64 are written: beyond, no product reads them
-            const uint32_t rows_used = n_rows - row_blk * 128u > 64u ? 128u : 64u;
-            const uint32_t halves = n_cols - col_blk * 128u > 64u ? 2u : 1u;
-            // the tile's own blocks: linear term, destination, destination of the transposed tile
-            const uint64_t at_m = ((uint64_t)k.i * (2 * v.s.mb) + 2 * k.j) * kBlock;  // in an m x m operand
-            const uint64_t at_mt = ((uint64_t)k.j * (2 * v.s.mb) + 2 * k.i) * kBlock;
-            const uint64_t at_x = ((uint64_t)k.i * (2 * v.s.nb) + 2 * k.j) * kBlock;
-            const unsigned char* lin = nullptr;
-            unsigned char *dst = nullptr, *dst_t = nullptr;
-            float fl, fa;  // value = fl * linear + fa * sum
-            if (k.phase == kGram) {
-                dst = v.op.a + at_m;
-                dst_t = k.i != k.j ? v.op.a + at_mt : nullptr;
-                fl = 0.0f; fa = inv_s;
-            } else if (k.phase == kPoly) {
-                lin = v.op.a + at_m;
-                dst = v.op.b + at_m;
-                dst_t = k.i != k.j ? v.op.b + at_mt : nullptr;
-                fl = cb; fa = __fmul_rn(cc, inv_s);
-            } else {
-                lin = k.swap ? v.op.xt[k.step & 1u] + at_mt : v.op.x + at_x;
-                dst = last ? nullptr : v.op.x + at_x;
-                dst_t = last ? nullptr : v.op.xt[(k.step & 1u) ^ 1u] + at_mt;
-                fl = ca; fa = inv_s;
+            const bool last = k.phase == kApply && k.step + 1 == a.ns.steps, has_lin = k.phase == kPoly || (k.phase == kApply && adds_x(a, k.step));
+            const uint32_t n_rows = k.swap ? v.s.n : v.s.m, n_cols = k.phase == kApply && !k.swap ? v.s.n : v.s.m;
+            const uint32_t row0 = k.rb * 128u, col0 = k.cb * 128u;
+            // Rows and columns up to a multiple of 64 are written: beyond, no product reads them.
+            const bool rows_used = row0 + (quad & 2u) * 32u < n_rows;
+            if (mine && rows_used) {
+                const float inv_s = 1.0f / orth_s(v.s);
+                float fl = 0.0f, fa = inv_s;  // value = fl * linear + fa * sum
+                if (k.phase == kPoly) { fl = a.ns.coef[k.step][1]; fa = __fmul_rn(a.ns.coef[k.step][2], inv_s); }
+                if (k.phase == kApply) fl = a.ns.coef[k.step][0];
                 if (last) {
                     const float f = __fmul_rn(v.t.scale, inv_s);
                     fl = __fmul_rn(fl, f);
                     fa = __fmul_rn(fa, f);
                 }
-            }
-            for (uint32_t h = 0; h < halves; ++h) {
-                if (half == h) {
+                // B takes a I in where the apply product does not add a X
+                const bool add_diag = k.phase == kPoly && k.diagonal && !adds_x(a, k.step);
+                const float diag = __fmul_rn(a.ns.coef[k.step][0], orth_s(v.s));
+                unsigned char* dst = nullptr;  // this block's part of the tile, 2 kCtas blocks in a row
+                if (k.phase != kApply) dst = (k.phase == kGram ? v.op.a : v.op.b) + ((uint64_t)k.rb * (2 * v.s.mb) + 2 * k.cb) * kBlock;
+                else if (!last) dst = v.op.x[(k.step & 1u) ^ 1u] + ((uint64_t)k.rb * (2 * v.s.nb) + 2 * k.cb) * kBlock;
 #pragma unroll
-                    for (int i = 0; i < 64; ++i) stage[i * kPitch + row] = acc[i];
-                }
-                epi_sync();
-                for (uint32_t i = et; i < rows_used * 8u; i += kEpiThreads) {
-                    const uint32_t r = i >> 3, piece = i & 7u;
-                    const uint64_t at = (uint64_t)h * kBlock + swizzled(r, piece);
-                    float w[8], l[8];
-                    if (lin) join8(__ldcg(reinterpret_cast<const uint4*>(lin + at)), __ldcg(reinterpret_cast<const uint4*>(lin + at + kPlane)), l);
+                for (int h = 0; h < kCtas; ++h) {  // 64 columns, one block, at a time
+                    const uint32_t cg = half * kCtas + h, c0 = col0 + cg * 64u;
+                    if (c0 >= n_cols) break;
+                    unsigned char* own = ring + (size_t)out_st * kStageBytes + (cg & 1u) * kBlock;
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        w[e] = __fmul_rn(fa, stage[(piece * 8 + e) * kPitch + r]);
-                        if (lin) w[e] = __fmaf_rn(fl, l[e], w[e]);
-                    }
-                    if (last) {
+                    for (int p = 0; p < 8; ++p) {
+                        float* w = acc + h * 64 + p * 8;
+                        const uint32_t at = swizzled(row, p);
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) stage[(piece * 8 + e) * kPitch + r] = w[e];
-                    } else {
-                        uint4 hi, lo;
-                        split8(w, hi, lo);
-                        *reinterpret_cast<uint4*>(dst + at) = hi;
-                        *reinterpret_cast<uint4*>(dst + at + kPlane) = lo;
-                        if (dst_t) {
-                            const uint32_t hs[4] = {hi.x, hi.y, hi.z, hi.w}, ls[4] = {lo.x, lo.y, lo.z, lo.w};
+                        for (int e = 0; e < 8; ++e) w[e] = __fmul_rn(fa, w[e]);
+                        if (has_lin) {
+                            float l[8];
+                            join8(*reinterpret_cast<const uint4*>(own + at), *reinterpret_cast<const uint4*>(own + at + kPlane), l);
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) w[e] = __fmaf_rn(fl, l[e], w[e]);
+                        }
+                        if (add_diag) {
 #pragma unroll
                             for (int e = 0; e < 8; ++e)
-                                stage[(piece * 8 + e) * kPitch + r] = __uint_as_float(__byte_perm(hs[e / 2], ls[e / 2], e & 1 ? 0x7632 : 0x5410));
+                                if (c0 + p * 8 + e == row0 + row) w[e] = __fadd_rn(w[e], diag);
+                        }
+                        if (!last) {
+                            uint4 hi, lo;
+                            split8(w, hi, lo);
+                            *reinterpret_cast<uint4*>(own + at) = hi;
+                            *reinterpret_cast<uint4*>(own + at + kPlane) = lo;
                         }
                     }
-                }
-                epi_sync();
-                if (last) {
-                    const uint32_t c = row_blk * 128u + (et & 127u);
-                    if (c < v.t.cols) {
-                        for (uint32_t i = et >> 7; i < 64u; i += 2) {
-                            const uint32_t r = col_blk * 128u + h * 64u + i;
-                            if (r >= v.t.rows) break;
-                            const float o = stage[i * kPitch + (et & 127u)];
-                            const uint64_t at = v.t.out_off + (uint64_t)r * v.t.out_stride + c;
-                            if (a.out_kind == kOutF32) static_cast<float*>(a.out)[at] = o;
-                            else if (a.out_kind == kOutF16) static_cast<__half*>(a.out)[at] = __float2half_rn(o);
-                            else if (a.out_kind == kOutBf16) static_cast<__nv_bfloat16*>(a.out)[at] = __float2bfloat16_rn(o);
-                            else {
-                                float* p = static_cast<float*>(a.out) + at;
-                                *p = __fmaf_rn(-a.lr, o, __fmul_rn(a.shrink, *p));
-                            }
+                    if (!last) {
+                        fence_async_smem();
+                        __syncwarp();
+                        if (lane < 2) {  // 32 rows of either plane lie in a row
+                            const uint32_t off = lane * kPlane + quad * 32u * 128u;
+                            bulk_copy_s2g(dst + (uint64_t)cg * kBlock + off, own + off, 32u * 128u);
+                            bulk_stores_commit();
                         }
-                    }
-                } else if (dst_t) {
-                    for (uint32_t i = et; i < 64u * 16u; i += kEpiThreads) {
-                        const uint32_t c = i >> 4, piece = i & 15u;
-                        if (piece * 8u >= rows_used) continue;
-                        uint32_t hs[4], ls[4];
+                    } else {
+                        // the tile's rows run along the caller's rows, its columns across them
+                        const uint32_t c = row0 + row;
+                        const uint64_t first = v.t.out_off + (uint64_t)c0 * v.t.out_stride + c;
+                        const uint32_t n = c < v.t.cols ? min(64u, v.t.rows - c0) : 0u;
+                        if (a.out_kind == kOutParams) {
+                            float* out = static_cast<float*>(a.out) + first;
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const uint32_t p = __float_as_uint(stage[c * kPitch + piece * 8 + 2 * e]);
-                            const uint32_t q = __float_as_uint(stage[c * kPitch + piece * 8 + 2 * e + 1]);
-                            hs[e] = __byte_perm(p, q, 0x5410);
-                            ls[e] = __byte_perm(p, q, 0x7632);
+                            for (int i0 = 0; i0 < 64; i0 += 16) {
+                                float old[16];
+#pragma unroll
+                                for (int i = 0; i < 16; ++i) old[i] = (uint32_t)(i0 + i) < n ? out[(uint64_t)(i0 + i) * v.t.out_stride] : 0.0f;
+#pragma unroll
+                                for (int i = 0; i < 16; ++i)
+                                    if ((uint32_t)(i0 + i) < n) out[(uint64_t)(i0 + i) * v.t.out_stride] = __fmaf_rn(-a.lr, acc[h * 64 + i0 + i], __fmul_rn(a.shrink, old[i]));
+                            }
+                        } else if (a.out_kind == kOutF32) {
+                            float* out = static_cast<float*>(a.out) + first;
+#pragma unroll
+                            for (int i = 0; i < 64; ++i)
+                                if ((uint32_t)i < n) out[(uint64_t)i * v.t.out_stride] = acc[h * 64 + i];
+                        } else {
+                            uint16_t* out = static_cast<uint16_t*>(a.out) + first;
+                            const bool f16 = a.out_kind == kOutF16;
+#pragma unroll
+                            for (int i = 0; i < 64; ++i)
+                                if ((uint32_t)i < n)
+                                    out[(uint64_t)i * v.t.out_stride] = f16 ? __half_as_ushort(__float2half_rn(acc[h * 64 + i]))
+                                                                            : __bfloat16_as_ushort(__float2bfloat16_rn(acc[h * 64 + i]));
                         }
-                        unsigned char* to = dst_t + (uint64_t)(piece >> 3) * kBlock + swizzled(h * 64u + c, piece & 7u);
-                        *reinterpret_cast<uint4*>(to) = make_uint4(hs[0], hs[1], hs[2], hs[3]);
-                        *reinterpret_cast<uint4*>(to + kPlane) = make_uint4(ls[0], ls[1], ls[2], ls[3]);
                     }
                 }
-                if (h + 1 < halves) epi_sync();
             }
-            if (!last) {
-                fence_async_all();  // the next products fetch these blocks with bulk copies
-                __threadfence();
-                epi_sync();
-                if (et == 0) asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(&a.ws.ctrl->done[k.mat]) : "memory");
-            } else {
-                epi_sync();  // the staged half is free again
+            // the ring's stage is free as soon as the copies have read it, the tile finished when they have written it
+            if (last) fence_async_smem();
+            if (lane < 2) bulk_stores_read();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sm.out_empty[out_st]);
+            if (mine && !last) {
+                if (lane < 2) {
+                    bulk_stores_done();
+                    fence_async_all();
+                    __threadfence();
+                }
+                __syncwarp();
+                if (lane == 0) asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(&a.ws.ctrl->done[k.mat]) : "memory");
             }
+            __syncwarp();
         }
     }
-    __syncthreads();
-    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+    __syncwarp();
+    tile_sync<kCtas>();
+    if (warp == 1) {
+        if constexpr (kCtas == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+        else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+    }
     if (threadIdx.x == 0 && *failed) {
         a.ws.ctrl->abort = 1u;
         __threadfence();
@@ -821,6 +980,7 @@ struct WsPlan {
 struct BatchNeeds {
     uint64_t slots, blocks;  // workspace
     uint64_t work;           // stages of one step
+    uint64_t ns;             // their time, about
 };
 WsPlan ws_plan(const OrthBatch* b, const BatchNeeds& needs) {
     WsPlan w;
@@ -829,7 +989,7 @@ WsPlan ws_plan(const OrthBatch* b, const BatchNeeds& needs) {
     w.arrive = w.ctrl + up256(sizeof(OrthCtrl));
     w.partial = w.arrive + up256(b ? 4ull * b->n_arrive : 0);
     w.slots = w.partial + up256(b ? 8ull * b->n_chunks : 0);
-    w.blocks = w.slots + needs.slots * (128 * 128 * 4);
+    w.blocks = w.slots + needs.slots * (128ull * 128 * 4);
     w.total = w.blocks + needs.blocks * kBlock;
     return w;
 }
@@ -837,24 +997,28 @@ WsPlan ws_plan(const OrthBatch* b, const BatchNeeds& needs) {
 // A tile whose sum is long is split so that the tasks of a phase are about as long as the phase's work spread over
 // all SMs, but no part is shorter than kMinPart stages.
 constexpr uint64_t kPlanSms = 148, kMinPart = 8, kMaxParts = 16;
+// Time of a stage of a 128 x 128 tile and of a 256 x 256 tile of two blocks, in nanoseconds.
+constexpr uint64_t kStageNs[2] = {900, 900};
 
-// Takes matrices from `at` on into one batch; returns how many, 0 if one is unusable.
-uint32_t make_batch(const co3_mat* in, const co3_mat* out, uint32_t n_mats, uint32_t at, bool muon, OrthBatch* b,
+// Takes matrices from `at` on into one batch with the given number of blocks per tile; returns how many, 0 if one is
+// unusable.
+uint32_t plan_batch(const co3_mat* in, const co3_mat* out, uint32_t n_mats, uint32_t at, bool muon, uint32_t ctas, OrthBatch* b,
                     BatchNeeds* needs) {
     uint32_t n = 0;
     uint64_t work[3] = {0, 0, 0};
+    const uint64_t units = kPlanSms / ctas;
     for (; at + n < n_mats && n < kOrthMats; ++n) {
         const co3_mat &ti = in[at + n], &to = out[at + n];
         if (!valid_mat(ti) || !valid_mat(to) || ti.rows != to.rows || ti.cols != to.cols) return 0;
         const bool plain = (to.flags & CO3_MAT_PLAIN) != 0u;
         if (plain && !muon) return 0;
         if (plain || ti.rows == 0 || ti.cols == 0) continue;
-        const OrthShape s = orth_shape(ti.rows, ti.cols);
-        const uint64_t sym = (uint64_t)s.mb * (s.mb + 1) / 2, km = (s.m + 63u) / 64u, kn = (s.n + 63u) / 64u;
-        if (sym >= (1u << 24) || (uint64_t)s.mb * s.nb >= (1u << 24)) return 0;
+        const OrthShape s = orth_shape(ti.rows, ti.cols, ctas);
+        const uint64_t sym = (uint64_t)s.mt * (s.mt + 1) / 2, km = (s.m + 63u) / 64u, kn = (s.n + 63u) / 64u;
+        if (sym >= (1u << 24) || (uint64_t)s.mt * s.nt >= (1u << 24)) return 0;
         work[kGram] += sym * kn;
         work[kPoly] += sym * km;
-        work[kApply] += (uint64_t)s.mb * s.nb * km;
+        work[kApply] += (uint64_t)s.mt * s.nt * km;
     }
     uint64_t chunks = 0, full = 0, arrive = 0, slots = 0, blocks = 0, tasks[3] = {0, 0, 0};
     for (uint32_t k = 0; k < n; ++k) {
@@ -873,19 +1037,19 @@ uint32_t make_batch(const co3_mat* in, const co3_mat* out, uint32_t n_mats, uint
         if (ti.rows == 0 || ti.cols == 0) continue;
         chunks += ((uint64_t)ti.rows * ti.cols + kBeginElems - 1) / kBeginElems;
         if (!plain) {
-            const OrthShape s = orth_shape(ti.rows, ti.cols);
-            const uint64_t sym = (uint64_t)s.mb * (s.mb + 1) / 2;
+            const OrthShape s = orth_shape(ti.rows, ti.cols, ctas);
+            const uint64_t sym = (uint64_t)s.mt * (s.mt + 1) / 2, all = (uint64_t)s.mt * s.nt;
             uint64_t most = 0;
             for (int p = 0; p < 3; ++p) {
-                const uint64_t depth = ((p == kGram ? s.n : s.m) + 63u) / 64u, tiles = p == kApply ? (uint64_t)s.mb * s.nb : sym;
-                const uint64_t part = std::max(kMinPart, (work[p] + kPlanSms - 1) / kPlanSms);
+                const uint64_t depth = ((p == kGram ? s.n : s.m) + 63u) / 64u, tiles = p == kApply ? all : sym;
+                const uint64_t part = std::max(kMinPart, (work[p] + units - 1) / units);
                 const uint64_t parts = std::min(kMaxParts, std::max<uint64_t>(1, depth / part));
                 m.splits[p] = (uint32_t)parts;
                 tasks[p] += tiles * parts;
-                if (parts > 1) most = std::max(most, tiles * parts);
+                if (parts > 1) most = std::max(most, tiles * parts * ctas);
             }
             slots += most;
-            arrive += 2 * sym + (uint64_t)s.mb * s.nb;
+            arrive += (2 * sym + all) * ctas * 8;
             full += (uint64_t)s.mb * s.nb;
             blocks += orth_blocks(s);
         }
@@ -895,11 +1059,26 @@ uint32_t make_batch(const co3_mat* in, const co3_mat* out, uint32_t n_mats, uint
     b->n_chunks = (uint32_t)chunks;
     b->n_full = (uint32_t)full;
     b->n_arrive = (uint32_t)arrive;
-    for (int p = 0; p < 3; ++p) b->n_tasks[p] = (uint32_t)tasks[p];
+    uint64_t ns = 0;
+    for (int p = 0; p < 3; ++p) {
+        b->n_tasks[p] = (uint32_t)tasks[p];
+        if (tasks[p]) ns += (tasks[p] + units - 1) / units * work[p] * kStageNs[ctas - 1] / tasks[p];
+    }
     b->index0 = at;
     b->first = at == 0 ? 1u : 0u;
-    *needs = {slots, blocks, work[0] + work[1] + work[2]};
+    b->ctas = ctas;
+    *needs = {slots * ctas, blocks, work[0] + work[1] + work[2], ns};
     return n;
+}
+
+// The number of blocks per tile that takes less time.
+uint32_t make_batch(const co3_mat* in, const co3_mat* out, uint32_t n_mats, uint32_t at, bool muon, OrthBatch* b, BatchNeeds* needs) {
+    BatchNeeds two;
+    const uint32_t n = plan_batch(in, out, n_mats, at, muon, 2, b, &two);
+    if (n == 0) return 0;
+    const uint32_t m = plan_batch(in, out, n_mats, at, muon, 1, b, needs);
+    if (m != 0 && needs->ns <= two.ns) return m;
+    return plan_batch(in, out, n_mats, at, muon, 2, b, needs);
 }
 
 bool valid_ns(const co3_ns& ns) {
@@ -911,12 +1090,51 @@ bool valid_ns(const co3_ns& ns) {
         double x = i / 4096.0;
         for (uint32_t k = 0; k < ns.steps; ++k) {
             const double q = x * x, g = q * (ns.coef[k][1] + q * ns.coef[k][2]);
-            if (!(fabs(g) <= 4.0)) return false;
+            if (!(fabs(g) <= 4.0) || !(fabs(ns.coef[k][0] + g) <= 4.0)) return false;
             x *= ns.coef[k][0] + g;
             if (!(fabs(x) <= 2.0)) return false;
         }
     }
     return true;
+}
+
+// All blocks have to be resident at once: as many tiles at a time as the device holds, asked for once per device.
+template <int kCtas>
+int launch_steps(const StepArgs& a, uint32_t widest, cudaStream_t st) {
+    static std::atomic<int> resident[64];
+    int dev = 0;
+    CO3_CUDA(cudaGetDevice(&dev));
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(kCtas);
+    cfg.blockDim = dim3(kStepThreads);
+    cfg.dynamicSmemBytes = kStepSmem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeCooperative;
+    attr[0].val.cooperative = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = kCtas;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = kCtas == 1 ? 1 : 2;
+    int n = dev < 64 ? resident[dev].load(std::memory_order_relaxed) : 0;
+    if (n == 0) {
+        CO3_CUDA(cudaFuncSetAttribute(orth_steps_kernel<kCtas>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kStepSmem));
+        if (kCtas == 1) {
+            CO3_CUDA(cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev));
+        } else {
+            cfg.attrs = attr + 1;
+            cfg.numAttrs = 1;
+            CO3_CUDA(cudaOccupancyMaxActiveClusters(&n, orth_steps_kernel<kCtas>, &cfg));
+            cfg.attrs = attr;
+            cfg.numAttrs = 2;
+        }
+        if (n < 1) return CO3_ERR_CUDA;
+        if (dev < 64) resident[dev].store(n, std::memory_order_relaxed);
+    }
+    cfg.gridDim = dim3(kCtas * std::min(widest, (uint32_t)n));
+    CO3_CUDA(cudaLaunchKernelEx(&cfg, orth_steps_kernel<kCtas>, a));
+    return CO3_OK;
 }
 
 struct OrthCall {
@@ -952,9 +1170,6 @@ int orth_run(const OrthCall& c, const co3_ns* ns_in, co3_result* res, void* work
     }
     const uint64_t least = ws_plan(nullptr, BatchNeeds{}).total;
     if (workspace_bytes < (need > least ? need : least)) return CO3_ERR_CAPACITY;
-    int dev = 0, sms = 0;
-    CO3_CUDA(cudaGetDevice(&dev));
-    CO3_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     uint32_t at = 0;
     do {
@@ -989,18 +1204,8 @@ int orth_run(const OrthCall& c, const co3_ns* ns_in, co3_result* res, void* work
             sa.limit_ns = 500000000ull + ns.steps * needs.work * 64ull;
             sa.res = res;
             const uint32_t widest = std::max(batch.n_tasks[0], std::max(batch.n_tasks[1], batch.n_tasks[2]));
-            cudaLaunchConfig_t cfg = {};
-            cfg.gridDim = dim3(std::min(widest, (uint32_t)sms));
-            cfg.blockDim = dim3(kStepThreads);
-            cfg.dynamicSmemBytes = kStepSmem;
-            cfg.stream = st;
-            cudaLaunchAttribute attr[1];
-            attr[0].id = cudaLaunchAttributeCooperative;
-            attr[0].val.cooperative = 1;
-            cfg.attrs = attr;
-            cfg.numAttrs = 1;
-            CO3_CUDA(cudaFuncSetAttribute(orth_steps_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kStepSmem));
-            CO3_CUDA(cudaLaunchKernelEx(&cfg, orth_steps_kernel, sa));
+            const int e = batch.ctas == 1 ? launch_steps<1>(sa, widest, st) : launch_steps<2>(sa, widest, st);
+            if (e != CO3_OK) return e;
         }
         at += k;
     } while (at < c.n_mats);
