@@ -6,8 +6,8 @@ import subprocess
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_PKG)
-SOURCES = [os.path.join(_PKG, "csrc", f) for f in ("co3_kernels.cu", "co3_orth.cu", "co3_norm.cu", "co3_code_build.cc")]
-HEADERS = [os.path.join(_PKG, "csrc", f) for f in ("co3_device.cuh", "co3_launch.cuh", "co3_types.cuh")] + [os.path.join(_ROOT, "include", "co3.h")]
+SOURCES = [os.path.join(_PKG, "csrc", f) for f in ("co3_kernels.cu", "co3_orth.cu", "co3_orth_small.cu", "co3_norm.cu", "co3_code_build.cc")]
+HEADERS = [os.path.join(_PKG, "csrc", f) for f in ("co3_device.cuh", "co3_launch.cuh", "co3_orth.cuh", "co3_orth_small.h", "co3_types.cuh")] + [os.path.join(_ROOT, "include", "co3.h")]
 LIB = os.path.join(_PKG, "libco3.so")
 
 NVCC_FLAGS = [

@@ -5,14 +5,6 @@
 //   orth_load_kernel    X_0 = G / (norm + eps) as operand blocks
 //   orth_steps_kernel   all products of all steps in one cooperative launch: per step A = X X^T; B = b A + c A A;
 //                       X <- a X + B X; the last product writes the result (or steps the parameters) instead of X
-//
-// Operands live in the workspace as blocks of 128 rows x 64 columns, each a pair of fp16 planes of 16 KB: hi = the
-// value rounded, lo = 2^11 times the remainder rounded, together 22 significant bits.  A plane is stored exactly as
-// the tensor core wants it in shared memory (128-byte rows, 16-byte pieces XORed with the row number modulo 8), so
-// that a tile is fetched by plain bulk copies, and padding of the matrix to whole blocks is stored as zeros.  The same
-// bytes serve as the transposed operand (a row of the block runs along the operand's rows instead of along the sum): X is
-// not stored transposed, and of the symmetric A and B only the tiles on and below the diagonal are computed and stored.
-// A product is hi*hi + 2^-11 (hi*lo + lo*hi): the part left out, lo*lo, is below 2^-22 of the whole.
 #include <cuda_runtime.h>
 #include <math.h>
 #include <stddef.h>
@@ -24,21 +16,16 @@
 #include "co3.h"
 #include "co3_device.cuh"
 #include "co3_launch.cuh"
+#include "co3_orth.cuh"
+#include "co3_orth_small.h"
 #include "co3_types.cuh"
 
 namespace co3 {
 
 constexpr uint32_t kOrthMats = 96;                  // matrices of one batch of launches
-constexpr uint32_t kPlane = 128 * 64 * 2;           // bytes of a plane of a block
-constexpr uint32_t kBlock = 2 * kPlane;             // hi, then lo
-constexpr uint32_t kHalfPlane = kPlane / 2;         // 64 rows
 constexpr uint32_t kBeginElems = 8192;              // elements per block of orth_begin_kernel
 constexpr int kBeginThreads = 256;
 constexpr int kLoadThreads = 256;
-constexpr int kLoBits = 11;
-constexpr float kLoScale = 2048.0f;
-constexpr int kMaxLogS = 13;                        // values are held times S = 2^min(13, log2 sqrt(m n)): entries about 1
-
 enum OrthPhase { kGram = 0, kPoly = 1, kApply = 2 };
 
 struct OrthMat {
@@ -114,13 +101,6 @@ __device__ inline OrthOperands orth_operands(const OrthWs& ws, const OrthMat& t,
     o.a = o.x[1] + xs;
     o.b = o.a + 2ull * s.mb * s.mb * kBlock;
     return o;
-}
-
-__host__ __device__ inline float orth_s(const OrthShape& s) {
-    const uint64_t p = (uint64_t)s.m * s.n;
-    int k = 0;
-    while (k < kMaxLogS && (1ull << (2 * (k + 1))) <= p) ++k;
-    return (float)(1u << k);
 }
 
 // Index of the matrix that owns item `x`: largest k with first(k) <= x.  Matrices without items are skipped because
@@ -223,33 +203,6 @@ struct LoadArgs {
     OrthWs ws;
 };
 
-__device__ __forceinline__ uint32_t swizzled(uint32_t row, uint32_t piece) { return row * 128u + ((piece ^ (row & 7u)) << 4); }
-
-// hi and lo of eight values, as 16-byte pieces.
-__device__ __forceinline__ void split8(const float* v, uint4& hi, uint4& lo) {
-    uint32_t h[4], l[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const __half2 a = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
-        const float2 f = __half22float2(a);
-        const __half2 b = __floats2half2_rn(__fmul_rn(__fsub_rn(v[2 * i], f.x), kLoScale), __fmul_rn(__fsub_rn(v[2 * i + 1], f.y), kLoScale));
-        h[i] = *reinterpret_cast<const uint32_t*>(&a);
-        l[i] = *reinterpret_cast<const uint32_t*>(&b);
-    }
-    hi = make_uint4(h[0], h[1], h[2], h[3]);
-    lo = make_uint4(l[0], l[1], l[2], l[3]);
-}
-
-__device__ __forceinline__ void join8(const uint4& hi, const uint4& lo, float (&v)[8]) {
-    const uint32_t h[4] = {hi.x, hi.y, hi.z, hi.w}, l[4] = {lo.x, lo.y, lo.z, lo.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&h[i])), b = __half22float2(*reinterpret_cast<const __half2*>(&l[i]));
-        v[2 * i] = __fmaf_rn(b.x, 1.0f / kLoScale, a.x);
-        v[2 * i + 1] = __fmaf_rn(b.y, 1.0f / kLoScale, a.y);
-    }
-}
-
 template <typename T>
 __global__ void __launch_bounds__(kLoadThreads) orth_load_kernel(LoadArgs a) {
     wait_for_previous_kernel();
@@ -273,7 +226,7 @@ __global__ void __launch_bounds__(kLoadThreads) orth_load_kernel(LoadArgs a) {
         double total = 0.0;
         for (int w = 0; w < kLoadThreads / 32; ++w) total += s_sum[w];
         const double d = sqrt(total) + (double)a.eps;
-        s_f = d > 0.0 ? (double)orth_s(s) / d : 0.0;  // an all-zero matrix without eps stays zero
+        s_f = d > 0.0 ? (double)orth_s(s.m, s.n) / d : 0.0;  // an all-zero matrix without eps stays zero
         if (!isfinite(total) && tile == t.full0 && (blockIdx.x & 3u) == 0) {
             set_status(a.res, CO3_ERR_NONFINITE);
             atomicMin(&a.res->first_bad_chunk, batch.index0 + k);
@@ -318,103 +271,6 @@ __global__ void __launch_bounds__(kLoadThreads) orth_load_kernel(LoadArgs a) {
         *reinterpret_cast<uint4*>(p) = hi;
         *reinterpret_cast<uint4*>(p + kPlane) = lo;
     }
-}
-
-// ------------------------------------------------------------------------------------------------
-// tcgen05: operands in shared memory (K-major, 128-byte swizzle), fp32 accumulators in tensor memory.
-// ------------------------------------------------------------------------------------------------
-// An operand of 128 rows and 64 columns of the sum in shared memory.  As it lies in memory: rows of 128 bytes along the
-// sum, 1024 bytes between groups of eight.  Transposed: two halves of 64 operand rows, 8 KB apart, each with a row of
-// 128 bytes per column of the sum, 1024 bytes between groups of eight columns.  Both swizzled.
-__device__ __forceinline__ uint64_t smem_desc(uint32_t addr, bool transposed) {
-    return (uint64_t)((addr >> 4) & 0x3fffu) | ((uint64_t)(transposed ? kHalfPlane >> 4 : 1u) << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
-}
-// 16 columns of the sum further
-__device__ __forceinline__ uint64_t desc_step(bool transposed) { return transposed ? 2048u >> 4 : 32u >> 4; }
-// D fp32, A and B fp16; one block: 128 x 128, a pair of blocks: 256 x 256
-template <int kCtas>
-__device__ __forceinline__ uint32_t instr_desc(bool a_transposed, bool b_transposed) {
-    return (1u << 4) | ((uint32_t)a_transposed << 15) | ((uint32_t)b_transposed << 16) | ((128u * kCtas / 8u) << 17) | ((128u * kCtas / 16u) << 24);
-}
-
-// kScale: what is there already counts 2^-kScale.
-template <int kCtas, int kScale = 0>
-__device__ __forceinline__ void tc_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t instr, bool accumulate) {
-    if constexpr (kCtas == 1) {
-        if constexpr (kScale == 0)
-            asm volatile(
-                "{\n\t.reg .pred p;\n\t"
-                "setp.ne.b32 p, %4, 0;\n\t"
-                "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(instr),
-                "r"((uint32_t)accumulate)
-                : "memory");
-        else
-            asm volatile(
-                "{\n\t.reg .pred p;\n\t"
-                "setp.ne.b32 p, %4, 0;\n\t"
-                "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p, %5;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(instr),
-                "r"((uint32_t)accumulate), "n"(kScale)
-                : "memory");
-    } else {
-        if constexpr (kScale == 0)
-            asm volatile(
-                "{\n\t.reg .pred p;\n\t"
-                "setp.ne.b32 p, %4, 0;\n\t"
-                "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(instr),
-                "r"((uint32_t)accumulate)
-                : "memory");
-        else
-            asm volatile(
-                "{\n\t.reg .pred p;\n\t"
-                "setp.ne.b32 p, %4, 0;\n\t"
-                "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p, %5;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(instr),
-                "r"((uint32_t)accumulate), "n"(kScale)
-                : "memory");
-    }
-}
-// The products issued so far arrive on this barrier when they are done; of a pair, on both blocks' barrier.
-template <int kCtas>
-__device__ __forceinline__ void tc_commit(uint64_t* bar) {
-    if constexpr (kCtas == 1)
-        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(bar)) : "memory");
-    else
-        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(smem_addr(bar)), "h"((uint16_t)3)
-                     : "memory");
-}
-__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(bar)) : "memory");
-}
-// The same on the barrier of the pair's first block.
-template <int kCtas>
-__device__ __forceinline__ void mbar_arrive_first(uint64_t* bar) {
-    if constexpr (kCtas == 1) {
-        mbar_arrive(bar);
-    } else {
-        asm volatile(
-            "{\n\t.reg .b32 r;\n\t"
-            "mapa.shared::cluster.u32 r, %0, 0;\n\t"
-            "mbarrier.arrive.release.cluster.shared::cluster.b64 _, [r];\n\t}" ::"r"(smem_addr(bar))
-            : "memory");
-    }
-}
-// 32 columns of this warp's 32 lanes
-__device__ __forceinline__ void tc_load32(uint32_t addr, float (&v)[32]) {
-    uint32_t r[32];
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
-        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n\t"
-        "tcgen05.wait::ld.sync.aligned;"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
-          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
-          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-        : "r"(addr)
-        : "memory");
-#pragma unroll
-    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -476,8 +332,6 @@ struct StepSmem {
 constexpr size_t kSmemOff = (size_t)kStages * kStageBytes;
 constexpr size_t kStepSmem = 1024 + kSmemOff + sizeof(StepSmem);
 static_assert(kStepSmem <= 227 * 1024 && kSmemOff % 8 == 0, "shared memory of a block");
-
-enum OrthOut { kOutF32 = 0, kOutF16 = 1, kOutBf16 = 2, kOutParams = 3 };
 
 struct StepArgs {
     OrthWs ws;
@@ -588,20 +442,6 @@ __device__ __forceinline__ uint32_t load_acquire(const uint32_t* p) {
     asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
     return v;
 }
-__device__ __forceinline__ void fence_async_all() { asm volatile("fence.proxy.async;" ::: "memory"); }
-
-__device__ __forceinline__ bool try_wait_cluster(uint64_t* bar, uint32_t parity) {
-    uint32_t done;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(done)
-        : "r"(smem_addr(bar)), "r"(parity)
-        : "memory");
-    return done != 0;
-}
-
 template <int kCtas>
 __device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity, uint64_t limit_ns) {
     auto test = [&]() { return kCtas == 1 ? mbar_try_wait(bar, parity) : try_wait_cluster(bar, parity); };
@@ -638,6 +478,30 @@ __device__ __forceinline__ void tile_sync() {  // all threads of the blocks that
     } else {
         asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
         asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    }
+}
+
+// The products of one stage: 64 columns of the sum, operands at a and b in shared memory.  The tensor core's queue holds
+// about four products: look() is called before the last four, so that what it waits for costs no time.
+template <int kCtas, bool kTa, bool kTb, typename Look>
+__device__ __forceinline__ void multiply_stage(uint32_t d, uint32_t a, uint32_t b, bool pairs, bool opens, Look look) {
+    constexpr uint32_t instr = instr_desc<kCtas>(kTa, kTb), da = desc_step(kTa), db = desc_step(kTb);
+    const uint64_t ah = smem_desc(a, kTa), bh = smem_desc(b, kTb);
+    const uint64_t al = ah + (kPlane >> 4), bl = bh + (kPlane >> 4);
+    if (pairs) {
+        // the corrections first, 2^11 times too large; the first product of the hi planes scales them down
+#pragma unroll
+        for (uint32_t e = 0; e < 4; ++e) tc_mma<kCtas>(d, ah + e * da, bl + e * db, instr, e > 0);
+#pragma unroll
+        for (uint32_t e = 0; e < 4; ++e) tc_mma<kCtas>(d, al + e * da, bh + e * db, instr, true);
+        tc_mma<kCtas, kLoBits>(d, ah, bh, instr, true);
+        look();
+#pragma unroll
+        for (uint32_t e = 1; e < 4; ++e) tc_mma<kCtas>(d, ah + e * da, bh + e * db, instr, true);
+    } else {
+#pragma unroll
+        for (uint32_t e = 0; e < 4; ++e) tc_mma<kCtas>(d, ah + e * da, bh + e * db, instr, !opens || e > 0);
+        look();
     }
 }
 
@@ -722,31 +586,30 @@ __global__ void __launch_bounds__(kStepThreads, 1) orth_steps_kernel(const __gri
             const Task k = find_task<kCtas>(a, sm, n_tasks, n_mats, g, rank, v);
             const bool pairs = (a.pairs >> k.step) & 1u;
             const uint32_t from_a = operand<kCtas>(k, v, rank, 0).from, from_b = operand<kCtas>(k, v, rank, 1).from;
-            bool ok = true;
+            bool ok = true, ready = false;
             for (uint32_t q = k.k0; q < k.k1; ++q, ++it) {
                 const uint32_t st = it % kStages, buf = chunk % kSums, d = tmem + buf * kCols;
                 const bool opens = pairs || q == k.k0, closes = pairs || q + 1 == k.k1;
-                if (opens && chunk >= kSums && !wait_for<kCtas>(&sm.sum_empty[buf], (chunk / kSums - 1) & 1u, a.limit_ns)) { ok = false; break; }
-                if (!wait_for<kCtas>(&sm.full[st], (it / kStages) & 1u, a.limit_ns)) { ok = false; break; }
-                if (kCtas == 2 && !wait_for<kCtas>(&sm.peer_full[st], (it / kStages) & 1u, a.limit_ns)) { ok = false; break; }
+                if (!ready) {
+                    if (opens && chunk >= kSums && !wait_for<kCtas>(&sm.sum_empty[buf], (chunk / kSums - 1) & 1u, a.limit_ns)) { ok = false; break; }
+                    if (!wait_for<kCtas>(&sm.full[st], (it / kStages) & 1u, a.limit_ns)) { ok = false; break; }
+                    if (kCtas == 2 && !wait_for<kCtas>(&sm.peer_full[st], (it / kStages) & 1u, a.limit_ns)) { ok = false; break; }
+                }
                 tc_fence_after();
                 const uint32_t at = smem_addr(ring + (size_t)st * kStageBytes), bt = k.diagonal ? at : at + kBlock;
-                const bool ta = q >= from_a, tb = q >= from_b;
-                const uint32_t instr = instr_desc<kCtas>(ta, tb);
-                const uint64_t ah = smem_desc(at, ta), bh = smem_desc(bt, tb), da = desc_step(ta), db = desc_step(tb);
-                const uint64_t al = ah + (kPlane >> 4), bl = bh + (kPlane >> 4);
-                if (pairs) {
-                    // the corrections first, 2^11 times too large; the first product of the hi planes scales them down
-#pragma unroll
-                    for (uint32_t e = 0; e < 4; ++e) tc_mma<kCtas>(d, ah + e * da, bl + e * db, instr, e > 0);
-#pragma unroll
-                    for (uint32_t e = 0; e < 4; ++e) tc_mma<kCtas>(d, al + e * da, bh + e * db, instr, true);
-                    tc_mma<kCtas, kLoBits>(d, ah, bh, instr, true);
-#pragma unroll
-                    for (uint32_t e = 1; e < 4; ++e) tc_mma<kCtas>(d, ah + e * da, bh + e * db, instr, true);
+                ready = false;
+                auto look = [&]() {  // is the next stage ready?
+                    if (q + 1 == k.k1) return;
+                    const uint32_t it1 = it + 1, st1 = it1 % kStages, ch1 = chunk + (closes ? 1u : 0u), buf1 = ch1 % kSums;
+                    ready = test_cluster(&sm.full[st1], (it1 / kStages) & 1u) && (kCtas == 1 || test_cluster(&sm.peer_full[st1], (it1 / kStages) & 1u)) &&
+                            (!closes || ch1 < kSums || test_cluster(&sm.sum_empty[buf1], (ch1 / kSums - 1) & 1u));
+                };
+                if (q >= from_a) {
+                    if (q >= from_b) multiply_stage<kCtas, true, true>(d, at, bt, pairs, opens, look);
+                    else multiply_stage<kCtas, true, false>(d, at, bt, pairs, opens, look);
                 } else {
-#pragma unroll
-                    for (uint32_t e = 0; e < 4; ++e) tc_mma<kCtas>(d, ah + e * da, bh + e * db, instr, !opens || e > 0);
+                    if (q >= from_b) multiply_stage<kCtas, false, true>(d, at, bt, pairs, opens, look);
+                    else multiply_stage<kCtas, false, false>(d, at, bt, pairs, opens, look);
                 }
                 if (closes) { tc_commit<kCtas>(&sm.sum_full[buf]); ++chunk; }
                 tc_commit<kCtas>(&sm.empty[st]);
@@ -786,7 +649,8 @@ __global__ void __launch_bounds__(kStepThreads, 1) orth_steps_kernel(const __gri
             bool ok = true;
             for (uint32_t q = 0; q < chunks; ++q, ++chunk) {
                 const uint32_t buf = chunk % kSums;
-                ok = wait_for<kCtas>(&sm.sum_full[buf], (chunk / kSums) & 1u, a.limit_ns);
+                // one lane looks: 256 threads at the barriers would slow down the one that issues the products
+                ok = lane != 0 || wait_for<kCtas>(&sm.sum_full[buf], (chunk / kSums) & 1u, a.limit_ns);
                 if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
                 tc_fence_after();
 #pragma unroll
@@ -803,7 +667,7 @@ __global__ void __launch_bounds__(kStepThreads, 1) orth_steps_kernel(const __gri
             // the stage with this warp's columns of the tile's own blocks
             const uint32_t out_it = it + (k.k1 - k.k0) + (kCtas == 1 ? 0u : half), out_st = out_it % kStages;
             it += k.k1 - k.k0 + kCtas;
-            ok = ok && wait_for<kCtas>(&sm.full[out_st], (out_it / kStages) & 1u, a.limit_ns);
+            ok = ok && (lane != 0 || wait_for<kCtas>(&sm.full[out_st], (out_it / kStages) & 1u, a.limit_ns));
             if (!__all_sync(0xffffffffu, ok)) { *failed = 1; break; }
 
             bool mine = true;  // this warp finishes its part of the tile
@@ -841,7 +705,7 @@ __global__ void __launch_bounds__(kStepThreads, 1) orth_steps_kernel(const __gri
             // Rows and columns up to a multiple of 64 are written: beyond, no product reads them.
             const bool rows_used = row0 + (quad & 2u) * 32u < n_rows;
             if (mine && rows_used) {
-                const float inv_s = 1.0f / orth_s(v.s);
+                const float inv_s = 1.0f / orth_s(v.s.m, v.s.n);
                 float fl = 0.0f, fa = inv_s;  // value = fl * linear + fa * sum
                 if (k.phase == kPoly) { fl = a.ns.coef[k.step][1]; fa = __fmul_rn(a.ns.coef[k.step][2], inv_s); }
                 if (k.phase == kApply) fl = a.ns.coef[k.step][0];
@@ -852,7 +716,7 @@ __global__ void __launch_bounds__(kStepThreads, 1) orth_steps_kernel(const __gri
                 }
                 // B takes a I in where the apply product does not add a X
                 const bool add_diag = k.phase == kPoly && k.diagonal && !adds_x(a, k.step);
-                const float diag = __fmul_rn(a.ns.coef[k.step][0], orth_s(v.s));
+                const float diag = __fmul_rn(a.ns.coef[k.step][0], orth_s(v.s.m, v.s.n));
                 unsigned char* dst = nullptr;  // this block's part of the tile, 2 kCtas blocks in a row
                 if (k.phase != kApply) dst = (k.phase == kGram ? v.op.a : v.op.b) + ((uint64_t)k.rb * (2 * v.s.mb) + 2 * k.cb) * kBlock;
                 else if (!last) dst = v.op.x[(k.step & 1u) ^ 1u] + ((uint64_t)k.rb * (2 * v.s.nb) + 2 * k.cb) * kBlock;
@@ -898,31 +762,7 @@ __global__ void __launch_bounds__(kStepThreads, 1) orth_steps_kernel(const __gri
                         const uint32_t c = row0 + row;
                         const uint64_t first = v.t.out_off + (uint64_t)c0 * v.t.out_stride + c;
                         const uint32_t n = c < v.t.cols ? min(64u, v.t.rows - c0) : 0u;
-                        if (a.out_kind == kOutParams) {
-                            float* out = static_cast<float*>(a.out) + first;
-#pragma unroll
-                            for (int i0 = 0; i0 < 64; i0 += 16) {
-                                float old[16];
-#pragma unroll
-                                for (int i = 0; i < 16; ++i) old[i] = (uint32_t)(i0 + i) < n ? out[(uint64_t)(i0 + i) * v.t.out_stride] : 0.0f;
-#pragma unroll
-                                for (int i = 0; i < 16; ++i)
-                                    if ((uint32_t)(i0 + i) < n) out[(uint64_t)(i0 + i) * v.t.out_stride] = __fmaf_rn(-a.lr, acc[h * 64 + i0 + i], __fmul_rn(a.shrink, old[i]));
-                            }
-                        } else if (a.out_kind == kOutF32) {
-                            float* out = static_cast<float*>(a.out) + first;
-#pragma unroll
-                            for (int i = 0; i < 64; ++i)
-                                if ((uint32_t)i < n) out[(uint64_t)i * v.t.out_stride] = acc[h * 64 + i];
-                        } else {
-                            uint16_t* out = static_cast<uint16_t*>(a.out) + first;
-                            const bool f16 = a.out_kind == kOutF16;
-#pragma unroll
-                            for (int i = 0; i < 64; ++i)
-                                if ((uint32_t)i < n)
-                                    out[(uint64_t)i * v.t.out_stride] = f16 ? __half_as_ushort(__float2half_rn(acc[h * 64 + i]))
-                                                                            : __bfloat16_as_ushort(__float2bfloat16_rn(acc[h * 64 + i]));
-                        }
+                        put_result<64>(a.out, a.out_kind, first, v.t.out_stride, n, 1.0f, acc + h * 64, a.lr, a.shrink);
                     }
                 }
             }
@@ -1071,6 +911,29 @@ uint32_t plan_batch(const co3_mat* in, const co3_mat* out, uint32_t n_mats, uint
     return n;
 }
 
+// Times in nanoseconds that decide whether small matrices go to clusters of their own: a phase through memory, a step of
+// a cluster of one block and of several, and what either call takes besides.
+constexpr uint64_t kPhaseNs = 7000, kSmallStepNs[2] = {4000, 7000}, kCallNs = 10000;
+
+// Fills `small` with a batch's matrices and returns true if they are all small and clusters take less time for them.
+bool small_batch(const co3_mat* in, const co3_mat* out, uint32_t n_mats, uint32_t at, const OrthBatch& b, const BatchNeeds& needs,
+                 uint32_t steps, SmallBatch* small) {
+    uint64_t ns = 0, blocks[kSmallCluster + 1] = {};
+    small->n_mats = 0;
+    for (uint32_t k = 0; k < b.n_mats; ++k) {
+        const co3_mat &ti = in[at + k], &to = out[at + k];
+        if ((to.flags & CO3_MAT_PLAIN) != 0u || ti.rows == 0 || ti.cols == 0) continue;
+        const uint32_t c = small_ctas(ti.rows, ti.cols);
+        if (c == 0 || small->n_mats == kSmallMats) return false;
+        blocks[c] += c;
+        small->mat[small->n_mats++] = {ti.offset, ti.row_stride, to.offset, to.row_stride, ti.rows, ti.cols, to.scale, at + k};
+    }
+    // clusters that fit the SMs at a time: whole ones within a group of about 16
+    for (uint32_t c = 1; c <= kSmallCluster; c *= 2)
+        if (blocks[c]) ns += (blocks[c] + (c > 4 ? 127 : 147)) / (c > 4 ? 128 : 148) * steps * kSmallStepNs[c > 1] + kCallNs;
+    return small->n_mats > 0 && ns <= steps * (needs.ns + 3 * kPhaseNs) + 2 * kCallNs;
+}
+
 // The number of blocks per tile that takes less time.
 uint32_t make_batch(const co3_mat* in, const co3_mat* out, uint32_t n_mats, uint32_t at, bool muon, OrthBatch* b, BatchNeeds* needs) {
     BatchNeeds two;
@@ -1086,8 +949,8 @@ bool valid_ns(const co3_ns& ns) {
     for (uint32_t k = 0; k < ns.steps; ++k)
         for (int j = 0; j < 3; ++j)
             if (!isfinite(ns.coef[k][j])) return false;
-    for (int i = 0; i <= 4096; ++i) {
-        double x = i / 4096.0;
+    for (int i = 0; i <= 512; ++i) {
+        double x = i / 512.0;
         for (uint32_t k = 0; k < ns.steps; ++k) {
             const double q = x * x, g = q * (ns.coef[k][1] + q * ns.coef[k][2]);
             if (!(fabs(g) <= 4.0) || !(fabs(ns.coef[k][0] + g) <= 4.0)) return false;
@@ -1096,6 +959,17 @@ bool valid_ns(const co3_ns& ns) {
         }
     }
     return true;
+}
+
+// Leaves orth_begin_kernel with the plain layers.
+void only_plain(OrthBatch* b) {
+    uint32_t chunks = 0;
+    for (uint32_t k = 0; k < b->n_mats; ++k) {
+        OrthMat& m = b->mat[k];
+        m.chunk0 = chunks;
+        if (m.plain) chunks += (uint32_t)(((uint64_t)m.rows * m.cols + kBeginElems - 1) / kBeginElems);
+    }
+    b->n_chunks = chunks;
 }
 
 // All blocks have to be resident at once: as many tiles at a time as the device holds, asked for once per device.
@@ -1153,7 +1027,7 @@ struct OrthCall {
 int orth_run(const OrthCall& c, const co3_ns* ns_in, co3_result* res, void* workspace, size_t workspace_bytes, void* stream) {
     co3_ns ns;
     if (ns_in) ns = *ns_in; else co3_ns_default(&ns);
-    if (!valid_ns(ns) || !res || !aligned(res, 8) || !workspace || !aligned(workspace, 256)) return CO3_ERR_INVALID_ARG;
+    if ((ns_in && !valid_ns(ns)) || !res || !aligned(res, 8) || !workspace || !aligned(workspace, 256)) return CO3_ERR_INVALID_ARG;
     size_t need = 0;
     if (c.n_mats && (!c.in || !c.out || !c.in_mats)) return CO3_ERR_INVALID_ARG;
     if (!aligned(c.in, type_size(c.in_type)) || !aligned(c.out, type_size(c.out_type))) return CO3_ERR_INVALID_ARG;
@@ -1174,7 +1048,10 @@ int orth_run(const OrthCall& c, const co3_ns* ns_in, co3_result* res, void* work
     uint32_t at = 0;
     do {
         const uint32_t k = make_batch(c.in_mats, c.out_mats, c.n_mats, at, muon, &batch, &needs);
+        SmallBatch small;
+        const bool is_small = small_batch(c.in_mats, c.out_mats, c.n_mats, at, batch, needs, ns.steps, &small);
         const WsPlan w = ws_plan(&batch, needs);
+        if (is_small) only_plain(&batch);
         unsigned char* base = static_cast<unsigned char*>(workspace);
         OrthWs ws = {reinterpret_cast<OrthBatch*>(base + w.batch), reinterpret_cast<OrthCtrl*>(base + w.ctrl),
                      reinterpret_cast<uint32_t*>(base + w.arrive), reinterpret_cast<double*>(base + w.partial),
@@ -1182,7 +1059,14 @@ int orth_run(const OrthCall& c, const co3_ns* ns_in, co3_result* res, void* work
         BeginArgs ba = {c.in, c.momentum, static_cast<float*>(c.out), c.mu, c.lr, c.shrink, c.nesterov, res, ws};
         LoadArgs la = {c.in, c.momentum, c.mu, ns.eps, c.nesterov, res, ws};
         const dim3 bg(batch.n_chunks ? batch.n_chunks : 1u), lg(4u * batch.n_full);
-        if (c.in_type == CO3_F32) {
+        if (is_small) {
+            // a lone matrix starts the result itself
+            const bool alone = c.n_mats == 1;
+            if (!alone) CO3_CUDA(launch_behind(orth_begin_kernel<float>, bg, dim3(kBeginThreads), 0, st, batch, ba));
+            const SmallCall sc = {c.in, c.momentum, c.out, muon ? (int)kOutParams : c.out_type, c.mu, c.lr, c.shrink, c.nesterov, alone ? 1 : 0, ns, res};
+            const int e = orth_small_run(small, sc, c.in_type, st);
+            if (e != CO3_OK) return e;
+        } else if (c.in_type == CO3_F32) {
             CO3_CUDA(launch_behind(orth_begin_kernel<float>, bg, dim3(kBeginThreads), 0, st, batch, ba));
             if (batch.n_full) CO3_CUDA(launch_behind(orth_load_kernel<float>, lg, dim3(kLoadThreads), 0, st, la));
         } else if (c.in_type == CO3_F16) {
@@ -1192,7 +1076,7 @@ int orth_run(const OrthCall& c, const co3_ns* ns_in, co3_result* res, void* work
             CO3_CUDA(launch_behind(orth_begin_kernel<__nv_bfloat16>, bg, dim3(kBeginThreads), 0, st, batch, ba));
             if (batch.n_full) CO3_CUDA(launch_behind(orth_load_kernel<__nv_bfloat16>, lg, dim3(kLoadThreads), 0, st, la));
         }
-        if (batch.n_full) {
+        if (batch.n_full && !is_small) {
             StepArgs sa = {};
             sa.ws = ws;
             sa.ns = ns;
