@@ -49,7 +49,7 @@ struct OrthBatch {
     uint32_t n_tasks[3];
     uint32_t index0;  // index of mat[0] in the caller's list
     uint32_t first;   // 1: the call's first batch, which clears the result
-    uint32_t ctas;    // blocks per tile: 1 or 2
+    uint32_t tile;    // OrthTile
 };
 
 struct OrthCtrl {
@@ -66,25 +66,46 @@ struct OrthWs {
     unsigned char* blocks;
 };
 
-struct OrthShape {
-    uint32_t m, n;    // small side, long side
-    uint32_t mt, nt;  // both in tiles (of ctas * 128)
-    uint32_t mb, nb;  // both in blocks of 128, filled up to whole tiles
-    bool tall;        // rows > cols: X is the transposed matrix
+// Tiles of a product: 128 x 64, 128 x 128, or 256 x 256 by a pair of blocks, each with 128 rows of it.
+enum OrthTile { kNarrow = 0, kSquare = 1, kPair = 2 };
+template <int kTile>
+struct Tiling {
+    static constexpr uint32_t kCtas = kTile == kPair ? 2 : 1, kRows = 128 * kCtas, kCols = kTile == kNarrow ? 64 : kRows;
+    static constexpr uint32_t kSums = 512 / kCols;                                   // tiles that tensor memory holds
+    static constexpr uint32_t kColPlane = kTile == kNarrow ? kHalfPlane : kPlane;    // of the columns' operand
+    static constexpr uint32_t kStageBytes = kBlock + 2 * kColPlane, kStages = kTile == kNarrow ? 4 : 3;
+    static constexpr uint32_t kOwnStages = kTile == kPair ? 2 : 1;                   // the tile's own blocks: this many stages
+    static constexpr uint32_t kOwnBytes = kTile == kNarrow ? kBlock : 2 * kBlock;    // of this size each
 };
 
-// ctas: blocks that work on a tile together, each on 128 rows of it: a tile is 128 x 128 or 256 x 256.
-__host__ __device__ inline OrthShape orth_shape(uint32_t rows, uint32_t cols, uint32_t ctas) {
+struct OrthShape {
+    uint32_t m, n;         // small side, long side
+    uint32_t mb, nb;       // both in blocks of 128, filled up to whole tiles
+    uint32_t mt, mc;       // the small side in tile rows and in tile columns
+    uint32_t nt, nc;       // the long side
+    uint32_t sym, per_row; // tiles of a symmetric product; tile columns per tile row
+    bool tall;             // rows > cols: X is the transposed matrix
+};
+
+__host__ __device__ inline OrthShape orth_shape(uint32_t rows, uint32_t cols, uint32_t tile) {
     OrthShape s;
+    const uint32_t ctas = tile == kPair ? 2u : 1u, tr = 128u * ctas, tc = tile == kNarrow ? 64u : tr;
     s.tall = rows > cols;
     s.m = s.tall ? cols : rows;
     s.n = s.tall ? rows : cols;
-    s.mt = (s.m + 128u * ctas - 1u) / (128u * ctas);
-    s.nt = (s.n + 128u * ctas - 1u) / (128u * ctas);
+    s.mt = (s.m + tr - 1u) / tr;
+    s.nt = (s.n + tr - 1u) / tr;
+    s.mc = (s.m + tc - 1u) / tc;
+    s.nc = (s.n + tc - 1u) / tc;
     s.mb = s.mt * ctas;
     s.nb = s.nt * ctas;
+    s.per_row = tr / tc;
+    // up to and including the diagonal: (i + 1) per_row tiles in row i, as far as the matrix reaches
+    s.sym = s.mt ? s.per_row * s.mt * (s.mt - 1u) / 2u + (s.mc < s.per_row * s.mt ? s.mc : s.per_row * s.mt) : 0u;
     return s;
 }
+// Tiles of the apply product, and of its last one, whose rows are the long side unless the matrix is tall.
+__host__ __device__ inline uint32_t orth_apply_tiles(const OrthShape& s, bool last) { return last && !s.tall ? s.nt * s.mc : s.mt * s.nc; }
 
 // Operand blocks of one matrix: X twice [mb][2 nb], A and B [mb][2 mb] (their lower triangles of tiles are used).
 __host__ __device__ inline uint64_t orth_blocks(const OrthShape& s) {
@@ -213,7 +234,7 @@ __global__ void __launch_bounds__(kLoadThreads) orth_load_kernel(LoadArgs a) {
     const uint32_t tile = blockIdx.x >> 2;  // tile of 128 x 128, quarter blockIdx.x & 3
     const uint32_t k = orth_find(batch.n_mats, tile, [&](uint32_t i) { return batch.mat[i].full0; });
     const OrthMat t = batch.mat[k];
-    const OrthShape s = orth_shape(t.rows, t.cols, batch.ctas);
+    const OrthShape s = orth_shape(t.rows, t.cols, batch.tile);
     // the norm: this matrix' partial sums in order
     const uint32_t n_part = (uint32_t)(((uint64_t)t.rows * t.cols + kBeginElems - 1) / kBeginElems);
     double sum = 0.0;
@@ -280,35 +301,39 @@ __global__ void __launch_bounds__(kLoadThreads) orth_load_kernel(LoadArgs a) {
 // of the phases before it are finished (a counter per matrix): the tasks waited for stand earlier in the list, so that
 // waiting always ends, and one matrix' tail is filled with other matrices' work.
 //
-// Warp 0 copies operand blocks into a ring, warp 1 issues the products, warps 2..9 take the sums: each of them 32 rows x
-// half of the tile's columns in registers, and from there on each works on its own.  Behind a task's operands the ring
-// carries its linear term (b A or a X, the tile's own blocks); the warps put the finished values in its place, from where
-// bulk copies take them to memory.
+// Warps 0 and 10 copy operand blocks into a ring (one thread each, for the rows' and the columns' operand: a copy costs its
+// thread about 100 cycles), warps 1 and 11 issue the products, every other stage each: looking at a barrier takes a thread 100 to
+// 200 cycles during which it issues nothing (12 products 770 cycles; with the looks by one thread 1000).  Warps 2..9 take the sums: each of them 32 rows x half of the tile's
+// columns in registers, and from there on each works on its own.  Behind a task's operands the ring carries its linear
+// term (b A or a X, the tile's own blocks); the warps put the finished values in its place, from where they go to memory.
 //
-// kCtas == 1: a tile of 128 x 128.  A stage (64 columns of the sum) is 64 KB for 3 x 2 x 128 x 128 x 64 operations, which
-// a GPU full of such blocks fetches from L2 at about 10 TB/s: 0.9 us where the products take 0.4.  kCtas == 2: two
-// blocks multiply one tile of 256 x 256 (each fetches 128 rows of either operand, the tensor cores read both blocks'
-// shared memory): the same 64 KB and twice the operations per block.
+// Which tiles: the tensor core reads its operands from shared memory, which gives 128 bytes a cycle, and the copies
+// write there too.  A stage (64 columns of the sum, 12 products) of a 128 x 128 tile moves 160 KB for 768 cycles of
+// products, of a 256 x 256 tile of two blocks 160 KB a block for 1536: there the products bound it.  The pairs take long
+// over each tile, though: small calls are faster with many small tiles.
 // ------------------------------------------------------------------------------------------------
 constexpr int kEpiThreads = 256;
-constexpr int kStepThreads = 64 + kEpiThreads;
-constexpr int kStages = 3;
+constexpr int kStepThreads = 64 + kEpiThreads + 64;
+constexpr int kMaxStages = 4;
 // The tensor core cuts what it adds to 26 bits below the largest term, always towards zero: sums of one sign (the
 // diagonal of A) drift.  The sum of each stage is therefore taken out and added up in registers, where fp32 rounds to
 // nearest.  1000 x 513, five steps, error against 64 bits: 1.3e-5 if the tensor core adds up all stages, 6.1e-6 if
 // four, 2.1e-6 if one (2.9e-6 with all sums in fp32 arithmetic).  Steps that multiply the hi planes alone leave all
 // sums to the tensor core.
-constexpr uint32_t kStageBytes = 2 * kBlock;
+constexpr size_t kRingBytes = 192 << 10;
+static_assert(Tiling<kNarrow>::kStages * Tiling<kNarrow>::kStageBytes == kRingBytes && Tiling<kSquare>::kStages * Tiling<kSquare>::kStageBytes == kRingBytes &&
+                  Tiling<kPair>::kStages * Tiling<kPair>::kStageBytes == kRingBytes, "one size of ring");
 
 struct Task {
     uint32_t step, phase, mat;
-    uint32_t rb, cb;      // block row and first block column of this block's part of the tile
+    uint32_t rb, cg;      // block row, and first group of 64 columns, of this block's part of the tile
     uint32_t k0, k1;      // operand blocks of the summed dimension
     uint32_t part, parts;
     uint32_t tile;        // index within the matrix and phase
     uint32_t before;      // warps' parts of this matrix' tiles that have to be finished
     bool swap;            // kApply: the tile's rows are the long side
     bool diagonal;        // both operands are the same blocks
+    bool skip;            // no such tile
 };
 
 struct MatView {
@@ -318,18 +343,18 @@ struct MatView {
 };
 
 struct StepSmem {
-    uint64_t full[kStages];
-    uint64_t empty[kStages];      // a stage of operands has been multiplied
-    uint64_t out_empty[kStages];  // a stage of the tile's own blocks has been stored
-    uint64_t peer_full[kStages];  // first block of a pair: the other block's stage is full
-    uint64_t sum_full[4], sum_empty[4];
-    uint64_t done;
+    uint64_t full[kMaxStages];
+    uint64_t empty[kMaxStages];      // a stage of operands has been multiplied, or one of the tile's own blocks stored
+    uint32_t stored[kMaxStages];     // warps that are done with a stage of the tile's own blocks
+    uint64_t peer_full[kMaxStages];  // first block of a pair: the other block's stage is full
+    uint64_t sum_full[8], sum_empty[8];
+    uint64_t done[2];
     uint32_t tmem, failed;
     uint32_t task0[3][kOrthMats];
     Task task[8];  // what warps 2..9 work on: in shared memory, the sums need the registers
     MatView view[8];
 };
-constexpr size_t kSmemOff = (size_t)kStages * kStageBytes;
+constexpr size_t kSmemOff = kRingBytes;
 constexpr size_t kStepSmem = 1024 + kSmemOff + sizeof(StepSmem);
 static_assert(kStepSmem <= 227 * 1024 && kSmemOff % 8 == 0, "shared memory of a block");
 
@@ -344,8 +369,9 @@ struct StepArgs {
     co3_result* res;
 };
 
-template <int kCtas>
+template <int kTile>
 __device__ __forceinline__ Task find_task(const StepArgs& a, const StepSmem& sm, const uint32_t* n_tasks, uint32_t n_mats, uint32_t g, uint32_t rank, MatView& v) {
+    using L = Tiling<kTile>;
     Task k;
     const uint32_t per_step = n_tasks[0] + n_tasks[1] + n_tasks[2];
     k.step = g / per_step;
@@ -355,34 +381,36 @@ __device__ __forceinline__ Task find_task(const StepArgs& a, const StepSmem& sm,
     const uint32_t* first = sm.task0[k.phase];
     k.mat = orth_find(n_mats, x, [&](uint32_t i) { return first[i]; });
     v.t = a.ws.batch->mat[k.mat];
-    v.s = orth_shape(v.t.rows, v.t.cols, kCtas);
+    v.s = orth_shape(v.t.rows, v.t.cols, kTile);
     v.op = orth_operands(a.ws, v.t, v.s);
     x -= first[k.mat];
     k.parts = v.t.splits[k.phase];
     k.tile = x / k.parts;
     k.part = x - k.tile * k.parts;
-    const uint32_t sym = v.s.mt * (v.s.mt + 1) / 2;
-    k.before = 8 * kCtas * (k.step * (2 * sym + v.s.mt * v.s.nt) + k.phase * sym);
-    k.swap = k.diagonal = false;
+    k.before = 8 * L::kCtas * (k.step * (2 * v.s.sym + orth_apply_tiles(v.s, false)) + k.phase * v.s.sym);
+    k.swap = k.diagonal = k.skip = false;
     uint32_t i, j, blocks;
     if (k.phase == kApply) {
-        i = k.tile / v.s.nt;  // small side
-        j = k.tile - i * v.s.nt;
         // in the last product of a matrix that is not tall the tile's rows are the long side, so that a warp's rows
         // are neighbours in the caller's memory
-        k.swap = k.step + 1 == a.ns.steps && !v.s.tall;
-        if (k.swap) { const uint32_t h = i; i = j; j = h; }
+        const bool last = k.step + 1 == a.ns.steps;
+        k.swap = last && !v.s.tall;
+        k.skip = k.tile >= orth_apply_tiles(v.s, last);
+        const uint32_t cols = k.swap ? v.s.mc : v.s.nc;
+        i = k.tile / cols;
+        j = k.tile - i * cols;
         blocks = (v.s.m + 63u) / 64u;
-    } else {  // the triangle i >= j
-        i = (uint32_t)((sqrtf(8.0f * (float)k.tile + 1.0f) - 1.0f) * 0.5f);
-        while (i * (i + 1) / 2 > k.tile) --i;
-        while ((i + 1) * (i + 2) / 2 <= k.tile) ++i;
-        j = k.tile - i * (i + 1) / 2;
-        k.diagonal = i == j;
+    } else {  // tiles on and below the diagonal
+        const uint32_t t = k.tile / (L::kRows / L::kCols);
+        i = (uint32_t)((sqrtf(8.0f * (float)t + 1.0f) - 1.0f) * 0.5f);
+        while (v.s.per_row * i * (i + 1) / 2 > k.tile) --i;
+        while (v.s.per_row * (i + 1) * (i + 2) / 2 <= k.tile) ++i;
+        j = k.tile - v.s.per_row * i * (i + 1) / 2;
+        k.diagonal = L::kCols == L::kRows && i == j;
         blocks = ((k.phase == kGram ? v.s.n : v.s.m) + 63u) / 64u;
     }
-    k.rb = i * kCtas + rank;
-    k.cb = j * kCtas;
+    k.rb = i * L::kCtas + rank;
+    k.cg = j * (L::kCols / 64u);
     k.k0 = (uint32_t)((uint64_t)blocks * k.part / k.parts);
     k.k1 = (uint32_t)((uint64_t)blocks * (k.part + 1) / k.parts);
     return k;
@@ -394,47 +422,59 @@ __device__ __forceinline__ Task find_task(const StepArgs& a, const StepSmem& sm,
 // are multiplied they would carry the rounding of X to 11 bits along.
 __device__ __forceinline__ bool adds_x(const StepArgs& a, uint32_t step) { return step + 1 < a.ns.steps; }
 
-// The tile's own blocks of the linear term, 2 kCtas of them in a row; null if there is none.
+// The tile's own blocks of the linear term, in a row; null if there is none.
 __device__ __forceinline__ const unsigned char* linear_term(const StepArgs& a, const Task& k, const MatView& v) {
-    if (k.phase == kPoly) return v.op.a + ((uint64_t)k.rb * (2 * v.s.mb) + 2 * k.cb) * kBlock;
-    if (k.phase == kApply && adds_x(a, k.step)) return v.op.x[k.step & 1u] + ((uint64_t)k.rb * (2 * v.s.nb) + 2 * k.cb) * kBlock;
+    if (k.phase == kPoly) return v.op.a + ((uint64_t)k.rb * (2 * v.s.mb) + k.cg) * kBlock;
+    if (k.phase == kApply && adds_x(a, k.step)) return v.op.x[k.step & 1u] + ((uint64_t)k.rb * (2 * v.s.nb) + k.cg) * kBlock;
     return nullptr;
 }
 
-// How one of a task's operands is fetched: for 128 rows from block r on, columns 64 q .. 64 q + 63 of the sum.
+// bulk_copy_g2s and mbar_arrive_expect_tx with shared-memory addresses as they are
+__device__ __forceinline__ void copy_in(uint32_t dst, const unsigned char* src, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void arrive_expect(uint32_t bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+
+// How one of a task's operands is fetched: columns 64 q .. 64 q + 63 of the sum, for 128 rows of block row r, or for 64
+// rows (r counts groups of 64).
 struct Operand {
     const unsigned char* base;
     uint64_t row;      // bytes between block rows
-    uint32_t r;        // block row of the operand
+    uint32_t r;
     uint32_t from;     // stages from this one on are fetched transposed
-    __device__ __forceinline__ void fetch(unsigned char* dst, uint32_t q, bool pairs, uint64_t* bar) const {
+    __device__ __forceinline__ void fetch128(uint32_t dst, uint32_t q, bool pairs, uint32_t bar) const {
         if (q < from) {
-            bulk_copy_g2s(dst, base + r * row + (uint64_t)q * kBlock, pairs ? kBlock : kPlane, bar);
+            copy_in(dst, base + r * row + (uint64_t)q * kBlock, pairs ? kBlock : kPlane, bar);
         } else {  // rows 64 q .. of block row q / 2, columns of blocks 2 r and 2 r + 1
             const unsigned char* p = base + (q >> 1) * row + (uint64_t)(2 * r) * kBlock + (q & 1u) * kHalfPlane;
-            bulk_copy_g2s(dst, p, kHalfPlane, bar);
-            bulk_copy_g2s(dst + kHalfPlane, p + kBlock, kHalfPlane, bar);
+            copy_in(dst, p, kHalfPlane, bar);
+            copy_in(dst + kHalfPlane, p + kBlock, kHalfPlane, bar);
             if (pairs) {
-                bulk_copy_g2s(dst + kPlane, p + kPlane, kHalfPlane, bar);
-                bulk_copy_g2s(dst + kPlane + kHalfPlane, p + kBlock + kPlane, kHalfPlane, bar);
+                copy_in(dst + kPlane, p + kPlane, kHalfPlane, bar);
+                copy_in(dst + kPlane + kHalfPlane, p + kBlock + kPlane, kHalfPlane, bar);
             }
         }
     }
-};
-// The operand of the tile's rows (which == 0) or columns (1), this block's 128 of them.
-template <int kCtas>
-__device__ __forceinline__ Operand operand(const Task& k, const MatView& v, uint32_t rank, int which) {
-    Operand o;
-    o.r = which == 0 ? k.rb : k.cb + rank;
-    const uint64_t row_x = (uint64_t)(2 * v.s.nb) * kBlock, row_m = (uint64_t)(2 * v.s.mb) * kBlock;
-    if (k.phase == kGram) {
-        o = {v.op.x[k.step & 1u], row_x, o.r, 0xffffffffu};
-    } else if (k.phase == kApply && (which == 1) != k.swap) {
-        o = {v.op.x[k.step & 1u], row_x, o.r, 0u};
-    } else {  // a symmetric matrix: stored up to and including the tile on the diagonal
-        o = {k.phase == kPoly ? v.op.a : v.op.b, row_m, o.r, (o.r / kCtas + 1) * (2 * kCtas)};
+    __device__ __forceinline__ void fetch64(uint32_t dst, uint32_t q, bool pairs, uint32_t bar) const {
+        const unsigned char* p = q < from ? base + (r >> 1) * row + (uint64_t)q * kBlock + (r & 1u) * kHalfPlane
+                                          : base + (q >> 1) * row + (uint64_t)r * kBlock + (q & 1u) * kHalfPlane;
+        copy_in(dst, p, kHalfPlane, bar);
+        if (pairs) copy_in(dst + kHalfPlane, p + kPlane, kHalfPlane, bar);
     }
-    return o;
+};
+// The operand of the tile's rows (which == 0) or columns (1), this block's share of it.
+template <int kTile>
+__device__ __forceinline__ Operand operand(const Task& k, const MatView& v, uint32_t rank, int which) {
+    using L = Tiling<kTile>;
+    const uint32_t r = which == 0 ? k.rb : kTile == kNarrow ? k.cg : k.cg / 2 + rank;
+    const uint32_t block_row = which == 1 && kTile == kNarrow ? r / 2 : r;
+    const uint64_t row_x = (uint64_t)(2 * v.s.nb) * kBlock, row_m = (uint64_t)(2 * v.s.mb) * kBlock;
+    if (k.phase == kGram) return {v.op.x[k.step & 1u], row_x, r, 0xffffffffu};
+    if (k.phase == kApply && (which == 1) != k.swap) return {v.op.x[k.step & 1u], row_x, r, 0u};
+    // a symmetric matrix: stored up to and including the tile row's part of the diagonal
+    return {k.phase == kPoly ? v.op.a : v.op.b, row_m, r, (block_row / L::kCtas + 1) * (2 * L::kCtas)};
 }
 
 __device__ __forceinline__ uint32_t load_acquire(const uint32_t* p) {
@@ -481,13 +521,14 @@ __device__ __forceinline__ void tile_sync() {  // all threads of the blocks that
     }
 }
 
-// The products of one stage: 64 columns of the sum, operands at a and b in shared memory.  The tensor core's queue holds
-// about four products: look() is called before the last four, so that what it waits for costs no time.
-template <int kCtas, bool kTa, bool kTb, typename Look>
-__device__ __forceinline__ void multiply_stage(uint32_t d, uint32_t a, uint32_t b, bool pairs, bool opens, Look look) {
-    constexpr uint32_t instr = instr_desc<kCtas>(kTa, kTb), da = desc_step(kTa), db = desc_step(kTb);
+// The products of one stage: 64 columns of the sum, operands at a and b in shared memory.
+template <int kTile, bool kTa, bool kTb>
+__device__ __forceinline__ void multiply_stage(uint32_t d, uint32_t a, uint32_t b, bool pairs, bool opens) {
+    using L = Tiling<kTile>;
+    constexpr int kCtas = L::kCtas;
+    constexpr uint32_t instr = instr_desc(kTa, kTb, L::kRows, L::kCols), da = desc_step(kTa), db = desc_step(kTb);
     const uint64_t ah = smem_desc(a, kTa), bh = smem_desc(b, kTb);
-    const uint64_t al = ah + (kPlane >> 4), bl = bh + (kPlane >> 4);
+    const uint64_t al = ah + (kPlane >> 4), bl = bh + (L::kColPlane >> 4);
     if (pairs) {
         // the corrections first, 2^11 times too large; the first product of the hi planes scales them down
 #pragma unroll
@@ -495,20 +536,19 @@ __device__ __forceinline__ void multiply_stage(uint32_t d, uint32_t a, uint32_t 
 #pragma unroll
         for (uint32_t e = 0; e < 4; ++e) tc_mma<kCtas>(d, al + e * da, bh + e * db, instr, true);
         tc_mma<kCtas, kLoBits>(d, ah, bh, instr, true);
-        look();
 #pragma unroll
         for (uint32_t e = 1; e < 4; ++e) tc_mma<kCtas>(d, ah + e * da, bh + e * db, instr, true);
     } else {
 #pragma unroll
         for (uint32_t e = 0; e < 4; ++e) tc_mma<kCtas>(d, ah + e * da, bh + e * db, instr, !opens || e > 0);
-        look();
     }
 }
 
-template <int kCtas>
+template <int kTile>
 __global__ void __launch_bounds__(kStepThreads, 1) orth_steps_kernel(const __grid_constant__ StepArgs a) {
     extern __shared__ unsigned char smem_raw[];
-    constexpr uint32_t kCols = 128 * kCtas, kSums = 512 / kCols;  // columns of a tile, sums that tensor memory holds
+    using L = Tiling<kTile>;
+    constexpr uint32_t kCtas = L::kCtas, kCols = L::kCols, kSums = L::kSums, kStages = L::kStages, kStageBytes = L::kStageBytes, kOwn = L::kOwnStages;
     unsigned char* ring = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
     StepSmem& sm = *reinterpret_cast<StepSmem*>(ring + kSmemOff);
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
@@ -519,9 +559,10 @@ __global__ void __launch_bounds__(kStepThreads, 1) orth_steps_kernel(const __gri
     for (uint32_t i = threadIdx.x; i < n_mats; i += kStepThreads)
         for (int p = 0; p < 3; ++p) sm.task0[p][i] = a.ws.batch->mat[i].task0[p];
     if (threadIdx.x == 0) {
-        for (int i = 0; i < kStages; ++i) { mbar_init(&sm.full[i], 1); mbar_init(&sm.empty[i], 1); mbar_init(&sm.out_empty[i], 8 / kCtas); mbar_init(&sm.peer_full[i], 1); }
+        for (uint32_t i = 0; i < kStages; ++i) { mbar_init(&sm.full[i], 2); mbar_init(&sm.empty[i], 1); mbar_init(&sm.peer_full[i], 1); sm.stored[i] = 0; }
         for (uint32_t i = 0; i < kSums; ++i) { mbar_init(&sm.sum_full[i], 1); mbar_init(&sm.sum_empty[i], 8 * kCtas); }
-        mbar_init(&sm.done, 1);
+        mbar_init(&sm.done[0], 1);
+        mbar_init(&sm.done[1], 1);
         sm.failed = 0;
     }
     if (warp == 1) {
@@ -541,107 +582,119 @@ __global__ void __launch_bounds__(kStepThreads, 1) orth_steps_kernel(const __gri
     volatile uint32_t* failed = &sm.failed;
     MatView v;
 
-    if (warp == 0 && lane == 0) {
-        uint32_t it = 0, held[kStages] = {}, uses[2][kStages] = {};  // held: 1 operands, 2 the tile's own blocks
+    if ((warp == 0 || warp == 10) && lane == 0) {
+        const int which = warp == 0 ? 0 : 1;
+        uint32_t it = 0, st = 0, turn = 0;  // stages filled; the ring's next one, and how often the ring has been gone through
+        const uint32_t ring_addr = smem_addr(ring), full0 = smem_addr(&sm.full[0]);
         for (uint32_t g = group; g < total && !*failed; g += groups) {
-            const Task k = find_task<kCtas>(a, sm, n_tasks, n_mats, g, rank, v);
-            const Operand oa = operand<kCtas>(k, v, rank, 0), ob = operand<kCtas>(k, v, rank, 1);
+            const Task k = find_task<kTile>(a, sm, n_tasks, n_mats, g, rank, v);
+            if (k.skip) continue;
+            const Operand o = operand<kTile>(k, v, rank, which);
             const bool pairs = (a.pairs >> k.step) & 1u;
-            const uint32_t bytes = pairs ? kBlock : kPlane;
             if (!wait_tiles(a.ws.ctrl, k.mat, k.before, a.limit_ns)) { *failed = 1; break; }
             fence_async_all();  // orders what the counter says after the copies that follow
-            auto begin = [&](bool out) {
-                const uint32_t st = it % kStages;
-                bool free = true;
-                if (held[st] == 1) free = wait_for<kCtas>(&sm.empty[st], (uses[0][st] - 1) & 1u, a.limit_ns);
-                if (held[st] == 2) free = wait_for<kCtas>(&sm.out_empty[st], (uses[1][st] - 1) & 1u, a.limit_ns);
-                if (!free) { *failed = 1; return false; }
-                held[st] = out ? 2 : 1;
-                ++uses[out ? 1 : 0][st];
+            auto begin = [&]() {
+                if (turn > 0 && !wait_for<kCtas>(&sm.empty[st], (turn - 1) & 1u, a.limit_ns)) { *failed = 1; return false; }
                 return true;
             };
-            for (uint32_t q = k.k0; q < k.k1 && begin(false); ++q, ++it) {
-                unsigned char* dst = ring + (size_t)(it % kStages) * kStageBytes;
-                uint64_t* bar = &sm.full[it % kStages];
-                mbar_arrive_expect_tx(bar, k.diagonal ? bytes : 2 * bytes);
-                oa.fetch(dst, q, pairs, bar);
-                if (!k.diagonal) ob.fetch(dst + kBlock, q, pairs, bar);
+            auto next = [&]() {
+                ++it;
+                if (++st == kStages) { st = 0; ++turn; }
+            };
+            const bool half_width = which == 1 && kTile == kNarrow;
+            const uint32_t part = half_width ? kHalfPlane : kPlane, bytes = pairs ? 2 * part : part;  // of a stage
+            for (uint32_t q = k.k0; q < k.k1; ++q, next()) {
+                if (!begin()) break;
+                const uint32_t dst = ring_addr + st * kStageBytes + (which ? kBlock : 0u), bar = full0 + st * 8u;
+                if (which == 1 && k.diagonal) { mbar_arrive(&sm.full[st]); continue; }
+                arrive_expect(bar, bytes);
+                if (half_width) o.fetch64(dst, q, pairs, bar); else o.fetch128(dst, q, pairs, bar);
             }
-            const unsigned char* lin = linear_term(a, k, v);
-            for (uint32_t q = 0; q < kCtas && begin(true); ++q, ++it) {
-                uint64_t* bar = &sm.full[it % kStages];
+            const unsigned char* lin = which == 0 ? linear_term(a, k, v) : nullptr;
+            for (uint32_t q = 0; q < kOwn && !*failed; ++q, next()) {
+                if (!begin()) break;
+                const uint32_t bar = full0 + st * 8u;
                 if (lin) {
-                    mbar_arrive_expect_tx(bar, kStageBytes);
-                    bulk_copy_g2s(ring + (size_t)(it % kStages) * kStageBytes, lin + (uint64_t)q * kStageBytes, kStageBytes, bar);
+                    arrive_expect(bar, L::kOwnBytes);
+                    copy_in(ring_addr + st * kStageBytes, lin + (uint64_t)q * L::kOwnBytes, L::kOwnBytes, bar);
                 } else {
-                    mbar_arrive(bar);  // nothing to fetch: the stage is there for the results
+                    mbar_arrive(&sm.full[st]);  // nothing to fetch: the stage is there for the results
                 }
             }
         }
         // copies in flight end before the block does, whoever else has given up
-        for (uint32_t q = it > (uint32_t)kStages ? it - kStages : 0; q < it; ++q) mbar_wait(&sm.full[q % kStages], (q / kStages) & 1u);
-    } else if (warp == 1 && lane == 0 && rank == 0) {
-        uint32_t it = 0, chunk = 0;
+        for (uint32_t q = it > kStages ? it - kStages : 0; q < it; ++q) mbar_wait(&sm.full[q % kStages], (q / kStages) & 1u);
+    } else if ((warp == 1 || warp == 11) && lane == 0 && rank == 0) {
+        const uint32_t mine = warp == 1 ? 0u : 1u;
+        uint32_t unit = 0;  // sums begun: a stage's, or where the hi planes alone are multiplied a task's
+        uint32_t st = 0, turn = 0, buf = 0, buf_turn = 0;  // next stage of the ring, next sum in tensor memory, and how often round
+        const uint32_t ring_addr = smem_addr(ring);
+        auto next_stage = [&]() {
+            if (++st == kStages) { st = 0; ++turn; }
+        };
+        // every stage is waited for, the other warp's too: a barrier tells only its last phase from the one before
+        auto full_stage = [&]() {
+            return wait_for<kCtas>(&sm.full[st], turn & 1u, a.limit_ns) && (kCtas == 1 || wait_for<kCtas>(&sm.peer_full[st], turn & 1u, a.limit_ns));
+        };
+        auto next_sum = [&]() {
+            ++unit;
+            if (++buf == kSums) { buf = 0; ++buf_turn; }
+        };
         for (uint32_t g = group; g < total && !*failed; g += groups) {
-            const Task k = find_task<kCtas>(a, sm, n_tasks, n_mats, g, rank, v);
+            const Task k = find_task<kTile>(a, sm, n_tasks, n_mats, g, rank, v);
+            if (k.skip) continue;
             const bool pairs = (a.pairs >> k.step) & 1u;
-            const uint32_t from_a = operand<kCtas>(k, v, rank, 0).from, from_b = operand<kCtas>(k, v, rank, 1).from;
-            bool ok = true, ready = false;
-            for (uint32_t q = k.k0; q < k.k1; ++q, ++it) {
-                const uint32_t st = it % kStages, buf = chunk % kSums, d = tmem + buf * kCols;
+            const uint32_t from_a = operand<kTile>(k, v, rank, 0).from, from_b = operand<kTile>(k, v, rank, 1).from;
+            bool ok = true;
+            for (uint32_t q = k.k0; q < k.k1; ++q, next_stage()) {
                 const bool opens = pairs || q == k.k0, closes = pairs || q + 1 == k.k1;
-                if (!ready) {
-                    if (opens && chunk >= kSums && !wait_for<kCtas>(&sm.sum_empty[buf], (chunk / kSums - 1) & 1u, a.limit_ns)) { ok = false; break; }
-                    if (!wait_for<kCtas>(&sm.full[st], (it / kStages) & 1u, a.limit_ns)) { ok = false; break; }
-                    if (kCtas == 2 && !wait_for<kCtas>(&sm.peer_full[st], (it / kStages) & 1u, a.limit_ns)) { ok = false; break; }
+                if (!full_stage()) { ok = false; break; }
+                if ((unit & 1u) == mine) {
+                    const uint32_t d = tmem + buf * kCols;
+                    if (opens && buf_turn > 0 && !wait_for<kCtas>(&sm.sum_empty[buf], (buf_turn - 1) & 1u, a.limit_ns)) { ok = false; break; }
+                    tc_fence_after();
+                    const uint32_t at = ring_addr + st * kStageBytes, bt = k.diagonal ? at : at + kBlock;
+                    if (q >= from_a) {
+                        if (q >= from_b) multiply_stage<kTile, true, true>(d, at, bt, pairs, opens);
+                        else multiply_stage<kTile, true, false>(d, at, bt, pairs, opens);
+                    } else {
+                        if (q >= from_b) multiply_stage<kTile, false, true>(d, at, bt, pairs, opens);
+                        else multiply_stage<kTile, false, false>(d, at, bt, pairs, opens);
+                    }
+                    if (closes) tc_commit<kCtas>(&sm.sum_full[buf]);
+                    tc_commit<kCtas>(&sm.empty[st]);
                 }
-                tc_fence_after();
-                const uint32_t at = smem_addr(ring + (size_t)st * kStageBytes), bt = k.diagonal ? at : at + kBlock;
-                ready = false;
-                auto look = [&]() {  // is the next stage ready?
-                    if (q + 1 == k.k1) return;
-                    const uint32_t it1 = it + 1, st1 = it1 % kStages, ch1 = chunk + (closes ? 1u : 0u), buf1 = ch1 % kSums;
-                    ready = test_cluster(&sm.full[st1], (it1 / kStages) & 1u) && (kCtas == 1 || test_cluster(&sm.peer_full[st1], (it1 / kStages) & 1u)) &&
-                            (!closes || ch1 < kSums || test_cluster(&sm.sum_empty[buf1], (ch1 / kSums - 1) & 1u));
-                };
-                if (q >= from_a) {
-                    if (q >= from_b) multiply_stage<kCtas, true, true>(d, at, bt, pairs, opens, look);
-                    else multiply_stage<kCtas, true, false>(d, at, bt, pairs, opens, look);
-                } else {
-                    if (q >= from_b) multiply_stage<kCtas, false, true>(d, at, bt, pairs, opens, look);
-                    else multiply_stage<kCtas, false, false>(d, at, bt, pairs, opens, look);
-                }
-                if (closes) { tc_commit<kCtas>(&sm.sum_full[buf]); ++chunk; }
-                tc_commit<kCtas>(&sm.empty[st]);
+                if (closes) next_sum();
             }
+            // the tile's own blocks pass from the copies to warps 2..9
+            for (uint32_t q = 0; ok && q < kOwn; ++q, next_stage()) ok = full_stage();
             if (!ok) { *failed = 1; break; }
-            // the stages of the tile's own blocks pass from the copies to warps 2..9
-            for (uint32_t q = 0; q < kCtas; ++q, ++it)
-                if (kCtas == 2 && !wait_for<kCtas>(&sm.peer_full[it % kStages], (it / kStages) & 1u, a.limit_ns)) { *failed = 1; break; }
         }
-        tc_commit<kCtas>(&sm.done);
-        mbar_wait(&sm.done, 0);
+        tc_commit<kCtas>(&sm.done[mine]);
+        mbar_wait(&sm.done[mine], 0);
     } else if (kCtas == 2 && warp == 1 && lane == 0) {
         // the pair's second block tells the first which of its stages are full
         uint32_t it = 0;
         for (uint32_t g = group; g < total && !*failed; g += groups) {
-            const Task k = find_task<kCtas>(a, sm, n_tasks, n_mats, g, rank, v);
-            const uint32_t n = k.k1 - k.k0 + kCtas;
+            const Task k = find_task<kTile>(a, sm, n_tasks, n_mats, g, rank, v);
+            if (k.skip) continue;
+            const uint32_t n = k.k1 - k.k0 + kOwn;
             for (uint32_t q = 0; q < n; ++q, ++it) {
                 if (!wait_for<kCtas>(&sm.full[it % kStages], (it / kStages) & 1u, a.limit_ns)) { *failed = 1; break; }
                 mbar_arrive_first<kCtas>(&sm.peer_full[it % kStages]);
             }
         }
-    } else if (warp >= 2) {
-        constexpr int kAcc = 64 * kCtas;  // columns of this warp
+    } else if (warp >= 2 && warp < 10) {
+        constexpr int kAcc = kCols / 2, kW = kAcc < 64 ? kAcc : 64;  // columns of this warp, and how many of them lie in one block
         const uint32_t quad = warp & 3u, half = (warp - 2u) >> 2, row = quad * 32u + lane;
         const uint32_t lane_base = tmem + ((quad * 32u) << 16) + half * kAcc;
         uint32_t it = 0, chunk = 0;
         for (uint32_t g = group; g < total; g += groups) {
-            if (lane == 0) sm.task[warp - 2] = find_task<kCtas>(a, sm, n_tasks, n_mats, g, rank, sm.view[warp - 2]);
+            if (lane == 0) sm.task[warp - 2] = find_task<kTile>(a, sm, n_tasks, n_mats, g, rank, sm.view[warp - 2]);
             __syncwarp();
             const Task& k = sm.task[warp - 2];
             const MatView& v = sm.view[warp - 2];
+            if (k.skip) { __syncwarp(); continue; }
             const uint32_t chunks = (a.pairs >> k.step) & 1u ? k.k1 - k.k0 : 1u;
             float acc[kAcc];
 #pragma unroll
@@ -665,8 +718,8 @@ __global__ void __launch_bounds__(kStepThreads, 1) orth_steps_kernel(const __gri
                 if (lane == 0) mbar_arrive_first<kCtas>(&sm.sum_empty[buf]);
             }
             // the stage with this warp's columns of the tile's own blocks
-            const uint32_t out_it = it + (k.k1 - k.k0) + (kCtas == 1 ? 0u : half), out_st = out_it % kStages;
-            it += k.k1 - k.k0 + kCtas;
+            const uint32_t out_it = it + (k.k1 - k.k0) + (kOwn == 1 ? 0u : half), out_st = out_it % kStages;
+            it += k.k1 - k.k0 + kOwn;
             ok = ok && (lane != 0 || wait_for<kCtas>(&sm.full[out_st], (out_it / kStages) & 1u, a.limit_ns));
             if (!__all_sync(0xffffffffu, ok)) { *failed = 1; break; }
 
@@ -682,8 +735,7 @@ __global__ void __launch_bounds__(kStepThreads, 1) orth_steps_kernel(const __gri
                 __syncwarp();
                 uint32_t old = 0;
                 if (lane == 0) {
-                    const uint32_t sym = v.s.mt * (v.s.mt + 1) / 2;
-                    old = atomicAdd(a.ws.arrive + v.t.arrive0 + ((k.phase * sym + k.tile) * kCtas + rank) * 8 + warp - 2, 1u);
+                    old = atomicAdd(a.ws.arrive + v.t.arrive0 + ((k.phase * v.s.sym + k.tile) * kCtas + rank) * 8 + warp - 2, 1u);
                     __threadfence();
                 }
                 old = __shfl_sync(0xffffffffu, old, 0);
@@ -701,7 +753,7 @@ __global__ void __launch_bounds__(kStepThreads, 1) orth_steps_kernel(const __gri
 
             const bool last = k.phase == kApply && k.step + 1 == a.ns.steps, has_lin = k.phase == kPoly || (k.phase == kApply && adds_x(a, k.step));
             const uint32_t n_rows = k.swap ? v.s.n : v.s.m, n_cols = k.phase == kApply && !k.swap ? v.s.n : v.s.m;
-            const uint32_t row0 = k.rb * 128u, col0 = k.cb * 128u;
+            const uint32_t row0 = k.rb * 128u, col0 = k.cg * 64u;
             // Rows and columns up to a multiple of 64 are written: beyond, no product reads them.
             const bool rows_used = row0 + (quad & 2u) * 32u < n_rows;
             if (mine && rows_used) {
@@ -715,20 +767,21 @@ __global__ void __launch_bounds__(kStepThreads, 1) orth_steps_kernel(const __gri
                     fa = __fmul_rn(fa, f);
                 }
                 // B takes a I in where the apply product does not add a X
-                const bool add_diag = k.phase == kPoly && k.diagonal && !adds_x(a, k.step);
+                const bool add_diag = k.phase == kPoly && !adds_x(a, k.step);
                 const float diag = __fmul_rn(a.ns.coef[k.step][0], orth_s(v.s.m, v.s.n));
-                unsigned char* dst = nullptr;  // this block's part of the tile, 2 kCtas blocks in a row
-                if (k.phase != kApply) dst = (k.phase == kGram ? v.op.a : v.op.b) + ((uint64_t)k.rb * (2 * v.s.mb) + 2 * k.cb) * kBlock;
-                else if (!last) dst = v.op.x[(k.step & 1u) ^ 1u] + ((uint64_t)k.rb * (2 * v.s.nb) + 2 * k.cb) * kBlock;
+                unsigned char* dst = nullptr;  // this block's part of the tile, its blocks in a row
+                if (k.phase != kApply) dst = (k.phase == kGram ? v.op.a : v.op.b) + ((uint64_t)k.rb * (2 * v.s.mb) + k.cg) * kBlock;
+                else if (!last) dst = v.op.x[(k.step & 1u) ^ 1u] + ((uint64_t)k.rb * (2 * v.s.nb) + k.cg) * kBlock;
 #pragma unroll
-                for (int h = 0; h < kCtas; ++h) {  // 64 columns, one block, at a time
-                    const uint32_t cg = half * kCtas + h, c0 = col0 + cg * 64u;
-                    if (c0 >= n_cols) break;
+                for (int h = 0; h < kAcc / kW; ++h) {  // one block at a time: all of its columns, or half of them
+                    const uint32_t cg = kTile == kNarrow ? 0u : half * (kAcc / 64) + h, p0 = kTile == kNarrow ? half * 4u : 0u;
+                    const uint32_t c0 = col0 + cg * 64u + p0 * 8u;
+                    if (col0 + cg * 64u >= n_cols) break;
                     unsigned char* own = ring + (size_t)out_st * kStageBytes + (cg & 1u) * kBlock;
 #pragma unroll
-                    for (int p = 0; p < 8; ++p) {
+                    for (int p = 0; p < kW / 8; ++p) {
                         float* w = acc + h * 64 + p * 8;
-                        const uint32_t at = swizzled(row, p);
+                        const uint32_t at = swizzled(row, p0 + p);
 #pragma unroll
                         for (int e = 0; e < 8; ++e) w[e] = __fmul_rn(fa, w[e]);
                         if (has_lin) {
@@ -749,7 +802,15 @@ __global__ void __launch_bounds__(kStepThreads, 1) orth_steps_kernel(const __gri
                             *reinterpret_cast<uint4*>(own + at + kPlane) = lo;
                         }
                     }
-                    if (!last) {
+                    if (!last && kTile == kNarrow) {
+                        // half a block's columns: 64 bytes of each row, four lanes to a row
+                        __syncwarp();
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const uint32_t r = quad * 32u + (i & 3) * 8u + (lane >> 2), off = (i >> 2) * kPlane + swizzled(r, p0 + (lane & 3u));
+                            *reinterpret_cast<uint4*>(dst + off) = *reinterpret_cast<const uint4*>(own + off);
+                        }
+                    } else if (!last) {
                         fence_async_smem();
                         __syncwarp();
                         if (lane < 2) {  // 32 rows of either plane lie in a row
@@ -761,23 +822,29 @@ __global__ void __launch_bounds__(kStepThreads, 1) orth_steps_kernel(const __gri
                         // the tile's rows run along the caller's rows, its columns across them
                         const uint32_t c = row0 + row;
                         const uint64_t first = v.t.out_off + (uint64_t)c0 * v.t.out_stride + c;
-                        const uint32_t n = c < v.t.cols ? min(64u, v.t.rows - c0) : 0u;
-                        put_result<64>(a.out, a.out_kind, first, v.t.out_stride, n, 1.0f, acc + h * 64, a.lr, a.shrink);
+                        const uint32_t n = c < v.t.cols && c0 < v.t.rows ? min((uint32_t)kW, v.t.rows - c0) : 0u;
+                        put_result<kW>(a.out, a.out_kind, first, v.t.out_stride, n, 1.0f, acc + h * 64, a.lr, a.shrink);
                     }
                 }
             }
             // the ring's stage is free as soon as the copies have read it, the tile finished when they have written it
-            if (last) fence_async_smem();
+            if (last || kTile == kNarrow) fence_async_all();  // ordinary accesses before the copies of others
             if (lane < 2) bulk_stores_read();
             __syncwarp();
-            if (lane == 0) mbar_arrive(&sm.out_empty[out_st]);
+            if (lane == 0) {
+                __threadfence_block();
+                if (atomicAdd(&sm.stored[out_st], 1u) == 8 / kOwn - 1) {
+                    sm.stored[out_st] = 0;
+                    __threadfence_block();
+                    mbar_arrive(&sm.empty[out_st]);
+                }
+            }
             if (mine && !last) {
                 if (lane < 2) {
                     bulk_stores_done();
                     fence_async_all();
-                    __threadfence();
                 }
-                __syncwarp();
+                __syncwarp();  // and the release takes all lanes' writes along
                 if (lane == 0) asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(&a.ws.ctrl->done[k.mat]) : "memory");
             }
             __syncwarp();
@@ -829,7 +896,7 @@ WsPlan ws_plan(const OrthBatch* b, const BatchNeeds& needs) {
     w.arrive = w.ctrl + up256(sizeof(OrthCtrl));
     w.partial = w.arrive + up256(b ? 4ull * b->n_arrive : 0);
     w.slots = w.partial + up256(b ? 8ull * b->n_chunks : 0);
-    w.blocks = w.slots + needs.slots * (128ull * 128 * 4);
+    w.blocks = w.slots + needs.slots * (128ull * 4) * (b && b->tile == kPair ? 256 : 128);
     w.total = w.blocks + needs.blocks * kBlock;
     return w;
 }
@@ -837,28 +904,27 @@ WsPlan ws_plan(const OrthBatch* b, const BatchNeeds& needs) {
 // A tile whose sum is long is split so that the tasks of a phase are about as long as the phase's work spread over
 // all SMs, but no part is shorter than kMinPart stages.
 constexpr uint64_t kPlanSms = 148, kMinPart = 8, kMaxParts = 16;
-// Time of a stage of a 128 x 128 tile and of a 256 x 256 tile of two blocks, in nanoseconds.
-constexpr uint64_t kStageNs[2] = {900, 900};
+// Time of a stage and of what a phase takes besides, in nanoseconds, by kind of tile.
+constexpr uint64_t kStageNs[3] = {450, 620, 1250}, kTilePhaseNs[3] = {6500, 7500, 18000};
 
-// Takes matrices from `at` on into one batch with the given number of blocks per tile; returns how many, 0 if one is
-// unusable.
-uint32_t plan_batch(const co3_mat* in, const co3_mat* out, uint32_t n_mats, uint32_t at, bool muon, uint32_t ctas, OrthBatch* b,
+// Takes matrices from `at` on into one batch with the given tiles; returns how many, 0 if one is unusable.
+uint32_t plan_batch(const co3_mat* in, const co3_mat* out, uint32_t n_mats, uint32_t at, bool muon, uint32_t tile, OrthBatch* b,
                     BatchNeeds* needs) {
     uint32_t n = 0;
     uint64_t work[3] = {0, 0, 0};
-    const uint64_t units = kPlanSms / ctas;
+    const uint64_t ctas = tile == kPair ? 2 : 1, units = kPlanSms / ctas;
     for (; at + n < n_mats && n < kOrthMats; ++n) {
         const co3_mat &ti = in[at + n], &to = out[at + n];
         if (!valid_mat(ti) || !valid_mat(to) || ti.rows != to.rows || ti.cols != to.cols) return 0;
         const bool plain = (to.flags & CO3_MAT_PLAIN) != 0u;
         if (plain && !muon) return 0;
         if (plain || ti.rows == 0 || ti.cols == 0) continue;
-        const OrthShape s = orth_shape(ti.rows, ti.cols, ctas);
-        const uint64_t sym = (uint64_t)s.mt * (s.mt + 1) / 2, km = (s.m + 63u) / 64u, kn = (s.n + 63u) / 64u;
-        if (sym >= (1u << 24) || (uint64_t)s.mt * s.nt >= (1u << 24)) return 0;
-        work[kGram] += sym * kn;
-        work[kPoly] += sym * km;
-        work[kApply] += (uint64_t)s.mt * s.nt * km;
+        const OrthShape s = orth_shape(ti.rows, ti.cols, tile);
+        const uint64_t km = (s.m + 63u) / 64u, kn = (s.n + 63u) / 64u;
+        if (s.mt >= (1u << 12) || (uint64_t)s.mb * s.nb >= (1u << 23)) return 0;
+        work[kGram] += s.sym * kn;
+        work[kPoly] += s.sym * km;
+        work[kApply] += orth_apply_tiles(s, false) * km;
     }
     uint64_t chunks = 0, full = 0, arrive = 0, slots = 0, blocks = 0, tasks[3] = {0, 0, 0};
     for (uint32_t k = 0; k < n; ++k) {
@@ -877,8 +943,8 @@ uint32_t plan_batch(const co3_mat* in, const co3_mat* out, uint32_t n_mats, uint
         if (ti.rows == 0 || ti.cols == 0) continue;
         chunks += ((uint64_t)ti.rows * ti.cols + kBeginElems - 1) / kBeginElems;
         if (!plain) {
-            const OrthShape s = orth_shape(ti.rows, ti.cols, ctas);
-            const uint64_t sym = (uint64_t)s.mt * (s.mt + 1) / 2, all = (uint64_t)s.mt * s.nt;
+            const OrthShape s = orth_shape(ti.rows, ti.cols, tile);
+            const uint64_t sym = s.sym, all = std::max(orth_apply_tiles(s, false), orth_apply_tiles(s, true));
             uint64_t most = 0;
             for (int p = 0; p < 3; ++p) {
                 const uint64_t depth = ((p == kGram ? s.n : s.m) + 63u) / 64u, tiles = p == kApply ? all : sym;
@@ -902,18 +968,18 @@ uint32_t plan_batch(const co3_mat* in, const co3_mat* out, uint32_t n_mats, uint
     uint64_t ns = 0;
     for (int p = 0; p < 3; ++p) {
         b->n_tasks[p] = (uint32_t)tasks[p];
-        if (tasks[p]) ns += (tasks[p] + units - 1) / units * work[p] * kStageNs[ctas - 1] / tasks[p];
+        if (tasks[p]) ns += (tasks[p] + units - 1) / units * work[p] * kStageNs[tile] / tasks[p] + kTilePhaseNs[tile];
     }
     b->index0 = at;
     b->first = at == 0 ? 1u : 0u;
-    b->ctas = ctas;
-    *needs = {slots * ctas, blocks, work[0] + work[1] + work[2], ns};
+    b->tile = tile;
+    *needs = {slots, blocks, work[0] + work[1] + work[2], ns};
     return n;
 }
 
-// Times in nanoseconds that decide whether small matrices go to clusters of their own: a phase through memory, a step of
+// Times in nanoseconds that decide whether small matrices go to clusters of their own: a step of
 // a cluster of one block and of several, and what either call takes besides.
-constexpr uint64_t kPhaseNs = 7000, kSmallStepNs[2] = {4000, 7000}, kCallNs = 10000;
+constexpr uint64_t kSmallStepNs[2] = {4000, 7000}, kCallNs = 10000;
 
 // Fills `small` with a batch's matrices and returns true if they are all small and clusters take less time for them.
 bool small_batch(const co3_mat* in, const co3_mat* out, uint32_t n_mats, uint32_t at, const OrthBatch& b, const BatchNeeds& needs,
@@ -931,17 +997,18 @@ bool small_batch(const co3_mat* in, const co3_mat* out, uint32_t n_mats, uint32_
     // clusters that fit the SMs at a time: whole ones within a group of about 16
     for (uint32_t c = 1; c <= kSmallCluster; c *= 2)
         if (blocks[c]) ns += (blocks[c] + (c > 4 ? 127 : 147)) / (c > 4 ? 128 : 148) * steps * kSmallStepNs[c > 1] + kCallNs;
-    return small->n_mats > 0 && ns <= steps * (needs.ns + 3 * kPhaseNs) + 2 * kCallNs;
+    return small->n_mats > 0 && ns <= steps * needs.ns + 2 * kCallNs;
 }
 
-// The number of blocks per tile that takes less time.
+// With the kind of tile that takes the least time.
 uint32_t make_batch(const co3_mat* in, const co3_mat* out, uint32_t n_mats, uint32_t at, bool muon, OrthBatch* b, BatchNeeds* needs) {
-    BatchNeeds two;
-    const uint32_t n = plan_batch(in, out, n_mats, at, muon, 2, b, &two);
-    if (n == 0) return 0;
-    const uint32_t m = plan_batch(in, out, n_mats, at, muon, 1, b, needs);
-    if (m != 0 && needs->ns <= two.ns) return m;
-    return plan_batch(in, out, n_mats, at, muon, 2, b, needs);
+    uint32_t best = kNarrow;
+    uint64_t ns = ~0ull;
+    for (uint32_t tile = kNarrow; tile <= kPair; ++tile) {
+        if (plan_batch(in, out, n_mats, at, muon, tile, b, needs) == 0) return 0;
+        if (needs->ns < ns) { ns = needs->ns; best = tile; }
+    }
+    return plan_batch(in, out, n_mats, at, muon, best, b, needs);
 }
 
 bool valid_ns(const co3_ns& ns) {
@@ -973,8 +1040,9 @@ void only_plain(OrthBatch* b) {
 }
 
 // All blocks have to be resident at once: as many tiles at a time as the device holds, asked for once per device.
-template <int kCtas>
+template <int kTile>
 int launch_steps(const StepArgs& a, uint32_t widest, cudaStream_t st) {
+    constexpr uint32_t kCtas = Tiling<kTile>::kCtas;
     static std::atomic<int> resident[64];
     int dev = 0;
     CO3_CUDA(cudaGetDevice(&dev));
@@ -993,13 +1061,13 @@ int launch_steps(const StepArgs& a, uint32_t widest, cudaStream_t st) {
     cfg.numAttrs = kCtas == 1 ? 1 : 2;
     int n = dev < 64 ? resident[dev].load(std::memory_order_relaxed) : 0;
     if (n == 0) {
-        CO3_CUDA(cudaFuncSetAttribute(orth_steps_kernel<kCtas>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kStepSmem));
+        CO3_CUDA(cudaFuncSetAttribute(orth_steps_kernel<kTile>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kStepSmem));
         if (kCtas == 1) {
             CO3_CUDA(cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev));
         } else {
             cfg.attrs = attr + 1;
             cfg.numAttrs = 1;
-            CO3_CUDA(cudaOccupancyMaxActiveClusters(&n, orth_steps_kernel<kCtas>, &cfg));
+            CO3_CUDA(cudaOccupancyMaxActiveClusters(&n, orth_steps_kernel<kTile>, &cfg));
             cfg.attrs = attr;
             cfg.numAttrs = 2;
         }
@@ -1007,7 +1075,7 @@ int launch_steps(const StepArgs& a, uint32_t widest, cudaStream_t st) {
         if (dev < 64) resident[dev].store(n, std::memory_order_relaxed);
     }
     cfg.gridDim = dim3(kCtas * std::min(widest, (uint32_t)n));
-    CO3_CUDA(cudaLaunchKernelEx(&cfg, orth_steps_kernel<kCtas>, a));
+    CO3_CUDA(cudaLaunchKernelEx(&cfg, orth_steps_kernel<kTile>, a));
     return CO3_OK;
 }
 
@@ -1088,7 +1156,8 @@ int orth_run(const OrthCall& c, const co3_ns* ns_in, co3_result* res, void* work
             sa.limit_ns = 500000000ull + ns.steps * needs.work * 64ull;
             sa.res = res;
             const uint32_t widest = std::max(batch.n_tasks[0], std::max(batch.n_tasks[1], batch.n_tasks[2]));
-            const int e = batch.ctas == 1 ? launch_steps<1>(sa, widest, st) : launch_steps<2>(sa, widest, st);
+            const int e = batch.tile == kNarrow ? launch_steps<kNarrow>(sa, widest, st)
+                          : batch.tile == kSquare ? launch_steps<kSquare>(sa, widest, st) : launch_steps<kPair>(sa, widest, st);
             if (e != CO3_OK) return e;
         }
         at += k;

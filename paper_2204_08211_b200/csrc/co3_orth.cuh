@@ -76,10 +76,9 @@ __device__ __forceinline__ uint64_t smem_desc(uint32_t addr, bool transposed, ui
 // 16 columns of the sum further.  Descriptors reach the tensor core through the warp's uniform registers: with a step
 // that is not known to the compiler each product costs about 120 cycles to issue, with one that is, 64 or 128 to do.
 __host__ __device__ constexpr uint32_t desc_step(bool transposed) { return transposed ? 2048u >> 4 : 32u >> 4; }
-// D fp32, A and B fp16; one block: 128 x 128, a pair of blocks: 256 x 256
-template <int kCtas>
-__host__ __device__ constexpr uint32_t instr_desc(bool a_transposed, bool b_transposed) {
-    return (1u << 4) | ((uint32_t)a_transposed << 15) | ((uint32_t)b_transposed << 16) | ((128u * kCtas / 8u) << 17) | ((128u * kCtas / 16u) << 24);
+// D fp32, A and B fp16
+__host__ __device__ constexpr uint32_t instr_desc(bool a_transposed, bool b_transposed, uint32_t rows, uint32_t cols) {
+    return (1u << 4) | ((uint32_t)a_transposed << 15) | ((uint32_t)b_transposed << 16) | ((cols / 8u) << 17) | ((rows / 16u) << 24);
 }
 
 // kScale: what is there already counts 2^-kScale.
@@ -175,19 +174,6 @@ __device__ __forceinline__ bool try_wait_cluster(uint64_t* bar, uint32_t parity)
         : "memory");
     return done != 0;
 }
-// The same without waiting at all.
-__device__ __forceinline__ bool test_cluster(uint64_t* bar, uint32_t parity) {
-    uint32_t done;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.test_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(done)
-        : "r"(smem_addr(bar)), "r"(parity)
-        : "memory");
-    return done != 0;
-}
-
 // A thread's kN sums times f into column `first` of the caller's matrix, down the rows from there on (cnt of them): as the
 // result, or as the step of parameters.  A warp's threads have neighbouring columns.
 template <int kN>

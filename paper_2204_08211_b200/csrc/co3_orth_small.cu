@@ -69,7 +69,7 @@ __device__ __forceinline__ void peer_store_f64(uint32_t addr, double v) {
 // Sums of 32 columns each of a product of 128 x 128 x (16 steps), into up to four accumulators of tensor memory.
 template <bool kTa, bool kTb>
 __device__ __forceinline__ void small_product(uint32_t tmem, uint32_t a, uint32_t b, uint32_t steps, uint64_t* done) {
-    constexpr uint32_t instr = instr_desc<1>(kTa, kTb), lo = kPlane >> 4;
+    constexpr uint32_t instr = instr_desc(kTa, kTb, 128, 128), lo = kPlane >> 4;
     const uint64_t a0 = smem_desc(a, kTa, kBlock), b0 = smem_desc(b, kTb, kBlock);
     auto at = [](uint64_t base, bool t, uint32_t s) { return base + (t ? s * (2048u >> 4) : (s >> 2) * (kBlock >> 4) + (s & 3u) * (32u >> 4)); };
 #pragma unroll
