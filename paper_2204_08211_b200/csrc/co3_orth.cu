@@ -66,46 +66,42 @@ struct OrthWs {
     unsigned char* blocks;
 };
 
-// Tiles of a product: 128 x 64, 128 x 128, or 256 x 256 by a pair of blocks, each with 128 rows of it.
-enum OrthTile { kNarrow = 0, kSquare = 1, kPair = 2 };
+// Tiles of a product: 128 x 64 or 128 x 128.
+enum OrthTile { kNarrow = 0, kSquare = 1 };
 template <int kTile>
 struct Tiling {
-    static constexpr uint32_t kCtas = kTile == kPair ? 2 : 1, kRows = 128 * kCtas, kCols = kTile == kNarrow ? 64 : kRows;
+    static constexpr uint32_t kCols = kTile == kNarrow ? 64 : 128;
     static constexpr uint32_t kSums = 512 / kCols;                                   // tiles that tensor memory holds
     static constexpr uint32_t kColPlane = kTile == kNarrow ? kHalfPlane : kPlane;    // of the columns' operand
     static constexpr uint32_t kStageBytes = kBlock + 2 * kColPlane, kStages = kTile == kNarrow ? 4 : 3;
-    static constexpr uint32_t kOwnStages = kTile == kPair ? 2 : 1;                   // the tile's own blocks: this many stages
-    static constexpr uint32_t kOwnBytes = kTile == kNarrow ? kBlock : 2 * kBlock;    // of this size each
+    static constexpr uint32_t kOwnBytes = kTile == kNarrow ? kBlock : 2 * kBlock;    // of the tile's own blocks
 };
 
 struct OrthShape {
     uint32_t m, n;         // small side, long side
-    uint32_t mb, nb;       // both in blocks of 128, filled up to whole tiles
-    uint32_t mt, mc;       // the small side in tile rows and in tile columns
-    uint32_t nt, nc;       // the long side
-    uint32_t sym, per_row; // tiles of a symmetric product; tile columns per tile row
+    uint32_t mb, nb;       // both in blocks of 128, which are the rows of tiles
+    uint32_t mc, nc;       // both in tile columns
+    uint32_t sym, per_row; // tiles of a symmetric product; tile columns per block
     bool tall;             // rows > cols: X is the transposed matrix
 };
 
 __host__ __device__ inline OrthShape orth_shape(uint32_t rows, uint32_t cols, uint32_t tile) {
     OrthShape s;
-    const uint32_t ctas = tile == kPair ? 2u : 1u, tr = 128u * ctas, tc = tile == kNarrow ? 64u : tr;
+    const uint32_t tc = tile == kNarrow ? 64u : 128u;
     s.tall = rows > cols;
     s.m = s.tall ? cols : rows;
     s.n = s.tall ? rows : cols;
-    s.mt = (s.m + tr - 1u) / tr;
-    s.nt = (s.n + tr - 1u) / tr;
+    s.mb = (s.m + 127u) / 128u;
+    s.nb = (s.n + 127u) / 128u;
     s.mc = (s.m + tc - 1u) / tc;
     s.nc = (s.n + tc - 1u) / tc;
-    s.mb = s.mt * ctas;
-    s.nb = s.nt * ctas;
-    s.per_row = tr / tc;
+    s.per_row = 128u / tc;
     // up to and including the diagonal: (i + 1) per_row tiles in row i, as far as the matrix reaches
-    s.sym = s.mt ? s.per_row * s.mt * (s.mt - 1u) / 2u + (s.mc < s.per_row * s.mt ? s.mc : s.per_row * s.mt) : 0u;
+    s.sym = s.mb ? s.per_row * s.mb * (s.mb - 1u) / 2u + s.mc : 0u;
     return s;
 }
 // Tiles of the apply product, and of its last one, whose rows are the long side unless the matrix is tall.
-__host__ __device__ inline uint32_t orth_apply_tiles(const OrthShape& s, bool last) { return last && !s.tall ? s.nt * s.mc : s.mt * s.nc; }
+__host__ __device__ inline uint32_t orth_apply_tiles(const OrthShape& s, bool last) { return last && !s.tall ? s.nb * s.mc : s.mb * s.nc; }
 
 // Operand blocks of one matrix: X twice [mb][2 nb], A and B [mb][2 mb] (their lower triangles of tiles are used).
 __host__ __device__ inline uint64_t orth_blocks(const OrthShape& s) {
@@ -307,10 +303,10 @@ __global__ void __launch_bounds__(kLoadThreads) orth_load_kernel(LoadArgs a) {
 // columns in registers, and from there on each works on its own.  Behind a task's operands the ring carries its linear
 // term (b A or a X, the tile's own blocks); the warps put the finished values in its place, from where they go to memory.
 //
-// Which tiles: the tensor core reads its operands from shared memory, which gives 128 bytes a cycle, and the copies
-// write there too.  A stage (64 columns of the sum, 12 products) of a 128 x 128 tile moves 160 KB for 768 cycles of
-// products, of a 256 x 256 tile of two blocks 160 KB a block for 1536: there the products bound it.  The pairs take long
-// over each tile, though: small calls are faster with many small tiles.
+// Which tiles: a stage (64 columns of the sum, 12 products) of a 128 x 128 tile takes about 0.6 us, of a 128 x 64 tile
+// 0.45: the smaller ones win while there are fewer tiles than SMs (1000 x 513: 0.19 against 0.22 ms, 2048 x 2048: 0.88
+// against 0.55).  Tiles of 256 x 256 by pairs of blocks, which read half as much per product, were no faster where the
+// power limit holds the clock down (4096 x 4096: 4.36 against 4.15 ms) and much slower for small matrices.
 // ------------------------------------------------------------------------------------------------
 constexpr int kEpiThreads = 256;
 constexpr int kStepThreads = 64 + kEpiThreads + 64;
@@ -321,12 +317,11 @@ constexpr int kMaxStages = 4;
 // four, 2.1e-6 if one (2.9e-6 with all sums in fp32 arithmetic).  Steps that multiply the hi planes alone leave all
 // sums to the tensor core.
 constexpr size_t kRingBytes = 192 << 10;
-static_assert(Tiling<kNarrow>::kStages * Tiling<kNarrow>::kStageBytes == kRingBytes && Tiling<kSquare>::kStages * Tiling<kSquare>::kStageBytes == kRingBytes &&
-                  Tiling<kPair>::kStages * Tiling<kPair>::kStageBytes == kRingBytes, "one size of ring");
+static_assert(Tiling<kNarrow>::kStages * Tiling<kNarrow>::kStageBytes == kRingBytes && Tiling<kSquare>::kStages * Tiling<kSquare>::kStageBytes == kRingBytes, "one size of ring");
 
 struct Task {
     uint32_t step, phase, mat;
-    uint32_t rb, cg;      // block row, and first group of 64 columns, of this block's part of the tile
+    uint32_t rb, cg;      // block row, and first group of 64 columns, of the tile
     uint32_t k0, k1;      // operand blocks of the summed dimension
     uint32_t part, parts;
     uint32_t tile;        // index within the matrix and phase
@@ -343,10 +338,11 @@ struct MatView {
 };
 
 struct StepSmem {
-    uint64_t full[kMaxStages];
+    // A barrier tells its last phase from the one before and no more: who waits on it has to see every phase.  So each
+    // stage of the ring has one per reader: warp 1, warp 11, warps 2..9.
+    uint64_t full[3][kMaxStages];
     uint64_t empty[kMaxStages];      // a stage of operands has been multiplied, or one of the tile's own blocks stored
     uint32_t stored[kMaxStages];     // warps that are done with a stage of the tile's own blocks
-    uint64_t peer_full[kMaxStages];  // first block of a pair: the other block's stage is full
     uint64_t sum_full[8], sum_empty[8];
     uint64_t done[2];
     uint32_t tmem, failed;
@@ -370,7 +366,7 @@ struct StepArgs {
 };
 
 template <int kTile>
-__device__ __forceinline__ Task find_task(const StepArgs& a, const StepSmem& sm, const uint32_t* n_tasks, uint32_t n_mats, uint32_t g, uint32_t rank, MatView& v) {
+__device__ __forceinline__ Task find_task(const StepArgs& a, const StepSmem& sm, const uint32_t* n_tasks, uint32_t n_mats, uint32_t g, MatView& v) {
     using L = Tiling<kTile>;
     Task k;
     const uint32_t per_step = n_tasks[0] + n_tasks[1] + n_tasks[2];
@@ -387,7 +383,7 @@ __device__ __forceinline__ Task find_task(const StepArgs& a, const StepSmem& sm,
     k.parts = v.t.splits[k.phase];
     k.tile = x / k.parts;
     k.part = x - k.tile * k.parts;
-    k.before = 8 * L::kCtas * (k.step * (2 * v.s.sym + orth_apply_tiles(v.s, false)) + k.phase * v.s.sym);
+    k.before = 8 * (k.step * (2 * v.s.sym + orth_apply_tiles(v.s, false)) + k.phase * v.s.sym);
     k.swap = k.diagonal = k.skip = false;
     uint32_t i, j, blocks;
     if (k.phase == kApply) {
@@ -401,15 +397,15 @@ __device__ __forceinline__ Task find_task(const StepArgs& a, const StepSmem& sm,
         j = k.tile - i * cols;
         blocks = (v.s.m + 63u) / 64u;
     } else {  // tiles on and below the diagonal
-        const uint32_t t = k.tile / (L::kRows / L::kCols);
+        const uint32_t t = k.tile / (128u / L::kCols);
         i = (uint32_t)((sqrtf(8.0f * (float)t + 1.0f) - 1.0f) * 0.5f);
         while (v.s.per_row * i * (i + 1) / 2 > k.tile) --i;
         while (v.s.per_row * (i + 1) * (i + 2) / 2 <= k.tile) ++i;
         j = k.tile - v.s.per_row * i * (i + 1) / 2;
-        k.diagonal = L::kCols == L::kRows && i == j;
+        k.diagonal = kTile == kSquare && i == j;
         blocks = ((k.phase == kGram ? v.s.n : v.s.m) + 63u) / 64u;
     }
-    k.rb = i * L::kCtas + rank;
+    k.rb = i;
     k.cg = j * (L::kCols / 64u);
     k.k0 = (uint32_t)((uint64_t)blocks * k.part / k.parts);
     k.k1 = (uint32_t)((uint64_t)blocks * (k.part + 1) / k.parts);
@@ -464,17 +460,16 @@ struct Operand {
         if (pairs) copy_in(dst + kHalfPlane, p + kPlane, kHalfPlane, bar);
     }
 };
-// The operand of the tile's rows (which == 0) or columns (1), this block's share of it.
+// The operand of the tile's rows (which == 0) or columns (1).
 template <int kTile>
-__device__ __forceinline__ Operand operand(const Task& k, const MatView& v, uint32_t rank, int which) {
-    using L = Tiling<kTile>;
-    const uint32_t r = which == 0 ? k.rb : kTile == kNarrow ? k.cg : k.cg / 2 + rank;
+__device__ __forceinline__ Operand operand(const Task& k, const MatView& v, int which) {
+    const uint32_t r = which == 0 ? k.rb : kTile == kNarrow ? k.cg : k.cg / 2;
     const uint32_t block_row = which == 1 && kTile == kNarrow ? r / 2 : r;
     const uint64_t row_x = (uint64_t)(2 * v.s.nb) * kBlock, row_m = (uint64_t)(2 * v.s.mb) * kBlock;
     if (k.phase == kGram) return {v.op.x[k.step & 1u], row_x, r, 0xffffffffu};
     if (k.phase == kApply && (which == 1) != k.swap) return {v.op.x[k.step & 1u], row_x, r, 0u};
-    // a symmetric matrix: stored up to and including the tile row's part of the diagonal
-    return {k.phase == kPoly ? v.op.a : v.op.b, row_m, r, (block_row / L::kCtas + 1) * (2 * L::kCtas)};
+    // a symmetric matrix: stored up to and including the block on the diagonal
+    return {k.phase == kPoly ? v.op.a : v.op.b, row_m, r, (block_row + 1) * 2};
 }
 
 __device__ __forceinline__ uint32_t load_acquire(const uint32_t* p) {
@@ -482,14 +477,12 @@ __device__ __forceinline__ uint32_t load_acquire(const uint32_t* p) {
     asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
     return v;
 }
-template <int kCtas>
 __device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity, uint64_t limit_ns) {
-    auto test = [&]() { return kCtas == 1 ? mbar_try_wait(bar, parity) : try_wait_cluster(bar, parity); };
-    if (test()) return true;
+    if (mbar_try_wait(bar, parity)) return true;
     const uint64_t t0 = global_timer_ns();
     for (;;) {
         for (int i = 0; i < 64; ++i)
-            if (test()) return true;
+            if (mbar_try_wait(bar, parity)) return true;
         if (global_timer_ns() - t0 > limit_ns) return false;
     }
 }
@@ -511,36 +504,25 @@ __device__ __forceinline__ void bulk_stores_commit() { asm volatile("cp.async.bu
 __device__ __forceinline__ void bulk_stores_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
 __device__ __forceinline__ void bulk_stores_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 
-template <int kCtas>
-__device__ __forceinline__ void tile_sync() {  // all threads of the blocks that share a tile
-    if constexpr (kCtas == 1) {
-        __syncthreads();
-    } else {
-        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-    }
-}
-
 // The products of one stage: 64 columns of the sum, operands at a and b in shared memory.
 template <int kTile, bool kTa, bool kTb>
-__device__ __forceinline__ void multiply_stage(uint32_t d, uint32_t a, uint32_t b, bool pairs, bool opens) {
+__device__ __forceinline__ void multiply_stage(uint32_t d, uint32_t a, uint32_t b, bool pairs) {
     using L = Tiling<kTile>;
-    constexpr int kCtas = L::kCtas;
-    constexpr uint32_t instr = instr_desc(kTa, kTb, L::kRows, L::kCols), da = desc_step(kTa), db = desc_step(kTb);
+    constexpr uint32_t instr = instr_desc(kTa, kTb, 128, L::kCols), da = desc_step(kTa), db = desc_step(kTb);
     const uint64_t ah = smem_desc(a, kTa), bh = smem_desc(b, kTb);
     const uint64_t al = ah + (kPlane >> 4), bl = bh + (L::kColPlane >> 4);
     if (pairs) {
         // the corrections first, 2^11 times too large; the first product of the hi planes scales them down
 #pragma unroll
-        for (uint32_t e = 0; e < 4; ++e) tc_mma<kCtas>(d, ah + e * da, bl + e * db, instr, e > 0);
+        for (uint32_t e = 0; e < 4; ++e) tc_mma(d, ah + e * da, bl + e * db, instr, e > 0);
 #pragma unroll
-        for (uint32_t e = 0; e < 4; ++e) tc_mma<kCtas>(d, al + e * da, bh + e * db, instr, true);
-        tc_mma<kCtas, kLoBits>(d, ah, bh, instr, true);
+        for (uint32_t e = 0; e < 4; ++e) tc_mma(d, al + e * da, bh + e * db, instr, true);
+        tc_mma<kLoBits>(d, ah, bh, instr, true);
 #pragma unroll
-        for (uint32_t e = 1; e < 4; ++e) tc_mma<kCtas>(d, ah + e * da, bh + e * db, instr, true);
+        for (uint32_t e = 1; e < 4; ++e) tc_mma(d, ah + e * da, bh + e * db, instr, true);
     } else {
 #pragma unroll
-        for (uint32_t e = 0; e < 4; ++e) tc_mma<kCtas>(d, ah + e * da, bh + e * db, instr, !opens || e > 0);
+        for (uint32_t e = 0; e < 4; ++e) tc_mma(d, ah + e * da, bh + e * db, instr, e > 0);
     }
 }
 
@@ -548,35 +530,33 @@ template <int kTile>
 __global__ void __launch_bounds__(kStepThreads, 1) orth_steps_kernel(const __grid_constant__ StepArgs a) {
     extern __shared__ unsigned char smem_raw[];
     using L = Tiling<kTile>;
-    constexpr uint32_t kCtas = L::kCtas, kCols = L::kCols, kSums = L::kSums, kStages = L::kStages, kStageBytes = L::kStageBytes, kOwn = L::kOwnStages;
+    constexpr uint32_t kCols = L::kCols, kSums = L::kSums, kStages = L::kStages, kStageBytes = L::kStageBytes;
     unsigned char* ring = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
     StepSmem& sm = *reinterpret_cast<StepSmem*>(ring + kSmemOff);
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
-    const uint32_t rank = blockIdx.x % kCtas, group = blockIdx.x / kCtas, groups = gridDim.x / kCtas;
     const uint32_t n_mats = a.ws.batch->n_mats;
     const uint32_t n_tasks[3] = {a.ws.batch->n_tasks[0], a.ws.batch->n_tasks[1], a.ws.batch->n_tasks[2]};
     const uint32_t total = a.ns.steps * (n_tasks[0] + n_tasks[1] + n_tasks[2]);
     for (uint32_t i = threadIdx.x; i < n_mats; i += kStepThreads)
         for (int p = 0; p < 3; ++p) sm.task0[p][i] = a.ws.batch->mat[i].task0[p];
     if (threadIdx.x == 0) {
-        for (uint32_t i = 0; i < kStages; ++i) { mbar_init(&sm.full[i], 2); mbar_init(&sm.empty[i], 1); mbar_init(&sm.peer_full[i], 1); sm.stored[i] = 0; }
-        for (uint32_t i = 0; i < kSums; ++i) { mbar_init(&sm.sum_full[i], 1); mbar_init(&sm.sum_empty[i], 8 * kCtas); }
+        for (uint32_t i = 0; i < kStages; ++i) {
+            for (int w = 0; w < 3; ++w) mbar_init(&sm.full[w][i], 2);
+            mbar_init(&sm.empty[i], 1);
+            sm.stored[i] = 0;
+        }
+        for (uint32_t i = 0; i < kSums; ++i) { mbar_init(&sm.sum_full[i], 1); mbar_init(&sm.sum_empty[i], 8); }
         mbar_init(&sm.done[0], 1);
         mbar_init(&sm.done[1], 1);
         sm.failed = 0;
     }
     if (warp == 1) {
-        if constexpr (kCtas == 1) {
-            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(&sm.tmem)) : "memory");
-            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-        } else {
-            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(&sm.tmem)) : "memory");
-            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
-        }
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(&sm.tmem)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     __syncwarp();
     tc_fence_before();
-    tile_sync<kCtas>();
+    __syncthreads();
     tc_fence_after();
     const uint32_t tmem = sm.tmem;
     volatile uint32_t* failed = &sm.failed;
@@ -584,118 +564,104 @@ __global__ void __launch_bounds__(kStepThreads, 1) orth_steps_kernel(const __gri
 
     if ((warp == 0 || warp == 10) && lane == 0) {
         const int which = warp == 0 ? 0 : 1;
-        uint32_t it = 0, st = 0, turn = 0;  // stages filled; the ring's next one, and how often the ring has been gone through
-        const uint32_t ring_addr = smem_addr(ring), full0 = smem_addr(&sm.full[0]);
-        for (uint32_t g = group; g < total && !*failed; g += groups) {
-            const Task k = find_task<kTile>(a, sm, n_tasks, n_mats, g, rank, v);
+        uint32_t st = 0, turn = 0;  // the ring's next stage, and how often the ring has been gone through
+        uint32_t unit = 0;          // stages of operands begun: warps 1 and 11 multiply every other one
+        uint32_t filled = 0;        // phases of sm.full begun, modulo 2: bit 4 reader + stage
+        const uint32_t ring_addr = smem_addr(ring), full0 = smem_addr(&sm.full[0][0]);
+        for (uint32_t g = blockIdx.x; g < total && !*failed; g += gridDim.x) {
+            const Task k = find_task<kTile>(a, sm, n_tasks, n_mats, g, v);
             if (k.skip) continue;
-            const Operand o = operand<kTile>(k, v, rank, which);
+            const Operand o = operand<kTile>(k, v, which);
             const bool pairs = (a.pairs >> k.step) & 1u;
             if (!wait_tiles(a.ws.ctrl, k.mat, k.before, a.limit_ns)) { *failed = 1; break; }
             fence_async_all();  // orders what the counter says after the copies that follow
             auto begin = [&]() {
-                if (turn > 0 && !wait_for<kCtas>(&sm.empty[st], (turn - 1) & 1u, a.limit_ns)) { *failed = 1; return false; }
+                if (turn > 0 && !wait_for(&sm.empty[st], (turn - 1) & 1u, a.limit_ns)) { *failed = 1; return false; }
                 return true;
             };
-            auto next = [&]() {
-                ++it;
+            auto next = [&](uint32_t reader) {
+                filled ^= 1u << (4 * reader + st);
                 if (++st == kStages) { st = 0; ++turn; }
             };
             const bool half_width = which == 1 && kTile == kNarrow;
             const uint32_t part = half_width ? kHalfPlane : kPlane, bytes = pairs ? 2 * part : part;  // of a stage
-            for (uint32_t q = k.k0; q < k.k1; ++q, next()) {
+            for (uint32_t q = k.k0; q < k.k1; ++q) {
                 if (!begin()) break;
-                const uint32_t dst = ring_addr + st * kStageBytes + (which ? kBlock : 0u), bar = full0 + st * 8u;
-                if (which == 1 && k.diagonal) { mbar_arrive(&sm.full[st]); continue; }
-                arrive_expect(bar, bytes);
-                if (half_width) o.fetch64(dst, q, pairs, bar); else o.fetch128(dst, q, pairs, bar);
+                const uint32_t reader = unit & 1u, bar = full0 + (reader * kMaxStages + st) * 8u;
+                const uint32_t dst = ring_addr + st * kStageBytes + (which ? kBlock : 0u);
+                if (which == 1 && k.diagonal) {
+                    mbar_arrive(&sm.full[reader][st]);
+                } else {
+                    arrive_expect(bar, bytes);
+                    if (half_width) o.fetch64(dst, q, pairs, bar); else o.fetch128(dst, q, pairs, bar);
+                }
+                next(reader);
+                ++unit;
             }
             const unsigned char* lin = which == 0 ? linear_term(a, k, v) : nullptr;
-            for (uint32_t q = 0; q < kOwn && !*failed; ++q, next()) {
-                if (!begin()) break;
-                const uint32_t bar = full0 + st * 8u;
+            if (!*failed && begin()) {
+                const uint32_t bar = full0 + (2 * kMaxStages + st) * 8u;
                 if (lin) {
                     arrive_expect(bar, L::kOwnBytes);
-                    copy_in(ring_addr + st * kStageBytes, lin + (uint64_t)q * L::kOwnBytes, L::kOwnBytes, bar);
+                    copy_in(ring_addr + st * kStageBytes, lin, L::kOwnBytes, bar);
                 } else {
-                    mbar_arrive(&sm.full[st]);  // nothing to fetch: the stage is there for the results
+                    mbar_arrive(&sm.full[2][st]);  // nothing to fetch: the stage is there for the results
                 }
+                next(2);
             }
         }
         // copies in flight end before the block does, whoever else has given up
-        for (uint32_t q = it > kStages ? it - kStages : 0; q < it; ++q) mbar_wait(&sm.full[q % kStages], (q / kStages) & 1u);
-    } else if ((warp == 1 || warp == 11) && lane == 0 && rank == 0) {
+        for (uint32_t b = 0; b < 12; ++b)
+            if (b % 4 < kStages) mbar_wait(&sm.full[b / 4][b % 4], ((filled >> b) & 1u) ^ 1u);
+    } else if ((warp == 1 || warp == 11) && lane == 0) {
         const uint32_t mine = warp == 1 ? 0u : 1u;
-        uint32_t unit = 0;  // sums begun: a stage's, or where the hi planes alone are multiplied a task's
-        uint32_t st = 0, turn = 0, buf = 0, buf_turn = 0;  // next stage of the ring, next sum in tensor memory, and how often round
+        uint32_t unit = 0, seen = 0;             // stages begun; phases of this warp's sm.full, modulo 2, by stage
+        uint32_t st = 0, buf = 0, buf_turn = 0;  // next stage of the ring; next sum in tensor memory, and how often round
         const uint32_t ring_addr = smem_addr(ring);
-        auto next_stage = [&]() {
-            if (++st == kStages) { st = 0; ++turn; }
-        };
-        // every stage is waited for, the other warp's too: a barrier tells only its last phase from the one before
-        auto full_stage = [&]() {
-            return wait_for<kCtas>(&sm.full[st], turn & 1u, a.limit_ns) && (kCtas == 1 || wait_for<kCtas>(&sm.peer_full[st], turn & 1u, a.limit_ns));
-        };
-        auto next_sum = [&]() {
-            ++unit;
-            if (++buf == kSums) { buf = 0; ++buf_turn; }
-        };
-        for (uint32_t g = group; g < total && !*failed; g += groups) {
-            const Task k = find_task<kTile>(a, sm, n_tasks, n_mats, g, rank, v);
+        for (uint32_t g = blockIdx.x; g < total && !*failed; g += gridDim.x) {
+            const Task k = find_task<kTile>(a, sm, n_tasks, n_mats, g, v);
             if (k.skip) continue;
             const bool pairs = (a.pairs >> k.step) & 1u;
-            const uint32_t from_a = operand<kTile>(k, v, rank, 0).from, from_b = operand<kTile>(k, v, rank, 1).from;
+            const uint32_t from_a = operand<kTile>(k, v, 0).from, from_b = operand<kTile>(k, v, 1).from;
             bool ok = true;
-            for (uint32_t q = k.k0; q < k.k1; ++q, next_stage()) {
-                const bool opens = pairs || q == k.k0, closes = pairs || q + 1 == k.k1;
-                if (!full_stage()) { ok = false; break; }
+            for (uint32_t q = k.k0; q < k.k1; ++q) {
                 if ((unit & 1u) == mine) {
-                    const uint32_t d = tmem + buf * kCols;
-                    if (opens && buf_turn > 0 && !wait_for<kCtas>(&sm.sum_empty[buf], (buf_turn - 1) & 1u, a.limit_ns)) { ok = false; break; }
+                    if (!wait_for(&sm.full[mine][st], (seen >> st) & 1u, a.limit_ns)) { ok = false; break; }
+                    seen ^= 1u << st;
+                    if (buf_turn > 0 && !wait_for(&sm.sum_empty[buf], (buf_turn - 1) & 1u, a.limit_ns)) { ok = false; break; }
                     tc_fence_after();
-                    const uint32_t at = ring_addr + st * kStageBytes, bt = k.diagonal ? at : at + kBlock;
+                    const uint32_t d = tmem + buf * kCols, at = ring_addr + st * kStageBytes, bt = k.diagonal ? at : at + kBlock;
                     if (q >= from_a) {
-                        if (q >= from_b) multiply_stage<kTile, true, true>(d, at, bt, pairs, opens);
-                        else multiply_stage<kTile, true, false>(d, at, bt, pairs, opens);
+                        if (q >= from_b) multiply_stage<kTile, true, true>(d, at, bt, pairs);
+                        else multiply_stage<kTile, true, false>(d, at, bt, pairs);
                     } else {
-                        if (q >= from_b) multiply_stage<kTile, false, true>(d, at, bt, pairs, opens);
-                        else multiply_stage<kTile, false, false>(d, at, bt, pairs, opens);
+                        if (q >= from_b) multiply_stage<kTile, false, true>(d, at, bt, pairs);
+                        else multiply_stage<kTile, false, false>(d, at, bt, pairs);
                     }
-                    if (closes) tc_commit<kCtas>(&sm.sum_full[buf]);
-                    tc_commit<kCtas>(&sm.empty[st]);
+                    tc_commit(&sm.sum_full[buf]);
+                    tc_commit(&sm.empty[st]);
                 }
-                if (closes) next_sum();
+                ++unit;
+                if (++st == kStages) st = 0;
+                if (++buf == kSums) { buf = 0; ++buf_turn; }
             }
-            // the tile's own blocks pass from the copies to warps 2..9
-            for (uint32_t q = 0; ok && q < kOwn; ++q, next_stage()) ok = full_stage();
             if (!ok) { *failed = 1; break; }
+            if (++st == kStages) st = 0;  // the tile's own blocks pass from the copies to warps 2..9
         }
-        tc_commit<kCtas>(&sm.done[mine]);
+        tc_commit(&sm.done[mine]);
         mbar_wait(&sm.done[mine], 0);
-    } else if (kCtas == 2 && warp == 1 && lane == 0) {
-        // the pair's second block tells the first which of its stages are full
-        uint32_t it = 0;
-        for (uint32_t g = group; g < total && !*failed; g += groups) {
-            const Task k = find_task<kTile>(a, sm, n_tasks, n_mats, g, rank, v);
-            if (k.skip) continue;
-            const uint32_t n = k.k1 - k.k0 + kOwn;
-            for (uint32_t q = 0; q < n; ++q, ++it) {
-                if (!wait_for<kCtas>(&sm.full[it % kStages], (it / kStages) & 1u, a.limit_ns)) { *failed = 1; break; }
-                mbar_arrive_first<kCtas>(&sm.peer_full[it % kStages]);
-            }
-        }
     } else if (warp >= 2 && warp < 10) {
-        constexpr int kAcc = kCols / 2, kW = kAcc < 64 ? kAcc : 64;  // columns of this warp, and how many of them lie in one block
+        constexpr int kAcc = kCols / 2;  // columns of this warp
         const uint32_t quad = warp & 3u, half = (warp - 2u) >> 2, row = quad * 32u + lane;
         const uint32_t lane_base = tmem + ((quad * 32u) << 16) + half * kAcc;
-        uint32_t it = 0, chunk = 0;
-        for (uint32_t g = group; g < total; g += groups) {
-            if (lane == 0) sm.task[warp - 2] = find_task<kTile>(a, sm, n_tasks, n_mats, g, rank, sm.view[warp - 2]);
+        uint32_t it = 0, chunk = 0, seen = 0;  // seen: phases of sm.full[2], modulo 2, by stage
+        for (uint32_t g = blockIdx.x; g < total; g += gridDim.x) {
+            if (lane == 0) sm.task[warp - 2] = find_task<kTile>(a, sm, n_tasks, n_mats, g, sm.view[warp - 2]);
             __syncwarp();
             const Task& k = sm.task[warp - 2];
             const MatView& v = sm.view[warp - 2];
             if (k.skip) { __syncwarp(); continue; }
-            const uint32_t chunks = (a.pairs >> k.step) & 1u ? k.k1 - k.k0 : 1u;
+            const uint32_t chunks = k.k1 - k.k0;
             float acc[kAcc];
 #pragma unroll
             for (int i = 0; i < kAcc; ++i) acc[i] = 0.0f;
@@ -703,7 +669,7 @@ __global__ void __launch_bounds__(kStepThreads, 1) orth_steps_kernel(const __gri
             for (uint32_t q = 0; q < chunks; ++q, ++chunk) {
                 const uint32_t buf = chunk % kSums;
                 // one lane looks: 256 threads at the barriers would slow down the one that issues the products
-                ok = lane != 0 || wait_for<kCtas>(&sm.sum_full[buf], (chunk / kSums) & 1u, a.limit_ns);
+                ok = lane != 0 || wait_for(&sm.sum_full[buf], (chunk / kSums) & 1u, a.limit_ns);
                 if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
                 tc_fence_after();
 #pragma unroll
@@ -715,19 +681,20 @@ __global__ void __launch_bounds__(kStepThreads, 1) orth_steps_kernel(const __gri
                 }
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive_first<kCtas>(&sm.sum_empty[buf]);
+                if (lane == 0) mbar_arrive(&sm.sum_empty[buf]);
             }
-            // the stage with this warp's columns of the tile's own blocks
-            const uint32_t out_it = it + (k.k1 - k.k0) + (kOwn == 1 ? 0u : half), out_st = out_it % kStages;
-            it += k.k1 - k.k0 + kOwn;
-            ok = ok && (lane != 0 || wait_for<kCtas>(&sm.full[out_st], (out_it / kStages) & 1u, a.limit_ns));
+            it += chunks;
+            const uint32_t out_st = it % kStages;  // the stage with the tile's own blocks
+            ++it;
+            ok = ok && (lane != 0 || wait_for(&sm.full[2][out_st], (seen >> out_st) & 1u, a.limit_ns));
+            seen ^= 1u << out_st;
             if (!__all_sync(0xffffffffu, ok)) { *failed = 1; break; }
 
             bool mine = true;  // this warp finishes its part of the tile
             if (k.parts > 1) {
                 // the sums of this part of the summed dimension into its slot; whoever arrives last adds all of them
                 // in order
-                const uint64_t slot0 = v.t.slot0 + ((uint64_t)k.tile * kCtas + rank) * k.parts;
+                const uint64_t slot0 = v.t.slot0 + (uint64_t)k.tile * k.parts;
                 float* to = a.ws.slots + (slot0 + k.part) * (128 * kCols);
 #pragma unroll
                 for (int i = 0; i < kAcc; ++i) __stcg(to + (half * kAcc + i) * 128 + row, acc[i]);
@@ -735,7 +702,7 @@ __global__ void __launch_bounds__(kStepThreads, 1) orth_steps_kernel(const __gri
                 __syncwarp();
                 uint32_t old = 0;
                 if (lane == 0) {
-                    old = atomicAdd(a.ws.arrive + v.t.arrive0 + ((k.phase * v.s.sym + k.tile) * kCtas + rank) * 8 + warp - 2, 1u);
+                    old = atomicAdd(a.ws.arrive + v.t.arrive0 + (k.phase * v.s.sym + k.tile) * 8 + warp - 2, 1u);
                     __threadfence();
                 }
                 old = __shfl_sync(0xffffffffu, old, 0);
@@ -755,8 +722,9 @@ __global__ void __launch_bounds__(kStepThreads, 1) orth_steps_kernel(const __gri
             const uint32_t n_rows = k.swap ? v.s.n : v.s.m, n_cols = k.phase == kApply && !k.swap ? v.s.n : v.s.m;
             const uint32_t row0 = k.rb * 128u, col0 = k.cg * 64u;
             // Rows and columns up to a multiple of 64 are written: beyond, no product reads them.
-            const bool rows_used = row0 + (quad & 2u) * 32u < n_rows;
-            if (mine && rows_used) {
+            // This warp's block of the tile, of which it has all columns or half of them, from piece p0 on.
+            const uint32_t cg = kTile == kNarrow ? 0u : half, p0 = kTile == kNarrow ? half * 4u : 0u, c0 = col0 + cg * 64u + p0 * 8u;
+            if (mine && row0 + (quad & 2u) * 32u < n_rows && col0 + cg * 64u < n_cols) {
                 const float inv_s = 1.0f / orth_s(v.s.m, v.s.n);
                 float fl = 0.0f, fa = inv_s;  // value = fl * linear + fa * sum
                 if (k.phase == kPoly) { fl = a.ns.coef[k.step][1]; fa = __fmul_rn(a.ns.coef[k.step][2], inv_s); }
@@ -772,59 +740,53 @@ __global__ void __launch_bounds__(kStepThreads, 1) orth_steps_kernel(const __gri
                 unsigned char* dst = nullptr;  // this block's part of the tile, its blocks in a row
                 if (k.phase != kApply) dst = (k.phase == kGram ? v.op.a : v.op.b) + ((uint64_t)k.rb * (2 * v.s.mb) + k.cg) * kBlock;
                 else if (!last) dst = v.op.x[(k.step & 1u) ^ 1u] + ((uint64_t)k.rb * (2 * v.s.nb) + k.cg) * kBlock;
+                unsigned char* own = ring + (size_t)out_st * kStageBytes + cg * kBlock;
 #pragma unroll
-                for (int h = 0; h < kAcc / kW; ++h) {  // one block at a time: all of its columns, or half of them
-                    const uint32_t cg = kTile == kNarrow ? 0u : half * (kAcc / 64) + h, p0 = kTile == kNarrow ? half * 4u : 0u;
-                    const uint32_t c0 = col0 + cg * 64u + p0 * 8u;
-                    if (col0 + cg * 64u >= n_cols) break;
-                    unsigned char* own = ring + (size_t)out_st * kStageBytes + (cg & 1u) * kBlock;
+                for (int p = 0; p < kAcc / 8; ++p) {
+                    float* w = acc + p * 8;
+                    const uint32_t at = swizzled(row, p0 + p);
 #pragma unroll
-                    for (int p = 0; p < kW / 8; ++p) {
-                        float* w = acc + h * 64 + p * 8;
-                        const uint32_t at = swizzled(row, p0 + p);
+                    for (int e = 0; e < 8; ++e) w[e] = __fmul_rn(fa, w[e]);
+                    if (has_lin) {
+                        float l[8];
+                        join8(*reinterpret_cast<const uint4*>(own + at), *reinterpret_cast<const uint4*>(own + at + kPlane), l);
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) w[e] = __fmul_rn(fa, w[e]);
-                        if (has_lin) {
-                            float l[8];
-                            join8(*reinterpret_cast<const uint4*>(own + at), *reinterpret_cast<const uint4*>(own + at + kPlane), l);
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) w[e] = __fmaf_rn(fl, l[e], w[e]);
-                        }
-                        if (add_diag) {
-#pragma unroll
-                            for (int e = 0; e < 8; ++e)
-                                if (c0 + p * 8 + e == row0 + row) w[e] = __fadd_rn(w[e], diag);
-                        }
-                        if (!last) {
-                            uint4 hi, lo;
-                            split8(w, hi, lo);
-                            *reinterpret_cast<uint4*>(own + at) = hi;
-                            *reinterpret_cast<uint4*>(own + at + kPlane) = lo;
-                        }
+                        for (int e = 0; e < 8; ++e) w[e] = __fmaf_rn(fl, l[e], w[e]);
                     }
-                    if (!last && kTile == kNarrow) {
-                        // half a block's columns: 64 bytes of each row, four lanes to a row
-                        __syncwarp();
+                    if (add_diag) {
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const uint32_t r = quad * 32u + (i & 3) * 8u + (lane >> 2), off = (i >> 2) * kPlane + swizzled(r, p0 + (lane & 3u));
-                            *reinterpret_cast<uint4*>(dst + off) = *reinterpret_cast<const uint4*>(own + off);
-                        }
-                    } else if (!last) {
-                        fence_async_smem();
-                        __syncwarp();
-                        if (lane < 2) {  // 32 rows of either plane lie in a row
-                            const uint32_t off = lane * kPlane + quad * 32u * 128u;
-                            bulk_copy_s2g(dst + (uint64_t)cg * kBlock + off, own + off, 32u * 128u);
-                            bulk_stores_commit();
-                        }
-                    } else {
-                        // the tile's rows run along the caller's rows, its columns across them
-                        const uint32_t c = row0 + row;
-                        const uint64_t first = v.t.out_off + (uint64_t)c0 * v.t.out_stride + c;
-                        const uint32_t n = c < v.t.cols && c0 < v.t.rows ? min((uint32_t)kW, v.t.rows - c0) : 0u;
-                        put_result<kW>(a.out, a.out_kind, first, v.t.out_stride, n, 1.0f, acc + h * 64, a.lr, a.shrink);
+                        for (int e = 0; e < 8; ++e)
+                            if (c0 + p * 8 + e == row0 + row) w[e] = __fadd_rn(w[e], diag);
                     }
+                    if (!last) {
+                        uint4 hi, lo;
+                        split8(w, hi, lo);
+                        *reinterpret_cast<uint4*>(own + at) = hi;
+                        *reinterpret_cast<uint4*>(own + at + kPlane) = lo;
+                    }
+                }
+                if (!last && kTile == kNarrow) {
+                    // half a block's columns: 64 bytes of each row, four lanes to a row
+                    __syncwarp();
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const uint32_t r = quad * 32u + (i & 3) * 8u + (lane >> 2), off = (i >> 2) * kPlane + swizzled(r, p0 + (lane & 3u));
+                        *reinterpret_cast<uint4*>(dst + off) = *reinterpret_cast<const uint4*>(own + off);
+                    }
+                } else if (!last) {
+                    fence_async_smem();
+                    __syncwarp();
+                    if (lane < 2) {  // 32 rows of either plane lie in a row
+                        const uint32_t off = lane * kPlane + quad * 32u * 128u;
+                        bulk_copy_s2g(dst + (uint64_t)cg * kBlock + off, own + off, 32u * 128u);
+                        bulk_stores_commit();
+                    }
+                } else {
+                    // the tile's rows run along the caller's rows, its columns across them
+                    const uint32_t c = row0 + row;
+                    const uint64_t first = v.t.out_off + (uint64_t)c0 * v.t.out_stride + c;
+                    const uint32_t n = c < v.t.cols && c0 < v.t.rows ? min((uint32_t)kAcc, v.t.rows - c0) : 0u;
+                    put_result<kAcc>(a.out, a.out_kind, first, v.t.out_stride, n, 1.0f, acc, a.lr, a.shrink);
                 }
             }
             // the ring's stage is free as soon as the copies have read it, the tile finished when they have written it
@@ -833,7 +795,7 @@ __global__ void __launch_bounds__(kStepThreads, 1) orth_steps_kernel(const __gri
             __syncwarp();
             if (lane == 0) {
                 __threadfence_block();
-                if (atomicAdd(&sm.stored[out_st], 1u) == 8 / kOwn - 1) {
+                if (atomicAdd(&sm.stored[out_st], 1u) == 7) {
                     sm.stored[out_st] = 0;
                     __threadfence_block();
                     mbar_arrive(&sm.empty[out_st]);
@@ -851,10 +813,9 @@ __global__ void __launch_bounds__(kStepThreads, 1) orth_steps_kernel(const __gri
         }
     }
     __syncwarp();
-    tile_sync<kCtas>();
+    __syncthreads();
     if (warp == 1) {
-        if constexpr (kCtas == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
-        else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
     }
     if (threadIdx.x == 0 && *failed) {
         a.ws.ctrl->abort = 1u;
@@ -896,7 +857,7 @@ WsPlan ws_plan(const OrthBatch* b, const BatchNeeds& needs) {
     w.arrive = w.ctrl + up256(sizeof(OrthCtrl));
     w.partial = w.arrive + up256(b ? 4ull * b->n_arrive : 0);
     w.slots = w.partial + up256(b ? 8ull * b->n_chunks : 0);
-    w.blocks = w.slots + needs.slots * (128ull * 4) * (b && b->tile == kPair ? 256 : 128);
+    w.blocks = w.slots + needs.slots * (128ull * 4) * 128;
     w.total = w.blocks + needs.blocks * kBlock;
     return w;
 }
@@ -905,14 +866,13 @@ WsPlan ws_plan(const OrthBatch* b, const BatchNeeds& needs) {
 // all SMs, but no part is shorter than kMinPart stages.
 constexpr uint64_t kPlanSms = 148, kMinPart = 8, kMaxParts = 16;
 // Time of a stage and of what a phase takes besides, in nanoseconds, by kind of tile.
-constexpr uint64_t kStageNs[3] = {450, 620, 1250}, kTilePhaseNs[3] = {6500, 7500, 18000};
+constexpr uint64_t kStageNs[2] = {450, 600}, kTilePhaseNs[2] = {6500, 7500};
 
 // Takes matrices from `at` on into one batch with the given tiles; returns how many, 0 if one is unusable.
 uint32_t plan_batch(const co3_mat* in, const co3_mat* out, uint32_t n_mats, uint32_t at, bool muon, uint32_t tile, OrthBatch* b,
                     BatchNeeds* needs) {
     uint32_t n = 0;
     uint64_t work[3] = {0, 0, 0};
-    const uint64_t ctas = tile == kPair ? 2 : 1, units = kPlanSms / ctas;
     for (; at + n < n_mats && n < kOrthMats; ++n) {
         const co3_mat &ti = in[at + n], &to = out[at + n];
         if (!valid_mat(ti) || !valid_mat(to) || ti.rows != to.rows || ti.cols != to.cols) return 0;
@@ -921,7 +881,7 @@ uint32_t plan_batch(const co3_mat* in, const co3_mat* out, uint32_t n_mats, uint
         if (plain || ti.rows == 0 || ti.cols == 0) continue;
         const OrthShape s = orth_shape(ti.rows, ti.cols, tile);
         const uint64_t km = (s.m + 63u) / 64u, kn = (s.n + 63u) / 64u;
-        if (s.mt >= (1u << 12) || (uint64_t)s.mb * s.nb >= (1u << 23)) return 0;
+        if (s.mb >= (1u << 12) || (uint64_t)s.mb * s.nb >= (1u << 23)) return 0;
         work[kGram] += s.sym * kn;
         work[kPoly] += s.sym * km;
         work[kApply] += orth_apply_tiles(s, false) * km;
@@ -948,14 +908,14 @@ uint32_t plan_batch(const co3_mat* in, const co3_mat* out, uint32_t n_mats, uint
             uint64_t most = 0;
             for (int p = 0; p < 3; ++p) {
                 const uint64_t depth = ((p == kGram ? s.n : s.m) + 63u) / 64u, tiles = p == kApply ? all : sym;
-                const uint64_t part = std::max(kMinPart, (work[p] + units - 1) / units);
+                const uint64_t part = std::max(kMinPart, (work[p] + kPlanSms - 1) / kPlanSms);
                 const uint64_t parts = std::min(kMaxParts, std::max<uint64_t>(1, depth / part));
                 m.splits[p] = (uint32_t)parts;
                 tasks[p] += tiles * parts;
-                if (parts > 1) most = std::max(most, tiles * parts * ctas);
+                if (parts > 1) most = std::max(most, tiles * parts);
             }
             slots += most;
-            arrive += (2 * sym + all) * ctas * 8;
+            arrive += (2 * sym + all) * 8;
             full += (uint64_t)s.mb * s.nb;
             blocks += orth_blocks(s);
         }
@@ -968,7 +928,7 @@ uint32_t plan_batch(const co3_mat* in, const co3_mat* out, uint32_t n_mats, uint
     uint64_t ns = 0;
     for (int p = 0; p < 3; ++p) {
         b->n_tasks[p] = (uint32_t)tasks[p];
-        if (tasks[p]) ns += (tasks[p] + units - 1) / units * work[p] * kStageNs[tile] / tasks[p] + kTilePhaseNs[tile];
+        if (tasks[p]) ns += (tasks[p] + kPlanSms - 1) / kPlanSms * work[p] * kStageNs[tile] / tasks[p] + kTilePhaseNs[tile];
     }
     b->index0 = at;
     b->first = at == 0 ? 1u : 0u;
@@ -1004,7 +964,7 @@ bool small_batch(const co3_mat* in, const co3_mat* out, uint32_t n_mats, uint32_
 uint32_t make_batch(const co3_mat* in, const co3_mat* out, uint32_t n_mats, uint32_t at, bool muon, OrthBatch* b, BatchNeeds* needs) {
     uint32_t best = kNarrow;
     uint64_t ns = ~0ull;
-    for (uint32_t tile = kNarrow; tile <= kPair; ++tile) {
+    for (uint32_t tile = kNarrow; tile <= kSquare; ++tile) {
         if (plan_batch(in, out, n_mats, at, muon, tile, b, needs) == 0) return 0;
         if (needs->ns < ns) { ns = needs->ns; best = tile; }
     }
@@ -1039,42 +999,28 @@ void only_plain(OrthBatch* b) {
     b->n_chunks = chunks;
 }
 
-// All blocks have to be resident at once: as many tiles at a time as the device holds, asked for once per device.
+// All blocks have to be resident at once: one per SM.
 template <int kTile>
 int launch_steps(const StepArgs& a, uint32_t widest, cudaStream_t st) {
-    constexpr uint32_t kCtas = Tiling<kTile>::kCtas;
-    static std::atomic<int> resident[64];
+    static std::atomic<int> sms[64];
     int dev = 0;
     CO3_CUDA(cudaGetDevice(&dev));
+    int n = dev < 64 ? sms[dev].load(std::memory_order_relaxed) : 0;
+    if (n == 0) {
+        CO3_CUDA(cudaFuncSetAttribute(orth_steps_kernel<kTile>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kStepSmem));
+        CO3_CUDA(cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev));
+        if (dev < 64) sms[dev].store(n, std::memory_order_relaxed);
+    }
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(kCtas);
+    cfg.gridDim = dim3(std::min(widest, (uint32_t)n));
     cfg.blockDim = dim3(kStepThreads);
     cfg.dynamicSmemBytes = kStepSmem;
     cfg.stream = st;
-    cudaLaunchAttribute attr[2];
+    cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeCooperative;
     attr[0].val.cooperative = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = kCtas;
-    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = kCtas == 1 ? 1 : 2;
-    int n = dev < 64 ? resident[dev].load(std::memory_order_relaxed) : 0;
-    if (n == 0) {
-        CO3_CUDA(cudaFuncSetAttribute(orth_steps_kernel<kTile>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kStepSmem));
-        if (kCtas == 1) {
-            CO3_CUDA(cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev));
-        } else {
-            cfg.attrs = attr + 1;
-            cfg.numAttrs = 1;
-            CO3_CUDA(cudaOccupancyMaxActiveClusters(&n, orth_steps_kernel<kTile>, &cfg));
-            cfg.attrs = attr;
-            cfg.numAttrs = 2;
-        }
-        if (n < 1) return CO3_ERR_CUDA;
-        if (dev < 64) resident[dev].store(n, std::memory_order_relaxed);
-    }
-    cfg.gridDim = dim3(kCtas * std::min(widest, (uint32_t)n));
+    cfg.numAttrs = 1;
     CO3_CUDA(cudaLaunchKernelEx(&cfg, orth_steps_kernel<kTile>, a));
     return CO3_OK;
 }
@@ -1156,8 +1102,7 @@ int orth_run(const OrthCall& c, const co3_ns* ns_in, co3_result* res, void* work
             sa.limit_ns = 500000000ull + ns.steps * needs.work * 64ull;
             sa.res = res;
             const uint32_t widest = std::max(batch.n_tasks[0], std::max(batch.n_tasks[1], batch.n_tasks[2]));
-            const int e = batch.tile == kNarrow ? launch_steps<kNarrow>(sa, widest, st)
-                          : batch.tile == kSquare ? launch_steps<kSquare>(sa, widest, st) : launch_steps<kPair>(sa, widest, st);
+            const int e = batch.tile == kNarrow ? launch_steps<kNarrow>(sa, widest, st) : launch_steps<kSquare>(sa, widest, st);
             if (e != CO3_OK) return e;
         }
         at += k;

@@ -82,66 +82,30 @@ __host__ __device__ constexpr uint32_t instr_desc(bool a_transposed, bool b_tran
 }
 
 // kScale: what is there already counts 2^-kScale.
-template <int kCtas, int kScale = 0>
+template <int kScale = 0>
 __device__ __forceinline__ void tc_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t instr, bool accumulate) {
-    if constexpr (kCtas == 1) {
-        if constexpr (kScale == 0)
-            asm volatile(
-                "{\n\t.reg .pred p;\n\t"
-                "setp.ne.b32 p, %4, 0;\n\t"
-                "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(instr),
-                "r"((uint32_t)accumulate)
-                : "memory");
-        else
-            asm volatile(
-                "{\n\t.reg .pred p;\n\t"
-                "setp.ne.b32 p, %4, 0;\n\t"
-                "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p, %5;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(instr),
-                "r"((uint32_t)accumulate), "n"(kScale)
-                : "memory");
-    } else {
-        if constexpr (kScale == 0)
-            asm volatile(
-                "{\n\t.reg .pred p;\n\t"
-                "setp.ne.b32 p, %4, 0;\n\t"
-                "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(instr),
-                "r"((uint32_t)accumulate)
-                : "memory");
-        else
-            asm volatile(
-                "{\n\t.reg .pred p;\n\t"
-                "setp.ne.b32 p, %4, 0;\n\t"
-                "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p, %5;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(instr),
-                "r"((uint32_t)accumulate), "n"(kScale)
-                : "memory");
-    }
-}
-// The products issued so far arrive on this barrier when they are done; of a pair, on both blocks' barrier.
-template <int kCtas>
-__device__ __forceinline__ void tc_commit(uint64_t* bar) {
-    if constexpr (kCtas == 1)
-        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(bar)) : "memory");
+    if constexpr (kScale == 0)
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "setp.ne.b32 p, %4, 0;\n\t"
+            "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(instr), "r"((uint32_t)accumulate)
+            : "memory");
     else
-        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(smem_addr(bar)), "h"((uint16_t)3)
-                     : "memory");
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "setp.ne.b32 p, %4, 0;\n\t"
+            "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p, %5;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(instr), "r"((uint32_t)accumulate),
+            "n"(kScale)
+            : "memory");
+}
+// The products issued so far arrive on this barrier when they are done.
+__device__ __forceinline__ void tc_commit(uint64_t* bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(bar)) : "memory");
 }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(bar)) : "memory");
-}
-// The same on the barrier of the pair's first block.
-template <int kCtas>
-__device__ __forceinline__ void mbar_arrive_first(uint64_t* bar) {
-    if constexpr (kCtas == 1) {
-        mbar_arrive(bar);
-    } else {
-        asm volatile(
-            "{\n\t.reg .b32 r;\n\t"
-            "mapa.shared::cluster.u32 r, %0, 0;\n\t"
-            "mbarrier.arrive.release.cluster.shared::cluster.b64 _, [r];\n\t}" ::"r"(smem_addr(bar))
-            : "memory");
-    }
 }
 // 32 columns of this warp's 32 lanes
 __device__ __forceinline__ void tc_load32(uint32_t addr, float (&v)[32]) {
@@ -163,17 +127,6 @@ __device__ __forceinline__ void tc_load32(uint32_t addr, float (&v)[32]) {
 
 __device__ __forceinline__ void fence_async_all() { asm volatile("fence.proxy.async;" ::: "memory"); }
 
-__device__ __forceinline__ bool try_wait_cluster(uint64_t* bar, uint32_t parity) {
-    uint32_t done;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(done)
-        : "r"(smem_addr(bar)), "r"(parity)
-        : "memory");
-    return done != 0;
-}
 // A thread's kN sums times f into column `first` of the caller's matrix, down the rows from there on (cnt of them): as the
 // result, or as the step of parameters.  A warp's threads have neighbouring columns.
 template <int kN>

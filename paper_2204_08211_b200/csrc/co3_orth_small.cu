@@ -77,19 +77,19 @@ __device__ __forceinline__ void small_product(uint32_t tmem, uint32_t a, uint32_
         const uint32_t d = tmem + (s / 2) * 128u;
         // the corrections first, 2^11 times too large; the first product of the hi planes scales them down
         if (s + 1 < steps) {
-            tc_mma<1>(d, at(a0, kTa, s), at(b0, kTb, s) + lo, instr, false);
-            tc_mma<1>(d, at(a0, kTa, s + 1), at(b0, kTb, s + 1) + lo, instr, true);
-            tc_mma<1>(d, at(a0, kTa, s) + lo, at(b0, kTb, s), instr, true);
-            tc_mma<1>(d, at(a0, kTa, s + 1) + lo, at(b0, kTb, s + 1), instr, true);
-            tc_mma<1, kLoBits>(d, at(a0, kTa, s), at(b0, kTb, s), instr, true);
-            tc_mma<1>(d, at(a0, kTa, s + 1), at(b0, kTb, s + 1), instr, true);
+            tc_mma(d, at(a0, kTa, s), at(b0, kTb, s) + lo, instr, false);
+            tc_mma(d, at(a0, kTa, s + 1), at(b0, kTb, s + 1) + lo, instr, true);
+            tc_mma(d, at(a0, kTa, s) + lo, at(b0, kTb, s), instr, true);
+            tc_mma(d, at(a0, kTa, s + 1) + lo, at(b0, kTb, s + 1), instr, true);
+            tc_mma<kLoBits>(d, at(a0, kTa, s), at(b0, kTb, s), instr, true);
+            tc_mma(d, at(a0, kTa, s + 1), at(b0, kTb, s + 1), instr, true);
         } else if (s < steps) {
-            tc_mma<1>(d, at(a0, kTa, s), at(b0, kTb, s) + lo, instr, false);
-            tc_mma<1>(d, at(a0, kTa, s) + lo, at(b0, kTb, s), instr, true);
-            tc_mma<1, kLoBits>(d, at(a0, kTa, s), at(b0, kTb, s), instr, true);
+            tc_mma(d, at(a0, kTa, s), at(b0, kTb, s) + lo, instr, false);
+            tc_mma(d, at(a0, kTa, s) + lo, at(b0, kTb, s), instr, true);
+            tc_mma<kLoBits>(d, at(a0, kTa, s), at(b0, kTb, s), instr, true);
         }
     }
-    tc_commit<1>(done);
+    tc_commit(done);
 }
 
 template <typename T>

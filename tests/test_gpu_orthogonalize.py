@@ -145,6 +145,27 @@ def test_in_place_and_repeated_calls_give_the_same_bits():
     assert torch.equal(a, b) and torch.equal(a, c)
 
 
+@pytest.mark.parametrize("shapes", [[(700, 300)] * 3 + [(64, 576)] * 4 + [(130, 2000), (5, 9), (256, 1152)], [(513, 1000)], [(40, 900)], [(1100, 1200)]])
+def test_many_calls_in_a_row(shapes):
+    """Every wait inside a call ends by itself, call after call: no status, and the same bits each time."""
+    mats, off = [], 0
+    for rows, cols in shapes:
+        mats.append((off, rows, cols))
+        off += rows * cols
+    mats = co3.make_mats(mats)
+    g = torch.randn(off, generator=torch.Generator().manual_seed(6)).cuda()
+    ws = torch.empty(co3.co3_orthogonalize_workspace_bytes(mats), dtype=torch.uint8, device="cuda")
+    want, out = torch.empty_like(g), torch.empty_like(g)
+    res = torch.zeros(1000 * co3.RESULT_DTYPE.itemsize, dtype=torch.uint8, device="cuda")
+    size = co3.RESULT_DTYPE.itemsize
+    assert co3.co3_orthogonalize(g, mats, want, None, ws, res[:size]) == co3.OK
+    for k in range(1, 1000):
+        assert co3.co3_orthogonalize(g, mats, out, None, ws, res[k * size:(k + 1) * size]) == co3.OK
+    torch.cuda.synchronize()
+    assert (co3.read_results(res, 1000)["status"] == co3.OK).all()
+    assert torch.equal(out, want)
+
+
 @pytest.mark.parametrize("rows,cols", [(40, 60), (300, 200)])
 def test_magnitudes(rows, cols):
     """The result does not depend on the input's scale, over nearly all of fp32's range."""
