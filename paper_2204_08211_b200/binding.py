@@ -31,6 +31,8 @@ assert MAT_DTYPE.itemsize == 32 and NS_DTYPE.itemsize == 8 + 12 * NS_MAX_STEPS
 _TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 
 _lib = None
+_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda device: torch.cuda.current_stream(device).cuda_stream)
 
 
 def library_path() -> str:
@@ -96,7 +98,7 @@ def _dev(t, allow_none: bool = False):
 
 def _stream(stream):
     if stream is None:
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+        return torch.cuda.current_stream().cuda_stream
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
@@ -320,6 +322,11 @@ def _rows(t, like=None):
     return t.data_ptr(), rows, cols, rs if rows > 1 else max(rs, cols)
 
 
+def _stream_of(t, stream):
+    """The current stream of t's device unless one is given (the short way: these calls can be microseconds long)."""
+    return _current_stream(t.get_device()) if stream is None else _stream(stream)
+
+
 def _vec(t, n):
     """Device pointer of n fp32 values (or None)."""
     if t is None:
@@ -334,7 +341,7 @@ def co3_layer_norm(x, weight, bias, y, mean=None, rstd=None, eps=1e-5, stream=No
     px, rows, cols, xs = _rows(x)
     py, _, _, ys = _rows(y, x)
     return (_lib or _load()).co3_layer_norm(px, _TYPES[x.dtype], _vec(weight, cols), _vec(bias, cols), py, rows, cols, xs,
-                                            ys, eps, _vec(mean, rows), _vec(rstd, rows), _stream(stream))
+                                            ys, eps, _vec(mean, rows), _vec(rstd, rows), _stream_of(x, stream))
 
 
 def co3_layer_norm_workspace_bytes(rows: int, cols: int, n_clients: int = 1) -> int:
@@ -356,10 +363,10 @@ def co3_layer_norm_backward(dy, x, weight, mean, rstd, dx, dweight, dbias, n_cli
     if n_clients < 1 or rows % n_clients:
         raise ValueError("co3_layer_norm_backward: the rows do not divide into n_clients batches")
     reach = (n_clients - 1) * client_stride_elems + cols
-    return _load().co3_layer_norm_backward(pd, px, _TYPES[dy.dtype], _vec(weight, cols), _vec(mean, rows), _vec(rstd, rows), po,
-                                           _vec(dweight, reach), _vec(dbias, reach), rows // n_clients, cols, ds, xs, os_,
-                                           n_clients, client_stride_elems, 1 if accumulate else 0, _dev(workspace),
-                                           workspace.numel() * workspace.element_size(), _stream(stream))
+    return (_lib or _load()).co3_layer_norm_backward(
+        pd, px, _TYPES[dy.dtype], _vec(weight, cols), _vec(mean, rows), _vec(rstd, rows), po, _vec(dweight, reach),
+        _vec(dbias, reach), rows // n_clients, cols, ds, xs, os_, n_clients, client_stride_elems, 1 if accumulate else 0,
+        _dev(workspace), workspace.numel() * workspace.element_size(), _stream_of(dy, stream))
 
 
 def _mats(mats):
@@ -376,13 +383,14 @@ def _ns(ns):
     return ns.ctypes.data
 
 
-def _fits(mats, t, what) -> None:
-    """The library cannot see a buffer's length: every listed matrix has to end inside the tensor."""
-    used = mats[(mats["rows"] > 0) & (mats["cols"] > 0)]
-    if used.size:
-        ends = used["offset"].astype(object) + (used["rows"].astype(object) - 1) * used["row_stride"].astype(object) + used["cols"].astype(object)
-        if ends.max() > t.numel():
-            raise ValueError("%s: a matrix ends beyond the tensor" % what)
+def _fits(mats, tensors, what) -> None:
+    """The library cannot see a buffer's length: every listed matrix has to end inside the tensors."""
+    room = min(t.numel() for t in tensors)
+    rows, cols, offset, stride = (mats[f].astype(np.float64) for f in ("rows", "cols", "offset", "row_stride"))
+    ends = np.where((rows > 0) & (cols > 0), offset + (rows - 1) * stride + cols, 0.0)
+    worst = ends.max(initial=0.0)
+    if worst > room:  # (a double counts exactly up to far beyond any memory)
+        raise ValueError("%s: a matrix ends beyond the tensor" % what)
 
 
 def co3_orthogonalize_workspace_bytes(mats: np.ndarray) -> int:
@@ -402,8 +410,11 @@ def co3_orthogonalize(inp, in_mats, out, out_mats, workspace, res, ns=None, stre
     q, nq = (None, n) if out_mats is None or out_mats is in_mats else _mats(out_mats)
     if nq != n or inp.dtype not in _TYPES or out.dtype not in _TYPES:
         raise ValueError("co3_orthogonalize: fp32, fp16 or bf16 tensors and as many layouts for out as for in")
-    _fits(in_mats, inp, "co3_orthogonalize")
-    _fits(in_mats if q is None else out_mats, out, "co3_orthogonalize")
+    if q is None:
+        _fits(in_mats, (inp, out), "co3_orthogonalize")
+    else:
+        _fits(in_mats, (inp,), "co3_orthogonalize")
+        _fits(out_mats, (out,), "co3_orthogonalize")
     return _load().co3_orthogonalize(_dev(inp), _TYPES[inp.dtype], p, _dev(out), _TYPES[out.dtype], q, n, _ns(ns),
                                      _dev(res), _dev(workspace), workspace.numel() * workspace.element_size(),
                                      _stream(stream))
@@ -416,7 +427,7 @@ def co3_muon_update(grad, momentum, params, mats, mu, nesterov, lr, weight_decay
     for t in (grad, momentum, params):
         if t.dtype != torch.float32:
             raise ValueError("co3_muon_update: fp32 tensors")
-        _fits(mats, t, "co3_muon_update")
+    _fits(mats, (grad, momentum, params), "co3_muon_update")
     return _load().co3_muon_update(_dev(grad), _dev(momentum), _dev(params), p, n, float(mu), 1 if nesterov else 0,
                                    float(lr), float(weight_decay), _ns(ns), _dev(res), _dev(workspace),
                                    workspace.numel() * workspace.element_size(), _stream(stream))

@@ -209,6 +209,20 @@ def test_other_iterations(rows, cols, coef):
     assert torch.linalg.norm(out.double().cpu() - want).item() <= bound(g, want, "f32", coef32)
 
 
+@pytest.mark.parametrize("steps", [1, 3, 5, 10])
+@pytest.mark.parametrize("rows,cols", [(300, 520), (1100, 1030)])
+def test_bf16_of_an_exactly_low_rank_matrix(rows, cols, steps):
+    """What early steps round into directions that the matrix lacks must not have grown into the result."""
+    gen = torch.Generator().manual_seed(steps)
+    whole = lambda *s: torch.randint(-2, 3, s, generator=gen, dtype=torch.float64)
+    g = (whole(rows, 8) @ whole(8, cols)).bfloat16().cuda()
+    out = torch.empty_like(g)
+    r = orthogonalize(g, co3.make_mats([(0, rows, cols)]), out, ns=co3.make_ns([COEF] * steps))
+    want = definition(g, (COEF,) * steps)
+    assert r["status"] == co3.OK
+    assert torch.linalg.norm(out.double().cpu() - want).item() <= bound(g, want, "bf16", (COEF,) * steps)
+
+
 def test_converges_to_the_polar_factor():
     """Second-order steps to convergence reach U V^T, whatever computes it."""
     g = torch.randn(96, 160, generator=torch.Generator().manual_seed(4)).cuda()
