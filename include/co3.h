@@ -456,7 +456,7 @@ int co3_muon_update(const float* grad, float* momentum, float* params, const co3
 
 /*
  * Diagnostics (no counterpart in the paper).  With profiling enabled every kernel launched by the
- * entry points above is bracketed by a CUDA event pair on the caller's stream; co3_profile_read
+ * entry points above (layer norm, co3_orthogonalize and co3_muon_update excepted: they are not recorded) is bracketed by a CUDA event pair on the caller's stream; co3_profile_read
  * waits for those events, adds up the elapsed time and the number of launches per kernel kind
  * (arrays of CO3_KERNEL_COUNT entries, [host]) and clears the records.  Off by default; at most
  * 16384 launches are recorded between reads.  Not thread-safe, and not to be left on inside a

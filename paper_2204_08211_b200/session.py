@@ -149,6 +149,61 @@ class Co3Session:
         self._check(st, "co3_decode_aggregate_update")
         return self.avg if want_avg else None
 
+    # -- layer norm at the clients ---------------------------------------------------------------
+    def new_layer_norm_workspace(self, rows: int, cols: int) -> torch.Tensor:
+        """Workspace for layer_norm_backward with `rows` rows of each client."""
+        return torch.empty(B.co3_layer_norm_workspace_bytes(rows, cols, self.n_clients), dtype=torch.uint8,
+                           device=self.device)
+
+    def layer_norm(self, x: torch.Tensor, params: torch.Tensor, gain: int, bias: int, y: torch.Tensor,
+                   mean=None, rstd=None, eps: float = 1e-5, stream=None) -> None:
+        """y <- layer norm of the rows of x with layers `gain` and `bias` of the parameter vector."""
+        st = B.co3_layer_norm(x, self._layer(params, gain), self._layer(params, bias), y, mean, rstd, eps, stream)
+        self._check(st, "co3_layer_norm")
+
+    def layer_norm_backward(self, dy, x, params, gain: int, bias: int, mean, rstd, dx, grads, workspace,
+                            accumulate: bool = False, stream=None) -> None:
+        """Its gradients for the rows of all clients, client after client: dx, and every client's gradients of the two
+        layers in its own vector of `grads`."""
+        if x.shape[1] != self.sizes[gain] or x.shape[1] != self.sizes[bias]:
+            raise ValueError("layers %d and %d are not of the rows' length" % (gain, bias))
+        at = [sum(self.sizes[:k]) for k in (gain, bias)]
+        st = B.co3_layer_norm_backward(dy, x, self._layer(params, gain), mean, rstd, dx, grads[at[0]:], grads[at[1]:],
+                                       self.n_clients, self.stride, workspace, accumulate, stream)
+        self._check(st, "co3_layer_norm_backward")
+
+    def _layer(self, vec: torch.Tensor, k: int) -> torch.Tensor:
+        at = sum(self.sizes[:k])
+        return vec[at:at + self.sizes[k]]
+
+    # -- the orthogonalised step at the server ---------------------------------------------------
+    def setup_muon(self, shapes, mu: float = 0.95, nesterov: bool = True, ns=None) -> None:
+        """shapes[k]: (rows, cols) of layer k, or None where the momentum itself is the update (gains, biases).
+        Matrices get the scale sqrt(max(1, rows / cols)), so that a step changes outputs alike at every shape."""
+        mats, at = [], 0
+        for n, shape in zip(self.sizes, shapes, strict=True):
+            rows, cols = (1, n) if shape is None else shape
+            if rows * cols != n:
+                raise ValueError("a layer of %d elements is no %d x %d matrix" % (n, rows, cols))
+            mats.append((at, rows, cols, cols, 1.0, B.MAT_PLAIN) if shape is None else
+                        (at, rows, cols, cols, max(1.0, rows / max(cols, 1)) ** 0.5, 0))
+            at += n
+        self.mats = B.make_mats(mats)
+        self.mu, self.nesterov, self.ns = float(mu), bool(nesterov), ns
+        self.momentum = torch.zeros(self.n_elem, dtype=torch.float32, device=self.device)
+        self.muon_workspace = torch.empty(B.co3_orthogonalize_workspace_bytes(self.mats), dtype=torch.uint8,
+                                          device=self.device)
+        self.res_muon = torch.zeros(B.RESULT_DTYPE.itemsize, dtype=torch.uint8, device=self.device)
+
+    def muon_update(self, params: torch.Tensor, lr: float, weight_decay: float = 0.0, stream=None) -> None:
+        """The server's step on the average that decode_aggregate left in self.avg (after setup_muon)."""
+        st = B.co3_muon_update(self.avg, self.momentum, params, self.mats, self.mu, self.nesterov, lr, weight_decay,
+                               self.muon_workspace, self.res_muon, self.ns, stream)
+        self._check(st, "co3_muon_update")
+
+    def muon_result(self) -> np.ndarray:
+        return B.read_results(self.res_muon, 1)
+
     # -- results --------------------------------------------------------------------------------
     def encode_results(self) -> np.ndarray:
         return B.read_results(self.res_enc, self.n_clients)
