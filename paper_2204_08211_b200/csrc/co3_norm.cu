@@ -29,7 +29,12 @@
 namespace co3 {
 
 constexpr uint32_t kMaxCols = 16384;   // 512 threads x 32 elements
-constexpr int kWarpRowThreads = 256;   // block of the kernels with one warp per row
+// Block of the kernels with one warp per row: with 32 elements a lane registers leave room for 12 warps on an SM, in one
+// block.  Backward in fp32 they do not quite suffice for that.  (us, 8 against 12 warps: backward 65536 x 1024 bf16 82.5
+// and 72.4, fp32 131 and 144; forward 47.4 and 46.1; 3001 x 1023 f16 backward 19.2 and 14.0, forward 9.5 and 7.3.  With
+// 16 warps registers spill: backward 65536 x 1024 bf16 124.)
+template <typename T, int kElems, bool kBackward>
+constexpr int kWarpRowThreads = kElems < 32 || (kBackward && sizeof(T) == 4) ? 256 : 384;
 constexpr size_t kRingBytes = 200 << 10;  // shared memory of an SM for rings
 constexpr int kLongThreads = 1024;
 constexpr uint64_t kPlanBlocks = 148 * 8;
@@ -130,9 +135,9 @@ struct Stretch {
     static constexpr int kPairs = kVec * kCh / 2;
 
     // Copies the stretch that starts at `p`.  The copies cover whole 16-byte pieces, so they may reach into the
-    // stretch's neighbours in the buffer; starts: nothing of the buffer lies before p, so that a piece cut by p is
-    // fetched element by element; ends: nothing lies behind, the last piece is cut short.
-    static __device__ __forceinline__ void fetch(unsigned char* dst, const T* p, uint32_t bytes, const bool (&valid)[kCh], bool starts, bool ends) {
+    // stretch's neighbours in the buffer, which begins at `lo` and ends at `hi`: within 16 bytes of these a piece that
+    // p cuts is fetched element by element, and the last piece is cut short.
+    static __device__ __forceinline__ void fetch(unsigned char* dst, const T* p, uint32_t bytes, const bool (&valid)[kCh], const T* lo, const T* hi) {
         const uint32_t lane = threadIdx.x & 31u, to = smem_addr(dst) + lane * 16u;
         if (kVec > 1) {
 #pragma unroll
@@ -141,6 +146,7 @@ struct Stretch {
         } else {
             const uint32_t ph = (uint32_t)reinterpret_cast<uintptr_t>(p) & 15u, len = ph + bytes;
             const unsigned char* src = reinterpret_cast<const unsigned char*>(p) - ph;
+            const bool starts = p - lo < int(16 / sizeof(T)), ends = (hi - p) * int(sizeof(T)) < (int64_t)bytes + 16;
             if (!starts && !ends) {
 #pragma unroll
                 for (uint32_t c = 0; c < (kBytes + 511u) / 512u; ++c) {
@@ -158,13 +164,24 @@ struct Stretch {
             }
         }
     }
+    // kVec > 1: zeros where no copy ever writes, so that `take` needs no conditions (kCleared).  Forward in blocks that
+    // is worth it (16384 x 2048 bf16 41.6 -> 27.5 us); elsewhere the loads then come too early for the registers
+    // (65536 x 1024 bf16: forward 46.3 -> 48.4, backward 72 -> 95).
+    static __device__ __forceinline__ void clear(unsigned char* dst, const bool (&valid)[kCh]) {
+        if (kVec == 1) return;
+#pragma unroll
+        for (int c = 0; c < kCh; ++c)
+            if (!valid[c]) *reinterpret_cast<uint4*>(dst + c * 512u + (threadIdx.x & 31u) * 16u) = make_uint4(0u, 0u, 0u, 0u);
+    }
     // The lane's elements, zeros beyond the row.  ph: the stretch's place within its first piece.
+    template <bool kCleared = false>
     static __device__ __forceinline__ void take(const unsigned char* from, uint32_t ph, const bool (&valid)[kCh], F2 (&v)[kPairs]) {
         const uint32_t lane = threadIdx.x & 31u;
         if (kVec > 1) {
 #pragma unroll
             for (int c = 0; c < kCh; ++c) {
-                const uint4 q = valid[c] ? *reinterpret_cast<const uint4*>(from + c * 512u + lane * 16u) : make_uint4(0u, 0u, 0u, 0u);
+                uint4 q = make_uint4(0u, 0u, 0u, 0u);
+                if (kCleared || valid[c]) q = *reinterpret_cast<const uint4*>(from + c * 512u + lane * 16u);
                 const uint32_t w[4] = {q.x, q.y, q.z, q.w};
                 if constexpr (sizeof(T) == 4) {
                     v[2 * c] = {__uint_as_float(w[0]), __uint_as_float(w[1])};
@@ -233,18 +250,19 @@ __global__ void __launch_bounds__(kMaxThreads) norm_forward_kernel(const NormArg
     __shared__ float4 s_part[2][16];
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u, warps = blockDim.x / 32u;
     const uint32_t col0 = kWarpRow ? 0u : warp * S::kElems, n_cols = min(a.cols - col0, S::kElems), bytes = n_cols * (uint32_t)sizeof(T);
-    const bool tail = kWarpRow || warp + 1 == warps;
     const uint64_t first = kWarpRow ? (uint64_t)blockIdx.x * warps + warp : blockIdx.x, step = kWarpRow ? (uint64_t)gridDim.x * warps : gridDim.x;
     unsigned char* ring = s_ring + (size_t)warp * a.ring * S::kBytes;
     bool valid[kCh];
 #pragma unroll
     for (int c = 0; c < kCh; ++c) valid[c] = (c * 32 + lane) * kVec < n_cols;
-    const T* src = static_cast<const T*>(a.x) + first * a.x_stride + col0;  // the row to be fetched next
+    for (uint32_t k = 0; !kWarpRow && k < a.ring; ++k) S::clear(ring + k * S::kBytes, valid);
+    const T *lo = static_cast<const T*>(a.x), *hi = lo + (a.rows - 1) * a.x_stride + a.cols;
+    const T* src = lo + first * a.x_stride + col0;  // the row to be fetched next
     uint64_t ahead = first;
     uint32_t slot = 0;
     const uint64_t src_step = step * a.x_stride;
     auto fetch = [&]() {
-        if (ahead < a.rows) S::fetch(ring + slot * S::kBytes, src, bytes, valid, ahead == 0 && col0 == 0, tail && ahead + 1 == a.rows);
+        if (ahead < a.rows) S::fetch(ring + slot * S::kBytes, src, bytes, valid, lo, hi);
         copies_commit();
         ahead += step;
         src += src_step;
@@ -288,7 +306,7 @@ __global__ void __launch_bounds__(kMaxThreads) norm_forward_kernel(const NormArg
         // with n1 and n2 elements grow by n1 n2 / (n1 + n2) (mean1 - mean2)^2 (Chan, Golub, LeVeque 1979).  One
         // reduction, and none of the cancellation of sum(x^2) - sum(x)^2 / n.
         F2 v[S::kPairs], s2 = both(0.0f), q2 = both(0.0f);
-        S::take(ring + now * S::kBytes, (uint32_t)reinterpret_cast<uintptr_t>(x_now) & 15u, valid, v);
+        S::template take<!kWarpRow>(ring + now * S::kBytes, (uint32_t)reinterpret_cast<uintptr_t>(x_now) & 15u, valid, v);
         now = now + 1 == a.ring ? 0u : now + 1;
 #pragma unroll
         for (int i = 0; i < S::kPairs; ++i) s2 = add2(s2, v[i]);
@@ -360,14 +378,15 @@ __global__ void __launch_bounds__(kMaxThreads) norm_backward_kernel(const NormAr
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u, warps = blockDim.x / 32u;
     const uint32_t client = blockIdx.x / a.parts, part = blockIdx.x - client * a.parts;
     const uint32_t col0 = kWarpRow ? 0u : warp * S::kElems, n_cols = min(a.cols - col0, S::kElems), bytes = n_cols * (uint32_t)sizeof(T);
-    const bool tail = kWarpRow || warp + 1 == warps;
     const uint64_t end = (uint64_t)(client + 1) * a.rows, step = kWarpRow ? (uint64_t)a.parts * warps : a.parts;
     const uint64_t first = (uint64_t)client * a.rows + (kWarpRow ? (uint64_t)part * warps + warp : part);
     unsigned char* ring = s_ring + (size_t)warp * a.ring * kSlot;
     bool valid[kCh];
 #pragma unroll
     for (int c = 0; c < kCh; ++c) valid[c] = (c * 32 + lane) * kVec < n_cols;
-    const T *x_next = static_cast<const T*>(a.x) + first * a.x_stride + col0, *d_next = static_cast<const T*>(a.dy) + first * a.dy_stride + col0;
+    const T *x_lo = static_cast<const T*>(a.x), *d_lo = static_cast<const T*>(a.dy);
+    const T *x_hi = x_lo + (a.all_rows - 1) * a.x_stride + a.cols, *d_hi = d_lo + (a.all_rows - 1) * a.dy_stride + a.cols;
+    const T *x_next = x_lo + first * a.x_stride + col0, *d_next = d_lo + first * a.dy_stride + col0;
     const T *x_now = x_next, *d_now = d_next;
     const uint64_t x_step = step * a.x_stride, d_step = step * a.dy_stride, out_step = step * a.out_stride;
     uint64_t ahead = first;
@@ -375,9 +394,8 @@ __global__ void __launch_bounds__(kMaxThreads) norm_backward_kernel(const NormAr
     auto fetch = [&]() {
         if (ahead < end) {
             unsigned char* dst = ring + slot * kSlot;
-            const bool starts = ahead == 0 && col0 == 0, ends = tail && ahead + 1 == a.all_rows;
-            S::fetch(dst, x_next, bytes, valid, starts, ends);
-            S::fetch(dst + S::kBytes, d_next, bytes, valid, starts, ends);
+            S::fetch(dst, x_next, bytes, valid, x_lo, x_hi);
+            S::fetch(dst + S::kBytes, d_next, bytes, valid, d_lo, d_hi);
             if (lane < 2)
                 asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_addr(dst) + 2 * S::kBytes + lane * 4u), "l"((lane ? a.rstd : a.mean) + ahead) : "memory");
         }
@@ -427,15 +445,18 @@ __global__ void __launch_bounds__(kMaxThreads) norm_backward_kernel(const NormAr
 #pragma unroll 4
                 for (uint32_t k = 0; k < warps; ++k) { s1 += s_part[flip][k].x; s2 += s_part[flip][k].y; }
             }
-            const F2 n2 = both(-s2 * inv_n), n1 = both(-s1 * inv_n);
-            if (!kKeep) {
+            // rstd (g - s1 / n - xh s2 / n) by two multiplications with additions
+            const float n2 = -s2 * inv_n * stat.y, n1 = -s1 * inv_n * stat.y;
+            if (kKeep) {
+#pragma unroll
+                for (int i = 0; i < S::kPairs; ++i) g[i] = fma2(g[i], r2, fma2(h[i], both(n2), both(n1)));
+            } else {
                 S::take(at, px, valid, h);
                 S::take(at + S::kBytes, pd, valid, g);
 #pragma unroll
-                for (int i = 0; i < S::kPairs; ++i) { h[i] = mul2(add2(h[i], m2), r2); g[i] = mul2(g[i], w[i]); }
+                for (int i = 0; i < S::kPairs; ++i)
+                    g[i] = fma2(mul2(g[i], w[i]), r2, fma2(add2(h[i], m2), both(n2 * stat.y), both(n1)));
             }
-#pragma unroll
-            for (int i = 0; i < S::kPairs; ++i) g[i] = mul2(fma2(h[i], n2, add2(g[i], n1)), r2);
             S::put(dx, g, valid);
         }
         if (a.ring == 1) __syncwarp();
@@ -460,7 +481,7 @@ __global__ void __launch_bounds__(kMaxThreads) norm_backward_kernel(const NormAr
                 }
         }
         __syncthreads();
-        for (uint32_t q = threadIdx.x; q < 2 * a.cols; q += kWarpRowThreads) {
+        for (uint32_t q = threadIdx.x; q < 2 * a.cols; q += blockDim.x) {
             float v = s_sum[q];
             for (uint32_t k = 1; k < used; ++k) v += s_sum[(size_t)k * 2 * a.cols + q];
             if (to) {
@@ -701,17 +722,17 @@ int launch_reduce(const NormArgs& a, const Launch& l) {
     return CO3_OK;
 }
 
-template <typename T, int kVec, int kCh, bool kWarpRow, int kMaxThreads>
+template <typename T, int kVec, int kCh, bool kWarpRow, bool kBackward, int kMaxThreads>
 int launch_rows(NormArgs a, const Launch& l, uint32_t threads) {
     const uint32_t warps = threads / 32u, rows_at_once = kWarpRow ? warps : 1;
     // the deepest ring with which two blocks fit an SM, or else one block
-    const size_t turn = (size_t)warps * (l.backward ? 2 * Stretch<T, kVec, kCh>::kBytes + 16 : Stretch<T, kVec, kCh>::kBytes);
+    const size_t turn = (size_t)warps * (kBackward ? 2 * Stretch<T, kVec, kCh>::kBytes + 16 : Stretch<T, kVec, kCh>::kBytes);
     a.ring = 1;
     for (uint32_t r : {8u, 4u, 3u, 2u})
         if (r * turn <= (r > 4 ? kRingBytes / 8 : r > 2 ? kRingBytes / 2 : kRingBytes)) { a.ring = r; break; }
     size_t smem = a.ring * turn;
     int per_sm = 0;
-    if (!l.backward) {
+    if constexpr (!kBackward) {
         auto* kernel = norm_forward_kernel<T, kVec, kCh, kWarpRow, kMaxThreads>;
         const int e = blocks_per_sm<norm_forward_kernel<T, kVec, kCh, kWarpRow, kMaxThreads>>(threads, smem, &per_sm);
         if (e != CO3_OK) return e;
@@ -719,32 +740,37 @@ int launch_rows(NormArgs a, const Launch& l, uint32_t threads) {
         const uint32_t grid = (uint32_t)std::min<uint64_t>(want, (uint64_t)l.sms * per_sm);
         CO3_CUDA(launch_behind(kernel, dim3(grid), dim3(threads), smem, l.st, a));
         return CO3_OK;
+    } else {
+        auto* kernel = norm_backward_kernel<T, kVec, kCh, kWarpRow, kMaxThreads>;
+        if (kWarpRow) smem = std::max(smem, (size_t)8 * a.cols * warps);
+        const int e = blocks_per_sm<norm_backward_kernel<T, kVec, kCh, kWarpRow, kMaxThreads>>(threads, smem, &per_sm);
+        if (e != CO3_OK) return e;
+        const uint64_t fill = std::max<uint64_t>(1, (uint64_t)l.sms * per_sm / l.n_clients);
+        const uint64_t most = std::max<uint64_t>(1, (a.rows + rows_at_once - 1) / rows_at_once);
+        a.parts = (uint32_t)std::min(std::min(fill, most), max_parts(a.rows, l.n_clients));
+        CO3_CUDA(launch_behind(kernel, dim3(a.parts * l.n_clients), dim3(threads), smem, l.st, a));
+        return launch_reduce(a, l);
     }
-    auto* kernel = norm_backward_kernel<T, kVec, kCh, kWarpRow, kMaxThreads>;
-    if (kWarpRow) smem = std::max(smem, (size_t)8 * a.cols * warps);
-    const int e = blocks_per_sm<norm_backward_kernel<T, kVec, kCh, kWarpRow, kMaxThreads>>(threads, smem, &per_sm);
-    if (e != CO3_OK) return e;
-    const uint64_t fill = std::max<uint64_t>(1, (uint64_t)l.sms * per_sm / l.n_clients);
-    const uint64_t most = std::max<uint64_t>(1, (a.rows + rows_at_once - 1) / rows_at_once);
-    a.parts = (uint32_t)std::min(std::min(fill, most), max_parts(a.rows, l.n_clients));
-    CO3_CUDA(launch_behind(kernel, dim3(a.parts * l.n_clients), dim3(threads), smem, l.st, a));
-    return launch_reduce(a, l);
 }
 
 template <typename T, int kVec, int kElems, int kMaxThreads>
 int launch_block(const NormArgs& a, const Launch& l) {
     constexpr int kCh = kElems / kVec;
     const uint32_t chunks = (a.cols + kVec - 1) / kVec, threads = (chunks + 32u * kCh - 1) / (32u * kCh) * 32u;
-    return threads <= (uint32_t)kMaxThreads ? launch_rows<T, kVec, kCh, false, kMaxThreads>(a, l, threads) : -1;
+    if (threads > (uint32_t)kMaxThreads) return -1;
+    return l.backward ? launch_rows<T, kVec, kCh, false, true, kMaxThreads>(a, l, threads) : launch_rows<T, kVec, kCh, false, false, kMaxThreads>(a, l, threads);
 }
 template <typename T, int kVec, int kCh>
 int launch_warp(const NormArgs& a, const Launch& l) {
-    return (uint64_t)kCh * kVec * 32 >= a.cols ? launch_rows<T, kVec, kCh, true, kWarpRowThreads>(a, l, kWarpRowThreads) : -1;
+    if ((uint64_t)kCh * kVec * 32 < a.cols) return -1;
+    constexpr int kForward = kWarpRowThreads<T, kCh * kVec, false>, kBackward = kWarpRowThreads<T, kCh * kVec, true>;
+    return l.backward ? launch_rows<T, kVec, kCh, true, true, kBackward>(a, l, kBackward) : launch_rows<T, kVec, kCh, true, false, kForward>(a, l, kForward);
 }
 
 // Elements a thread.  A warp takes the row if up to 32 elements a lane suffice, the fewest that do; wider rows go to
-// blocks of up to 512 threads.  (Backward at 65536 x 1024, bf16: a warp with 32 elements 95 us, two warps with 16 90 us,
-// but the many small blocks of the latter leave four times the partial sums: 3001 x 1023 26 against 20 us.)
+// blocks of up to 512 threads, forward and at any alignment with 32 elements a thread, backward with 16, since its sums
+// take registers too (us, 32 against 16 elements: forward bf16 16384 x 4096 48 and 66, 16384 x 2048 27.5 and 32; backward
+// bf16 16384 x 4096 87 and 82, 16384 x 2048 60 and 50; backward 65536 x 1024, a warp with 32 against two with 16: 72 and 90).
 template <typename T, int kVec, int... kChs>
 int launch_width(const NormArgs& a, const Launch& l) {
     int e = -1;
