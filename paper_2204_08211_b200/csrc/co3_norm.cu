@@ -246,6 +246,9 @@ template <typename T, int kVec, int kCh, bool kWarpRow, int kMaxThreads>
 __global__ void __launch_bounds__(kMaxThreads) norm_forward_kernel(const NormArgs a) {
     wait_for_previous_kernel();
     using S = Stretch<T, kVec, kCh>;
+    // blocks of up to 512 threads have 128 registers a thread: 16-bit rows are taken from shared memory again after their
+    // sums (8192 x 8192 bf16 66 -> 50 us; in the smaller blocks, 16384 x 4096, 48 -> 51; fp32 4096 x 16384 89 -> 95)
+    constexpr bool kAgain = kMaxThreads > 384 && sizeof(T) == 2;
     extern __shared__ __align__(16) unsigned char s_ring[];
     __shared__ float4 s_part[2][16];
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u, warps = blockDim.x / 32u;
@@ -306,7 +309,9 @@ __global__ void __launch_bounds__(kMaxThreads) norm_forward_kernel(const NormArg
         // with n1 and n2 elements grow by n1 n2 / (n1 + n2) (mean1 - mean2)^2 (Chan, Golub, LeVeque 1979).  One
         // reduction, and none of the cancellation of sum(x^2) - sum(x)^2 / n.
         F2 v[S::kPairs], s2 = both(0.0f), q2 = both(0.0f);
-        S::template take<!kWarpRow>(ring + now * S::kBytes, (uint32_t)reinterpret_cast<uintptr_t>(x_now) & 15u, valid, v);
+        const unsigned char* at = ring + now * S::kBytes;
+        const uint32_t ph = (uint32_t)reinterpret_cast<uintptr_t>(x_now) & 15u;
+        S::template take<!kWarpRow>(at, ph, valid, v);
         now = now + 1 == a.ring ? 0u : now + 1;
 #pragma unroll
         for (int i = 0; i < S::kPairs; ++i) s2 = add2(s2, v[i]);
@@ -350,9 +355,16 @@ __global__ void __launch_bounds__(kMaxThreads) norm_forward_kernel(const NormArg
             }
         }
         const float rstd = rsqrtf(__fmaf_rn(sq, inv_n, a.eps));
-        const F2 r2 = both(rstd), k2 = both((own - mean) * rstd);
+        const F2 r2 = both(rstd);
+        if (kAgain) {
+            S::template take<!kWarpRow>(at, ph, valid, v);
 #pragma unroll
-        for (int i = 0; i < S::kPairs; ++i) v[i] = fma2(fma2(v[i], r2, k2), w[i], b[i]);
+            for (int i = 0; i < S::kPairs; ++i) v[i] = fma2(mul2(add2(v[i], both(-mean)), r2), w[i], b[i]);
+        } else {
+            const F2 k2 = both((own - mean) * rstd);
+#pragma unroll
+            for (int i = 0; i < S::kPairs; ++i) v[i] = fma2(fma2(v[i], r2, k2), w[i], b[i]);
+        }
         S::put(y, v, valid);
         if (threadIdx.x == (kWarpRow ? warp * 32u : 0u)) {
             if (a.mean) a.mean[row] = mean;
@@ -768,9 +780,10 @@ int launch_warp(const NormArgs& a, const Launch& l) {
 }
 
 // Elements a thread.  A warp takes the row if up to 32 elements a lane suffice, the fewest that do; wider rows go to
-// blocks of up to 512 threads, forward and at any alignment with 32 elements a thread, backward with 16, since its sums
-// take registers too (us, 32 against 16 elements: forward bf16 16384 x 4096 48 and 66, 16384 x 2048 27.5 and 32; backward
-// bf16 16384 x 4096 87 and 82, 16384 x 2048 60 and 50; backward 65536 x 1024, a warp with 32 against two with 16: 72 and 90).
+// blocks of up to 512 threads, forward with 32 elements a thread, backward with 16 as far as they reach, since its sums
+// take registers too (unaligned rows of up to 4096 columns excepted: 128 threads suffice for them).  us, 32 against 16
+// elements: forward bf16 16384 x 4096 48 and 66, 16384 x 2048 27.5 and 32; backward bf16 16384 x 4096 87 and 82, 16384 x
+// 2048 60 and 50, 8192 x 8191 f16 265 and 140; backward 65536 x 1024, a warp with 32 against two with 16: 72 and 90.
 template <typename T, int kVec, int... kChs>
 int launch_width(const NormArgs& a, const Launch& l) {
     int e = -1;
@@ -781,6 +794,7 @@ int launch_width(const NormArgs& a, const Launch& l) {
         if (e < 0) e = launch_block<T, kVec, 16, 512>(a, l);
     } else {
         e = launch_block<T, kVec, 32, 128>(a, l);
+        if (e < 0 && l.backward) e = launch_block<T, kVec, 16, 512>(a, l);
     }
     return e >= 0 ? e : launch_block<T, kVec, 32, 512>(a, l);
 }
