@@ -31,6 +31,7 @@ assert MAT_DTYPE.itemsize == 32 and NS_DTYPE.itemsize == 8 + 12 * NS_MAX_STEPS
 _TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 
 _lib = None
+_F32 = torch.float32
 _current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
     lambda device: torch.cuda.current_stream(device).cuda_stream)
 
@@ -310,16 +311,18 @@ def co3_decode(stream_in, stream_bytes, fmts, codes, segs, n_seg, n_elem, ghat_o
 
 
 def _rows(t, like=None):
-    """(pointer, rows, cols, row stride) of a 2-D CUDA tensor whose rows are contiguous."""
-    if not t.is_cuda or t.dim() != 2 or t.dtype not in _TYPES:
-        raise ValueError("expected a 2-D CUDA tensor of fp32, fp16 or bf16")
-    rows, cols = t.shape
+    """(pointer, rows, cols, row stride) of a 2-D CUDA tensor whose rows are contiguous, of the shape and type of `like`."""
+    shape = t.shape
+    if like is None:
+        if not t.is_cuda or len(shape) != 2 or t.dtype not in _TYPES:
+            raise ValueError("expected a 2-D CUDA tensor of fp32, fp16 or bf16")
+    elif shape != like.shape or t.dtype is not like.dtype or not t.is_cuda:
+        raise ValueError("expected tensors of one shape and type")
+    rows, cols = shape
     rs, cs = t.stride()
     if (cs != 1 and cols > 1) or (rs < cols and rows > 1):
         raise ValueError("expected contiguous rows that do not overlap")
-    if like is not None and (t.dtype != like.dtype or t.shape != like.shape):
-        raise ValueError("expected tensors of one shape and type")
-    return t.data_ptr(), rows, cols, rs if rows > 1 else max(rs, cols)
+    return t.data_ptr(), rows, cols, rs if rows > 1 or rs > cols else cols
 
 
 def _stream_of(t, stream):
@@ -331,7 +334,7 @@ def _vec(t, n):
     """Device pointer of n fp32 values (or None)."""
     if t is None:
         return None
-    if t.dtype != torch.float32 or t.numel() < n or not t.is_cuda or not t.is_contiguous():
+    if t.dtype is not _F32 or not t.is_cuda or t.numel() < n or not t.is_contiguous():
         raise ValueError("expected a contiguous fp32 CUDA tensor of at least %d elements" % n)
     return t.data_ptr()
 
