@@ -520,27 +520,28 @@ __global__ void __launch_bounds__(kMaxThreads) norm_backward_kernel(const NormAr
     }
 }
 
-// Sums over the parts of a client: 32 columns x 16 groups of parts per block, groups added in order.
-constexpr int kReduceGroups = 16;
-__global__ void __launch_bounds__(32 * kReduceGroups) norm_reduce_kernel(const NormArgs a) {
+// Sums over the parts of a client: a block's threads are `groups` of parts x columns, groups added in order.  As many
+// groups as there are parts, 16 at most: with 16 for 2 parts 100 x 8 x 4096 bf16 took 61 us instead of 27.
+constexpr uint32_t kReduceThreads = 512, kReduceGroups = 16;
+__global__ void __launch_bounds__(kReduceThreads) norm_reduce_kernel(const NormArgs a, uint32_t groups) {
     wait_for_previous_kernel();
-    __shared__ float s_v[kReduceGroups][33];
-    const uint32_t lane = threadIdx.x & 31u, group = threadIdx.x >> 5;
-    const uint32_t col_blocks = (a.cols + 31u) / 32u;
+    __shared__ float s_v[kReduceThreads];
+    const uint32_t width = kReduceThreads / groups, group = threadIdx.x / width, lane = threadIdx.x % width;
+    const uint32_t col_blocks = (a.cols + width - 1) / width;
     const uint32_t cb = blockIdx.x % col_blocks, rest = blockIdx.x / col_blocks, which = rest & 1u, client = rest >> 1;
-    const uint32_t col = cb * 32u + lane;
+    const uint32_t col = cb * width + lane;
     float* dst = which ? a.dbias : a.dweight;
     if (!dst) return;
     float sum = 0.0f;
     if (col < a.cols) {
         const float* p = a.partial + ((uint64_t)client * a.parts * 2 + which) * a.cols + col;
 #pragma unroll 8
-        for (uint32_t k = group; k < a.parts; k += kReduceGroups) sum += p[(uint64_t)k * 2 * a.cols];
+        for (uint32_t k = group; k < a.parts; k += groups) sum += p[(uint64_t)k * 2 * a.cols];
     }
-    s_v[group][lane] = sum;
+    s_v[threadIdx.x] = sum;
     __syncthreads();
     if (group == 0 && col < a.cols) {
-        for (int k = 1; k < kReduceGroups; ++k) sum += s_v[k][lane];
+        for (uint32_t k = 1; k < groups; ++k) sum += s_v[k * width + lane];
         put_sum(dst + (uint64_t)client * a.client_stride + col, sum, a.accumulate);
     }
 }
@@ -729,8 +730,11 @@ struct Launch {
 
 int launch_reduce(const NormArgs& a, const Launch& l) {
     if (a.parts < 2 || (!a.dweight && !a.dbias)) return CO3_OK;
-    const uint64_t blocks = (uint64_t)((a.cols + 31u) / 32u) * 2 * l.n_clients;
-    CO3_CUDA(launch_behind(norm_reduce_kernel, dim3((uint32_t)blocks), dim3(32 * kReduceGroups), 0, l.st, a));
+    uint32_t groups = kReduceGroups;
+    while (groups > a.parts) groups /= 2;
+    const uint32_t width = kReduceThreads / groups;
+    const uint64_t blocks = (uint64_t)((a.cols + width - 1) / width) * 2 * l.n_clients;
+    CO3_CUDA(launch_behind(norm_reduce_kernel, dim3((uint32_t)blocks), dim3(kReduceThreads), 0, l.st, a, groups));
     return CO3_OK;
 }
 
@@ -760,6 +764,11 @@ int launch_rows(NormArgs a, const Launch& l, uint32_t threads) {
         const uint64_t fill = std::max<uint64_t>(1, (uint64_t)l.sms * per_sm / l.n_clients);
         const uint64_t most = std::max<uint64_t>(1, (a.rows + rows_at_once - 1) / rows_at_once);
         a.parts = (uint32_t)std::min(std::min(fill, most), max_parts(a.rows, l.n_clients));
+        // One block a client needs no second launch and no partial sums: taken where the turns it adds cost less, a turn
+        // about 40 ns an element of a lane, the launch 4.6 us, partial sums 5000 bytes a ns.  (us, one block against
+        // several: 100 clients x 64 x 512 fp32 15.8 and 20.3, 100 x 16 x 4096 bf16 19 and 31, 30 x 64 x 1024 bf16 17 and 14.)
+        const uint64_t added = most - (most + a.parts - 1) / a.parts;
+        if ((a.dweight || a.dbias) && added * 40 * kVec * kCh < 4600 + l.n_clients * (uint64_t)a.parts * a.cols * 16 / 5000) a.parts = 1;
         CO3_CUDA(launch_behind(kernel, dim3(a.parts * l.n_clients), dim3(threads), smem, l.st, a));
         return launch_reduce(a, l);
     }
