@@ -250,7 +250,8 @@ __global__ void __launch_bounds__(kMaxThreads) norm_forward_kernel(const NormArg
     // sums (8192 x 8192 bf16 66 -> 50 us; in the smaller blocks, 16384 x 4096, 48 -> 51; fp32 4096 x 16384 89 -> 95)
     constexpr bool kAgain = kMaxThreads > 384 && sizeof(T) == 2;
     extern __shared__ __align__(16) unsigned char s_ring[];
-    __shared__ float4 s_part[2][16];
+    constexpr uint32_t kWarps = kMaxThreads / 32;
+    __shared__ float4 s_part[2][kWarpRow ? 1 : kWarps];
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u, warps = blockDim.x / 32u;
     const uint32_t col0 = kWarpRow ? 0u : warp * S::kElems, n_cols = min(a.cols - col0, S::kElems), bytes = n_cols * (uint32_t)sizeof(T);
     const uint64_t first = kWarpRow ? (uint64_t)blockIdx.x * warps + warp : blockIdx.x, step = kWarpRow ? (uint64_t)gridDim.x * warps : gridDim.x;
@@ -259,6 +260,9 @@ __global__ void __launch_bounds__(kMaxThreads) norm_forward_kernel(const NormArg
 #pragma unroll
     for (int c = 0; c < kCh; ++c) valid[c] = (c * 32 + lane) * kVec < n_cols;
     for (uint32_t k = 0; !kWarpRow && k < a.ring; ++k) S::clear(ring + k * S::kBytes, valid);
+    if (!kWarpRow && threadIdx.x < 32) {
+        for (uint32_t k = warps + lane; k < kWarps; k += 32) s_part[0][k] = s_part[1][k] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    }
     const T *lo = static_cast<const T*>(a.x), *hi = lo + (a.rows - 1) * a.x_stride + a.cols;
     const T* src = lo + first * a.x_stride + col0;  // the row to be fetched next
     uint64_t ahead = first;
@@ -344,14 +348,26 @@ __global__ void __launch_bounds__(kMaxThreads) norm_forward_kernel(const NormArg
             if (lane == 0) s_part[flip][warp] = make_float4(sum, sq, warp_n, warp_inv);
             __syncthreads();
             sum = sq = 0.0f;
+            if (kWarps <= 4) {  // absent warps' entries are zero
+                float4 p[kWarps];
+#pragma unroll
+                for (uint32_t k = 0; k < kWarps; ++k) { p[k] = s_part[flip][k]; sum += p[k].x; }
+                mean = sum * inv_n;
+#pragma unroll
+                for (uint32_t k = 0; k < kWarps; ++k) {
+                    const float d = __fmaf_rn(p[k].x, p[k].w, -mean);
+                    sq += __fmaf_rn(d * p[k].z, d, p[k].y);
+                }
+            } else {
 #pragma unroll 4
-            for (uint32_t k = 0; k < warps; ++k) sum += s_part[flip][k].x;
-            mean = sum * inv_n;
+                for (uint32_t k = 0; k < warps; ++k) sum += s_part[flip][k].x;
+                mean = sum * inv_n;
 #pragma unroll 4
-            for (uint32_t k = 0; k < warps; ++k) {
-                const float4 p = s_part[flip][k];
-                const float d = __fmaf_rn(p.x, p.w, -mean);
-                sq += __fmaf_rn(d * p.z, d, p.y);
+                for (uint32_t k = 0; k < warps; ++k) {
+                    const float4 p = s_part[flip][k];
+                    const float d = __fmaf_rn(p.x, p.w, -mean);
+                    sq += __fmaf_rn(d * p.z, d, p.y);
+                }
             }
         }
         const float rstd = rsqrtf(__fmaf_rn(sq, inv_n, a.eps));
@@ -386,7 +402,8 @@ __global__ void __launch_bounds__(kMaxThreads) norm_backward_kernel(const NormAr
     constexpr bool kKeep = kCh * kVec <= 16;
     constexpr uint32_t kSlot = 2 * S::kBytes + 16;  // x, dy, mean and rstd of a row
     extern __shared__ __align__(16) unsigned char s_ring[];
-    __shared__ float2 s_part[2][16];
+    constexpr uint32_t kWarps = kMaxThreads / 32;
+    __shared__ __align__(16) float2 s_part[2][kWarpRow ? 2 : kWarps];
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u, warps = blockDim.x / 32u;
     const uint32_t client = blockIdx.x / a.parts, part = blockIdx.x - client * a.parts;
     const uint32_t col0 = kWarpRow ? 0u : warp * S::kElems, n_cols = min(a.cols - col0, S::kElems), bytes = n_cols * (uint32_t)sizeof(T);
@@ -396,6 +413,9 @@ __global__ void __launch_bounds__(kMaxThreads) norm_backward_kernel(const NormAr
     bool valid[kCh];
 #pragma unroll
     for (int c = 0; c < kCh; ++c) valid[c] = (c * 32 + lane) * kVec < n_cols;
+    if (!kWarpRow && threadIdx.x < 32) {
+        for (uint32_t k = warps + lane; k < kWarps; k += 32) s_part[0][k] = s_part[1][k] = make_float2(0.0f, 0.0f);
+    }
     const T *x_lo = static_cast<const T*>(a.x), *d_lo = static_cast<const T*>(a.dy);
     const T *x_hi = x_lo + (a.all_rows - 1) * a.x_stride + a.cols, *d_hi = d_lo + (a.all_rows - 1) * a.dy_stride + a.cols;
     const T *x_next = x_lo + first * a.x_stride + col0, *d_next = d_lo + first * a.dy_stride + col0;
@@ -454,8 +474,17 @@ __global__ void __launch_bounds__(kMaxThreads) norm_backward_kernel(const NormAr
                 if (lane == 0) s_part[flip][warp] = make_float2(s1, s2);
                 __syncthreads();  // two buffers: the next row's sums go into the other one
                 s1 = s2 = 0.0f;
+                if (kWarps <= 8) {  // absent warps' entries are zero
+#pragma unroll
+                    for (uint32_t k = 0; k < kWarps; k += 2) {
+                        const float4 p = *reinterpret_cast<const float4*>(&s_part[flip][k]);
+                        s1 += p.x; s2 += p.y;
+                        s1 += p.z; s2 += p.w;
+                    }
+                } else {
 #pragma unroll 4
-                for (uint32_t k = 0; k < warps; ++k) { s1 += s_part[flip][k].x; s2 += s_part[flip][k].y; }
+                    for (uint32_t k = 0; k < warps; ++k) { s1 += s_part[flip][k].x; s2 += s_part[flip][k].y; }
+                }
             }
             // rstd (g - s1 / n - xh s2 / n) by two multiplications with additions
             const float n2 = -s2 * inv_n * stat.y, n1 = -s1 * inv_n * stat.y;
@@ -520,13 +549,15 @@ __global__ void __launch_bounds__(kMaxThreads) norm_backward_kernel(const NormAr
     }
 }
 
-// Sums over the parts of a client: a block's threads are `groups` of parts x columns, groups added in order.  As many
+// Sums over the parts of a client: a block's threads are kGroups of parts x columns, groups added in order.  As many
 // groups as there are parts, 16 at most: with 16 for 2 parts 100 x 8 x 4096 bf16 took 61 us instead of 27.
-constexpr uint32_t kReduceThreads = 512, kReduceGroups = 16;
-__global__ void __launch_bounds__(kReduceThreads) norm_reduce_kernel(const NormArgs a, uint32_t groups) {
+constexpr uint32_t kReduceThreads = 512;
+template <uint32_t kGroups>
+__global__ void __launch_bounds__(kReduceThreads) norm_reduce_kernel(const NormArgs a) {
     wait_for_previous_kernel();
     __shared__ float s_v[kReduceThreads];
-    const uint32_t width = kReduceThreads / groups, group = threadIdx.x / width, lane = threadIdx.x % width;
+    constexpr uint32_t width = kReduceThreads / kGroups;
+    const uint32_t group = threadIdx.x / width, lane = threadIdx.x % width;
     const uint32_t col_blocks = (a.cols + width - 1) / width;
     const uint32_t cb = blockIdx.x % col_blocks, rest = blockIdx.x / col_blocks, which = rest & 1u, client = rest >> 1;
     const uint32_t col = cb * width + lane;
@@ -536,12 +567,12 @@ __global__ void __launch_bounds__(kReduceThreads) norm_reduce_kernel(const NormA
     if (col < a.cols) {
         const float* p = a.partial + ((uint64_t)client * a.parts * 2 + which) * a.cols + col;
 #pragma unroll 8
-        for (uint32_t k = group; k < a.parts; k += groups) sum += p[(uint64_t)k * 2 * a.cols];
+        for (uint32_t k = group; k < a.parts; k += kGroups) sum += p[(uint64_t)k * 2 * a.cols];
     }
     s_v[threadIdx.x] = sum;
     __syncthreads();
     if (group == 0 && col < a.cols) {
-        for (uint32_t k = 1; k < groups; ++k) sum += s_v[k * width + lane];
+        for (uint32_t k = 1; k < kGroups; ++k) sum += s_v[k * width + lane];
         put_sum(dst + (uint64_t)client * a.client_stride + col, sum, a.accumulate);
     }
 }
@@ -728,14 +759,17 @@ struct Launch {
     cudaStream_t st;
 };
 
+template <uint32_t kGroups>
+int launch_groups(const NormArgs& a, const Launch& l) {
+    constexpr uint32_t width = kReduceThreads / kGroups;
+    const uint64_t blocks = (uint64_t)((a.cols + width - 1) / width) * 2 * l.n_clients;
+    CO3_CUDA(launch_behind(norm_reduce_kernel<kGroups>, dim3((uint32_t)blocks), dim3(kReduceThreads), 0, l.st, a));
+    return CO3_OK;
+}
+
 int launch_reduce(const NormArgs& a, const Launch& l) {
     if (a.parts < 2 || (!a.dweight && !a.dbias)) return CO3_OK;
-    uint32_t groups = kReduceGroups;
-    while (groups > a.parts) groups /= 2;
-    const uint32_t width = kReduceThreads / groups;
-    const uint64_t blocks = (uint64_t)((a.cols + width - 1) / width) * 2 * l.n_clients;
-    CO3_CUDA(launch_behind(norm_reduce_kernel, dim3((uint32_t)blocks), dim3(kReduceThreads), 0, l.st, a, groups));
-    return CO3_OK;
+    return a.parts < 4 ? launch_groups<2>(a, l) : a.parts < 8 ? launch_groups<4>(a, l) : a.parts < 16 ? launch_groups<8>(a, l) : launch_groups<16>(a, l);
 }
 
 template <typename T, int kVec, int kCh, bool kWarpRow, bool kBackward, int kMaxThreads>
