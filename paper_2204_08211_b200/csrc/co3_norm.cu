@@ -825,7 +825,7 @@ int launch_warp(const NormArgs& a, const Launch& l) {
 // Elements a thread.  A warp takes the row if up to 32 elements a lane suffice, the fewest that do; wider rows go to
 // blocks of up to 512 threads, forward with 32 elements a thread, backward with 16 as far as they reach, since its sums
 // take registers too (unaligned rows of up to 4096 columns excepted: 128 threads suffice for them).  us, 32 against 16
-// elements: forward bf16 16384 x 4096 48 and 66, 16384 x 2048 27.5 and 32; backward bf16 16384 x 4096 87 and 82, 16384 x
+// elements: forward bf16 16384 x 4096 48 and 66, 16384 x 2048 27 and 32; backward bf16 16384 x 4096 87 and 82, 16384 x
 // 2048 60 and 50, 8192 x 8191 f16 265 and 140; backward 65536 x 1024, a warp with 32 against two with 16: 72 and 90.
 template <typename T, int kVec, int... kChs>
 int launch_width(const NormArgs& a, const Launch& l) {

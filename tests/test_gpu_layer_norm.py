@@ -277,3 +277,21 @@ def test_another_stream():
     side.synchronize()
     torch.cuda.synchronize()
     assert torch.equal(want, got)
+
+
+def test_rows_beyond_32_bit_offsets():
+    """Rows 2^31 elements apart: element and byte offsets that 32 bits do not hold."""
+    step, cols = 2 ** 31 + 24, 1000
+    x, dy, w, b = inputs(2, cols, 12)
+    bufs = [torch.empty(step + cols, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    xs, ys = (t.as_strided((2, cols), (step, 1)) for t in bufs)
+    xs.copy_(x)
+    mean, rstd = torch.empty(2, device="cuda"), torch.empty(2, device="cuda")
+    assert co3.co3_layer_norm(xs, w, b, ys, mean, rstd) == co3.OK
+    torch.cuda.synchronize()
+    check_forward(xs, w, b, ys, mean, rstd, "bf16")
+    ys.copy_(dy)
+    d = ys.clone()
+    grads = torch.full((1 + 2 * cols,), 7.0, device="cuda")
+    run_backward(ys, xs, w, mean, rstd, ys, grads, 1, 2 * cols, cols)      # dx over dy, in place
+    check_backward(d, xs, w, mean, rstd, ys, grads, 1, 2 * cols, cols, "bf16")

@@ -332,3 +332,20 @@ def test_another_stream_and_a_graph():
     graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("rows,cols", [(40, 60), (150, 90)])
+def test_offsets_beyond_32_bits(rows, cols):
+    """A matrix that starts 2^32 elements into its buffer, and one whose rows are far apart."""
+    far = torch.empty(2 ** 32 + 5 + rows * (cols + 3), dtype=torch.float16, device="cuda")
+    gen = torch.Generator().manual_seed(rows)
+    g = torch.randn(rows, cols, generator=gen).half()
+    step = 2 ** 32 // rows
+    for offset, stride in ((2 ** 32 + 5, cols + 3), (1, step)):
+        view = far.as_strided((rows, cols), (stride, 1), offset)
+        view.copy_(g)
+        table = co3.make_mats([(offset, rows, cols, stride)])
+        r = orthogonalize(far, table, far)
+        want = definition(g)
+        assert r["status"] == co3.OK
+        assert torch.linalg.norm(view.double().cpu() - want).item() <= bound(g, want, "f16")
