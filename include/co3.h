@@ -104,7 +104,7 @@ typedef struct {
 const char* co3_status_string(int status);
 
 /*
- * Bytes of device workspace needed by any entry point for vectors of n_elem elements in n_seg
+ * Bytes of device workspace needed by any entry point without a query of its own for vectors of n_elem elements in n_seg
  * segments with n_clients clients per encode call (pass n_clients = 0 if only co3_convert,
  * co3_decode and co3_decode_aggregate are used).  Returns CO3_ERR_INVALID_ARG for an
  * unsupported chunk_syms or out == NULL.
