@@ -168,10 +168,11 @@ struct Stretch {
     // is worth it (16384 x 2048 bf16 41.6 -> 27.5 us); elsewhere the loads then come too early for the registers
     // (65536 x 1024 bf16: forward 46.3 -> 48.4, backward 72 -> 95).
     static __device__ __forceinline__ void clear(unsigned char* dst, const bool (&valid)[kCh]) {
-        if (kVec == 1) return;
+        if constexpr (kVec > 1) {
 #pragma unroll
-        for (int c = 0; c < kCh; ++c)
-            if (!valid[c]) *reinterpret_cast<uint4*>(dst + c * 512u + (threadIdx.x & 31u) * 16u) = make_uint4(0u, 0u, 0u, 0u);
+            for (int c = 0; c < kCh; ++c)
+                if (!valid[c]) *reinterpret_cast<uint4*>(dst + c * 512u + (threadIdx.x & 31u) * 16u) = make_uint4(0u, 0u, 0u, 0u);
+        }
     }
     // The lane's elements, zeros beyond the row.  ph: the stretch's place within its first piece.
     template <bool kCleared = false>
