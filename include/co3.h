@@ -434,8 +434,7 @@ int co3_orthogonalize_workspace_bytes(const co3_mat* mats /* [host] */, uint32_t
  *   res [device]        one co3_result: CO3_ERR_NONFINITE if a matrix holds a NaN or an infinity (its result is NaN;
  *                       n_nonfinite counts such matrices, first_bad_chunk is the first); CO3_ERR_CUDA as elsewhere
  * Inputs of any magnitude are handled (the norm is formed in fp64).  Products run on the tensor cores from pairs of
- * fp16 values that hold 22 significant bits, accumulated in fp32; for bf16 results from single fp16 values (11 bits) in
- * the steps before the last two or three, where that stays below the rounding of the result.
+ * fp16 values that hold 22 significant bits, accumulated in fp32, whatever the types of the buffers.
  */
 int co3_orthogonalize(const void* in, int in_type, const co3_mat* in_mats, void* out, int out_type,
                       const co3_mat* out_mats, uint32_t n_mats, const co3_ns* ns /* [host], nullable */, co3_result* res,

@@ -314,8 +314,7 @@ constexpr int kMaxStages = 4;
 // The tensor core cuts what it adds to 26 bits below the largest term, always towards zero: sums of one sign (the
 // diagonal of A) drift.  The sum of each stage is therefore taken out and added up in registers, where fp32 rounds to
 // nearest.  1000 x 513, five steps, error against 64 bits: 1.3e-5 if the tensor core adds up all stages, 6.1e-6 if
-// four, 2.1e-6 if one (2.9e-6 with all sums in fp32 arithmetic).  Steps that multiply the hi planes alone leave all
-// sums to the tensor core.
+// four, 2.1e-6 if one (2.9e-6 with all sums in fp32 arithmetic).
 constexpr size_t kRingBytes = 192 << 10;
 static_assert(Tiling<kNarrow>::kStages * Tiling<kNarrow>::kStageBytes == kRingBytes && Tiling<kSquare>::kStages * Tiling<kSquare>::kStageBytes == kRingBytes, "one size of ring");
 
@@ -357,7 +356,6 @@ static_assert(kStepSmem <= 227 * 1024 && kSmemOff % 8 == 0, "shared memory of a 
 struct StepArgs {
     OrthWs ws;
     co3_ns ns;
-    uint32_t pairs;  // bit k: step k multiplies pairs of halves (three products), otherwise the hi planes alone
     int out_kind;
     void* out;
     float lr, shrink;
@@ -414,8 +412,7 @@ __device__ __forceinline__ Task find_task(const StepArgs& a, const StepSmem& sm,
 
 // Whether the apply product of a step adds a X in fp32.  In the last step a I is part of B instead: the result's tiles may
 // lie the other way round there, where X has no blocks to add.  In the steps before, the rounding of B + a I to pairs
-// would grow with the small singular values (130 x 70: error 2.5e-6 instead of 1.5e-6), and where the hi planes alone
-// are multiplied they would carry the rounding of X to 11 bits along.
+// would grow with the small singular values (130 x 70: error 2.5e-6 instead of 1.5e-6).
 __device__ __forceinline__ bool adds_x(const StepArgs& a, uint32_t step) { return step + 1 < a.ns.steps; }
 
 // The tile's own blocks of the linear term, in a row; null if there is none.
@@ -440,24 +437,22 @@ struct Operand {
     uint64_t row;      // bytes between block rows
     uint32_t r;
     uint32_t from;     // stages from this one on are fetched transposed
-    __device__ __forceinline__ void fetch128(uint32_t dst, uint32_t q, bool pairs, uint32_t bar) const {
+    __device__ __forceinline__ void fetch128(uint32_t dst, uint32_t q, uint32_t bar) const {
         if (q < from) {
-            copy_in(dst, base + r * row + (uint64_t)q * kBlock, pairs ? kBlock : kPlane, bar);
+            copy_in(dst, base + r * row + (uint64_t)q * kBlock, kBlock, bar);
         } else {  // rows 64 q .. of block row q / 2, columns of blocks 2 r and 2 r + 1
             const unsigned char* p = base + (q >> 1) * row + (uint64_t)(2 * r) * kBlock + (q & 1u) * kHalfPlane;
             copy_in(dst, p, kHalfPlane, bar);
             copy_in(dst + kHalfPlane, p + kBlock, kHalfPlane, bar);
-            if (pairs) {
-                copy_in(dst + kPlane, p + kPlane, kHalfPlane, bar);
-                copy_in(dst + kPlane + kHalfPlane, p + kBlock + kPlane, kHalfPlane, bar);
-            }
+            copy_in(dst + kPlane, p + kPlane, kHalfPlane, bar);
+            copy_in(dst + kPlane + kHalfPlane, p + kBlock + kPlane, kHalfPlane, bar);
         }
     }
-    __device__ __forceinline__ void fetch64(uint32_t dst, uint32_t q, bool pairs, uint32_t bar) const {
+    __device__ __forceinline__ void fetch64(uint32_t dst, uint32_t q, uint32_t bar) const {
         const unsigned char* p = q < from ? base + (r >> 1) * row + (uint64_t)q * kBlock + (r & 1u) * kHalfPlane
                                           : base + (q >> 1) * row + (uint64_t)r * kBlock + (q & 1u) * kHalfPlane;
         copy_in(dst, p, kHalfPlane, bar);
-        if (pairs) copy_in(dst + kHalfPlane, p + kPlane, kHalfPlane, bar);
+        copy_in(dst + kHalfPlane, p + kPlane, kHalfPlane, bar);
     }
 };
 // The operand of the tile's rows (which == 0) or columns (1).
@@ -506,24 +501,19 @@ __device__ __forceinline__ void bulk_stores_done() { asm volatile("cp.async.bulk
 
 // The products of one stage: 64 columns of the sum, operands at a and b in shared memory.
 template <int kTile, bool kTa, bool kTb>
-__device__ __forceinline__ void multiply_stage(uint32_t d, uint32_t a, uint32_t b, bool pairs) {
+__device__ __forceinline__ void multiply_stage(uint32_t d, uint32_t a, uint32_t b) {
     using L = Tiling<kTile>;
     constexpr uint32_t instr = instr_desc(kTa, kTb, 128, L::kCols), da = desc_step(kTa), db = desc_step(kTb);
     const uint64_t ah = smem_desc(a, kTa), bh = smem_desc(b, kTb);
     const uint64_t al = ah + (kPlane >> 4), bl = bh + (L::kColPlane >> 4);
-    if (pairs) {
-        // the corrections first, 2^11 times too large; the first product of the hi planes scales them down
+    // the corrections first, 2^11 times too large; the first product of the hi planes scales them down
 #pragma unroll
-        for (uint32_t e = 0; e < 4; ++e) tc_mma(d, ah + e * da, bl + e * db, instr, e > 0);
+    for (uint32_t e = 0; e < 4; ++e) tc_mma(d, ah + e * da, bl + e * db, instr, e > 0);
 #pragma unroll
-        for (uint32_t e = 0; e < 4; ++e) tc_mma(d, al + e * da, bh + e * db, instr, true);
-        tc_mma<kLoBits>(d, ah, bh, instr, true);
+    for (uint32_t e = 0; e < 4; ++e) tc_mma(d, al + e * da, bh + e * db, instr, true);
+    tc_mma<kLoBits>(d, ah, bh, instr, true);
 #pragma unroll
-        for (uint32_t e = 1; e < 4; ++e) tc_mma(d, ah + e * da, bh + e * db, instr, true);
-    } else {
-#pragma unroll
-        for (uint32_t e = 0; e < 4; ++e) tc_mma(d, ah + e * da, bh + e * db, instr, e > 0);
-    }
+    for (uint32_t e = 1; e < 4; ++e) tc_mma(d, ah + e * da, bh + e * db, instr, true);
 }
 
 template <int kTile>
@@ -572,7 +562,6 @@ __global__ void __launch_bounds__(kStepThreads, 1) orth_steps_kernel(const __gri
             const Task k = find_task<kTile>(a, sm, n_tasks, n_mats, g, v);
             if (k.skip) continue;
             const Operand o = operand<kTile>(k, v, which);
-            const bool pairs = (a.pairs >> k.step) & 1u;
             if (!wait_tiles(a.ws.ctrl, k.mat, k.before, a.limit_ns)) { *failed = 1; break; }
             fence_async_all();  // orders what the counter says after the copies that follow
             auto begin = [&]() {
@@ -584,7 +573,7 @@ __global__ void __launch_bounds__(kStepThreads, 1) orth_steps_kernel(const __gri
                 if (++st == kStages) { st = 0; ++turn; }
             };
             const bool half_width = which == 1 && kTile == kNarrow;
-            const uint32_t part = half_width ? kHalfPlane : kPlane, bytes = pairs ? 2 * part : part;  // of a stage
+            const uint32_t bytes = half_width ? kPlane : kBlock;  // of a stage
             for (uint32_t q = k.k0; q < k.k1; ++q) {
                 if (!begin()) break;
                 const uint32_t reader = unit & 1u, bar = full0 + (reader * kMaxStages + st) * 8u;
@@ -593,7 +582,7 @@ __global__ void __launch_bounds__(kStepThreads, 1) orth_steps_kernel(const __gri
                     mbar_arrive(&sm.full[reader][st]);
                 } else {
                     arrive_expect(bar, bytes);
-                    if (half_width) o.fetch64(dst, q, pairs, bar); else o.fetch128(dst, q, pairs, bar);
+                    if (half_width) o.fetch64(dst, q, bar); else o.fetch128(dst, q, bar);
                 }
                 next(reader);
                 ++unit;
@@ -621,7 +610,6 @@ __global__ void __launch_bounds__(kStepThreads, 1) orth_steps_kernel(const __gri
         for (uint32_t g = blockIdx.x; g < total && !*failed; g += gridDim.x) {
             const Task k = find_task<kTile>(a, sm, n_tasks, n_mats, g, v);
             if (k.skip) continue;
-            const bool pairs = (a.pairs >> k.step) & 1u;
             const uint32_t from_a = operand<kTile>(k, v, 0).from, from_b = operand<kTile>(k, v, 1).from;
             bool ok = true;
             for (uint32_t q = k.k0; q < k.k1; ++q) {
@@ -632,11 +620,11 @@ __global__ void __launch_bounds__(kStepThreads, 1) orth_steps_kernel(const __gri
                     tc_fence_after();
                     const uint32_t d = tmem + buf * kCols, at = ring_addr + st * kStageBytes, bt = k.diagonal ? at : at + kBlock;
                     if (q >= from_a) {
-                        if (q >= from_b) multiply_stage<kTile, true, true>(d, at, bt, pairs);
-                        else multiply_stage<kTile, true, false>(d, at, bt, pairs);
+                        if (q >= from_b) multiply_stage<kTile, true, true>(d, at, bt);
+                        else multiply_stage<kTile, true, false>(d, at, bt);
                     } else {
-                        if (q >= from_b) multiply_stage<kTile, false, true>(d, at, bt, pairs);
-                        else multiply_stage<kTile, false, false>(d, at, bt, pairs);
+                        if (q >= from_b) multiply_stage<kTile, false, true>(d, at, bt);
+                        else multiply_stage<kTile, false, false>(d, at, bt);
                     }
                     tc_commit(&sm.sum_full[buf]);
                     tc_commit(&sm.empty[st]);
@@ -999,20 +987,6 @@ void only_plain(OrthBatch* b) {
     b->n_chunks = chunks;
 }
 
-// Steps that multiply pairs of halves.  A result in bf16 is rounded to 8 bits, 1.66e-3 of its norm; the hi planes alone
-// hold 11.  With them in all steps but the last three the error is at most 1.69e-3 at every size, in all but the last two
-// at most 1.70e-3 for small sides from 1024 on but 2.3e-3 at 512 x 512, in all but the last one 1.9e-3 to 4.5e-3 (normal,
-// low-rank, decaying and orthogonal inputs; 256 x 256 to 2048 x 2048).  Rounding in directions that the input lacks grows
-// by the coefficient a in each step, so this holds as far as the usual five steps grow (3.4445^5 = 485).
-// 2 x 2048 x 8192: 3.4 ms with pairs throughout, 2.65 ms with the last two.
-uint32_t pair_steps(const OrthBatch& b, const co3_ns& ns) {
-    double growth = 1.0;
-    for (uint32_t k = 0; k < ns.steps; ++k) growth *= std::max(1.0, fabs(double(ns.coef[k][0])));
-    uint32_t last = 2;
-    for (uint32_t k = 0; k < b.n_mats; ++k) last = std::min(b.mat[k].rows, b.mat[k].cols) < 1024 ? 3 : last;
-    return growth > 512.0 || ns.steps <= last ? ~0u : ~((1u << (ns.steps - last)) - 1u);
-}
-
 // All blocks have to be resident at once: one per SM.
 template <int kTile>
 int launch_steps(const StepArgs& a, uint32_t widest, cudaStream_t st) {
@@ -1108,7 +1082,6 @@ int orth_run(const OrthCall& c, const co3_ns* ns_in, co3_result* res, void* work
             StepArgs sa = {};
             sa.ws = ws;
             sa.ns = ns;
-            sa.pairs = !muon && c.out_type == CO3_BF16 ? pair_steps(batch, ns) : ~0u;
             sa.out_kind = muon ? kOutParams : c.out_type;
             sa.out = c.out;
             sa.lr = c.lr;
