@@ -852,13 +852,16 @@ int launch_type(NormArgs a, const Launch& l) {
             CO3_CUDA(launch_behind(norm_forward_long_kernel<T>, dim3(grid), dim3(kLongThreads), 0, l.st, a));
             return CO3_OK;
         }
+        if (a.dweight || a.dbias) {  // before dx, which may lie over dy or x
+            const uint64_t col_blocks = (a.cols + 255u) / 256u;
+            const uint64_t fill = std::max<uint64_t>(1, 8ull * l.sms / (col_blocks * l.n_clients));
+            a.parts = (uint32_t)std::min(fill, max_parts(a.rows, l.n_clients));
+            CO3_CUDA(launch_behind(norm_dw_long_kernel<T>, dim3((uint32_t)(col_blocks * l.n_clients * a.parts)), dim3(256), 0, l.st, a));
+            const int e = launch_reduce(a, l);
+            if (e != CO3_OK) return e;
+        }
         if (a.out && rows) CO3_CUDA(launch_behind(norm_dx_long_kernel<T>, dim3(grid), dim3(kLongThreads), 0, l.st, a, rows));
-        if (!a.dweight && !a.dbias) return CO3_OK;
-        const uint64_t col_blocks = (a.cols + 255u) / 256u;
-        const uint64_t fill = std::max<uint64_t>(1, 8ull * l.sms / (col_blocks * l.n_clients));
-        a.parts = (uint32_t)std::min(fill, max_parts(a.rows, l.n_clients));
-        CO3_CUDA(launch_behind(norm_dw_long_kernel<T>, dim3((uint32_t)(col_blocks * l.n_clients * a.parts)), dim3(256), 0, l.st, a));
-        return launch_reduce(a, l);
+        return CO3_OK;
     }
     constexpr int kVec = 16 / sizeof(T);
     const size_t s = sizeof(T);
