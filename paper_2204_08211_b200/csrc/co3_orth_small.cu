@@ -27,6 +27,11 @@ namespace co3 {
 constexpr int kSmallThreads = 512;  // a thread has 32 columns of a row of every product
 constexpr uint32_t kOperand = 2 * kBlock;  // 128 x 128
 constexpr uint32_t kRawPitch = 129;        // floats between rows of X before it is scaled
+constexpr uint32_t kRawBytes = 128 * kRawPitch * 4;
+// From A's operand to the shares that other blocks send.  X before it is scaled lies over A's operand, and as no barrier
+// of the cluster stands between its last use in one block and the first shares sent by another, it has to end before them.
+constexpr uint32_t kSharesOff = kRawBytes > kOperand ? kRawBytes : kOperand;
+static_assert(kSharesOff >= kRawBytes && kSharesOff >= kOperand && kSharesOff % 16 == 0, "nothing that others write overlaps");
 
 struct SmallSmem {
     double sums[kSmallCluster];
@@ -35,7 +40,8 @@ struct SmallSmem {
     uint32_t tmem;
     double factor;
 };
-constexpr size_t kSmallBytes = 1024 + 3 * kOperand + sizeof(SmallSmem);
+constexpr size_t kSmallBytes = 1024 + kOperand + kSharesOff + kOperand + sizeof(SmallSmem);
+static_assert(kSmallBytes <= 227 * 1024, "shared memory of a block");
 
 struct SmallKernelArgs {
     SmallBatch batch;
@@ -97,7 +103,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) orth_small_kernel(const __gr
     wait_for_previous_kernel();
     extern __shared__ unsigned char smem_raw[];
     unsigned char* op_x = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
-    unsigned char *op_a = op_x + kOperand, *shares = op_a + kOperand;  // op_a: A, then B in its place
+    unsigned char *op_a = op_x + kOperand, *shares = op_a + kSharesOff;  // op_a: A, then B in its place
     SmallSmem& sm = *reinterpret_cast<SmallSmem*>(shares + kOperand);
     float* raw = reinterpret_cast<float*>(op_a);  // [128][kRawPitch], before the first step
     const SmallCall& call = a.call;
