@@ -445,8 +445,8 @@ int co3_orthogonalize(const void* in, int in_type, const co3_mat* in_mats, void*
  *     buf <- mu * buf + g;   u = nesterov ? g + mu * buf : buf;
  *     w <- (1 - lr * weight_decay) * w - lr * scale * (CO3_MAT_PLAIN ? u : orthogonalised u)
  *   grad [device] fp32, read only;  momentum, params [device] fp32, updated in place; one layout for the three
- * Elements outside the listed layers stay as they are.  res as above; a layer that holds a NaN or an infinity gets
- * NaN parameters, as the formula has it.
+ * Elements outside the listed layers stay as they are.  res as above, plain layers counted too; a layer whose u holds a
+ * NaN or an infinity gets NaN parameters, as the formula has it (a plain one in those entries alone).
  */
 int co3_muon_update(const float* grad, float* momentum, float* params, const co3_mat* mats /* [host] */,
                     uint32_t n_mats, float mu, int nesterov, float lr, float weight_decay,

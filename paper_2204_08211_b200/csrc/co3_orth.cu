@@ -204,12 +204,20 @@ __global__ void __launch_bounds__(kBeginThreads) orth_begin_kernel(const __grid_
         double s = 0.0;
         for (int w = 0; w < kBeginThreads / 32; ++w) s += s_sum[w];
         a.ws.partial[blockIdx.x] = s;
-        if (!isfinite(s) && a.momentum && t.plain) set_status(a.res, CO3_ERR_NONFINITE);
     }
 }
 
+// A layer that holds a NaN or an infinity goes into the result.  By kernels behind orth_begin_kernel only: block 0 of that
+// clears the result, in no order with its other blocks.
+__device__ __forceinline__ void report_nonfinite(co3_result* res, uint32_t index) {
+    set_status(res, CO3_ERR_NONFINITE);
+    atomicMin(&res->first_bad_chunk, index);
+    atomicAdd(reinterpret_cast<unsigned long long*>(&res->n_nonfinite), 1ull);
+}
+
 // ------------------------------------------------------------------------------------------------
-// load: one block per 64 x 64 piece of X (padding included): S * G / (norm + eps).
+// load: one block per 64 x 64 piece of X (padding included): S * G / (norm + eps).  If there are plain layers, one block
+// more looks at their sums of squares, a warp to a layer.
 // ------------------------------------------------------------------------------------------------
 struct LoadArgs {
     const void* in;
@@ -228,6 +236,17 @@ __global__ void __launch_bounds__(kLoadThreads) orth_load_kernel(LoadArgs a) {
     __shared__ double s_f;
     const OrthBatch& batch = *a.ws.batch;
     const uint32_t tile = blockIdx.x >> 2;  // tile of 128 x 128, quarter blockIdx.x & 3
+    if (tile == batch.n_full) {
+        for (uint32_t k = threadIdx.x >> 5; k < batch.n_mats; k += kLoadThreads / 32) {
+            const OrthMat& t = batch.mat[k];
+            if (!t.plain) continue;
+            const uint32_t n_part = (uint32_t)(((uint64_t)t.rows * t.cols + kBeginElems - 1) / kBeginElems);
+            bool good = true;
+            for (uint32_t i = threadIdx.x & 31u; i < n_part; i += 32) good = good && isfinite(a.ws.partial[t.chunk0 + i]);
+            if (!__all_sync(0xffffffffu, good) && (threadIdx.x & 31u) == 0) report_nonfinite(a.res, batch.index0 + k);
+        }
+        return;
+    }
     const uint32_t k = orth_find(batch.n_mats, tile, [&](uint32_t i) { return batch.mat[i].full0; });
     const OrthMat t = batch.mat[k];
     const OrthShape s = orth_shape(t.rows, t.cols, batch.tile);
@@ -244,12 +263,7 @@ __global__ void __launch_bounds__(kLoadThreads) orth_load_kernel(LoadArgs a) {
         for (int w = 0; w < kLoadThreads / 32; ++w) total += s_sum[w];
         const double d = sqrt(total) + (double)a.eps;
         s_f = d > 0.0 ? (double)orth_s(s.m, s.n) / d : 0.0;  // an all-zero matrix without eps stays zero
-        if (!isfinite(total) && tile == t.full0 && (blockIdx.x & 3u) == 0) {
-            set_status(a.res, CO3_ERR_NONFINITE);
-            atomicMin(&a.res->first_bad_chunk, batch.index0 + k);
-            atomicAdd(reinterpret_cast<unsigned long long*>(&a.res->n_nonfinite), 1ull);
-            s_f = (double)NAN;
-        }
+        if (!isfinite(total) && tile == t.full0 && (blockIdx.x & 3u) == 0) report_nonfinite(a.res, batch.index0 + k);
         if (!isfinite(total)) s_f = (double)NAN;
     }
     __syncthreads();
@@ -976,7 +990,7 @@ bool valid_ns(const co3_ns& ns) {
     return true;
 }
 
-// Leaves orth_begin_kernel with the plain layers.
+// Leaves orth_begin_kernel and orth_load_kernel with the plain layers.
 void only_plain(OrthBatch* b) {
     uint32_t chunks = 0;
     for (uint32_t k = 0; k < b->n_mats; ++k) {
@@ -985,6 +999,7 @@ void only_plain(OrthBatch* b) {
         if (m.plain) chunks += (uint32_t)(((uint64_t)m.rows * m.cols + kBeginElems - 1) / kBeginElems);
     }
     b->n_chunks = chunks;
+    b->n_full = 0;
 }
 
 // All blocks have to be resident at once: one per SM.
@@ -1010,6 +1025,17 @@ int launch_steps(const StepArgs& a, uint32_t widest, cudaStream_t st) {
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     CO3_CUDA(cudaLaunchKernelEx(&cfg, orth_steps_kernel<kTile>, a));
+    return CO3_OK;
+}
+
+// The momentum update with the sums of squares, and what it takes of orth_load_kernel's blocks.
+template <typename T>
+int enqueue_load(const OrthBatch& batch, const BeginArgs& ba, const LoadArgs& la, cudaStream_t st) {
+    CO3_CUDA(launch_behind(orth_begin_kernel<T>, dim3(std::max(1u, batch.n_chunks)), dim3(kBeginThreads), 0, st, batch, ba));
+    uint32_t blocks = 4u * batch.n_full;
+    for (uint32_t k = 0; k < batch.n_mats; ++k)
+        if (batch.mat[k].plain) { ++blocks; break; }
+    if (blocks) CO3_CUDA(launch_behind(orth_load_kernel<T>, dim3(blocks), dim3(kLoadThreads), 0, st, la));
     return CO3_OK;
 }
 
@@ -1060,25 +1086,17 @@ int orth_run(const OrthCall& c, const co3_ns* ns_in, co3_result* res, void* work
                      reinterpret_cast<float*>(base + w.slots), base + w.blocks};
         BeginArgs ba = {c.in, c.momentum, static_cast<float*>(c.out), c.mu, c.lr, c.shrink, c.nesterov, res, ws};
         LoadArgs la = {c.in, c.momentum, c.mu, ns.eps, c.nesterov, res, ws};
-        const dim3 bg(batch.n_chunks ? batch.n_chunks : 1u), lg(4u * batch.n_full);
+        int e = CO3_OK;
+        if (!is_small || c.n_mats > 1)  // a lone small matrix starts the result itself
+            e = c.in_type == CO3_F32 ? enqueue_load<float>(batch, ba, la, st)
+                : c.in_type == CO3_F16 ? enqueue_load<__half>(batch, ba, la, st) : enqueue_load<__nv_bfloat16>(batch, ba, la, st);
+        if (e != CO3_OK) return e;
         if (is_small) {
-            // a lone matrix starts the result itself
-            const bool alone = c.n_mats == 1;
-            if (!alone) CO3_CUDA(launch_behind(orth_begin_kernel<float>, bg, dim3(kBeginThreads), 0, st, batch, ba));
-            const SmallCall sc = {c.in, c.momentum, c.out, muon ? (int)kOutParams : c.out_type, c.mu, c.lr, c.shrink, c.nesterov, alone ? 1 : 0, ns, res};
-            const int e = orth_small_run(small, sc, c.in_type, st);
+            const SmallCall sc = {c.in, c.momentum, c.out, muon ? (int)kOutParams : c.out_type, c.mu, c.lr, c.shrink, c.nesterov, c.n_mats == 1 ? 1 : 0, ns, res};
+            e = orth_small_run(small, sc, c.in_type, st);
             if (e != CO3_OK) return e;
-        } else if (c.in_type == CO3_F32) {
-            CO3_CUDA(launch_behind(orth_begin_kernel<float>, bg, dim3(kBeginThreads), 0, st, batch, ba));
-            if (batch.n_full) CO3_CUDA(launch_behind(orth_load_kernel<float>, lg, dim3(kLoadThreads), 0, st, la));
-        } else if (c.in_type == CO3_F16) {
-            CO3_CUDA(launch_behind(orth_begin_kernel<__half>, bg, dim3(kBeginThreads), 0, st, batch, ba));
-            if (batch.n_full) CO3_CUDA(launch_behind(orth_load_kernel<__half>, lg, dim3(kLoadThreads), 0, st, la));
-        } else {
-            CO3_CUDA(launch_behind(orth_begin_kernel<__nv_bfloat16>, bg, dim3(kBeginThreads), 0, st, batch, ba));
-            if (batch.n_full) CO3_CUDA(launch_behind(orth_load_kernel<__nv_bfloat16>, lg, dim3(kLoadThreads), 0, st, la));
         }
-        if (batch.n_full && !is_small) {
+        if (batch.n_full) {
             StepArgs sa = {};
             sa.ws = ws;
             sa.ns = ns;
@@ -1089,7 +1107,7 @@ int orth_run(const OrthCall& c, const co3_ns* ns_in, co3_result* res, void* work
             sa.limit_ns = 500000000ull + ns.steps * needs.work * 64ull;
             sa.res = res;
             const uint32_t widest = std::max(batch.n_tasks[0], std::max(batch.n_tasks[1], batch.n_tasks[2]));
-            const int e = batch.tile == kNarrow ? launch_steps<kNarrow>(sa, widest, st) : launch_steps<kSquare>(sa, widest, st);
+            e = batch.tile == kNarrow ? launch_steps<kNarrow>(sa, widest, st) : launch_steps<kSquare>(sa, widest, st);
             if (e != CO3_OK) return e;
         }
         at += k;
