@@ -158,6 +158,7 @@ class Co3Session:
     def layer_norm(self, x: torch.Tensor, params: torch.Tensor, gain: int, bias: int, y: torch.Tensor,
                    mean=None, rstd=None, eps: float = 1e-5, stream=None) -> None:
         """y <- layer norm of the rows of x with layers `gain` and `bias` of the parameter vector."""
+        self._check_width(x, gain, bias)
         st = B.co3_layer_norm(x, self._layer(params, gain), self._layer(params, bias), y, mean, rstd, eps, stream)
         self._check(st, "co3_layer_norm")
 
@@ -165,12 +166,15 @@ class Co3Session:
                             accumulate: bool = False, stream=None) -> None:
         """Its gradients for the rows of all clients, client after client: dx, and every client's gradients of the two
         layers in its own vector of `grads`."""
-        if x.shape[1] != self.sizes[gain] or x.shape[1] != self.sizes[bias]:
-            raise ValueError("layers %d and %d are not of the rows' length" % (gain, bias))
+        self._check_width(x, gain, bias)
         at = [sum(self.sizes[:k]) for k in (gain, bias)]
         st = B.co3_layer_norm_backward(dy, x, self._layer(params, gain), mean, rstd, dx, grads[at[0]:], grads[at[1]:],
                                        self.n_clients, self.stride, workspace, accumulate, stream)
         self._check(st, "co3_layer_norm_backward")
+
+    def _check_width(self, x: torch.Tensor, gain: int, bias: int) -> None:
+        if x.dim() != 2 or x.shape[1] != self.sizes[gain] or x.shape[1] != self.sizes[bias]:
+            raise ValueError("layers %d and %d are not of the rows' length" % (gain, bias))
 
     def _layer(self, vec: torch.Tensor, k: int) -> torch.Tensor:
         at = sum(self.sizes[:k])
