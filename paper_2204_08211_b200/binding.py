@@ -365,6 +365,8 @@ def co3_layer_norm_backward(dy, x, weight, mean, rstd, dx, dweight, dbias, n_cli
     po, _, _, os_ = (None, 0, 0, 0) if dx is None else _rows(dx, dy)
     if n_clients < 1 or rows % n_clients:
         raise ValueError("co3_layer_norm_backward: the rows do not divide into n_clients batches")
+    if client_stride_elems < 0:  # the library takes it as unsigned
+        raise ValueError("co3_layer_norm_backward: clients' vectors that lie backwards")
     reach = (n_clients - 1) * client_stride_elems + cols
     return (_lib or _load()).co3_layer_norm_backward(
         pd, px, _TYPES[dy.dtype], _vec(weight, cols), _vec(mean, rows), _vec(rstd, rows), po, _vec(dweight, reach),

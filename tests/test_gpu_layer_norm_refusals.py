@@ -25,3 +25,16 @@ def test_session_refuses_layers_of_another_width():
     torch.cuda.synchronize()
     want = torch.nn.functional.layer_norm(x.double(), (12,)) + 1.0
     assert (y.double() - want).abs().max() <= 1e-5          # twelve fp32 terms a sum, values of a few units
+
+
+@pytest.mark.parametrize("stride", [-1, -64, -128, -2 ** 40])
+def test_backward_refuses_negative_client_strides(stride):
+    """They would pass the library's check as very large unsigned ones and place client 1 before the tensor."""
+    x = torch.randn(4, 64, device="cuda")
+    stats, w, dx = torch.ones(4, device="cuda"), torch.ones(64, device="cuda"), torch.full_like(x, 7.0)
+    g = torch.full((512,), 7.0, device="cuda")
+    ws = torch.empty(co3.co3_layer_norm_workspace_bytes(2, 64, 2), dtype=torch.uint8, device="cuda")
+    with pytest.raises(ValueError):
+        co3.co3_layer_norm_backward(x, x, w, stats, stats, dx, g[256:], g[320:], 2, stride, ws)
+    torch.cuda.synchronize()
+    assert (g == 7.0).all() and (dx == 7.0).all()
