@@ -926,7 +926,8 @@ int co3_layer_norm_backward(const void* dy, const void* x, int type, const float
         return CO3_ERR_INVALID_ARG;
     if (rows && dx && !valid_layout(type, dx, dx_row_stride, rows, cols)) return CO3_ERR_INVALID_ARG;
     if (!aligned(weight, 4) || !aligned(mean, 4) || !aligned(rstd, 4) || !aligned(dweight, 4) || !aligned(dbias, 4) ||
-        rows * n_clients >= (1ull << 40) || (n_clients > 1 && (dweight || dbias) && client_stride_elems < cols))
+        rows >= ((1ull << 40) + n_clients - 1) / n_clients ||  // 2^40 rows of all clients
+        (n_clients > 1 && (dweight || dbias) && client_stride_elems < cols))
         return CO3_ERR_INVALID_ARG;
     size_t need = 0;
     co3_layer_norm_workspace_bytes(rows, cols, n_clients, &need);
