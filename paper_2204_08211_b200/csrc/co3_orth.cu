@@ -973,19 +973,47 @@ uint32_t make_batch(const co3_mat* in, const co3_mat* out, uint32_t n_mats, uint
     return plan_batch(in, out, n_mats, at, muon, best, b, needs);
 }
 
+// Whether every singular value in [0, 1] keeps within the limits.  What a step makes of an interval is an interval, whose
+// ends it takes at the ends or where its derivative vanishes; it is widened by kSlack a step for what the products round
+// (a few 2^-22), so that an iteration which holds the limits in exact arithmetic alone is refused too.
 bool valid_ns(const co3_ns& ns) {
+    constexpr double kSlack = 1.0 / 65536, kRoom = 1.0 + 1.0 / 1024;  // fp16 pairs hold four times the limits
     if (ns.steps < 1 || ns.steps > CO3_NS_MAX_STEPS || !(ns.eps >= 0.0f) || !isfinite(ns.eps)) return false;
-    for (uint32_t k = 0; k < ns.steps; ++k)
-        for (int j = 0; j < 3; ++j)
-            if (!isfinite(ns.coef[k][j])) return false;
-    for (int i = 0; i <= 512; ++i) {
-        double x = i / 512.0;
-        for (uint32_t k = 0; k < ns.steps; ++k) {
-            const double q = x * x, g = q * (ns.coef[k][1] + q * ns.coef[k][2]);
-            if (!(fabs(g) <= 4.0) || !(fabs(ns.coef[k][0] + g) <= 4.0)) return false;
-            x *= ns.coef[k][0] + g;
-            if (!(fabs(x) <= 2.0)) return false;
+    double lo = 0.0, hi = 1.0;
+    for (uint32_t k = 0; k < ns.steps; ++k) {
+        const double a = ns.coef[k][0], b = ns.coef[k][1], c = ns.coef[k][2];
+        if (!isfinite(a) || !isfinite(b) || !isfinite(c)) return false;
+        lo -= kSlack;
+        hi += kSlack;
+        // factors b q + c q^2 and a + b q + c q^2 over the squares q
+        const double q0 = lo < 0.0 && hi > 0.0 ? 0.0 : std::min(lo * lo, hi * hi), q1 = std::max(lo * lo, hi * hi);
+        const double q_top = c != 0.0 ? -b / (2.0 * c) : -1.0;
+        for (double q : {q0, q1, q_top > q0 && q_top < q1 ? q_top : q0}) {
+            const double g = q * (b + q * c);
+            if (!(fabs(g) <= 4.0 * kRoom) || !(fabs(a + g) <= 4.0 * kRoom)) return false;
         }
+        auto step = [&](double x) { return x * (a + x * x * (b + x * x * c)); };
+        double least = std::min(step(lo), step(hi)), most = std::max(step(lo), step(hi));
+        auto turn = [&](double q) {  // a + 3 b q + 5 c q^2 = 0
+            if (!(q > 0.0)) return;
+            for (double x : {sqrt(q), -sqrt(q)})
+                if (x > lo && x < hi) {
+                    least = std::min(least, step(x));
+                    most = std::max(most, step(x));
+                }
+        };
+        if (c != 0.0) {
+            const double d = 9.0 * b * b - 20.0 * a * c;
+            if (d >= 0.0) {
+                turn((-3.0 * b + sqrt(d)) / (10.0 * c));
+                turn((-3.0 * b - sqrt(d)) / (10.0 * c));
+            }
+        } else if (b != 0.0) {
+            turn(-a / (3.0 * b));
+        }
+        if (!(most <= 2.0 * kRoom) || !(least >= -2.0 * kRoom)) return false;
+        lo = least;
+        hi = most;
     }
     return true;
 }
