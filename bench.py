@@ -3,12 +3,14 @@
 
 One step = one training round of the workload: every client's gradient is corrected, converted,
 entropy-coded (memory updated) in one batched `co3_encode` call, then all streams are decoded and
-averaged by `co3_decode_aggregate`.  Prints one JSON line (the README lists the keys).
+averaged by `co3_decode_aggregate`.  Prints one JSON line (the README lists the keys);
+what would make it too long to be read whole, every kernel's and every configuration's figures, goes to standard error
+as a JSON line of its own (`details`).
 
     python bench.py [--gpus N] [--steps K] [--warmup W] [--impl ours|reference] [--config 3] [--no-table]
 
 The headline workload is the largest configuration that fits one GPU (100 clients x 11.2 M elements); the
-other configurations are measured in the same run with fewer steps and reported under roofline.per_config.
+other configurations are measured in the same run with fewer steps and reported under details.per_config.
 """
 from __future__ import annotations
 
@@ -747,9 +749,7 @@ def run_ours(args):
                 "nominal_peak_gbs": NOMINAL_HBM_GBS,
                 "timed": "second pass of the same calls with CUDA events around every launch",
                 "encode_call": {k: v for k, v in row["encode_call"].items() if k != "kernels"},
-                "decode_call": {k: v for k, v in row["decode_call"].items() if k != "kernels"},
-                "kernels": dict(kern, **alone),
-                "per_config": [row] + table}
+                "decode_call": {k: v for k, v in row["decode_call"].items() if k != "kernels"}}
 
     if "decode" in kern and clocks.get("sm_mhz"):
         wf = NCU_DECODE_SMEM_WAVEFRONTS_PER_SYMBOL["batched" if clients > 16 else "side_by_side"]
@@ -781,6 +781,7 @@ def run_ours(args):
         "roofline": roofline, "clocks": clocks,
         "e2e": e2e, "cpu_baseline": cpu,
     }
+    print(json.dumps({"details": {"kernels": dict(kern, **alone), "per_config": [row] + table}}), file=sys.stderr, flush=True)
     print(json.dumps(line), flush=True)
     if world > 1:
         dist.destroy_process_group()
