@@ -419,7 +419,7 @@ typedef struct {
 } co3_ns;
 
 /* The iteration used where `ns` is NULL: 5 steps of (3.4445, -4.7750, 2.0315), eps 1e-7.  It takes singular values
- * from about 0.002 up to within [0.68, 1.14]. */
+ * from about 0.002 up to within [0.68, 1.21]. */
 int co3_ns_default(co3_ns* out /* [host] */);
 
 /* Device workspace of the two calls below for these matrices. */
@@ -434,7 +434,9 @@ int co3_orthogonalize_workspace_bytes(const co3_mat* mats /* [host] */, uint32_t
  *   res [device]        one co3_result: CO3_ERR_NONFINITE if a matrix holds a NaN or an infinity (its result is NaN;
  *                       n_nonfinite counts such matrices, first_bad_chunk is the first); CO3_ERR_CUDA as elsewhere
  * Inputs of any magnitude are handled (the norm is formed in fp64).  Products run on the tensor cores from pairs of
- * fp16 values that hold 22 significant bits, accumulated in fp32, whatever the types of the buffers.
+ * fp16 values that hold 22 significant bits, accumulated in fp32, whatever the types of the buffers.  The same call gives
+ * the same bits; in which pieces sums are formed depends on the whole list, so that a matrix among others may differ from
+ * the same matrix alone by such roundings.
  */
 int co3_orthogonalize(const void* in, int in_type, const co3_mat* in_mats, void* out, int out_type,
                       const co3_mat* out_mats, uint32_t n_mats, const co3_ns* ns /* [host], nullable */, co3_result* res,

@@ -306,7 +306,7 @@ __global__ void __launch_bounds__(kLoadThreads) orth_load_kernel(LoadArgs a) {
 
 // ------------------------------------------------------------------------------------------------
 // steps: persistent blocks (all resident: a cooperative launch).  The products of all steps form one list of tasks,
-// phase by phase; a task is a tile, or a part of its sum where there are fewer tiles than SMs.  Block (or pair) b takes
+// phase by phase; a task is a tile, or a part of its sum where there are fewer tiles than SMs.  Block b takes
 // tasks b, b + number of blocks, ... in order, and before a task's operands are fetched it waits until the matrix' tiles
 // of the phases before it are finished (a counter per matrix): the tasks waited for stand earlier in the list, so that
 // waiting always ends, and one matrix' tail is filled with other matrices' work.
