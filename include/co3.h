@@ -387,6 +387,92 @@ int co3_layer_norm_backward(const void* dy, const void* x, int type, const float
                             void* stream);
 
 /*
+ * Linear layers on 8-bit activations (no counterpart in the paper, which lowers the resolution of what is sent; here it is what
+ * the clients' passes keep and multiply).  A buffer of 8-bit blocks holds a matrix of `rows` x `cols` as e4m3 values (sign, four bits
+ * of exponent, three of mantissa) with one scale for each block, a power of two:
+ *     s = the smallest 2^k, k >= -126, with max|x| <= 448 s over the block;   value = s * (x / s rounded to e4m3, ties to even)
+ *   CO3_F8_ROWS    a block is 128 columns of a row, from a multiple of 128 on: activations and gradients
+ *   CO3_F8_SQUARE  a block is 128 x 128 entries: weights, which are summed over along either side
+ * What lies beyond the last row or column counts as zero.  NaN and infinities become NaN and do not count in their block's
+ * maximum; a value whose nearest is 2^128 becomes the largest below.  Values of such buffers are exact in fp32, and in bf16
+ * from 2^-126 up.
+ * The layout is the library's own (tiles as the tensor cores read them); such a buffer is 256-byte aligned, its size is
+ * co3_f8_bytes', and every call names the rows, columns and kind that it was packed with.
+ */
+#define CO3_F8_ROWS 0
+#define CO3_F8_SQUARE 1
+
+/* Size of a buffer of 8-bit blocks.  rows and cols below 2^31, rows * cols (each padded to 128) below 2^40. */
+int co3_f8_bytes(uint64_t rows, uint32_t cols, int kind, size_t* out /* [host] */);
+
+/*
+ * x to 8-bit blocks, and back.
+ *   x, y [device]    `type` elements (CO3_F32, CO3_F16, CO3_BF16), aligned to their size; row r starts r * row_stride elements after
+ *                    the base.  16-byte aligned bases, strides and widths are read and written 16 bytes at a time
+ *   y                gets the values, rounded to `type` (exact but for fp16's and bf16's range)
+ * rows == 0 or cols == 0: nothing is done.
+ */
+int co3_f8_pack(const void* x, int type, uint64_t rows, uint32_t cols, uint64_t x_row_stride, int kind, void* out,
+                size_t out_bytes, void* stream);
+int co3_f8_unpack(const void* in, size_t in_bytes, int kind, void* y, int type, uint64_t rows, uint32_t cols,
+                  uint64_t y_row_stride, void* stream);
+
+/*
+ * The activation between two linear layers, and its backward pass from the 8 bits that were kept:
+ *     y = act(x);   y8 = y in blocks (the next layer's operand);   x8 = x in blocks;   dx = dy * act'(values of x8)
+ *   act              CO3_ACT_NONE (x), CO3_ACT_RELU (max(x, 0), slope 0 at 0), CO3_ACT_GELU (x Phi(x), Phi the normal distribution
+ *                    function), CO3_ACT_SILU (x / (1 + exp(-x)))
+ *   y, y8, x8        each nullable, not all; y may be x (same stride); y8 holds act(x) as fp32 arithmetic gives it, before
+ *                    it is rounded to `type`; both of CO3_F8_ROWS and of at least f8_bytes bytes
+ *   dx               may be dy (same stride)
+ */
+#define CO3_ACT_NONE 0
+#define CO3_ACT_RELU 1
+#define CO3_ACT_GELU 2
+#define CO3_ACT_SILU 3
+int co3_f8_activation(const void* x, int type, uint64_t rows, uint32_t cols, uint64_t x_row_stride, int act, void* y,
+                      uint64_t y_row_stride, void* y8, void* x8, size_t f8_bytes, void* stream);
+int co3_f8_activation_backward(const void* dy, int type, uint64_t rows, uint32_t cols, uint64_t dy_row_stride, const void* x8,
+                               size_t x8_bytes, int act, void* dx, uint64_t dx_row_stride, void* stream);
+
+/*
+ * A linear layer with weights W of `outs` rows and `ins` columns:
+ *     y[r][o] = sum over i of x8[r][i] w8[o][i] (+ bias[o]),   or transposed, towards the inputs,   y[r][i] = sum over o of x8[r][o] w8[o][i] (+ bias[i])
+ *   x [device]       nullable: `rows` rows of x_type that are packed into x8 first; NULL: x8 holds them already
+ *   x8 [device]      8-bit blocks, CO3_F8_ROWS, rows x ins (transposed: rows x outs): what the weight gradient reads later
+ *   w8 [device]      8-bit blocks, CO3_F8_SQUARE, outs x ins
+ *   bias [device]    nullable; fp32, one for each column of y
+ *   y [device]       y_type elements, rows x outs (transposed: rows x ins), aligned to their size; must not overlap x, x8 or w8
+ *   res [device]     nullable: one co3_result that the caller has cleared; its status becomes CO3_ERR_CUDA if a copy inside the
+ *                    kernel never completed (y is undefined then), and is left alone otherwise
+ * Products are exact and sums fp32; y is rounded once.  The same call gives the same bits.  ins == 0 (transposed: outs == 0)
+ * is refused; rows == 0 or an empty y: nothing is done.
+ */
+int co3_f8_linear(const void* x, int x_type, uint64_t x_row_stride, void* x8, size_t x8_bytes, const void* w8, size_t w8_bytes,
+                  uint32_t outs, uint32_t ins, int transposed, const float* bias, void* y, int y_type, uint64_t y_row_stride,
+                  uint64_t rows, co3_result* res, void* stream);
+
+/* Device workspace of co3_f8_weight_gradient. */
+int co3_f8_weight_gradient_workspace_bytes(uint64_t rows, uint32_t outs, uint32_t ins, uint32_t n_clients, size_t* out /* [host] */);
+
+/*
+ * Gradients of a linear layer's weights and biases, for n_clients batches of `rows` rows each (rows of client u are u * rows ..
+ * u * rows + rows - 1), from the inputs that co3_f8_linear, co3_f8_pack or co3_f8_activation left in 8-bit blocks:
+ *     dw_u[o][i] = sum over the client's rows of dy[r][o] x8[r][i];   db_u[o] = sum over the client's rows of dy[r][o]
+ *   dy [device]      `type` elements, n_clients * rows x outs, aligned to their size
+ *   x8 [device]      8-bit blocks, CO3_F8_ROWS, n_clients * rows x ins
+ *   dw, db [device]  fp32, each nullable: client u's outs x ins (outs) sums go to dw (db) + u * client_stride_elems, so that they
+ *                    can be layers of the gradient vectors that co3_encode reads; added to what is there if `accumulate` is not
+ *                    0.  No rows: zeros (or nothing, if accumulating)
+ *   res              as above
+ * dy is used to the last bit, products are exact, sums are fp32 in an order that depends on the sizes alone: the same call
+ * gives the same bits.
+ */
+int co3_f8_weight_gradient(const void* dy, int type, uint64_t dy_row_stride, const void* x8, size_t x8_bytes, uint64_t rows,
+                           uint32_t outs, uint32_t ins, float* dw, float* db, uint32_t n_clients, uint64_t client_stride_elems,
+                           int accumulate, void* workspace, size_t workspace_bytes, co3_result* res, void* stream);
+
+/*
  * Orthogonalised updates (no counterpart in the paper, whose server step is w <- w - lr * avg: this is the step of the
  * Muon optimiser for the weight matrices of a model).  A gradient G of a layer with `rows` outputs and `cols` inputs (a
  * convolution: cols = input channels x kernel size) is replaced by the nearest semi-orthogonal matrix, approximated

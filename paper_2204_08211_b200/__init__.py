@@ -11,6 +11,9 @@ from .binding import (  # noqa: F401
     MAT_DTYPE, MAT_PLAIN, NS_DTYPE, NS_MAX_STEPS, make_mats, make_ns,
     co3_layer_norm, co3_layer_norm_backward, co3_layer_norm_workspace_bytes,
     co3_orthogonalize, co3_orthogonalize_workspace_bytes, co3_muon_update,
+    F8_ROWS, F8_SQUARE, ACT_NONE, ACT_RELU, ACT_GELU, ACT_SILU,
+    co3_f8_bytes, co3_f8_pack, co3_f8_unpack, co3_f8_activation, co3_f8_activation_backward, co3_f8_linear,
+    co3_f8_weight_gradient, co3_f8_weight_gradient_workspace_bytes,
     co3_profile_enable, co3_profile_read, co3_status_string, KERNEL_NAMES, co3_stream_capacity_bytes, co3_workspace_bytes,
     library_path, make_fmts, make_segs, to_device, read_results,
 )

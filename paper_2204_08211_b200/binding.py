@@ -28,6 +28,8 @@ MAT_PLAIN = 1
 NS_MAX_STEPS = 16
 NS_DTYPE = np.dtype([("steps", np.uint32), ("eps", np.float32), ("coef", np.float32, (NS_MAX_STEPS, 3))])
 assert MAT_DTYPE.itemsize == 32 and NS_DTYPE.itemsize == 8 + 12 * NS_MAX_STEPS
+F8_ROWS, F8_SQUARE = 0, 1
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_SILU = range(4)
 _TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 
 _lib = None
@@ -77,9 +79,18 @@ def _load():
     L.co3_orthogonalize_workspace_bytes.argtypes = [vp, u32, C.POINTER(sz)]
     L.co3_orthogonalize.argtypes = [vp, C.c_int, vp, vp, C.c_int, vp, u32, vp, vp, vp, sz, vp]
     L.co3_muon_update.argtypes = [vp, vp, vp, vp, u32, f32, C.c_int, f32, f32, vp, vp, vp, sz, vp]
+    L.co3_f8_bytes.argtypes = [u64, u32, C.c_int, C.POINTER(sz)]
+    L.co3_f8_pack.argtypes = [vp, C.c_int, u64, u32, u64, C.c_int, vp, sz, vp]
+    L.co3_f8_unpack.argtypes = [vp, sz, C.c_int, vp, C.c_int, u64, u32, u64, vp]
+    L.co3_f8_activation.argtypes = [vp, C.c_int, u64, u32, u64, C.c_int, vp, u64, vp, vp, sz, vp]
+    L.co3_f8_activation_backward.argtypes = [vp, C.c_int, u64, u32, u64, vp, sz, C.c_int, vp, u64, vp]
+    L.co3_f8_linear.argtypes = [vp, C.c_int, u64, vp, sz, vp, sz, u32, u32, C.c_int, vp, vp, C.c_int, u64, u64, vp, vp]
+    L.co3_f8_weight_gradient_workspace_bytes.argtypes = [u64, u32, u32, u32, C.POINTER(sz)]
+    L.co3_f8_weight_gradient.argtypes = [vp, C.c_int, u64, vp, sz, u64, u32, u32, vp, vp, u32, u64, C.c_int, vp, sz, vp, vp]
     L.co3_profile_enable.argtypes = [C.c_int]
     L.co3_profile_read.argtypes = [vp, vp]
-    for name in ("co3_layer_norm", "co3_layer_norm_workspace_bytes", "co3_layer_norm_backward", "co3_ns_default", "co3_orthogonalize_workspace_bytes", "co3_orthogonalize", "co3_muon_update", "co3_histogram", "co3_convert_dither", "co3_histogram_dither", "co3_encode_dither", "co3_error_magnitude", "co3_model_weights", "co3_fit_scale", "co3_profile_enable", "co3_profile_read", "co3_convert_static", "co3_workspace_bytes", "co3_stream_capacity_bytes", "co3_convert", "co3_code_build", "co3_code_build_device", "co3_encode",
+    for name in ("co3_f8_bytes", "co3_f8_pack", "co3_f8_unpack", "co3_f8_activation", "co3_f8_activation_backward", "co3_f8_linear",
+                 "co3_f8_weight_gradient_workspace_bytes", "co3_f8_weight_gradient", "co3_layer_norm", "co3_layer_norm_workspace_bytes", "co3_layer_norm_backward", "co3_ns_default", "co3_orthogonalize_workspace_bytes", "co3_orthogonalize", "co3_muon_update", "co3_histogram", "co3_convert_dither", "co3_histogram_dither", "co3_encode_dither", "co3_error_magnitude", "co3_model_weights", "co3_fit_scale", "co3_profile_enable", "co3_profile_read", "co3_convert_static", "co3_workspace_bytes", "co3_stream_capacity_bytes", "co3_convert", "co3_code_build", "co3_code_build_device", "co3_encode",
                  "co3_encode_symbols", "co3_decode_aggregate", "co3_decode_aggregate_update", "co3_decode"):
         getattr(L, name).restype = C.c_int
     _lib = L
@@ -436,6 +447,114 @@ def co3_muon_update(grad, momentum, params, mats, mu, nesterov, lr, weight_decay
     return _load().co3_muon_update(_dev(grad), _dev(momentum), _dev(params), p, n, float(mu), 1 if nesterov else 0,
                                    float(lr), float(weight_decay), _ns(ns), _dev(res), _dev(workspace),
                                    workspace.numel() * workspace.element_size(), _stream(stream))
+
+
+def co3_f8_bytes(rows: int, cols: int, kind: int = F8_ROWS) -> int:
+    """Size of the buffer that holds a rows x cols matrix in 8-bit blocks."""
+    out = C.c_size_t(0)
+    st = _load().co3_f8_bytes(rows, cols, kind, C.byref(out))
+    if st != OK:
+        raise ValueError("co3_f8_bytes: " + co3_status_string(st))
+    return out.value
+
+
+def _f8(t):
+    """(pointer, bytes) of a buffer of 8-bit blocks."""
+    if t is None:
+        return None, 0
+    if t.dtype is not torch.uint8 or not t.is_cuda or not t.is_contiguous():
+        raise ValueError("expected a contiguous uint8 CUDA tensor of co3_f8_bytes bytes")
+    return t.data_ptr(), t.numel()
+
+
+def _res(t):
+    """Device pointer of a co3_result (or None)."""
+    if t is None:
+        return None
+    if not t.is_cuda or not t.is_contiguous() or t.numel() * t.element_size() < RESULT_DTYPE.itemsize:
+        raise ValueError("expected a CUDA tensor that holds a co3_result")
+    return t.data_ptr()
+
+
+def co3_f8_pack(x, out, kind: int = F8_ROWS, stream=None) -> int:
+    """out (uint8, co3_f8_bytes of x's rows and columns) <- x in 8-bit blocks."""
+    p, rows, cols, xs = _rows(x)
+    q, n = _f8(out)
+    return (_lib or _load()).co3_f8_pack(p, _TYPES[x.dtype], rows, cols, xs, kind, q, n, _stream_of(x, stream))
+
+
+def co3_f8_unpack(f8, y, kind: int = F8_ROWS, stream=None) -> int:
+    """y <- the values of a buffer of 8-bit blocks that holds a matrix of y's shape."""
+    p, rows, cols, ys = _rows(y)
+    q, n = _f8(f8)
+    return (_lib or _load()).co3_f8_unpack(q, n, kind, p, _TYPES[y.dtype], rows, cols, ys, _stream_of(y, stream))
+
+
+def co3_f8_activation(x, act: int, y=None, y8=None, x8=None, stream=None) -> int:
+    """y <- act(x), y8 <- act(x) in 8-bit blocks, x8 <- x in 8-bit blocks; each of the three may be None."""
+    p, rows, cols, xs = _rows(x)
+    py, ys = (None, 0) if y is None else _rows(y, x)[::3]
+    q, n = _f8(y8)
+    k, m = _f8(x8)
+    size = n if k is None else m if q is None else min(n, m)
+    return (_lib or _load()).co3_f8_activation(p, _TYPES[x.dtype], rows, cols, xs, act, py, ys, q, k, size, _stream_of(x, stream))
+
+
+def co3_f8_activation_backward(dy, x8, act: int, dx, stream=None) -> int:
+    """dx <- dy * act'(x) with the values of x that co3_f8_activation left in x8; dx may be dy."""
+    p, rows, cols, ds = _rows(dy)
+    po, _, _, os_ = _rows(dx, dy)
+    k, n = _f8(x8)
+    return (_lib or _load()).co3_f8_activation_backward(p, _TYPES[dy.dtype], rows, cols, ds, k, n, act, po, os_, _stream_of(dy, stream))
+
+
+def co3_f8_linear(x, x8, w8, bias, y, transposed: bool = False, cols: int | None = None, res=None, stream=None) -> int:
+    """y <- x W^T + bias, or (transposed) x W, from 8-bit blocks: x (may be None) is packed into x8 first, w8 holds the weights
+    (F8_SQUARE).  cols: the columns of x8's matrix, needed without x.  res: a cleared co3_result, or None."""
+    py, rows, to, ys = _rows(y)
+    if x is None:
+        px, type_, xs, rx = None, 0, 0, rows
+        if cols is None:
+            raise ValueError("co3_f8_linear: cols is needed without x")
+    else:
+        px, rx, width, xs = _rows(x)
+        type_ = _TYPES[x.dtype]
+        if cols is not None and cols != width:
+            raise ValueError("co3_f8_linear: x has other columns")
+        cols = width
+    if rx != rows:
+        raise ValueError("co3_f8_linear: x and y have different rows")
+    q, n = _f8(x8)
+    w, m = _f8(w8)
+    outs, ins = (cols, to) if transposed else (to, cols)
+    return (_lib or _load()).co3_f8_linear(px, type_, xs, q, n, w, m, outs, ins, 1 if transposed else 0, _vec(bias, to), py, _TYPES[y.dtype], ys,
+                                           rows, _res(res), _stream_of(y, stream))
+
+
+def co3_f8_weight_gradient_workspace_bytes(rows: int, outs: int, ins: int, n_clients: int = 1) -> int:
+    """Device workspace of co3_f8_weight_gradient for n_clients batches of `rows` rows each."""
+    out = C.c_size_t(0)
+    st = _load().co3_f8_weight_gradient_workspace_bytes(rows, outs, ins, n_clients, C.byref(out))
+    if st != OK:
+        raise ValueError("co3_f8_weight_gradient_workspace_bytes: " + co3_status_string(st))
+    return out.value
+
+
+def co3_f8_weight_gradient(dy, x8, ins: int, dw, db, n_clients: int, client_stride_elems: int, workspace, accumulate: bool = False,
+                           res=None, stream=None) -> int:
+    """Gradients of weights and biases of a linear layer with `ins` inputs from dy and the packed inputs x8; the rows are n_clients
+    equal batches.  dw and db are fp32 tensors that start at client 0's gradient of that layer; each may be None."""
+    p, rows, outs, ds = _rows(dy)
+    if n_clients < 1 or rows % n_clients:
+        raise ValueError("co3_f8_weight_gradient: the rows do not divide into n_clients batches")
+    if client_stride_elems < 0 or ins < 0:  # the library takes them as unsigned
+        raise ValueError("co3_f8_weight_gradient: negative sizes")
+    q, n = _f8(x8)
+    before = (n_clients - 1) * client_stride_elems
+    return (_lib or _load()).co3_f8_weight_gradient(
+        p, _TYPES[dy.dtype], ds, q, n, rows // n_clients, outs, ins, _vec(dw, before + outs * ins), _vec(db, before + outs), n_clients,
+        client_stride_elems, 1 if accumulate else 0, _dev(workspace), workspace.numel() * workspace.element_size(), _res(res),
+        _stream_of(dy, stream))
 
 
 KERNEL_NAMES = ("prepare", "convert", "pack", "scan", "compact", "code_build", "decode", "fit", "clear")

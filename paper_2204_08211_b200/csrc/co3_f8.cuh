@@ -1,0 +1,106 @@
+// What the kernels on 8-bit blocks share: where values and scales lie, and the conversions.
+//
+// A block of 128 columns of a row (or of 128 x 128 entries, CO3_F8_SQUARE) has one scale, the smallest power of two s with
+// max|x| <= 448 s, and its entries are x / s in e4m3 (sign, four bits of exponent, three of mantissa), rounded to nearest, ties
+// to even.  A power of two loses nothing against an fp32 scale but at most one bit of the smallest, sub-normal steps; x / s, the
+// value read back and its bf16 form are exact; and the tensor cores apply such scales themselves (an exponent byte, 2^(byte - 127)).
+//
+// The memory holds what the tensor cores read: for each 128 columns, rows of 128 bytes one behind the other, the 16-byte pieces
+// of a row XORed with the row number modulo 8.  Any rows that start at a multiple of 8 are fetched by one plain bulk copy, and the
+// same bytes serve as the operand and as the transposed operand.  Exponent bytes lie in tiles of 512 bytes for 128 rows and four
+// blocks of columns: byte 16 (r % 32) + 4 (r / 32) + block, as they are copied into tensor memory.  Square blocks have
+// them once more for the transposed operand.
+#pragma once
+
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "co3.h"
+#include "co3_device.cuh"
+#include "co3_types.cuh"
+
+namespace co3 {
+
+constexpr uint32_t kF8Block = 128;
+constexpr uint32_t kF8Tile = 128 * 128;        // bytes of 128 rows of a block of columns
+constexpr uint32_t kF8Scales = 512;            // bytes of a tile of exponent bytes
+constexpr int kF8MinExp = -126, kF8MaxExp = 120;
+
+struct F8Layout {
+    uint64_t rows;         // rows padded to whole tiles
+    uint32_t kb;           // blocks of columns
+    uint64_t scales;       // byte offset of the exponent bytes
+    uint64_t scales_t;     // the same for the transposed operand (square blocks)
+    uint64_t bytes;
+};
+
+inline bool f8_layout(uint64_t rows, uint64_t cols, int kind, F8Layout* out) {
+    if (kind != CO3_F8_ROWS && kind != CO3_F8_SQUARE) return false;
+    if (rows >= (1ull << 31) || cols >= (1ull << 31)) return false;
+    out->rows = (rows + 127u) & ~(uint64_t)127u;
+    out->kb = (uint32_t)((cols + 127u) / 128u);
+    if (out->kb && out->rows >= (1ull << 40) / 128u / out->kb) return false;
+    const uint64_t tiles = out->rows / 128u;
+    out->scales = out->rows * out->kb * 128u;
+    out->scales_t = out->scales + (uint64_t)((out->kb + 3u) / 4u) * tiles * kF8Scales;
+    out->bytes = out->scales_t + (kind == CO3_F8_SQUARE ? (tiles + 3u) / 4u * out->kb * kF8Scales : 0u);
+    if (out->bytes < 256u) out->bytes = 256u;
+    return true;
+}
+
+// Offset of a row's 128 bytes of a block of columns, and of a 16-byte piece in them.
+__device__ __forceinline__ uint64_t f8_row(uint64_t rows_padded, uint32_t block, uint64_t row) { return (block * rows_padded + row) * 128u; }
+__device__ __forceinline__ uint32_t f8_piece(uint32_t row, uint32_t piece) { return (piece ^ (row & 7u)) << 4; }
+// Offset of a row's exponent byte among those of a tile.
+__host__ __device__ inline uint32_t f8_scale_at(uint32_t row_in_tile, uint32_t block) {
+    return (row_in_tile & 31u) * 16u + (row_in_tile >> 5) * 4u + (block & 3u);
+}
+
+// Exponent of the scale of a block whose largest magnitude has these bits (finite; 448 = 1.75 * 2^8).  Never below -126, so that
+// the scale and its inverse are normal numbers: entries below 2^-136 become zero.
+__device__ __forceinline__ int f8_exponent(uint32_t most) {
+    const int e = (int)(most >> 23) - 127 - 8 + ((most & 0x7fffffu) > 0x600000u ? 1 : 0);
+    return max(e, kF8MinExp);
+}
+__device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
+
+// Four values to e4m3, the first in the lowest byte.  NaN stays NaN.
+__device__ __forceinline__ uint32_t f8_from4(float a, float b, float c, float d) {
+    uint16_t lo, hi;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(b), "f"(a));
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(d), "f"(c));
+    return (uint32_t)lo | ((uint32_t)hi << 16);
+}
+// Two of them back.
+__device__ __forceinline__ float2 f8_to2(uint32_t two) {
+    uint32_t h;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)two));
+    return __half22float2(*reinterpret_cast<const __half2*>(&h));
+}
+
+// Bits of the largest magnitude from which a block is not on the short way: infinities and NaN, and magnitudes whose nearest value
+// may be 2^128.
+constexpr uint32_t kF8Rare = 0x7f600000u;
+
+__device__ __forceinline__ uint32_t f8_magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+// What a non-finite value counts in its block's largest magnitude, and what it becomes.
+__device__ __forceinline__ uint32_t f8_finite_magnitude(float v) {
+    const uint32_t m = f8_magnitude(v);
+    return m < 0x7f800000u ? m : 0u;
+}
+__device__ __forceinline__ float f8_rare(float v, int exponent) {
+    if (f8_magnitude(v) >= 0x7f800000u) return __uint_as_float(0x7fffffffu);
+    const float most = exponent == kF8MaxExp ? __uint_as_float(0x7f700000u) : __uint_as_float(0x7f600000u);  // 240 or 448 scales
+    return fminf(fmaxf(v, -most), most);
+}
+
+// Registers are shared out between three groups of four warps that start with 168 each: the first group's warps issue
+// copies and products, the eight others hold a tile's sums.
+constexpr uint32_t kF8Threads = 384;
+constexpr uint32_t kFewRegs = 56, kManyRegs = 224;
+static_assert(kFewRegs + 2 * kManyRegs == 3 * 168, "registers of the block");
+__device__ __forceinline__ void few_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFewRegs)); }
+__device__ __forceinline__ void many_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kManyRegs)); }
+
+}  // namespace co3

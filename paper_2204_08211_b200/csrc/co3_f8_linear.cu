@@ -1,0 +1,420 @@
+// Products of 8-bit blocks on the tensor cores: y = x W^T + b and its counterpart towards the inputs, x W.
+//
+// The weights are the first operand, 128 of their rows (or, transposed, of their columns) per tile, and the rows of x the second,
+// 16 to 256 of them: tensor memory then holds an output feature per lane and a row of x per column, so that a warp's 32 lanes
+// write neighbouring entries of y, and few rows of x cost little.  The tensor core applies both operands' scales while it multiplies
+// (kind::mxf8f6f4, an exponent byte for each 32 columns of the sum: the same four times); sums are fp32 in tensor memory over the
+// whole length.
+//
+// A block of threads: one thread issues bulk copies, one the products, eight warps take the sums out.  A stage of the ring is a
+// block of 128 columns of the sum; exponent bytes come with every fourth.  Few tiles: the blocks of a cluster divide the
+// sum's length, and add their parts through shared memory in order.
+#include <algorithm>
+#include <atomic>
+
+#include "co3_f8.cuh"
+#include "co3_launch.cuh"
+#include "co3_orth.cuh"
+
+namespace co3 {
+
+namespace {
+
+constexpr uint32_t kMaxSplit = 8;
+constexpr uint32_t kTmemScales = 256;        // first column of the exponent bytes; eight turns of 16 columns
+constexpr uint32_t kScaleTurns = 8, kScaleCols = 16;
+// The tensor core cuts what it adds towards zero, about 2^-25 of the sum each time: a sum is taken out and added up in registers,
+// to nearest, after so many blocks.  Results of 16 bits round by 2^-12 and more.
+constexpr uint32_t kBlocksF32 = 8, kBlocks16 = 32;
+
+struct LinearArgs {
+    const uint8_t *a, *a_scales, *b, *b_scales;
+    uint64_t a_block, a_tile;                // bytes between blocks of the sum, between tiles
+    uint64_t a_group, b_group;               // bytes between groups of four blocks' exponent bytes
+    uint64_t b_block;
+    uint32_t kb;                             // blocks of the sum
+    uint32_t features, rows;
+    uint32_t m_tiles, n_tiles;
+    uint32_t split;
+    uint32_t blocks;                         // blocks that tensor memory adds up
+    void* y;
+    uint64_t y_stride;
+    int y_type;
+    const float* bias;
+    co3_result* res;
+};
+
+template <int kN>
+struct Shape {
+    static constexpr uint32_t kStages = kN == 256 ? 4 : kN == 128 ? 6 : 8;
+    static constexpr uint32_t kStageBytes = kF8Tile + kN * 128;
+    static constexpr uint32_t kScaleBytes = kF8Scales * (kN == 256 ? 3 : 2);       // first operand's, then the second's
+    static constexpr uint32_t kRing = kStages * kStageBytes;
+    static constexpr uint32_t kSums = kN == 256 ? 1 : 2;                           // tiles that tensor memory holds
+    static constexpr uint32_t kSmem = 1024 + kRing + kStages * kScaleBytes + 256;
+    static_assert(kN * 128 * 4 <= kRing, "a tile's sums fit the ring");
+};
+
+template <int kN>
+struct LinearSmem {
+    uint64_t full[Shape<kN>::kStages], empty[Shape<kN>::kStages], sum_full[2], sum_empty[2], done;
+    uint32_t tmem, failed;
+};
+
+// D fp32, A and B e4m3, scales of eight bits of exponent; `block` says which byte of the scales' columns counts.
+__host__ __device__ constexpr uint32_t f8_instr(bool a_transposed, uint32_t cols, uint32_t block) {
+    return (block << 4) | ((uint32_t)a_transposed << 15) | ((cols / 8u) << 17) | (1u << 23) | (1u << 27) | (block << 29);
+}
+__device__ __forceinline__ void f8_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t instr, uint32_t sa, uint32_t sb, bool accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(instr), "r"(sa),
+        "r"(sb), "r"((uint32_t)accumulate)
+        : "memory");
+}
+// 512 bytes of shared memory, 32 rows of 16, to four columns of tensor memory, the same for each 32 lanes.
+__device__ __forceinline__ void f8_scales_in(uint32_t to, uint32_t from) {
+    const uint64_t desc = (uint64_t)((from >> 4) & 0x3fffu) | (8ull << 32) | (1ull << 46);
+    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(to), "l"(desc) : "memory");
+}
+// Operands as co3_orth.cuh has them, here of one-byte elements: 32 columns of the sum are 32 bytes of a row or, transposed, 32 rows
+// of 128 bytes.
+__device__ __forceinline__ uint64_t f8_desc(uint32_t addr) { return (uint64_t)((addr >> 4) & 0x3fffu) | (1ull << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61); }
+__host__ __device__ constexpr uint32_t f8_step(bool transposed) { return transposed ? 4096u >> 4 : 32u >> 4; }
+
+// The four products of a stage.
+template <bool kTransposed, uint32_t kBlock4>
+__device__ __forceinline__ void multiply_block(uint32_t d, uint32_t a, uint32_t b, uint32_t cols, uint32_t sa, uint32_t sb, bool accumulate) {
+    const uint64_t da = f8_desc(a), db = f8_desc(b);
+    const uint32_t instr = f8_instr(kTransposed, 0, kBlock4) | ((cols / 8u) << 17);
+#pragma unroll
+    for (uint32_t e = 0; e < 4; ++e) f8_mma(d, da + e * f8_step(kTransposed), db + e * f8_step(false), instr, sa, sb, accumulate || e > 0);
+}
+
+template <int kCount>
+__device__ __forceinline__ void tc_load(uint32_t addr, float* v) {
+    if constexpr (kCount == 8) {
+        uint32_t r[8];
+        asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];\n\ttcgen05.wait::ld.sync.aligned;"
+                     : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                     : "r"(addr)
+                     : "memory");
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r[i]);
+    } else {
+        static_assert(kCount == 32, "8 or 32 columns");
+        tc_load32(addr, *reinterpret_cast<float(*)[32]>(v));
+    }
+}
+
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ float load_peer(uint32_t addr, uint32_t rank) {
+    uint32_t at;
+    float v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(addr), "r"(rank));
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
+    return v;
+}
+
+// A lane's sums of kCount rows of x, from row `first` on.
+template <typename T, int kCount>
+__device__ __forceinline__ void write_sums(const LinearArgs& a, uint32_t feature, uint32_t first, float bias, const float* v) {
+    T* p = static_cast<T*>(a.y) + (uint64_t)first * a.y_stride + feature;
+#pragma unroll
+    for (int i = 0; i < kCount; ++i)
+        if (first + i < a.rows) p[i * a.y_stride] = from_float<T>(__fadd_rn(v[i], bias));
+}
+template <int kCount>
+__device__ __forceinline__ void write_any(const LinearArgs& a, uint32_t feature, uint32_t first, float bias, const float* v) {
+    if (feature >= a.features) return;
+    if (a.y_type == CO3_F32) write_sums<float, kCount>(a, feature, first, bias, v);
+    else if (a.y_type == CO3_F16) write_sums<__half, kCount>(a, feature, first, bias, v);
+    else write_sums<__nv_bfloat16, kCount>(a, feature, first, bias, v);
+}
+
+template <int kN, bool kTransposed, bool kSplit>
+__global__ void __launch_bounds__(kF8Threads, 1) f8_linear_kernel(const __grid_constant__ LinearArgs a) {
+    extern __shared__ unsigned char smem_raw[];
+    using S = Shape<kN>;
+    constexpr uint32_t kStages = S::kStages;
+    unsigned char* ring = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
+    unsigned char* scales = ring + S::kRing;
+    LinearSmem<kN>& sm = *reinterpret_cast<LinearSmem<kN>*>(scales + kStages * S::kScaleBytes);
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
+    if (threadIdx.x == 0) {
+        for (uint32_t i = 0; i < kStages; ++i) { mbar_init(&sm.full[i], 1); mbar_init(&sm.empty[i], 1); }
+        for (uint32_t i = 0; i < 2; ++i) { mbar_init(&sm.sum_full[i], 1); mbar_init(&sm.sum_empty[i], 8); }
+        mbar_init(&sm.done, 1);
+        sm.failed = 0;
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(&sm.tmem)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = sm.tmem;
+    volatile uint32_t* failed = &sm.failed;
+    wait_for_previous_kernel();
+
+    const uint32_t tiles = a.m_tiles * a.n_tiles;
+    const uint32_t part = kSplit ? blockIdx.x % a.split : 0u, step = kSplit ? gridDim.x / a.split : gridDim.x;
+    const uint32_t first = kSplit ? blockIdx.x / a.split : blockIdx.x;  // one tile a cluster when split
+    const uint32_t k0 = kSplit ? (uint32_t)((uint64_t)a.kb * part / a.split) : 0u, k1 = kSplit ? (uint32_t)((uint64_t)a.kb * (part + 1) / a.split) : a.kb;
+
+    if (warp < 4) few_registers();
+    if (warp == 0 && lane == 0) {
+        uint32_t st = 0, turn = 0;
+        for (uint32_t t = first; t < tiles && !*failed; t += step) {
+            const uint32_t mt = t % a.m_tiles, nt = t / a.m_tiles, n0 = nt * kN;
+            const uint32_t n = min((uint32_t)kN, (a.rows - n0 + 15u) & ~15u);
+            for (uint32_t q = k0; q < k1; ++q) {
+                if (turn > 0 && !mbar_wait(&sm.empty[st], (turn - 1) & 1u)) { *failed = 1; break; }
+                unsigned char* to = ring + st * S::kStageBytes;
+                const bool with_scales = q == k0 || (q & 3u) == 0;
+                const uint32_t b_scales = n > 128 ? 2 * kF8Scales : kF8Scales;
+                mbar_arrive_expect_tx(&sm.full[st], kF8Tile + n * 128u + (with_scales ? kF8Scales + b_scales : 0u));
+                bulk_copy_g2s(to, a.a + q * a.a_block + mt * a.a_tile, kF8Tile, &sm.full[st]);
+                bulk_copy_g2s(to + kF8Tile, a.b + q * a.b_block + (uint64_t)n0 * 128u, n * 128u, &sm.full[st]);
+                if (with_scales) {
+                    unsigned char* s = scales + st * S::kScaleBytes;
+                    bulk_copy_g2s(s, a.a_scales + (q >> 2) * a.a_group + (uint64_t)mt * kF8Scales, kF8Scales, &sm.full[st]);
+                    bulk_copy_g2s(s + kF8Scales, a.b_scales + (q >> 2) * a.b_group + (uint64_t)(n0 >> 7) * kF8Scales, b_scales, &sm.full[st]);
+                }
+                if (++st == kStages) { st = 0; ++turn; }
+            }
+        }
+        // copies in flight end before the block does, whoever else has given up
+        for (uint32_t i = 0; i < kStages; ++i) {
+            const uint32_t begun = turn + (i < st ? 1u : 0u);
+            if (begun > 0) mbar_wait(&sm.full[i], (begun - 1) & 1u);
+        }
+    } else if (warp == 1 && lane == 0) {
+        uint32_t st = 0, turn = 0, sum = 0, sum_turn = 0, group = 0;
+        bool ok = true;
+        for (uint32_t t = first; t < tiles && ok && !*failed; t += step) {
+            const uint32_t n0 = t / a.m_tiles * kN, n = min((uint32_t)kN, (a.rows - n0 + 15u) & ~15u);
+            uint32_t left = 0;  // blocks that the present sum still takes
+            for (uint32_t q = k0; q < k1; ++q) {
+                const bool fresh = left == 0;
+                if (fresh) {
+                    left = min(a.blocks, k1 - q);
+                    if (sum_turn > 0 && !mbar_wait(&sm.sum_empty[sum], (sum_turn - 1) & 1u)) { ok = false; break; }
+                }
+                --left;
+                const uint32_t d = tmem + sum * kN;
+                if (!mbar_wait(&sm.full[st], turn & 1u)) { ok = false; break; }
+                tc_fence_after();
+                if (q == k0 || (q & 3u) == 0) {
+                    // the columns of eight groups ago are free: fewer than kStages <= 8 blocks are under way
+                    group = group + 1 == kScaleTurns ? 0 : group + 1;
+                    const uint32_t to = tmem + kTmemScales + group * kScaleCols, from = smem_addr(scales + st * S::kScaleBytes);
+                    f8_scales_in(to, from);
+                    f8_scales_in(to + 4, from + kF8Scales);
+                    if (kN == 256) f8_scales_in(to + 8, from + 2 * kF8Scales);
+                }
+                const uint32_t sa = tmem + kTmemScales + group * kScaleCols, sb = sa + 4 + ((n0 & 127u) >> 5);
+                const uint32_t at = smem_addr(ring + st * S::kStageBytes), bt = at + kF8Tile;
+                switch (q & 3u) {
+                    case 0: multiply_block<kTransposed, 0>(d, at, bt, n, sa, sb, !fresh); break;
+                    case 1: multiply_block<kTransposed, 1>(d, at, bt, n, sa, sb, !fresh); break;
+                    case 2: multiply_block<kTransposed, 2>(d, at, bt, n, sa, sb, !fresh); break;
+                    default: multiply_block<kTransposed, 3>(d, at, bt, n, sa, sb, !fresh); break;
+                }
+                tc_commit(&sm.empty[st]);
+                if (left == 0) {
+                    tc_commit(&sm.sum_full[sum]);
+                    if (++sum == S::kSums) { sum = 0; ++sum_turn; }
+                }
+                if (++st == kStages) { st = 0; ++turn; }
+            }
+        }
+        if (!ok) *failed = 1;
+        tc_commit(&sm.done);
+        mbar_wait(&sm.done, 0);
+    } else if (warp >= 4) {
+        many_registers();
+        // columns of a tile by halves; 16 columns are one warp's of each 32 lanes
+        constexpr int kHalf = kN / 2, kLoad = kHalf < 32 ? 8 : 32;
+        static_assert(kHalf % kLoad == 0, "halves are whole loads");
+        const uint32_t quad = warp & 3u, half = (warp - 4u) >> 2, row = quad * 32u + lane;
+        uint32_t sum = 0, sum_turn = 0;
+        for (uint32_t t = first; t < tiles; t += step) {
+            const uint32_t mt = t % a.m_tiles, n0 = t / a.m_tiles * kN, feature = mt * 128u + row;
+            bool ok = true;
+            float acc[kHalf];
+            for (uint32_t q = k0; q < k1; q += a.blocks) {
+                ok = lane != 0 || mbar_wait(&sm.sum_full[sum], sum_turn & 1u);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t from = tmem + ((quad * 32u) << 16) + sum * kN + half * kHalf;
+                if (q == k0) {
+#pragma unroll
+                    for (int h = 0; h < kHalf; h += kLoad) tc_load<kLoad>(from + h, acc + h);
+                } else {
+#pragma unroll
+                    for (int h = 0; h < kHalf; h += kLoad) {
+                        float w[kLoad];
+                        tc_load<kLoad>(from + h, w);
+#pragma unroll
+                        for (int i = 0; i < kLoad; ++i) acc[h + i] = __fadd_rn(acc[h + i], w[i]);
+                    }
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sm.sum_empty[sum]);
+                if (++sum == S::kSums) { sum = 0; ++sum_turn; }
+            }
+            if (!ok) { *failed = 1; break; }
+            if constexpr (kSplit) {  // into the ring, of which no copy and no product is left
+                float* to = reinterpret_cast<float*>(ring) + (uint64_t)half * kHalf * 128u + row;
+#pragma unroll
+                for (int i = 0; i < kHalf; ++i) to[i * 128] = acc[i];
+            } else {
+                const float bias = a.bias && feature < a.features ? a.bias[feature] : 0.0f;
+                write_any<kHalf>(a, feature, n0 + half * kHalf, bias, acc);
+            }
+        }
+        if constexpr (kSplit) {
+            // everybody's part is there; each block takes some of the columns
+            __syncwarp();
+            cluster_sync();
+            const uint32_t mt = first % a.m_tiles, n0 = first / a.m_tiles * kN, feature = mt * 128u + row;
+            const float bias = a.bias && feature < a.features ? a.bias[feature] : 0.0f;
+            const uint32_t c0 = kN * part / a.split, c1 = kN * (part + 1) / a.split;
+            for (uint32_t c = c0 + half; c < c1 && n0 + c < a.rows && !*failed; c += 2) {
+                const uint32_t at = smem_addr(ring) + (c * 128u + row) * 4u;
+                float v = 0.0f;
+                for (uint32_t p = 0; p < a.split; ++p) v = __fadd_rn(v, load_peer(at, p));
+                write_any<1>(a, feature, n0 + c, bias, &v);
+            }
+        }
+    }
+    __syncwarp();
+    if constexpr (kSplit) {
+        if (warp < 4) cluster_sync();
+        cluster_sync();  // nobody leaves while its part is read
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+    if (threadIdx.x == 0 && *failed && a.res) atomicExch(&a.res->status, CO3_ERR_CUDA);
+}
+
+int device_sms(uint32_t* out) {
+    static std::atomic<int> known[64];
+    int dev = 0;
+    CO3_CUDA(cudaGetDevice(&dev));
+    int n = dev < 64 ? known[dev].load(std::memory_order_relaxed) : 0;
+    if (n == 0) {
+        CO3_CUDA(cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev));
+        if (dev < 64) known[dev].store(n, std::memory_order_relaxed);
+    }
+    *out = (uint32_t)n;
+    return CO3_OK;
+}
+
+template <int kN, bool kTransposed, bool kSplit>
+int launch_linear(const LinearArgs& a, uint32_t sms, cudaStream_t st) {
+    auto* kernel = f8_linear_kernel<kN, kTransposed, kSplit>;
+    constexpr uint32_t kSmem = Shape<kN>::kSmem;
+    static std::atomic<bool> ready[64];
+    int dev = 0;
+    CO3_CUDA(cudaGetDevice(&dev));
+    if (dev >= 64 || !ready[dev].load(std::memory_order_relaxed)) {
+        CO3_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem));
+        if (dev < 64) ready[dev].store(true, std::memory_order_relaxed);
+    }
+    const uint32_t tiles = a.m_tiles * a.n_tiles;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(kSplit ? tiles * a.split : std::min(tiles, sms));
+    cfg.blockDim = dim3(kF8Threads);
+    cfg.dynamicSmemBytes = kSmem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = a.split;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = kSplit ? 2 : 1;
+    CO3_CUDA(cudaLaunchKernelEx(&cfg, kernel, a));
+    return CO3_OK;
+}
+
+template <int kN>
+int launch_tile(LinearArgs a, bool transposed, uint32_t sms, cudaStream_t st) {
+    a.n_tiles = (a.rows + kN - 1) / kN;
+    const uint64_t tiles = (uint64_t)a.m_tiles * a.n_tiles;
+    if (tiles >= (1ull << 31) / kMaxSplit) return CO3_ERR_INVALID_ARG;
+    a.split = 1;
+    while (a.split < kMaxSplit && tiles * a.split * 2 <= sms && a.kb >= a.split * 4) a.split *= 2;
+    if (a.split > 1) return transposed ? launch_linear<kN, true, true>(a, sms, st) : launch_linear<kN, false, true>(a, sms, st);
+    return transposed ? launch_linear<kN, true, false>(a, sms, st) : launch_linear<kN, false, false>(a, sms, st);
+}
+
+}  // namespace
+}  // namespace co3
+
+using namespace co3;
+
+extern "C" {
+
+int co3_f8_linear(const void* x, int x_type, uint64_t x_row_stride, void* x8, size_t x8_bytes, const void* w8, size_t w8_bytes, uint32_t outs, uint32_t ins,
+                  int transposed, const float* bias, void* y, int y_type, uint64_t y_row_stride, uint64_t rows, co3_result* res, void* stream) {
+    F8Layout lx, lw;
+    const uint32_t from = transposed ? outs : ins, to = transposed ? ins : outs;
+    if ((x && (x_type < CO3_F32 || x_type > CO3_BF16)) || y_type < CO3_F32 || y_type > CO3_BF16 || !f8_layout(outs, ins, CO3_F8_SQUARE, &lw) ||
+        !f8_layout(rows, from, CO3_F8_ROWS, &lx))
+        return CO3_ERR_INVALID_ARG;
+    if (rows == 0 || to == 0) return CO3_OK;
+    if (from == 0) return CO3_ERR_INVALID_ARG;
+    if (!x8 || !aligned(x8, 256) || !w8 || !aligned(w8, 256) || !y || !aligned(y, type_size(y_type)) || y_row_stride < to || y_row_stride >= (1ull << 40) ||
+        !aligned(bias, 4) || !aligned(res, 8))
+        return CO3_ERR_INVALID_ARG;
+    if (x8_bytes < lx.bytes || w8_bytes < lw.bytes) return CO3_ERR_CAPACITY;
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    uint32_t sms = 0;
+    int e = device_sms(&sms);
+    if (e != CO3_OK) return e;
+    if (x) {
+        e = co3_f8_pack(x, x_type, rows, from, x_row_stride, CO3_F8_ROWS, x8, x8_bytes, stream);
+        if (e != CO3_OK) return e;
+    }
+    const uint8_t *w = static_cast<const uint8_t*>(w8), *b = static_cast<const uint8_t*>(x8);
+    LinearArgs a = {};
+    a.a = w;
+    a.a_block = transposed ? kF8Tile : lw.rows * 128u;
+    a.a_tile = transposed ? lw.rows * 128u : kF8Tile;
+    a.a_scales = w + (transposed ? lw.scales_t : lw.scales);
+    a.a_group = transposed ? (uint64_t)lw.kb * kF8Scales : lw.rows / 128u * kF8Scales;
+    a.b = b;
+    a.b_block = lx.rows * 128u;
+    a.b_scales = b + lx.scales;
+    a.b_group = lx.rows / 128u * kF8Scales;
+    a.kb = lx.kb;
+    a.features = to;
+    a.rows = (uint32_t)rows;
+    a.m_tiles = (to + 127u) / 128u;
+    a.y = y;
+    a.y_stride = y_row_stride;
+    a.y_type = y_type;
+    a.blocks = y_type == CO3_F32 ? kBlocksF32 : kBlocks16;
+    a.bias = bias;
+    a.res = res;
+    if (rows <= 16) return launch_tile<16>(a, transposed != 0, sms, st);
+    if (rows <= 64 || (uint64_t)a.m_tiles * ((rows + 127u) / 128u) * 2 <= sms) return launch_tile<64>(a, transposed != 0, sms, st);
+    if (rows <= 128 || (uint64_t)a.m_tiles * ((rows + 255u) / 256u) <= sms) return launch_tile<128>(a, transposed != 0, sms, st);
+    return launch_tile<256>(a, transposed != 0, sms, st);
+}
+
+}  // extern "C"
