@@ -108,10 +108,6 @@ __device__ __forceinline__ void tc_load(uint32_t addr, float* v) {
     }
 }
 
-__device__ __forceinline__ void cluster_sync() {
-    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
 __device__ __forceinline__ float load_peer(uint32_t addr, uint32_t rank) {
     uint32_t at;
     float v;
