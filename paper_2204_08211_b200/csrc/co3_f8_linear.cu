@@ -171,7 +171,7 @@ __global__ void __launch_bounds__(kF8Threads, 1) f8_linear_kernel(const __grid_c
             const uint32_t mt = t % a.m_tiles, nt = t / a.m_tiles, n0 = nt * kN;
             const uint32_t n = min((uint32_t)kN, (a.rows - n0 + 15u) & ~15u);
             for (uint32_t q = k0; q < k1; ++q) {
-                if (turn > 0 && !mbar_wait(&sm.empty[st], (turn - 1) & 1u)) { *failed = 1; break; }
+                if (turn > 0 && !f8_wait(&sm.empty[st], (turn - 1) & 1u)) { *failed = 1; break; }
                 unsigned char* to = ring + st * S::kStageBytes;
                 const bool with_scales = q == k0 || (q & 3u) == 0;
                 const uint32_t b_scales = n > 128 ? 2 * kF8Scales : kF8Scales;
@@ -189,7 +189,7 @@ __global__ void __launch_bounds__(kF8Threads, 1) f8_linear_kernel(const __grid_c
         // copies in flight end before the block does, whoever else has given up
         for (uint32_t i = 0; i < kStages; ++i) {
             const uint32_t begun = turn + (i < st ? 1u : 0u);
-            if (begun > 0) mbar_wait(&sm.full[i], (begun - 1) & 1u);
+            if (begun > 0) f8_wait(&sm.full[i], (begun - 1) & 1u);
         }
     } else if (warp == 1 && lane == 0) {
         uint32_t st = 0, turn = 0, sum = 0, sum_turn = 0, group = 0;
@@ -201,11 +201,11 @@ __global__ void __launch_bounds__(kF8Threads, 1) f8_linear_kernel(const __grid_c
                 const bool fresh = left == 0;
                 if (fresh) {
                     left = min(a.blocks, k1 - q);
-                    if (sum_turn > 0 && !mbar_wait(&sm.sum_empty[sum], (sum_turn - 1) & 1u)) { ok = false; break; }
+                    if (sum_turn > 0 && !f8_wait(&sm.sum_empty[sum], (sum_turn - 1) & 1u)) { ok = false; break; }
                 }
                 --left;
                 const uint32_t d = tmem + sum * kN;
-                if (!mbar_wait(&sm.full[st], turn & 1u)) { ok = false; break; }
+                if (!f8_wait(&sm.full[st], turn & 1u)) { ok = false; break; }
                 tc_fence_after();
                 if (q == k0 || (q & 3u) == 0) {
                     // the columns of eight groups ago are free: fewer than kStages <= 8 blocks are under way
@@ -233,7 +233,7 @@ __global__ void __launch_bounds__(kF8Threads, 1) f8_linear_kernel(const __grid_c
         }
         if (!ok) *failed = 1;
         tc_commit(&sm.done);
-        mbar_wait(&sm.done, 0);
+        f8_wait(&sm.done, 0);
     } else if (warp >= 4) {
         many_registers();
         // columns of a tile by halves; 16 columns are one warp's of each 32 lanes
@@ -246,7 +246,7 @@ __global__ void __launch_bounds__(kF8Threads, 1) f8_linear_kernel(const __grid_c
             bool ok = true;
             float acc[kHalf];
             for (uint32_t q = k0; q < k1; q += a.blocks) {
-                ok = lane != 0 || mbar_wait(&sm.sum_full[sum], sum_turn & 1u);
+                ok = lane != 0 || f8_wait(&sm.sum_full[sum], sum_turn & 1u);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 tc_fence_after();

@@ -282,7 +282,7 @@ __global__ void __launch_bounds__(kF8Threads, 1) f8_weight_kernel(const __grid_c
                 const unsigned char* x = a.ws_x + ((uint64_t)p.u * a.k_tiles + kt) * a.chunks * kPlane16;
                 const unsigned char* dy = a.ws_dy + ((uint64_t)p.u * a.groups + g) * a.chunks * (kParts * kPlane16);
                 for (uint32_t c = p.c0; c < p.c1; ++c) {
-                    if (turn > 0 && !mbar_wait(&sm.empty[st], (turn - 1) & 1u)) { *failed = 1; break; }
+                    if (turn > 0 && !f8_wait(&sm.empty[st], (turn - 1) & 1u)) { *failed = 1; break; }
                     unsigned char* to = ring + st * kStageBytes;
                     mbar_arrive_expect_tx(&sm.full[st], kPlane16 + kParts * (both ? kPlane16 : kAtom));
                     bulk_copy_g2s(to, x + (uint64_t)c * kPlane16, kPlane16, &sm.full[st]);
@@ -298,7 +298,7 @@ __global__ void __launch_bounds__(kF8Threads, 1) f8_weight_kernel(const __grid_c
             // copies in flight end before the block does, whoever else has given up
             for (uint32_t i = 0; i < kStages; ++i) {
                 const uint32_t begun = turn + (i < st ? 1u : 0u);
-                if (begun > 0) mbar_wait(&sm.full[i], (begun - 1) & 1u);
+                if (begun > 0) f8_wait(&sm.full[i], (begun - 1) & 1u);
             }
         } else if (warp == 1 && lane == 0 && rank == 1) {
             // tells the first block what has arrived here
@@ -307,7 +307,7 @@ __global__ void __launch_bounds__(kF8Threads, 1) f8_weight_kernel(const __grid_c
             for (uint32_t t = first; t < tiles && ok; t += step) {
                 const Place p = find_place(a, t);
                 for (uint32_t c = p.c0; c < p.c1; ++c) {
-                    if (!mbar_wait(&sm.full[st], turn & 1u)) { ok = false; break; }
+                    if (!f8_wait(&sm.full[st], turn & 1u)) { ok = false; break; }
                     mbar_arrive_at(&sm.peer[st], 0);
                     if (++st == kStages) { st = 0; ++turn; }
                 }
@@ -321,8 +321,8 @@ __global__ void __launch_bounds__(kF8Threads, 1) f8_weight_kernel(const __grid_c
                 const uint32_t instr = weight_instr(0) | ((tile_cols(a, p.n0) / 8u) << 17);
                 for (uint32_t c = p.c0; c < p.c1; ++c) {
                     const uint32_t in_sum = (c - p.c0) % kSumChunks;
-                    if (in_sum == 0 && sum_turn > 0 && !mbar_wait_cluster(&sm.sum_empty[sum], (sum_turn - 1) & 1u)) { ok = false; break; }
-                    if (!mbar_wait(&sm.full[st], turn & 1u) || !mbar_wait_cluster(&sm.peer[st], turn & 1u)) { ok = false; break; }
+                    if (in_sum == 0 && sum_turn > 0 && !f8_wait(&sm.sum_empty[sum], (sum_turn - 1) & 1u)) { ok = false; break; }
+                    if (!f8_wait(&sm.full[st], turn & 1u) || !f8_wait(&sm.peer[st], turn & 1u)) { ok = false; break; }
                     tc_fence_after();
                     const uint32_t d = tmem + sum * kOuts, at = smem_addr(ring + st * kStageBytes);
                     const uint64_t dx = smem_desc(at, true, kAtom);
@@ -343,7 +343,7 @@ __global__ void __launch_bounds__(kF8Threads, 1) f8_weight_kernel(const __grid_c
             }
             if (!ok) *failed = 1;
             tc_commit_first(&sm.done);
-            mbar_wait(&sm.done, 0);
+            f8_wait(&sm.done, 0);
         }
     } else {
         many_registers();
@@ -355,7 +355,7 @@ __global__ void __launch_bounds__(kF8Threads, 1) f8_weight_kernel(const __grid_c
             const uint32_t o0 = p.n0 + half * (kOuts / 2);
             float acc[kOuts / 2];
             for (uint32_t c = p.c0; c < p.c1; c += kSumChunks) {
-                ok = lane != 0 || mbar_wait(&sm.sum_full[sum], sum_turn & 1u);
+                ok = lane != 0 || f8_wait(&sm.sum_full[sum], sum_turn & 1u);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 tc_fence_after();
