@@ -125,6 +125,13 @@ __device__ __forceinline__ void mbar_arrive_at(uint64_t* bar, uint32_t rank) {
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_addr(bar)), "r"(rank));
     asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(at) : "memory");
 }
+// One lane of a converged warp.  The warps that issue copies and products run their loops with all lanes and let this one issue:
+// addresses and descriptors then stay in the warp's uniform registers.
+__device__ __forceinline__ bool elected() {
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
+}
 // mbar_wait with the clock looked at less often, here too for at most half a second or so.  What is already there is found by the
 // first try: 50 cycles, against 240 through the loop, of which a stage has two while its products take 512.
 __device__ __forceinline__ bool f8_wait(uint64_t* bar, uint32_t parity) {

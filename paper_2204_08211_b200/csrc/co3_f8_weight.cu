@@ -272,7 +272,8 @@ __global__ void __launch_bounds__(kF8Threads, 1) f8_weight_kernel(const __grid_c
 
     if (warp < 4) {
         few_registers();
-        if (warp == 0 && lane == 0) {
+        const bool issues = elected();
+        if (warp == 0) {
             uint32_t st = 0, turn = 0;
             for (uint32_t t = first; t < tiles && !*failed; t += step) {
                 const Place p = find_place(a, t);
@@ -283,14 +284,16 @@ __global__ void __launch_bounds__(kF8Threads, 1) f8_weight_kernel(const __grid_c
                 const unsigned char* dy = a.ws_dy + ((uint64_t)p.u * a.groups + g) * a.chunks * (kParts * kPlane16);
                 for (uint32_t c = p.c0; c < p.c1; ++c) {
                     if (turn > 0 && !f8_wait(&sm.empty[st], (turn - 1) & 1u)) { *failed = 1; break; }
-                    unsigned char* to = ring + st * kStageBytes;
-                    mbar_arrive_expect_tx(&sm.full[st], kPlane16 + kParts * (both ? kPlane16 : kAtom));
-                    bulk_copy_g2s(to, x + (uint64_t)c * kPlane16, kPlane16, &sm.full[st]);
-                    const unsigned char* from = dy + (uint64_t)c * (kParts * kPlane16);
-                    if (both) {
-                        bulk_copy_g2s(to + kPlane16, from, kParts * kPlane16, &sm.full[st]);
-                    } else {
-                        for (uint32_t m = 0; m < kParts; ++m) bulk_copy_g2s(to + kPlane16 * (1 + m), from + m * kPlane16 + rank * kAtom, kAtom, &sm.full[st]);
+                    if (issues) {
+                        unsigned char* to = ring + st * kStageBytes;
+                        mbar_arrive_expect_tx(&sm.full[st], kPlane16 + kParts * (both ? kPlane16 : kAtom));
+                        bulk_copy_g2s(to, x + (uint64_t)c * kPlane16, kPlane16, &sm.full[st]);
+                        const unsigned char* from = dy + (uint64_t)c * (kParts * kPlane16);
+                        if (both) {
+                            bulk_copy_g2s(to + kPlane16, from, kParts * kPlane16, &sm.full[st]);
+                        } else {
+                            for (uint32_t m = 0; m < kParts; ++m) bulk_copy_g2s(to + kPlane16 * (1 + m), from + m * kPlane16 + rank * kAtom, kAtom, &sm.full[st]);
+                        }
                     }
                     if (++st == kStages) { st = 0; ++turn; }
                 }
@@ -300,7 +303,7 @@ __global__ void __launch_bounds__(kF8Threads, 1) f8_weight_kernel(const __grid_c
                 const uint32_t begun = turn + (i < st ? 1u : 0u);
                 if (begun > 0) f8_wait(&sm.full[i], (begun - 1) & 1u);
             }
-        } else if (warp == 1 && lane == 0 && rank == 1) {
+        } else if (warp == 1 && rank == 1) {
             // tells the first block what has arrived here
             uint32_t st = 0, turn = 0;
             bool ok = true;
@@ -308,12 +311,12 @@ __global__ void __launch_bounds__(kF8Threads, 1) f8_weight_kernel(const __grid_c
                 const Place p = find_place(a, t);
                 for (uint32_t c = p.c0; c < p.c1; ++c) {
                     if (!f8_wait(&sm.full[st], turn & 1u)) { ok = false; break; }
-                    mbar_arrive_at(&sm.peer[st], 0);
+                    if (issues) mbar_arrive_at(&sm.peer[st], 0);
                     if (++st == kStages) { st = 0; ++turn; }
                 }
             }
             if (!ok) *failed = 1;
-        } else if (warp == 1 && lane == 0) {
+        } else if (warp == 1) {
             uint32_t st = 0, turn = 0, sum = 0, sum_turn = 0;
             bool ok = true;
             for (uint32_t t = first; t < tiles && ok; t += step) {
@@ -324,25 +327,26 @@ __global__ void __launch_bounds__(kF8Threads, 1) f8_weight_kernel(const __grid_c
                     if (in_sum == 0 && sum_turn > 0 && !f8_wait(&sm.sum_empty[sum], (sum_turn - 1) & 1u)) { ok = false; break; }
                     if (!f8_wait(&sm.full[st], turn & 1u) || !f8_wait(&sm.peer[st], turn & 1u)) { ok = false; break; }
                     tc_fence_after();
-                    const uint32_t d = tmem + sum * kOuts, at = smem_addr(ring + st * kStageBytes);
-                    const uint64_t dx = smem_desc(at, true, kAtom);
+                    const bool last = in_sum == kSumChunks - 1 || c + 1 == p.c1;
+                    if (issues) {
+                        const uint32_t d = tmem + sum * kOuts, at = smem_addr(ring + st * kStageBytes);
+                        const uint64_t dx = smem_desc(at, true, kAtom);
 #pragma unroll
-                    for (int m = kParts - 1; m >= 0; --m) {
-                        const uint64_t dd = smem_desc(at + kPlane16 * (1 + m), true, kAtom);
+                        for (int m = kParts - 1; m >= 0; --m) {
+                            const uint64_t dd = smem_desc(at + kPlane16 * (1 + m), true, kAtom);
 #pragma unroll
-                        for (uint32_t e = 0; e < kChunk / 16u; ++e)
-                            pair_mma(d, dx + e * desc_step(true), dd + e * desc_step(true), instr, in_sum > 0 || m < kParts - 1 || e > 0);
+                            for (uint32_t e = 0; e < kChunk / 16u; ++e)
+                                pair_mma(d, dx + e * desc_step(true), dd + e * desc_step(true), instr, in_sum > 0 || m < kParts - 1 || e > 0);
+                        }
+                        tc_commit_pair(&sm.empty[st]);
+                        if (last) tc_commit_pair(&sm.sum_full[sum]);
                     }
-                    tc_commit_pair(&sm.empty[st]);
-                    if (in_sum == kSumChunks - 1 || c + 1 == p.c1) {
-                        tc_commit_pair(&sm.sum_full[sum]);
-                        if (++sum == 2) { sum = 0; ++sum_turn; }
-                    }
+                    if (last && ++sum == 2) { sum = 0; ++sum_turn; }
                     if (++st == kStages) { st = 0; ++turn; }
                 }
             }
             if (!ok) *failed = 1;
-            tc_commit_first(&sm.done);
+            if (issues) tc_commit_first(&sm.done);
             f8_wait(&sm.done, 0);
         }
     } else {
