@@ -103,6 +103,29 @@ static_assert(kFewRegs + 2 * kManyRegs == 3 * 168, "registers of the block");
 __device__ __forceinline__ void few_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFewRegs)); }
 __device__ __forceinline__ void many_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kManyRegs)); }
 
+// kCount columns (a multiple of 32) of this warp's 32 lanes, all loads under way at once.  (Volatile statements keep their order, so
+// that no sum is used before the wait.)
+template <int kCount>
+__device__ __forceinline__ void tc_load(uint32_t addr, float (&v)[kCount]) {
+    static_assert(kCount % 32 == 0, "whole loads");
+    uint32_t* r = reinterpret_cast<uint32_t*>(v);
+#pragma unroll
+    for (int h = 0; h < kCount; h += 32)
+        asm volatile(
+            "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+            "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+            "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+            : "=r"(r[h + 0]), "=r"(r[h + 1]), "=r"(r[h + 2]), "=r"(r[h + 3]), "=r"(r[h + 4]), "=r"(r[h + 5]), "=r"(r[h + 6]), "=r"(r[h + 7]), "=r"(r[h + 8]),
+              "=r"(r[h + 9]), "=r"(r[h + 10]), "=r"(r[h + 11]), "=r"(r[h + 12]), "=r"(r[h + 13]), "=r"(r[h + 14]), "=r"(r[h + 15]), "=r"(r[h + 16]), "=r"(r[h + 17]),
+              "=r"(r[h + 18]), "=r"(r[h + 19]), "=r"(r[h + 20]), "=r"(r[h + 21]), "=r"(r[h + 22]), "=r"(r[h + 23]), "=r"(r[h + 24]), "=r"(r[h + 25]), "=r"(r[h + 26]),
+              "=r"(r[h + 27]), "=r"(r[h + 28]), "=r"(r[h + 29]), "=r"(r[h + 30]), "=r"(r[h + 31])
+            : "r"(addr + h)
+            : "memory");
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < kCount; ++i) asm volatile("" : "+r"(r[i]));
+}
+
 // ------------------------------------------------------------------------------------------------
 // Pairs of blocks (a cluster of two) that multiply together: each holds 128 rows of the first operand and half of the second,
 // and gets the sums of its own 128 rows.  The pair's first block issues the products for both, which halves what each of

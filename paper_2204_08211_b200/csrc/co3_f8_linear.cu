@@ -44,13 +44,12 @@ struct LinearArgs {
     co3_result* res;
 };
 
+constexpr uint32_t kScaleBytes = 2 * kF8Scales;  // of a stage: first operand's, then the second's
 template <int kN>
 struct Shape {
-    static constexpr uint32_t kStages = kN == 256 ? 4 : kN == 128 ? 6 : 8;
+    static constexpr uint32_t kStages = kN == 128 ? 6 : 8;
     static constexpr uint32_t kStageBytes = kF8Tile + kN * 128;
-    static constexpr uint32_t kScaleBytes = kF8Scales * (kN == 256 ? 3 : 2);       // first operand's, then the second's
     static constexpr uint32_t kRing = kStages * kStageBytes;
-    static constexpr uint32_t kSums = kN == 256 ? 1 : 2;                           // tiles that tensor memory holds
     static constexpr uint32_t kSmem = 1024 + kRing + kStages * kScaleBytes + 256;
     static_assert(kN * 128 * 4 <= kRing, "a tile's sums fit the ring");
 };
@@ -92,19 +91,31 @@ __device__ __forceinline__ void multiply_block(uint32_t d, uint32_t a, uint32_t 
     for (uint32_t e = 0; e < 4; ++e) f8_mma(d, da + e * f8_step(kTransposed), db + e * f8_step(false), instr, sa, sb, accumulate || e > 0);
 }
 
-template <int kCount>
-__device__ __forceinline__ void tc_load(uint32_t addr, float* v) {
-    if constexpr (kCount == 8) {
-        uint32_t r[8];
-        asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];\n\ttcgen05.wait::ld.sync.aligned;"
-                     : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
-                     : "r"(addr)
-                     : "memory");
+__device__ __forceinline__ void tc_load8(uint32_t addr, float (&v)[8]) {
+    uint32_t r[8];
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];\n\ttcgen05.wait::ld.sync.aligned;"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                 : "r"(addr)
+                 : "memory");
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r[i]);
+    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r[i]);
+}
+// Adds a half tile's columns to acc, or (first) puts them there.
+template <int kHalf>
+__device__ __forceinline__ void take_sums(uint32_t from, bool first, float (&acc)[kHalf]) {
+    constexpr int kLoad = kHalf < 32 ? kHalf : 32;
+    if (first) {
+        if constexpr (kHalf == 8) tc_load8(from, acc);
+        else tc_load(from, acc);
     } else {
-        static_assert(kCount == 32, "8 or 32 columns");
-        tc_load32(addr, *reinterpret_cast<float(*)[32]>(v));
+#pragma unroll
+        for (int h = 0; h < kHalf; h += kLoad) {
+            float w[kLoad];
+            if constexpr (kHalf == 8) tc_load8(from + h, w);
+            else tc_load(from + h, w);
+#pragma unroll
+            for (int i = 0; i < kLoad; ++i) acc[h + i] = __fadd_rn(acc[h + i], w[i]);
+        }
     }
 }
 
@@ -139,7 +150,7 @@ __global__ void __launch_bounds__(kF8Threads, 1) f8_linear_kernel(const __grid_c
     constexpr uint32_t kStages = S::kStages;
     unsigned char* ring = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
     unsigned char* scales = ring + S::kRing;
-    LinearSmem<kN>& sm = *reinterpret_cast<LinearSmem<kN>*>(scales + kStages * S::kScaleBytes);
+    LinearSmem<kN>& sm = *reinterpret_cast<LinearSmem<kN>*>(scales + kStages * kScaleBytes);
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
     if (threadIdx.x == 0) {
         for (uint32_t i = 0; i < kStages; ++i) { mbar_init(&sm.full[i], 1); mbar_init(&sm.empty[i], 1); }
@@ -165,23 +176,25 @@ __global__ void __launch_bounds__(kF8Threads, 1) f8_linear_kernel(const __grid_c
     const uint32_t k0 = kSplit ? (uint32_t)((uint64_t)a.kb * part / a.split) : 0u, k1 = kSplit ? (uint32_t)((uint64_t)a.kb * (part + 1) / a.split) : a.kb;
 
     if (warp < 4) few_registers();
-    if (warp == 0 && lane == 0) {
+    const bool issues = warp < 2 && elected();
+    if (warp == 0) {
         uint32_t st = 0, turn = 0;
         for (uint32_t t = first; t < tiles && !*failed; t += step) {
             const uint32_t mt = t % a.m_tiles, nt = t / a.m_tiles, n0 = nt * kN;
             const uint32_t n = min((uint32_t)kN, (a.rows - n0 + 15u) & ~15u);
             for (uint32_t q = k0; q < k1; ++q) {
                 if (turn > 0 && !f8_wait(&sm.empty[st], (turn - 1) & 1u)) { *failed = 1; break; }
-                unsigned char* to = ring + st * S::kStageBytes;
-                const bool with_scales = q == k0 || (q & 3u) == 0;
-                const uint32_t b_scales = n > 128 ? 2 * kF8Scales : kF8Scales;
-                mbar_arrive_expect_tx(&sm.full[st], kF8Tile + n * 128u + (with_scales ? kF8Scales + b_scales : 0u));
-                bulk_copy_g2s(to, a.a + q * a.a_block + mt * a.a_tile, kF8Tile, &sm.full[st]);
-                bulk_copy_g2s(to + kF8Tile, a.b + q * a.b_block + (uint64_t)n0 * 128u, n * 128u, &sm.full[st]);
-                if (with_scales) {
-                    unsigned char* s = scales + st * S::kScaleBytes;
-                    bulk_copy_g2s(s, a.a_scales + (q >> 2) * a.a_group + (uint64_t)mt * kF8Scales, kF8Scales, &sm.full[st]);
-                    bulk_copy_g2s(s + kF8Scales, a.b_scales + (q >> 2) * a.b_group + (uint64_t)(n0 >> 7) * kF8Scales, b_scales, &sm.full[st]);
+                if (issues) {
+                    unsigned char* to = ring + st * S::kStageBytes;
+                    const bool with_scales = q == k0 || (q & 3u) == 0;
+                    mbar_arrive_expect_tx(&sm.full[st], kF8Tile + n * 128u + (with_scales ? 2 * kF8Scales : 0u));
+                    bulk_copy_g2s(to, a.a + q * a.a_block + mt * a.a_tile, kF8Tile, &sm.full[st]);
+                    bulk_copy_g2s(to + kF8Tile, a.b + q * a.b_block + (uint64_t)n0 * 128u, n * 128u, &sm.full[st]);
+                    if (with_scales) {
+                        unsigned char* s = scales + st * kScaleBytes;
+                        bulk_copy_g2s(s, a.a_scales + (q >> 2) * a.a_group + (uint64_t)mt * kF8Scales, kF8Scales, &sm.full[st]);
+                        bulk_copy_g2s(s + kF8Scales, a.b_scales + (q >> 2) * a.b_group + (uint64_t)(n0 >> 7) * kF8Scales, kF8Scales, &sm.full[st]);
+                    }
                 }
                 if (++st == kStages) { st = 0; ++turn; }
             }
@@ -191,7 +204,7 @@ __global__ void __launch_bounds__(kF8Threads, 1) f8_linear_kernel(const __grid_c
             const uint32_t begun = turn + (i < st ? 1u : 0u);
             if (begun > 0) f8_wait(&sm.full[i], (begun - 1) & 1u);
         }
-    } else if (warp == 1 && lane == 0) {
+    } else if (warp == 1) {
         uint32_t st = 0, turn = 0, sum = 0, sum_turn = 0, group = 0;
         bool ok = true;
         for (uint32_t t = first; t < tiles && ok && !*failed; t += step) {
@@ -204,41 +217,39 @@ __global__ void __launch_bounds__(kF8Threads, 1) f8_linear_kernel(const __grid_c
                     if (sum_turn > 0 && !f8_wait(&sm.sum_empty[sum], (sum_turn - 1) & 1u)) { ok = false; break; }
                 }
                 --left;
-                const uint32_t d = tmem + sum * kN;
                 if (!f8_wait(&sm.full[st], turn & 1u)) { ok = false; break; }
                 tc_fence_after();
-                if (q == k0 || (q & 3u) == 0) {
-                    // the columns of eight groups ago are free: fewer than kStages <= 8 blocks are under way
-                    group = group + 1 == kScaleTurns ? 0 : group + 1;
-                    const uint32_t to = tmem + kTmemScales + group * kScaleCols, from = smem_addr(scales + st * S::kScaleBytes);
-                    f8_scales_in(to, from);
-                    f8_scales_in(to + 4, from + kF8Scales);
-                    if (kN == 256) f8_scales_in(to + 8, from + 2 * kF8Scales);
+                const bool with_scales = q == k0 || (q & 3u) == 0;
+                // the columns of eight groups ago are free: fewer than kStages <= 8 blocks are under way
+                if (with_scales) group = (group + 1) % kScaleTurns;
+                if (issues) {
+                    const uint32_t d = tmem + sum * kN, sa = tmem + kTmemScales + group * kScaleCols;
+                    if (with_scales) {
+                        const uint32_t from = smem_addr(scales + st * kScaleBytes);
+                        f8_scales_in(sa, from);
+                        f8_scales_in(sa + 4, from + kF8Scales);
+                    }
+                    const uint32_t sb = sa + 4 + ((n0 & 127u) >> 5), at = smem_addr(ring + st * S::kStageBytes), bt = at + kF8Tile;
+                    switch (q & 3u) {
+                        case 0: multiply_block<kTransposed, 0>(d, at, bt, n, sa, sb, !fresh); break;
+                        case 1: multiply_block<kTransposed, 1>(d, at, bt, n, sa, sb, !fresh); break;
+                        case 2: multiply_block<kTransposed, 2>(d, at, bt, n, sa, sb, !fresh); break;
+                        default: multiply_block<kTransposed, 3>(d, at, bt, n, sa, sb, !fresh); break;
+                    }
+                    tc_commit(&sm.empty[st]);
+                    if (left == 0) tc_commit(&sm.sum_full[sum]);
                 }
-                const uint32_t sa = tmem + kTmemScales + group * kScaleCols, sb = sa + 4 + ((n0 & 127u) >> 5);
-                const uint32_t at = smem_addr(ring + st * S::kStageBytes), bt = at + kF8Tile;
-                switch (q & 3u) {
-                    case 0: multiply_block<kTransposed, 0>(d, at, bt, n, sa, sb, !fresh); break;
-                    case 1: multiply_block<kTransposed, 1>(d, at, bt, n, sa, sb, !fresh); break;
-                    case 2: multiply_block<kTransposed, 2>(d, at, bt, n, sa, sb, !fresh); break;
-                    default: multiply_block<kTransposed, 3>(d, at, bt, n, sa, sb, !fresh); break;
-                }
-                tc_commit(&sm.empty[st]);
-                if (left == 0) {
-                    tc_commit(&sm.sum_full[sum]);
-                    if (++sum == S::kSums) { sum = 0; ++sum_turn; }
-                }
+                if (left == 0 && ++sum == 2) { sum = 0; ++sum_turn; }
                 if (++st == kStages) { st = 0; ++turn; }
             }
         }
         if (!ok) *failed = 1;
-        tc_commit(&sm.done);
+        if (issues) tc_commit(&sm.done);
         f8_wait(&sm.done, 0);
     } else if (warp >= 4) {
         many_registers();
-        // columns of a tile by halves; 16 columns are one warp's of each 32 lanes
-        constexpr int kHalf = kN / 2, kLoad = kHalf < 32 ? 8 : 32;
-        static_assert(kHalf % kLoad == 0, "halves are whole loads");
+        // lanes of a tile by quarters, columns by halves
+        constexpr int kHalf = kN / 2;
         const uint32_t quad = warp & 3u, half = (warp - 4u) >> 2, row = quad * 32u + lane;
         uint32_t sum = 0, sum_turn = 0;
         for (uint32_t t = first; t < tiles; t += step) {
@@ -251,22 +262,11 @@ __global__ void __launch_bounds__(kF8Threads, 1) f8_linear_kernel(const __grid_c
                 if (!ok) break;
                 tc_fence_after();
                 const uint32_t from = tmem + ((quad * 32u) << 16) + sum * kN + half * kHalf;
-                if (q == k0) {
-#pragma unroll
-                    for (int h = 0; h < kHalf; h += kLoad) tc_load<kLoad>(from + h, acc + h);
-                } else {
-#pragma unroll
-                    for (int h = 0; h < kHalf; h += kLoad) {
-                        float w[kLoad];
-                        tc_load<kLoad>(from + h, w);
-#pragma unroll
-                        for (int i = 0; i < kLoad; ++i) acc[h + i] = __fadd_rn(acc[h + i], w[i]);
-                    }
-                }
+                take_sums(from, q == k0, acc);
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&sm.sum_empty[sum]);
-                if (++sum == S::kSums) { sum = 0; ++sum_turn; }
+                if (++sum == 2u) { sum = 0; ++sum_turn; }
             }
             if (!ok) { *failed = 1; break; }
             if constexpr (kSplit) {  // into the ring, of which no copy and no product is left
@@ -305,6 +305,185 @@ __global__ void __launch_bounds__(kF8Threads, 1) f8_linear_kernel(const __grid_c
     if (threadIdx.x == 0 && *failed && a.res) atomicExch(&a.res->status, CO3_ERR_CUDA);
 }
 
+// ------------------------------------------------------------------------------------------------
+// Tiles of 256 features by 256 rows of x, by pairs of blocks.
+// ------------------------------------------------------------------------------------------------
+constexpr uint32_t kPairCols = 256, kPairStages = 6;
+constexpr uint32_t kPairStageBytes = 2 * kF8Tile, kPairScaleBytes = 3 * kF8Scales;  // the second operand's scales for all 256 rows
+constexpr uint32_t kPairSmem = 1024 + kPairStages * (kPairStageBytes + kPairScaleBytes) + 256;
+
+struct PairSmem {
+    uint64_t full[kPairStages], peer[kPairStages], empty[kPairStages], sum_full, sum_empty, done;
+    uint32_t tmem, failed;
+};
+static_assert(sizeof(PairSmem) <= 256, "barriers");
+
+__device__ __forceinline__ void pair_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t instr, uint32_t sa, uint32_t sb, bool accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(instr), "r"(sa),
+        "r"(sb), "r"((uint32_t)accumulate)
+        : "memory");
+}
+// In each of the two blocks, from its own shared memory.
+__device__ __forceinline__ void pair_scales_in(uint32_t to, uint32_t from) {
+    const uint64_t desc = (uint64_t)((from >> 4) & 0x3fffu) | (8ull << 32) | (1ull << 46);
+    asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(to), "l"(desc) : "memory");
+}
+template <bool kTransposed, uint32_t kBlock4>
+__device__ __forceinline__ void multiply_block_pair(uint32_t d, uint32_t a, uint32_t b, uint32_t cols, uint32_t sa, uint32_t sb, bool accumulate) {
+    const uint64_t da = f8_desc(a), db = f8_desc(b);
+    const uint32_t instr = (f8_instr(kTransposed, 0, kBlock4) + (1u << 27)) | ((cols / 8u) << 17);  // 256 rows of A
+#pragma unroll
+    for (uint32_t e = 0; e < 4; ++e) pair_mma(d, da + e * f8_step(kTransposed), db + e * f8_step(false), instr, sa, sb, accumulate || e > 0);
+}
+
+template <bool kTransposed>
+__global__ void __launch_bounds__(kF8Threads, 1) f8_pair_kernel(const __grid_constant__ LinearArgs a) {
+    extern __shared__ unsigned char smem_raw[];
+    unsigned char* ring = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
+    unsigned char* scales = ring + kPairStages * kPairStageBytes;
+    PairSmem& sm = *reinterpret_cast<PairSmem*>(scales + kPairStages * kPairScaleBytes);
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u, rank = cluster_rank();
+    if (threadIdx.x == 0) {
+        for (uint32_t i = 0; i < kPairStages; ++i) { mbar_init(&sm.full[i], 1); mbar_init(&sm.peer[i], 1); mbar_init(&sm.empty[i], 1); }
+        mbar_init(&sm.sum_full, 1);
+        mbar_init(&sm.sum_empty, 16);
+        mbar_init(&sm.done, 1);
+        sm.failed = 0;
+    }
+    if (warp == 1) tmem_alloc_pair(&sm.tmem);
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync();
+    tc_fence_after();
+    const uint32_t tmem = sm.tmem;
+    volatile uint32_t* failed = &sm.failed;
+    wait_for_previous_kernel();
+    const uint32_t m_pairs = (a.m_tiles + 1) / 2, tiles = m_pairs * a.n_tiles, first = blockIdx.x >> 1, step = gridDim.x >> 1;
+
+    if (warp < 4) {
+        few_registers();
+        const bool issues = elected();
+        if (warp == 0) {
+            uint32_t st = 0, turn = 0;
+            for (uint32_t t = first; t < tiles && !*failed; t += step) {
+                const uint32_t mt = min(2 * (t % m_pairs) + rank, a.m_tiles - 1);  // (an odd last tile: the second block's sums go nowhere)
+                const uint32_t n0 = t / m_pairs * kPairCols, n = min(kPairCols, (a.rows - n0 + 15u) & ~15u);
+                const uint32_t b_scales = n > 128 ? 2 * kF8Scales : kF8Scales, half = n / 2;
+                const uint8_t *from_a = a.a + mt * a.a_tile, *from_b = a.b + (n0 + rank * half) * 128ull;
+                for (uint32_t q = 0; q < a.kb; ++q) {
+                    if (turn > 0 && !f8_wait(&sm.empty[st], (turn - 1) & 1u)) { *failed = 1; break; }
+                    if (issues) {
+                        unsigned char* to = ring + st * kPairStageBytes;
+                        const bool with_scales = (q & 3u) == 0;
+                        mbar_arrive_expect_tx(&sm.full[st], kF8Tile + half * 128u + (with_scales ? kF8Scales + b_scales : 0u));
+                        bulk_copy_g2s(to, from_a + q * a.a_block, kF8Tile, &sm.full[st]);
+                        bulk_copy_g2s(to + kF8Tile, from_b + q * a.b_block, half * 128u, &sm.full[st]);
+                        if (with_scales) {
+                            unsigned char* s = scales + st * kPairScaleBytes;
+                            bulk_copy_g2s(s, a.a_scales + (q >> 2) * a.a_group + (uint64_t)mt * kF8Scales, kF8Scales, &sm.full[st]);
+                            bulk_copy_g2s(s + kF8Scales, a.b_scales + (q >> 2) * a.b_group + (uint64_t)(n0 >> 7) * kF8Scales, b_scales, &sm.full[st]);
+                        }
+                    }
+                    if (++st == kPairStages) { st = 0; ++turn; }
+                }
+            }
+            // copies in flight end before the block does, whoever else has given up
+            for (uint32_t i = 0; i < kPairStages; ++i) {
+                const uint32_t begun = turn + (i < st ? 1u : 0u);
+                if (begun > 0) f8_wait(&sm.full[i], (begun - 1) & 1u);
+            }
+        } else if (warp == 1 && rank == 1) {
+            // tells the first block what has arrived here
+            uint32_t st = 0, turn = 0;
+            bool ok = true;
+            for (uint32_t t = first; t < tiles && ok; t += step)
+                for (uint32_t q = 0; q < a.kb; ++q) {
+                    if (!f8_wait(&sm.full[st], turn & 1u)) { ok = false; break; }
+                    if (issues) mbar_arrive_at(&sm.peer[st], 0);
+                    if (++st == kPairStages) { st = 0; ++turn; }
+                }
+            if (!ok) *failed = 1;
+        } else if (warp == 1) {
+            uint32_t st = 0, turn = 0, sums = 0, group = 0;  // sums: begun
+            bool ok = true;
+            for (uint32_t t = first; t < tiles && ok; t += step) {
+                const uint32_t n = min(kPairCols, (a.rows - t / m_pairs * kPairCols + 15u) & ~15u);
+                uint32_t left = 0;  // blocks that the present sum still takes
+                for (uint32_t q = 0; q < a.kb; ++q) {
+                    const bool fresh = left == 0;
+                    if (fresh) {
+                        left = min(a.blocks, a.kb - q);
+                        if (sums > 0 && !f8_wait(&sm.sum_empty, (sums - 1) & 1u)) { ok = false; break; }
+                        ++sums;
+                    }
+                    --left;
+                    if (!f8_wait(&sm.full[st], turn & 1u) || !f8_wait(&sm.peer[st], turn & 1u)) { ok = false; break; }
+                    tc_fence_after();
+                    // the columns of eight groups ago are free: fewer than kPairStages blocks are under way
+                    if ((q & 3u) == 0) group = (group + 1) % kScaleTurns;
+                    if (issues) {
+                        const uint32_t sa = tmem + kTmemScales + group * kScaleCols, sb = sa + 4;
+                        if ((q & 3u) == 0) {
+                            const uint32_t from = smem_addr(scales + st * kPairScaleBytes);
+                            pair_scales_in(sa, from);
+                            pair_scales_in(sb, from + kF8Scales);
+                            if (n > 128) pair_scales_in(sb + 4, from + 2 * kF8Scales);
+                        }
+                        const uint32_t at = smem_addr(ring + st * kPairStageBytes), bt = at + kF8Tile;
+                        switch (q & 3u) {
+                            case 0: multiply_block_pair<kTransposed, 0>(tmem, at, bt, n, sa, sb, !fresh); break;
+                            case 1: multiply_block_pair<kTransposed, 1>(tmem, at, bt, n, sa, sb, !fresh); break;
+                            case 2: multiply_block_pair<kTransposed, 2>(tmem, at, bt, n, sa, sb, !fresh); break;
+                            default: multiply_block_pair<kTransposed, 3>(tmem, at, bt, n, sa, sb, !fresh); break;
+                        }
+                        tc_commit_pair(&sm.empty[st]);
+                        if (left == 0) tc_commit_pair(&sm.sum_full);
+                    }
+                    if (++st == kPairStages) { st = 0; ++turn; }
+                }
+            }
+            if (!ok) *failed = 1;
+            if (issues) tc_commit_first(&sm.done);
+            f8_wait(&sm.done, 0);
+        }
+    } else {
+        many_registers();
+        constexpr int kHalf = kPairCols / 2;
+        const uint32_t quad = warp & 3u, half = (warp - 4u) >> 2, row = quad * 32u + lane;
+        uint32_t sums = 0;
+        bool ok = true;
+        for (uint32_t t = first; t < tiles && ok; t += step) {
+            const uint32_t n0 = t / m_pairs * kPairCols, feature = (2 * (t % m_pairs) + rank) * 128u + row;
+            float acc[kHalf];
+            for (uint32_t q = 0; q < a.kb; q += a.blocks, ++sums) {
+                ok = lane != 0 || f8_wait(&sm.sum_full, sums & 1u);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                tc_fence_after();
+                take_sums(tmem + ((quad * 32u) << 16) + half * kHalf, q == 0, acc);
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_at(&sm.sum_empty, 0);
+            }
+            if (!ok) break;
+            const float bias = a.bias && feature < a.features ? a.bias[feature] : 0.0f;
+            write_any<kHalf>(a, feature, n0 + half * kHalf, bias, acc);
+        }
+        if (!ok) *failed = 1;
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync();  // the other block's arrivals and products need this one's shared memory
+    tc_fence_after();
+    if (warp == 1) tmem_free_pair(tmem);
+    if (threadIdx.x == 0 && *failed && a.res) atomicExch(&a.res->status, CO3_ERR_CUDA);
+}
+
 int device_sms(uint32_t* out) {
     static std::atomic<int> known[64];
     int dev = 0;
@@ -318,20 +497,18 @@ int device_sms(uint32_t* out) {
     return CO3_OK;
 }
 
-template <int kN, bool kTransposed, bool kSplit>
-int launch_linear(const LinearArgs& a, uint32_t sms, cudaStream_t st) {
-    auto* kernel = f8_linear_kernel<kN, kTransposed, kSplit>;
-    constexpr uint32_t kSmem = Shape<kN>::kSmem;
+// Blocks of a cluster (1: none) work on kernel<smem>.
+template <auto* kKernel, uint32_t kSmem>
+int launch_clusters(const LinearArgs& a, uint32_t blocks, uint32_t cluster, cudaStream_t st) {
     static std::atomic<bool> ready[64];
     int dev = 0;
     CO3_CUDA(cudaGetDevice(&dev));
     if (dev >= 64 || !ready[dev].load(std::memory_order_relaxed)) {
-        CO3_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem));
+        CO3_CUDA(cudaFuncSetAttribute(kKernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem));
         if (dev < 64) ready[dev].store(true, std::memory_order_relaxed);
     }
-    const uint32_t tiles = a.m_tiles * a.n_tiles;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(kSplit ? tiles * a.split : std::min(tiles, sms));
+    cfg.gridDim = dim3(blocks);
     cfg.blockDim = dim3(kF8Threads);
     cfg.dynamicSmemBytes = kSmem;
     cfg.stream = st;
@@ -339,12 +516,25 @@ int launch_linear(const LinearArgs& a, uint32_t sms, cudaStream_t st) {
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = a.split;
+    attr[1].val.clusterDim.x = cluster;
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = kSplit ? 2 : 1;
-    CO3_CUDA(cudaLaunchKernelEx(&cfg, kernel, a));
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    CO3_CUDA(cudaLaunchKernelEx(&cfg, kKernel, a));
     return CO3_OK;
+}
+template <int kN, bool kTransposed>
+int launch_linear(const LinearArgs& a, uint32_t sms, cudaStream_t st) {
+    const uint32_t tiles = a.m_tiles * a.n_tiles;
+    if (a.split > 1) return launch_clusters<f8_linear_kernel<kN, kTransposed, true>, Shape<kN>::kSmem>(a, tiles * a.split, a.split, st);
+    return launch_clusters<f8_linear_kernel<kN, kTransposed, false>, Shape<kN>::kSmem>(a, std::min(tiles, sms), 1, st);
+}
+int launch_pairs(LinearArgs a, bool transposed, uint32_t sms, cudaStream_t st) {
+    a.n_tiles = (a.rows + kPairCols - 1) / kPairCols;
+    const uint64_t tiles = (uint64_t)((a.m_tiles + 1) / 2) * a.n_tiles;
+    if (tiles >= (1ull << 30)) return CO3_ERR_INVALID_ARG;
+    const uint32_t blocks = 2 * (uint32_t)std::min<uint64_t>(tiles, sms / 2);
+    return transposed ? launch_clusters<f8_pair_kernel<true>, kPairSmem>(a, blocks, 2, st) : launch_clusters<f8_pair_kernel<false>, kPairSmem>(a, blocks, 2, st);
 }
 
 template <int kN>
@@ -354,8 +544,7 @@ int launch_tile(LinearArgs a, bool transposed, uint32_t sms, cudaStream_t st) {
     if (tiles >= (1ull << 31) / kMaxSplit) return CO3_ERR_INVALID_ARG;
     a.split = 1;
     while (a.split < kMaxSplit && tiles * a.split * 2 <= sms && a.kb >= a.split * 4) a.split *= 2;
-    if (a.split > 1) return transposed ? launch_linear<kN, true, true>(a, sms, st) : launch_linear<kN, false, true>(a, sms, st);
-    return transposed ? launch_linear<kN, true, false>(a, sms, st) : launch_linear<kN, false, false>(a, sms, st);
+    return transposed ? launch_linear<kN, true>(a, sms, st) : launch_linear<kN, false>(a, sms, st);
 }
 
 }  // namespace
@@ -410,7 +599,7 @@ int co3_f8_linear(const void* x, int x_type, uint64_t x_row_stride, void* x8, si
     if (rows <= 16) return launch_tile<16>(a, transposed != 0, sms, st);
     if (rows <= 64 || (uint64_t)a.m_tiles * ((rows + 127u) / 128u) * 2 <= sms) return launch_tile<64>(a, transposed != 0, sms, st);
     if (rows <= 128 || (uint64_t)a.m_tiles * ((rows + 255u) / 256u) <= sms) return launch_tile<128>(a, transposed != 0, sms, st);
-    return launch_tile<256>(a, transposed != 0, sms, st);
+    return launch_pairs(a, transposed != 0, sms, st);
 }
 
 }  // extern "C"
