@@ -6,6 +6,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "co3_f8.cuh"
 #include "co3_launch.cuh"
@@ -17,45 +18,96 @@ constexpr int kWarps = 8;
 constexpr int kRowsAtOnce = 2;
 enum Way { kWide, kSingle };  // 16 bytes at a time, or one element at a time
 
+// Four fp32 or eight 16-bit values as 16 bytes.
+template <typename T>
+__device__ __forceinline__ uint4 rounded16(const float* v) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (std::is_same<T, float>::value) {
+            w[i] = __float_as_uint(v[i]);
+        } else if constexpr (std::is_same<T, __half>::value) {
+            const __half2 h = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
+            w[i] = *reinterpret_cast<const uint32_t*>(&h);
+        } else {
+            const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+            w[i] = *reinterpret_cast<const uint32_t*>(&h);
+        }
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
 // How a warp's lanes share 512 columns of a row: kChunks loads of kVals values.
 template <typename T, Way kWay>
 struct Lanes {
     static constexpr bool kPairs = kWay == kWide && sizeof(T) == 2;    // 16 lanes a block instead of 32
-    static constexpr int kChunks = kPairs ? 2 : 4, kVals = kPairs ? 8 : 4;
+    static constexpr int kChunks = kPairs ? 2 : 4, kVals = kPairs ? 8 : 4, kBlocks = 4 / kChunks;
     static constexpr uint32_t kChunkCols = 512 / kChunks;
-    // block of this lane's values of chunk h among the four
-    static __device__ __forceinline__ uint32_t block(int h, uint32_t lane) { return kPairs ? 2 * h + (lane >> 4) : h; }
-    // first column of its values, and how far apart they are
-    static __device__ __forceinline__ uint32_t column(int h, uint32_t lane) { return h * kChunkCols + (kWay == kSingle ? lane : lane * kVals); }
+    struct Single { T v[4]; };
+    using Raw = typename std::conditional<kWay == kWide, uint4, Single>::type;
+    // block of this lane's values of the first chunk among the four (kBlocks further for each chunk)
+    static __device__ __forceinline__ uint32_t block0(uint32_t lane) { return kPairs ? lane >> 4 : 0u; }
+    // first column of its values; they are neighbours, or 32 columns apart
+    static __device__ __forceinline__ uint32_t column0(uint32_t lane) { return kWay == kSingle ? lane : lane * kVals; }
 
-    // p: element at column(h, lane) of the row; `left`: columns from there to the row's end (none if <= 0)
-    static __device__ __forceinline__ void load(const T* p, int64_t left, float (&v)[kVals]) {
+    // p: element at column0 of the chunk; `left`: columns from there to the row's end (none if <= 0)
+    static __device__ __forceinline__ Raw load(const T* p, int32_t left) {
+        Raw raw;
         if constexpr (kWay == kWide) {
-            uint4 raw = make_uint4(0, 0, 0, 0);
+            raw = make_uint4(0, 0, 0, 0);
             if (left > 0) raw = __ldcs(reinterpret_cast<const uint4*>(p));
-            const T* e = reinterpret_cast<const T*>(&raw);
-#pragma unroll
-            for (int i = 0; i < kVals; ++i) v[i] = to_float(e[i]);
         } else {
 #pragma unroll
-            for (int i = 0; i < kVals; ++i) v[i] = (int64_t)(i * 32) < left ? to_float(p[i * 32]) : 0.0f;
+            for (int i = 0; i < kVals; ++i) raw.v[i] = i * 32 < left ? p[i * 32] : from_float<T>(0.0f);
+        }
+        return raw;
+    }
+    static __device__ __forceinline__ float value(const Raw& raw, int i) {
+        if constexpr (kWay == kSingle) {
+            return to_float(raw.v[i]);
+        } else {
+            const uint32_t w = (&raw.x)[i * sizeof(T) / 4];
+            if constexpr (sizeof(T) == 4) return __uint_as_float(w);
+            else if constexpr (std::is_same<T, __nv_bfloat16>::value) return __uint_as_float(i & 1 ? w & 0xffff0000u : w << 16);
+            else return __half2float(__ushort_as_half((unsigned short)(i & 1 ? w >> 16 : w & 0xffffu)));
         }
     }
-    static __device__ __forceinline__ void store(T* p, int64_t left, const float (&v)[kVals]) {
+    static __device__ __forceinline__ void store(T* p, int32_t left, const float (&v)[kVals]) {
         if constexpr (kWay == kWide) {
-            uint4 raw;
-            T* e = reinterpret_cast<T*>(&raw);
-#pragma unroll
-            for (int i = 0; i < kVals; ++i) e[i] = from_float<T>(v[i]);
-            if (left > 0) *reinterpret_cast<uint4*>(p) = raw;
+            if (left > 0) *reinterpret_cast<uint4*>(p) = rounded16<T>(v);
         } else {
 #pragma unroll
             for (int i = 0; i < kVals; ++i)
-                if ((int64_t)(i * 32) < left) p[i * 32] = from_float<T>(v[i]);
+                if (i * 32 < left) p[i * 32] = from_float<T>(v[i]);
         }
     }
 
-    // largest over the lanes that share a block
+    // Largest magnitude of each chunk's block, over the lanes that share it.  16-bit values are compared two at a time, and both
+    // chunks' maxima travel together.
+    static __device__ __forceinline__ void largest(const Raw (&raw)[kChunks], uint32_t (&m)[kChunks]) {
+        if constexpr (kPairs) {
+            uint32_t two[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                constexpr uint32_t kAbs = 0x7fff7fffu;
+                const uint32_t w = __vmaxu2(__vmaxu2(raw[h].x & kAbs, raw[h].y & kAbs), __vmaxu2(raw[h].z & kAbs, raw[h].w & kAbs));
+                two[h] = __vmaxu2(w, w >> 16);
+            }
+            uint32_t w = __byte_perm(two[0], two[1], 0x5410);
+#pragma unroll
+            for (int d = 8; d > 0; d >>= 1) w = __vmaxu2(w, __shfl_xor_sync(0xffffffffu, w, d));
+            m[0] = __float_as_uint(value(make_uint4(w, 0, 0, 0), 0));
+            m[1] = __float_as_uint(value(make_uint4(w, 0, 0, 0), 1));
+        } else {
+#pragma unroll
+            for (int h = 0; h < kChunks; ++h) {
+                uint32_t w = 0;
+#pragma unroll
+                for (int i = 0; i < kVals; ++i) w = max(w, f8_magnitude(value(raw[h], i)));
+                m[h] = most(w);
+            }
+        }
+    }
     static __device__ __forceinline__ uint32_t most(uint32_t m) {
         if constexpr (kPairs) {
 #pragma unroll
@@ -75,11 +127,11 @@ struct Lanes {
         for (uint32_t d = 1; d < 4; ++d) r |= ((__shfl_xor_sync(0xffffffffu, w, d) >> (8 * q)) & 0xffu) << (8 * (q ^ d));
         return r;
     }
-    // offset of this lane's bytes in a block's 128
-    static __device__ __forceinline__ uint32_t at(uint32_t lane, uint32_t row) {
-        if constexpr (kPairs) return f8_piece(row, (lane & 15u) >> 1) + 8u * (lane & 1u);
-        if constexpr (kWay == kWide) return f8_piece(row, lane >> 2) + 4u * (lane & 3u);
-        return f8_piece(row, 2u * (lane & 3u) + (lane >> 4)) + 4u * ((lane >> 2) & 3u);
+    // offset of this lane's bytes in a block's 128 of row 0; row r: XOR 16 (r % 8)
+    static __device__ __forceinline__ uint32_t at(uint32_t lane) {
+        if constexpr (kPairs) return (lane & 15u) * 8u;
+        if constexpr (kWay == kWide) return lane * 4u;
+        return 32u * (lane & 3u) + 4u * (lane >> 2);
     }
     // whole warps, whether or not `valid`
     static __device__ __forceinline__ void put(uint8_t* p, bool valid, const float (&v)[kVals], float inverse, uint32_t lane) {
@@ -92,24 +144,29 @@ struct Lanes {
         if constexpr (kPairs) *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
         else *reinterpret_cast<uint32_t*>(p) = w[0];
     }
-    static __device__ __forceinline__ void get(const uint8_t* p, bool valid, float scale, uint32_t lane, float (&v)[kVals]) {
-        uint32_t w[2] = {0, 0};
+    // this lane's bytes of a block, and their values
+    struct Bytes { uint32_t w[kVals / 4]; };
+    static __device__ __forceinline__ Bytes get(const uint8_t* p, bool valid) {
+        Bytes b = {};
         if (valid) {
             if constexpr (kPairs) {
                 const uint2 two = __ldcs(reinterpret_cast<const uint2*>(p));
-                w[0] = two.x; w[1] = two.y;
+                b.w[0] = two.x; b.w[1] = two.y;
             } else {
-                w[0] = __ldcs(reinterpret_cast<const uint32_t*>(p));
+                b.w[0] = __ldcs(reinterpret_cast<const uint32_t*>(p));
             }
         }
-        if constexpr (kWay == kSingle) w[0] = turn(w[0], lane);
+        return b;
+    }
+    static __device__ __forceinline__ void values(Bytes b, float scale, uint32_t lane, float (&v)[kVals]) {
+        if constexpr (kWay == kSingle) b.w[0] = turn(b.w[0], lane);
 #pragma unroll
         for (int i = 0; i < kVals / 4; ++i) {
-            const float2 a = f8_to2(w[i]), b = f8_to2(w[i] >> 16);
-            v[4 * i] = __fmul_rn(a.x, scale);
-            v[4 * i + 1] = __fmul_rn(a.y, scale);
-            v[4 * i + 2] = __fmul_rn(b.x, scale);
-            v[4 * i + 3] = __fmul_rn(b.y, scale);
+            const float2 x = f8_to2(b.w[i]), y = f8_to2(b.w[i] >> 16);
+            v[4 * i] = __fmul_rn(x.x, scale);
+            v[4 * i + 1] = __fmul_rn(x.y, scale);
+            v[4 * i + 2] = __fmul_rn(y.x, scale);
+            v[4 * i + 3] = __fmul_rn(y.y, scale);
         }
     }
 };
@@ -117,29 +174,75 @@ struct Lanes {
 // ------------------------------------------------------------------------------------------------
 // Activations
 // ------------------------------------------------------------------------------------------------
-template <int kAct>
+// For 16-bit results kShort forms take the place of the library's functions, with which the kernels are bound by instructions
+// (16384 x 8192 bf16, GELU: forward 299, backward 338 us; with these FORWARD_US and BACKWARD_US).
+__device__ __forceinline__ float exp2_short(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float inverse_short(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// Phi(-|x|), Phi the normal distribution function, is 1/2 erfc(z) with z = |x| / sqrt(2), and erfc(z) exp(z^2) = t P(t), t = 1 / (1 + 0.375 z).
+// P is a polynomial of degree 6 fitted to the smallest relative error over 0 <= z <= 12 (1e-6); with the roundings 1.5e-6 for |x| <= 4
+// and 5e-6 for |x| <= 10, far below half a step of 16 bits.  e: exp(-x^2 / 2).
+__device__ __forceinline__ float normal_below_short(float x, float& e) {
+    const float ax = fabsf(x);
+    e = exp2_short(__fmul_rn(__fmul_rn(ax, ax), -0.72134752044448170f));
+    const float t = inverse_short(__fmaf_rn(ax, 0.26516504294495533f, 1.0f));
+    float p = __fmaf_rn(-0.0666150079f, t, 0.19073585385f);  // P / 2
+    p = __fmaf_rn(p, t, -0.06032206705f);
+    p = __fmaf_rn(p, t, 0.13837517965f);
+    p = __fmaf_rn(p, t, 0.0845211864f);
+    p = __fmaf_rn(p, t, 0.1076185385f);
+    p = __fmaf_rn(p, t, 0.1056866174f);
+    return __fmul_rn(e, __fmul_rn(t, p));
+}
+template <bool kShort>
+__device__ __forceinline__ float logistic(float x) {
+    if constexpr (kShort) return inverse_short(__fadd_rn(1.0f, exp2_short(__fmul_rn(x, -1.4426950408889634f))));
+    return __fdiv_rn(1.0f, __fadd_rn(1.0f, expf(-x)));
+}
+
+// Infinities give the limits (the bounds below lie where the other factor is zero), NaN stays.
+template <int kAct, bool kShort>
 __device__ __forceinline__ float act(float x) {
-    if constexpr (kAct == CO3_ACT_RELU) return x < 0.0f ? 0.0f : x;  // NaN stays
-    if constexpr (kAct == CO3_ACT_GELU) return __fmul_rn(x, __fmul_rn(0.5f, erfcf(__fmul_rn(x, -0.70710678118654752f))));
-    if constexpr (kAct == CO3_ACT_SILU) return __fdiv_rn(x, __fadd_rn(1.0f, expf(-x)));
+    if constexpr (kAct == CO3_ACT_RELU) return x < 0.0f ? 0.0f : x;
+    if constexpr (kAct == CO3_ACT_GELU && kShort) {
+        float e;
+        return __fmaf_rn(-fminf(fabsf(x), 64.0f), normal_below_short(x, e), x < 0.0f ? 0.0f : x);
+    }
+    if constexpr (kAct == CO3_ACT_GELU) return __fmul_rn(fmaxf(x, -64.0f), __fmul_rn(0.5f, erfcf(__fmul_rn(x, -0.70710678118654752f))));
+    if constexpr (kAct == CO3_ACT_SILU && kShort) return __fmul_rn(fmaxf(x, -200.0f), logistic<true>(x));
+    if constexpr (kAct == CO3_ACT_SILU) return __fdiv_rn(fmaxf(x, -200.0f), __fadd_rn(1.0f, expf(-x)));
     return x;
 }
-template <int kAct>
+template <int kAct, bool kShort>
 __device__ __forceinline__ float act_slope(float x) {
-    if constexpr (kAct == CO3_ACT_RELU) return x > 0.0f ? 1.0f : x <= 0.0f ? 0.0f : x;  // NaN stays
+    if constexpr (kAct == CO3_ACT_RELU) return x > 0.0f ? 1.0f : x <= 0.0f ? 0.0f : x;
     if constexpr (kAct == CO3_ACT_GELU) {
-        const float below = __fmul_rn(0.5f, erfcf(__fmul_rn(x, -0.70710678118654752f)));
-        return __fmaf_rn(x, __fmul_rn(0.39894228040143268f, expf(__fmul_rn(__fmul_rn(-0.5f, x), x))), below);
+        float e, below;
+        if constexpr (kShort) {
+            const float q = normal_below_short(x, e);
+            below = __fadd_rn(0.5f, copysignf(__fsub_rn(0.5f, q), x));
+        } else {
+            below = __fmul_rn(0.5f, erfcf(__fmul_rn(x, -0.70710678118654752f)));
+            e = expf(__fmul_rn(__fmul_rn(-0.5f, x), x));
+        }
+        return __fmaf_rn(x, __fmul_rn(0.39894228040143268f, e), below);
     }
     if constexpr (kAct == CO3_ACT_SILU) {
-        const float p = __fdiv_rn(1.0f, __fadd_rn(1.0f, expf(-x)));
+        const float p = logistic<kShort>(x);
         return __fmul_rn(p, __fmaf_rn(x, __fsub_rn(1.0f, p), 1.0f));
     }
     return 1.0f;
 }
 
 // ------------------------------------------------------------------------------------------------
-// Rows
+// Rows: a warp takes unit_rows (2 or 8) rows of four blocks, two rows at a time.
 // ------------------------------------------------------------------------------------------------
 struct RowsArgs {
     const void* x;      // or dy
@@ -148,138 +251,199 @@ struct RowsArgs {
     uint64_t rows, x_stride, y_stride;
     uint32_t cols, kb, groups;   // groups of four blocks
     uint64_t rows_padded, scales;
-    uint32_t units;              // pairs of rows x groups
+    uint32_t units, unit_rows;   // row groups x groups of blocks
 };
 
-// Where a warp's unit lies.
-struct Unit {
-    uint64_t row;
-    uint32_t group;
-};
-__device__ __forceinline__ bool find_unit(const RowsArgs& a, Unit& u) {
-    const uint32_t unit = blockIdx.x * kWarps + (threadIdx.x >> 5);
-    u.row = (uint64_t)(unit / a.groups) * kRowsAtOnce;
-    u.group = unit % a.groups;
-    return unit < a.units;
-}
-__device__ __forceinline__ uint64_t scale_word(const RowsArgs& a, uint64_t row, uint32_t group) {
-    return a.scales + (group * (a.rows_padded >> 7) + (row >> 7)) * kF8Scales + f8_scale_at((uint32_t)row & 127u, 0);
-}
-
-// A row's four blocks into one buffer.
+// Where a warp's unit lies, for this lane.
 template <typename T, Way kWay>
-__device__ __forceinline__ void put_row(const RowsArgs& a, uint8_t* to, uint64_t row, uint32_t group, uint32_t lane,
-                                        float (&v)[Lanes<T, kWay>::kChunks][Lanes<T, kWay>::kVals]) {
+struct Unit {
     using L = Lanes<T, kWay>;
-    uint32_t bytes[L::kChunks];
+    uint64_t row0;
+    uint32_t group, lane;
+    uint64_t col;           // column of its first chunk
+    uint64_t f8, f8_chunk;  // offset of row0's 128 bytes of its first block, bytes from chunk to chunk
+    uint64_t word;          // offset of row0's four exponent bytes
+    uint32_t blocks;        // of this group, from the lane's first one on
+
+    __device__ __forceinline__ Unit(const RowsArgs& a, uint32_t unit) {
+        lane = threadIdx.x & 31u;
+        const uint32_t r = unit / a.groups;
+        group = unit - r * a.groups;
+        row0 = (uint64_t)r * a.unit_rows;
+        col = (uint64_t)group * 512u + L::column0(lane);
+        f8 = f8_row(a.rows_padded, group * 4u + L::block0(lane), row0);
+        f8_chunk = a.rows_padded * (128u * L::kBlocks);
+        word = a.scales + (group * (a.rows_padded >> 7) + (row0 >> 7)) * kF8Scales + f8_scale_at((uint32_t)row0 & 127u, 0);
+        blocks = min(4u, a.kb - group * 4u);
+    }
+    // columns from a chunk's first one of this lane to the row's end
+    __device__ __forceinline__ int32_t left(const RowsArgs& a, int h) const { return (int32_t)(a.cols - min((uint64_t)a.cols, col + h * L::kChunkCols)); }
+    __device__ __forceinline__ bool has(int h) const { return L::block0(lane) + h * L::kBlocks < blocks; }
+    // offset of this lane's bytes of row row0 + r (rows of a unit lie in one atom of eight)
+    __device__ __forceinline__ uint64_t bytes(uint32_t r, int h) const { return f8 + h * f8_chunk + r * 128u + (L::at(lane) ^ ((((uint32_t)row0 + r) & 7u) << 4)); }
+};
+
+// A row's four blocks into one buffer; m: their largest magnitudes.
+template <typename T, Way kWay>
+__device__ __forceinline__ void put_row(const Unit<T, kWay>& u, uint8_t* to, uint32_t r, float (&v)[Lanes<T, kWay>::kChunks][Lanes<T, kWay>::kVals],
+                                        const uint32_t (&m)[Lanes<T, kWay>::kChunks]) {
+    using L = Lanes<T, kWay>;
+    int e[L::kChunks];
+    bool rare = false;
 #pragma unroll
     for (int h = 0; h < L::kChunks; ++h) {
-        uint32_t m = 0;
+        e[h] = f8_exponent(m[h]);
+        rare |= m[h] > kF8Rare;
+    }
+    if (__any_sync(0xffffffffu, rare)) {
 #pragma unroll
-        for (int i = 0; i < L::kVals; ++i) m = max(m, f8_magnitude(v[h][i]));
-        m = L::most(m);
-        int e = f8_exponent(m);
-        if (__any_sync(0xffffffffu, m > kF8Rare)) {
-            m = 0;
+        for (int h = 0; h < L::kChunks; ++h) {
+            uint32_t finite = 0;
 #pragma unroll
-            for (int i = 0; i < L::kVals; ++i) m = max(m, f8_finite_magnitude(v[h][i]));
-            e = f8_exponent(L::most(m));
+            for (int i = 0; i < L::kVals; ++i) finite = max(finite, f8_finite_magnitude(v[h][i]));
+            e[h] = f8_exponent(L::most(finite));
 #pragma unroll
-            for (int i = 0; i < L::kVals; ++i) v[h][i] = f8_rare(v[h][i], e);
+            for (int i = 0; i < L::kVals; ++i) v[h][i] = f8_rare(v[h][i], e[h]);
         }
-        const uint32_t block = group * 4u + L::block(h, lane);
-        L::put(to + f8_row(a.rows_padded, block, row) + L::at(lane, (uint32_t)row), block < a.kb, v[h], power_of_two(-e), lane);
-        bytes[h] = (uint32_t)(e + 127);
     }
-    uint32_t word;
-    if constexpr (L::kPairs) {
-        word = bytes[0] | (bytes[1] << 16);
-        word |= __shfl_down_sync(0xffffffffu, word, 16) << 8;
-    } else {
-        word = bytes[0] | (bytes[1] << 8) | (bytes[2] << 16) | (bytes[3] << 24);
-    }
-    if (lane == 0) *reinterpret_cast<uint32_t*>(to + scale_word(a, row, group)) = word;
+#pragma unroll
+    for (int h = 0; h < L::kChunks; ++h) L::put(to + u.bytes(r, h), u.has(h), v[h], power_of_two(-e[h]), u.lane);
+    uint32_t word = 0;
+#pragma unroll
+    for (int h = 0; h < L::kChunks; ++h) word |= (uint32_t)(e[h] + 127) << (8 * L::kBlocks * h);
+    if constexpr (L::kPairs) word |= __shfl_down_sync(0xffffffffu, word, 16) << 8;
+    if (u.lane == 0) *reinterpret_cast<uint32_t*>(to + u.word + r * 16u) = word;
 }
 
 // x to x8 (if given), act(x) to y and to y8 (if given).  Rows up to a multiple of 16 are written, as zeros: the products read
 // so many.
 template <typename T, Way kWay, int kAct>
-__global__ void __launch_bounds__(kWarps * 32) f8_rows_kernel(const __grid_constant__ RowsArgs a) {
+__global__ void __launch_bounds__(kWarps * 32, 3) f8_rows_kernel(const __grid_constant__ RowsArgs a) {
     using L = Lanes<T, kWay>;
     wait_for_previous_kernel();
-    Unit u;
-    if (!find_unit(a, u)) return;
-    const uint32_t lane = threadIdx.x & 31u;
-    float v[kRowsAtOnce][L::kChunks][L::kVals];
-    const T* x = static_cast<const T*>(a.x);
-    T* y = static_cast<T*>(a.y);
+    const uint32_t unit = blockIdx.x * kWarps + (threadIdx.x >> 5);
+    if (unit >= a.units) return;
+    const Unit<T, kWay> u(a, unit);
+    const T* x = static_cast<const T*>(a.x) + u.row0 * a.x_stride + u.col;
+    T* y = static_cast<T*>(a.y) + u.row0 * a.y_stride + u.col;
+    const uint32_t rows = (uint32_t)min((uint64_t)a.unit_rows, a.rows - min(a.rows, u.row0));
+    int32_t left[L::kChunks];
 #pragma unroll
-    for (int r = 0; r < kRowsAtOnce; ++r)
+    for (int h = 0; h < L::kChunks; ++h) left[h] = u.left(a, h);
+    typename L::Raw raw[kRowsAtOnce][L::kChunks];
+    auto fetch = [&](uint32_t r0) {
 #pragma unroll
-        for (int h = 0; h < L::kChunks; ++h) {
-            const uint64_t col = (uint64_t)u.group * 512u + L::column(h, lane);
-            L::load(x + (u.row + r) * a.x_stride + col, u.row + r < a.rows ? (int64_t)a.cols - (int64_t)col : 0, v[r][h]);
+        for (int r = 0; r < kRowsAtOnce; ++r) {
+#pragma unroll
+            for (int h = 0; h < L::kChunks; ++h) raw[r][h] = L::load(x + h * L::kChunkCols, r0 + r < rows ? left[h] : 0);
+            x += a.x_stride;
         }
+    };
+#pragma unroll 1
+    for (uint32_t r0 = 0; r0 < a.unit_rows; r0 += kRowsAtOnce) {
+        fetch(r0);
 #pragma unroll
-    for (int r = 0; r < kRowsAtOnce; ++r) {
-        const uint64_t row = u.row + r;
-        float t[L::kChunks][L::kVals];
-        if constexpr (kAct != CO3_ACT_NONE) {
+        for (int r = 0; r < kRowsAtOnce; ++r) {
+            float v[L::kChunks][L::kVals];
 #pragma unroll
             for (int h = 0; h < L::kChunks; ++h)
 #pragma unroll
-                for (int i = 0; i < L::kVals; ++i) t[h][i] = act<kAct>(v[r][h][i]);
-        } else {
+                for (int i = 0; i < L::kVals; ++i) v[h][i] = L::value(raw[r][h], i);
+            uint32_t m[L::kChunks];
+            if (a.x8) {
+                L::largest(raw[r], m);
+                if constexpr (kAct == CO3_ACT_NONE) {
+                    put_row<T, kWay>(u, a.x8, r0 + r, v, m);
+                } else {  // (the rare way changes them)
+                    float t[L::kChunks][L::kVals];
 #pragma unroll
-            for (int h = 0; h < L::kChunks; ++h)
+                    for (int h = 0; h < L::kChunks; ++h)
 #pragma unroll
-                for (int i = 0; i < L::kVals; ++i) t[h][i] = v[r][h][i];
-        }
-        if (y)
-#pragma unroll
-            for (int h = 0; h < L::kChunks; ++h) {
-                const uint64_t col = (uint64_t)u.group * 512u + L::column(h, lane);
-                L::store(y + row * a.y_stride + col, row < a.rows ? (int64_t)a.cols - (int64_t)col : 0, t[h]);
+                        for (int i = 0; i < L::kVals; ++i) t[h][i] = v[h][i];
+                    put_row<T, kWay>(u, a.x8, r0 + r, t, m);
+                }
             }
-        if (a.x8) put_row<T, kWay>(a, a.x8, row, u.group, lane, v[r]);
-        if (a.y8) put_row<T, kWay>(a, a.y8, row, u.group, lane, t);
+            if (a.y || a.y8) {
+                if constexpr (kAct == CO3_ACT_NONE) {
+#pragma unroll
+                    for (int h = 0; h < L::kChunks; ++h)
+#pragma unroll
+                        for (int i = 0; i < L::kVals; ++i) v[h][i] = L::value(raw[r][h], i);
+                } else {
+#pragma unroll
+                    for (int h = 0; h < L::kChunks; ++h)
+#pragma unroll
+                        for (int i = 0; i < L::kVals; ++i) v[h][i] = act<kAct, sizeof(T) == 2>(v[h][i]);
+                }
+                if (a.y)
+#pragma unroll
+                    for (int h = 0; h < L::kChunks; ++h) L::store(y + h * L::kChunkCols, r0 + r < rows ? left[h] : 0, v[h]);
+                if (a.y8) {
+#pragma unroll
+                    for (int h = 0; h < L::kChunks; ++h) {
+                        uint32_t w = 0;
+#pragma unroll
+                        for (int i = 0; i < L::kVals; ++i) w = max(w, f8_magnitude(v[h][i]));
+                        m[h] = L::most(w);
+                    }
+                    put_row<T, kWay>(u, a.y8, r0 + r, v, m);
+                }
+            }
+            y += a.y_stride;
+        }
     }
 }
 
 // y <- the values of x8, or (kBackward) dx <- dy * act'(values of x8).
 template <typename T, Way kWay, int kAct, bool kBackward>
-__global__ void __launch_bounds__(kWarps * 32) f8_values_kernel(const __grid_constant__ RowsArgs a) {
+__global__ void __launch_bounds__(kWarps * 32, 3) f8_values_kernel(const __grid_constant__ RowsArgs a) {
     using L = Lanes<T, kWay>;
     wait_for_previous_kernel();
-    Unit u;
-    if (!find_unit(a, u)) return;
-    const uint32_t lane = threadIdx.x & 31u;
-    float v[kRowsAtOnce][L::kChunks][L::kVals], d[kRowsAtOnce][L::kChunks][L::kVals];
-    const T* dy = static_cast<const T*>(a.x);
+    const uint32_t unit = blockIdx.x * kWarps + (threadIdx.x >> 5);
+    if (unit >= a.units) return;
+    const Unit<T, kWay> u(a, unit);
+    const T* dy = static_cast<const T*>(a.x) + u.row0 * a.x_stride + u.col;
+    T* y = static_cast<T*>(a.y) + u.row0 * a.y_stride + u.col;
+    const uint32_t rows = (uint32_t)min((uint64_t)a.unit_rows, a.rows - min(a.rows, u.row0));
+    int32_t left[L::kChunks];
 #pragma unroll
-    for (int r = 0; r < kRowsAtOnce; ++r) {
-        const uint64_t row = u.row + r;
-        const uint32_t word = row < a.rows ? __ldg(reinterpret_cast<const uint32_t*>(a.x8 + scale_word(a, row, u.group))) : 0x7f7f7f7fu;
+    for (int h = 0; h < L::kChunks; ++h) left[h] = u.left(a, h);
+    struct {
+        uint32_t word;
+        typename L::Bytes f8[L::kChunks];
+        typename L::Raw dy[kBackward ? L::kChunks : 1];
+    } in[kRowsAtOnce];
+    auto fetch = [&](uint32_t r0) {
 #pragma unroll
-        for (int h = 0; h < L::kChunks; ++h) {
-            const uint64_t col = (uint64_t)u.group * 512u + L::column(h, lane);
-            if constexpr (kBackward) L::load(dy + row * a.x_stride + col, row < a.rows ? (int64_t)a.cols - (int64_t)col : 0, d[r][h]);
-            const uint32_t block = u.group * 4u + L::block(h, lane);
-            const float scale = __uint_as_float(((word >> (8u * L::block(h, lane))) & 0xffu) << 23);
-            L::get(a.x8 + f8_row(a.rows_padded, block, row) + L::at(lane, (uint32_t)row), row < a.rows && block < a.kb, scale, lane, v[r][h]);
-        }
-    }
+        for (int r = 0; r < kRowsAtOnce; ++r) {
+            const bool valid = r0 + r < rows;
+            in[r].word = valid ? __ldg(reinterpret_cast<const uint32_t*>(a.x8 + u.word + (r0 + r) * 16u)) : 0x7f7f7f7fu;
 #pragma unroll
-    for (int r = 0; r < kRowsAtOnce; ++r) {
-        const uint64_t row = u.row + r;
-#pragma unroll
-        for (int h = 0; h < L::kChunks; ++h) {
-            const uint64_t col = (uint64_t)u.group * 512u + L::column(h, lane);
-            if constexpr (kBackward) {
-#pragma unroll
-                for (int i = 0; i < L::kVals; ++i) v[r][h][i] = __fmul_rn(d[r][h][i], act_slope<kAct>(v[r][h][i]));
+            for (int h = 0; h < L::kChunks; ++h) {
+                in[r].f8[h] = L::get(a.x8 + u.bytes(r0 + r, h), valid && u.has(h));
+                if constexpr (kBackward) in[r].dy[h] = L::load(dy + h * L::kChunkCols, valid ? left[h] : 0);
             }
-            L::store(static_cast<T*>(a.y) + row * a.y_stride + col, row < a.rows ? (int64_t)a.cols - (int64_t)col : 0, v[r][h]);
+            if constexpr (kBackward) dy += a.x_stride;
+        }
+    };
+#pragma unroll 1
+    for (uint32_t r0 = 0; r0 < rows; r0 += kRowsAtOnce) {
+        fetch(r0);
+#pragma unroll
+        for (int r = 0; r < kRowsAtOnce; ++r) {
+            const auto& now = in[r];
+            const uint32_t word = now.word >> (8u * L::block0(u.lane));
+#pragma unroll
+            for (int h = 0; h < L::kChunks; ++h) {
+                float v[L::kVals];
+                L::values(now.f8[h], __uint_as_float(((word >> (8 * L::kBlocks * h)) & 0xffu) << 23), u.lane, v);
+                if constexpr (kBackward) {
+#pragma unroll
+                    for (int i = 0; i < L::kVals; ++i) v[i] = __fmul_rn(L::value(now.dy[h], i), act_slope<kAct, sizeof(T) == 2>(v[i]));
+                }
+                L::store(y + h * L::kChunkCols, r0 + r < rows ? left[h] : 0, v);
+            }
+            y += a.y_stride;
         }
     }
 }
@@ -302,14 +466,16 @@ __global__ void __launch_bounds__(256) f8_square_kernel(const __grid_constant__ 
     wait_for_previous_kernel();
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
     const uint32_t block = blockIdx.x % a.kb, tile = blockIdx.x / a.kb;
-    const uint32_t row0 = warp * 16u + (L::kPairs ? lane >> 4 : 0u);
-    const uint32_t in_block = kWay == kSingle ? lane : (lane & (L::kPairs ? 15u : 31u)) * L::kVals;
-    const uint64_t col = (uint64_t)block * 128u + in_block;
+    const uint32_t row0 = warp * 16u + L::block0(lane);
+    const uint64_t col = (uint64_t)block * 128u + (kWay == kSingle ? lane : (lane & (L::kPairs ? 15u : 31u)) * L::kVals);
+    const int32_t left = (int32_t)(a.cols - min((uint64_t)a.cols, col));
     float v[kTurns][L::kVals];
 #pragma unroll
     for (int i = 0; i < kTurns; ++i) {
         const uint64_t row = (uint64_t)tile * 128u + row0 + i * kRows;
-        L::load(static_cast<const T*>(a.x) + row * a.x_stride + col, row < a.rows ? (int64_t)a.cols - (int64_t)col : 0, v[i]);
+        const typename L::Raw raw = L::load(static_cast<const T*>(a.x) + row * a.x_stride + col, row < a.rows ? left : 0);
+#pragma unroll
+        for (int k = 0; k < L::kVals; ++k) v[i][k] = L::value(raw, k);
     }
     auto largest = [&](bool finite) {
         uint32_t m = 0;
@@ -338,7 +504,7 @@ __global__ void __launch_bounds__(256) f8_square_kernel(const __grid_constant__ 
 #pragma unroll
     for (int i = 0; i < kTurns; ++i) {
         const uint32_t r = row0 + i * kRows;
-        L::put(a.out + f8_row(a.rows_padded, block, (uint64_t)tile * 128u + r) + L::at(lane, r), true, v[i], inverse, lane);
+        L::put(a.out + f8_row(a.rows_padded, block, (uint64_t)tile * 128u + r) + (L::at(lane) ^ ((r & 7u) << 4)), true, v[i], inverse, lane);
     }
     const uint32_t t = threadIdx.x & 127u;
     const uint64_t at = threadIdx.x < 128 ? a.scales + ((block >> 2) * (a.rows_padded >> 7) + tile) * kF8Scales + f8_scale_at(t, block)
@@ -365,7 +531,10 @@ void fill(RowsArgs& a, const F8Layout& l, uint64_t rows, uint32_t cols) {
     a.groups = (l.kb + 3u) / 4u;
     a.rows_padded = l.rows;
     a.scales = l.scales;
-    a.units = (uint32_t)((rows + 15u) / 16u * (16u / kRowsAtOnce)) * a.groups;
+    // eight rows a warp where that still gives every multiprocessor eight warps (148 of them), two otherwise
+    const uint64_t padded = (rows + 15u) / 16u * 16u;
+    a.unit_rows = padded / 8u * a.groups >= 148u * 8u ? 8 : kRowsAtOnce;
+    a.units = (uint32_t)(padded / a.unit_rows * a.groups);
 }
 
 template <typename T, Way kWay>

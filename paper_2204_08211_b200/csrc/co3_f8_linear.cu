@@ -378,14 +378,16 @@ __global__ void __launch_bounds__(kF8Threads, 1) f8_pair_kernel(const __grid_con
                     if (turn > 0 && !f8_wait(&sm.empty[st], (turn - 1) & 1u)) { *failed = 1; break; }
                     if (issues) {
                         unsigned char* to = ring + st * kPairStageBytes;
-                        const bool with_scales = (q & 3u) == 0;
+                        // exponent bytes of a tile's first group, and then of each next one a few blocks ahead
+                        const uint32_t group = q == 0 ? 0u : (q >> 2) + 1;
+                        const bool with_scales = q == 0 || ((q & 3u) == 1u && group * 4u < a.kb);
                         mbar_arrive_expect_tx(&sm.full[st], kF8Tile + half * 128u + (with_scales ? kF8Scales + b_scales : 0u));
                         bulk_copy_g2s(to, from_a + q * a.a_block, kF8Tile, &sm.full[st]);
                         bulk_copy_g2s(to + kF8Tile, from_b + q * a.b_block, half * 128u, &sm.full[st]);
                         if (with_scales) {
                             unsigned char* s = scales + st * kPairScaleBytes;
-                            bulk_copy_g2s(s, a.a_scales + (q >> 2) * a.a_group + (uint64_t)mt * kF8Scales, kF8Scales, &sm.full[st]);
-                            bulk_copy_g2s(s + kF8Scales, a.b_scales + (q >> 2) * a.b_group + (uint64_t)(n0 >> 7) * kF8Scales, b_scales, &sm.full[st]);
+                            bulk_copy_g2s(s, a.a_scales + group * a.a_group + (uint64_t)mt * kF8Scales, kF8Scales, &sm.full[st]);
+                            bulk_copy_g2s(s + kF8Scales, a.b_scales + group * a.b_group + (uint64_t)(n0 >> 7) * kF8Scales, b_scales, &sm.full[st]);
                         }
                     }
                     if (++st == kPairStages) { st = 0; ++turn; }
@@ -423,23 +425,26 @@ __global__ void __launch_bounds__(kF8Threads, 1) f8_pair_kernel(const __grid_con
                     --left;
                     if (!f8_wait(&sm.full[st], turn & 1u) || !f8_wait(&sm.peer[st], turn & 1u)) { ok = false; break; }
                     tc_fence_after();
-                    // the columns of eight groups ago are free: fewer than kPairStages blocks are under way
                     if ((q & 3u) == 0) group = (group + 1) % kScaleTurns;
                     if (issues) {
                         const uint32_t sa = tmem + kTmemScales + group * kScaleCols, sb = sa + 4;
-                        if ((q & 3u) == 0) {
-                            const uint32_t from = smem_addr(scales + st * kPairScaleBytes);
-                            pair_scales_in(sa, from);
-                            pair_scales_in(sb, from + kF8Scales);
-                            if (n > 128) pair_scales_in(sb + 4, from + 2 * kF8Scales);
-                        }
-                        const uint32_t at = smem_addr(ring + st * kPairStageBytes), bt = at + kF8Tile;
+                        const uint32_t from = smem_addr(scales + st * kPairScaleBytes), at = smem_addr(ring + st * kPairStageBytes), bt = at + kF8Tile;
+                        // to columns of eight groups ago, which are free: fewer than kPairStages blocks are under way
+                        auto bring_scales = [&](uint32_t to) {
+                            pair_scales_in(to, from);
+                            pair_scales_in(to + 4, from + kF8Scales);
+                            if (n > 128) pair_scales_in(to + 8, from + 2 * kF8Scales);
+                        };
+                        if (q == 0) bring_scales(sa);
                         switch (q & 3u) {
                             case 0: multiply_block_pair<kTransposed, 0>(tmem, at, bt, n, sa, sb, !fresh); break;
                             case 1: multiply_block_pair<kTransposed, 1>(tmem, at, bt, n, sa, sb, !fresh); break;
                             case 2: multiply_block_pair<kTransposed, 2>(tmem, at, bt, n, sa, sb, !fresh); break;
                             default: multiply_block_pair<kTransposed, 3>(tmem, at, bt, n, sa, sb, !fresh); break;
                         }
+                        // the next group's, while this one is multiplied: right before their use they cost 25 us of 16384 x 4096 x 4096's
+                        // 245, here 14
+                        if ((q & 3u) == 1u && ((q >> 2) + 1) * 4u < a.kb) bring_scales(tmem + kTmemScales + (group + 1) % kScaleTurns * kScaleCols);
                         tc_commit_pair(&sm.empty[st]);
                         if (left == 0) tc_commit_pair(&sm.sum_full);
                     }
