@@ -227,7 +227,7 @@ __device__ __forceinline__ float act_slope(float x) {
         float e, below;
         if constexpr (kShort) {
             const float q = normal_below_short(x, e);
-            below = __fadd_rn(0.5f, copysignf(__fsub_rn(0.5f, q), x));
+            below = x < 0.0f ? q : __fsub_rn(1.0f, q);
         } else {
             below = __fmul_rn(0.5f, erfcf(__fmul_rn(x, -0.70710678118654752f)));
             e = expf(__fmul_rn(__fmul_rn(-0.5f, x), x));
@@ -515,15 +515,10 @@ __global__ void __launch_bounds__(256) f8_square_kernel(const __grid_constant__ 
 // ------------------------------------------------------------------------------------------------
 // Launches
 // ------------------------------------------------------------------------------------------------
-bool valid_rows(int type, const void* p, uint64_t stride, uint32_t cols) {
-    return type >= CO3_F32 && type <= CO3_BF16 && p && aligned(p, type_size(type)) && stride >= cols && stride < (1ull << 40);
-}
 bool wide(int type, const void* p, uint64_t stride, uint32_t cols) {
     const size_t s = type_size(type);
     return !p || (aligned(p, 16) && stride * s % 16 == 0 && cols * s % 16 == 0);
 }
-bool valid_f8(const void* p) { return p && aligned(p, 256); }
-
 void fill(RowsArgs& a, const F8Layout& l, uint64_t rows, uint32_t cols) {
     a.rows = rows;
     a.cols = cols;
@@ -588,7 +583,7 @@ int co3_f8_pack(const void* x, int type, uint64_t rows, uint32_t cols, uint64_t 
     F8Layout l;
     if (type < CO3_F32 || type > CO3_BF16 || !f8_layout(rows, cols, kind, &l)) return CO3_ERR_INVALID_ARG;
     if (rows == 0 || cols == 0) return CO3_OK;
-    if (!valid_rows(type, x, x_row_stride, cols) || !valid_f8(out)) return CO3_ERR_INVALID_ARG;
+    if (!f8_valid_rows(type, x, x_row_stride, cols) || !f8_valid(out)) return CO3_ERR_INVALID_ARG;
     if (out_bytes < l.bytes) return CO3_ERR_CAPACITY;
     SquareArgs a = {x, static_cast<uint8_t*>(out), rows, x_row_stride, l.rows, l.scales, l.scales_t, cols, l.kb};
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -600,7 +595,7 @@ int co3_f8_activation(const void* x, int type, uint64_t rows, uint32_t cols, uin
     F8Layout l;
     if (type < CO3_F32 || type > CO3_BF16 || act < CO3_ACT_NONE || act > CO3_ACT_SILU || !f8_layout(rows, cols, CO3_F8_ROWS, &l)) return CO3_ERR_INVALID_ARG;
     if (rows == 0 || cols == 0) return CO3_OK;
-    if (!valid_rows(type, x, x_row_stride, cols) || (y && !valid_rows(type, y, y_row_stride, cols)) || (y8 && !valid_f8(y8)) || (x8 && !valid_f8(x8)) ||
+    if (!f8_valid_rows(type, x, x_row_stride, cols) || (y && !f8_valid_rows(type, y, y_row_stride, cols)) || (y8 && !f8_valid(y8)) || (x8 && !f8_valid(x8)) ||
         (!y && !y8 && !x8) || (y8 && y8 == x8))
         return CO3_ERR_INVALID_ARG;
     if ((y8 || x8) && f8_bytes < l.bytes) return CO3_ERR_CAPACITY;
@@ -618,7 +613,7 @@ static int values(const void* dy, uint64_t dy_row_stride, const void* x8, size_t
     F8Layout l;
     if (type < CO3_F32 || type > CO3_BF16 || act > CO3_ACT_SILU || !f8_layout(rows, cols, kind, &l)) return CO3_ERR_INVALID_ARG;
     if (rows == 0 || cols == 0) return CO3_OK;
-    if (!valid_rows(type, out, out_row_stride, cols) || !valid_f8(x8) || (act >= 0 && !valid_rows(type, dy, dy_row_stride, cols))) return CO3_ERR_INVALID_ARG;
+    if (!f8_valid_rows(type, out, out_row_stride, cols) || !f8_valid(x8) || (act >= 0 && !f8_valid_rows(type, dy, dy_row_stride, cols))) return CO3_ERR_INVALID_ARG;
     if (x8_bytes < l.bytes) return CO3_ERR_CAPACITY;
     RowsArgs a = {};
     a.x = dy; a.y = out;

@@ -49,6 +49,12 @@ inline bool f8_layout(uint64_t rows, uint64_t cols, int kind, F8Layout* out) {
     return true;
 }
 
+// Arguments that name a matrix of `type` elements, or a buffer of 8-bit blocks.
+inline bool f8_valid_rows(int type, const void* p, uint64_t stride, uint32_t cols) {
+    return type >= CO3_F32 && type <= CO3_BF16 && p && reinterpret_cast<uintptr_t>(p) % type_size(type) == 0 && stride >= cols && stride < (1ull << 40);
+}
+inline bool f8_valid(const void* p) { return p && reinterpret_cast<uintptr_t>(p) % 256u == 0; }
+
 // Offset of a row's 128 bytes of a block of columns, and of a 16-byte piece in them.
 __device__ __forceinline__ uint64_t f8_row(uint64_t rows_padded, uint32_t block, uint64_t row) { return (block * rows_padded + row) * 128u; }
 __device__ __forceinline__ uint32_t f8_piece(uint32_t row, uint32_t piece) { return (piece ^ (row & 7u)) << 4; }

@@ -537,7 +537,6 @@ int launch_linear(const LinearArgs& a, uint32_t sms, cudaStream_t st) {
 int launch_pairs(LinearArgs a, bool transposed, uint32_t sms, cudaStream_t st) {
     a.n_tiles = (a.rows + kPairCols - 1) / kPairCols;
     const uint64_t tiles = (uint64_t)((a.m_tiles + 1) / 2) * a.n_tiles;
-    if (tiles >= (1ull << 30)) return CO3_ERR_INVALID_ARG;
     const uint32_t blocks = 2 * (uint32_t)std::min<uint64_t>(tiles, sms / 2);
     return transposed ? launch_clusters<f8_pair_kernel<true>, kPairSmem>(a, blocks, 2, st) : launch_clusters<f8_pair_kernel<false>, kPairSmem>(a, blocks, 2, st);
 }
@@ -546,7 +545,6 @@ template <int kN>
 int launch_tile(LinearArgs a, bool transposed, uint32_t sms, cudaStream_t st) {
     a.n_tiles = (a.rows + kN - 1) / kN;
     const uint64_t tiles = (uint64_t)a.m_tiles * a.n_tiles;
-    if (tiles >= (1ull << 31) / kMaxSplit) return CO3_ERR_INVALID_ARG;
     a.split = 1;
     while (a.split < kMaxSplit && tiles * a.split * 2 <= sms && a.kb >= a.split * 4) a.split *= 2;
     return transposed ? launch_linear<kN, true>(a, sms, st) : launch_linear<kN, false>(a, sms, st);
@@ -568,8 +566,8 @@ int co3_f8_linear(const void* x, int x_type, uint64_t x_row_stride, void* x8, si
         return CO3_ERR_INVALID_ARG;
     if (rows == 0 || to == 0) return CO3_OK;
     if (from == 0) return CO3_ERR_INVALID_ARG;
-    if (!x8 || !aligned(x8, 256) || !w8 || !aligned(w8, 256) || !y || !aligned(y, type_size(y_type)) || y_row_stride < to || y_row_stride >= (1ull << 40) ||
-        !aligned(bias, 4) || !aligned(res, 8))
+    if ((x && !f8_valid_rows(x_type, x, x_row_stride, from)) || !f8_valid(x8) || !f8_valid(w8) || !f8_valid_rows(y_type, y, y_row_stride, to) ||
+        !aligned(bias, 4) || !aligned(res, 8) || (uint64_t)((to + 127u) / 128u) * ((rows + 15u) / 16u) >= (1ull << 30))
         return CO3_ERR_INVALID_ARG;
     if (x8_bytes < lx.bytes || w8_bytes < lw.bytes) return CO3_ERR_CAPACITY;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
