@@ -36,6 +36,7 @@ class Co3Session:
         self.res_dec = torch.zeros(B.RESULT_DTYPE.itemsize, dtype=torch.uint8, device=self.device)
         self.res_fit = torch.zeros(B.RESULT_DTYPE.itemsize, dtype=torch.uint8, device=self.device)
         self.res_model = torch.zeros(B.RESULT_DTYPE.itemsize, dtype=torch.uint8, device=self.device)
+        self.res_f8 = torch.zeros(B.RESULT_DTYPE.itemsize, dtype=torch.uint8, device=self.device)
         self.avg = torch.empty(self.n_elem, dtype=torch.float32, device=self.device)
         self.hist = torch.zeros(max(1, self.n_seg) * 256, dtype=torch.int64, device=self.device)
 
@@ -171,6 +172,48 @@ class Co3Session:
         st = B.co3_layer_norm_backward(dy, x, self._layer(params, gain), mean, rstd, dx, grads[at[0]:], grads[at[1]:],
                                        self.n_clients, self.stride, workspace, accumulate, stream)
         self._check(st, "co3_layer_norm_backward")
+
+    # -- linear layers on 8-bit blocks at the clients ----------------------------------------------
+    def new_f8(self, rows: int, cols: int, kind: int = B.F8_ROWS) -> torch.Tensor:
+        """Room for a rows x cols matrix in 8-bit blocks."""
+        return torch.empty(B.co3_f8_bytes(rows, cols, kind), dtype=torch.uint8, device=self.device)
+
+    def new_linear_workspace(self, rows: int, outs: int, ins: int) -> torch.Tensor:
+        """Workspace for linear_backward with `rows` rows of each client."""
+        return torch.empty(B.co3_f8_weight_gradient_workspace_bytes(rows, outs, ins, self.n_clients), dtype=torch.uint8,
+                           device=self.device)
+
+    def pack_weights(self, params: torch.Tensor, weight: int, shape, w8: torch.Tensor, stream=None) -> None:
+        """w8 (new_f8(*shape, F8_SQUARE)) <- layer `weight` of the parameter vector, (outputs, inputs) = shape."""
+        st = B.co3_f8_pack(self._layer(params, weight).view(shape), w8, B.F8_SQUARE, stream)
+        self._check(st, "co3_f8_pack")
+
+    def linear(self, x, x8: torch.Tensor, w8: torch.Tensor, params: torch.Tensor, bias, y: torch.Tensor, cols=None, stream=None) -> None:
+        """y <- x W^T + layer `bias` of the parameter vector (None: without); x is kept in x8 for linear_backward.  x None: x8
+        holds the inputs (`cols` of them a row) already, from co3_f8_activation for instance."""
+        b = None if bias is None else self._layer(params, bias)
+        if b is not None and b.numel() != y.shape[1]:
+            raise ValueError("layer %d is not of the outputs' length" % bias)
+        st = B.co3_f8_linear(x, x8, w8, b, y, False, cols, self.res_f8, stream)
+        self._check(st, "co3_f8_linear")
+
+    def linear_backward(self, dy, dy8, x8, w8, weight: int, bias, shape, dx, grads, workspace, accumulate: bool = False, stream=None) -> None:
+        """Gradients of `linear` for the rows of all clients, client after client: every client's gradients of layers `weight`
+        and `bias` in its own vector of `grads`, and dx (None: not wanted; otherwise dy8 is room for dy in 8-bit blocks)."""
+        outs, ins = shape
+        if self.sizes[weight] != outs * ins or (bias is not None and self.sizes[bias] != outs) or dy.dim() != 2 or dy.shape[1] != outs:
+            raise ValueError("layers and gradients are not of this shape")
+        at = sum(self.sizes[:weight])
+        db = None if bias is None else grads[sum(self.sizes[:bias]):]
+        st = B.co3_f8_weight_gradient(dy, x8, ins, grads[at:], db, self.n_clients, self.stride, workspace, accumulate, self.res_f8, stream)
+        self._check(st, "co3_f8_weight_gradient")
+        if dx is not None:
+            st = B.co3_f8_linear(dy, dy8, w8, None, dx, True, None, self.res_f8, stream)
+            self._check(st, "co3_f8_linear")
+
+    def f8_result(self) -> np.ndarray:
+        """The last failure of the calls above, if any (cleared at the start of the session)."""
+        return B.read_results(self.res_f8, 1)
 
     def _check_width(self, x: torch.Tensor, gain: int, bias: int) -> None:
         if x.dim() != 2 or x.shape[1] != self.sizes[gain] or x.shape[1] != self.sizes[bias]:
