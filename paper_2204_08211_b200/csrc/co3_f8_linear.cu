@@ -489,6 +489,239 @@ __global__ void __launch_bounds__(kF8Threads, 1) f8_pair_kernel(const __grid_con
     if (threadIdx.x == 0 && *failed && a.res) atomicExch(&a.res->status, CO3_ERR_CUDA);
 }
 
+// ------------------------------------------------------------------------------------------------
+// Up to 16 rows of x (tokens of a decoding loop): a cluster's blocks divide the sum, each brings its own columns of x into shared
+// memory as 8-bit blocks while the first tiles of the weights are on their way, so that there is one launch, and the packed rows go
+// to memory from the first tile's blocks alone.
+// ------------------------------------------------------------------------------------------------
+constexpr uint32_t kFewRows = 16, kFewStages = 8, kFewBlocks = 32;  // blocks of columns of x that a block of threads holds
+constexpr uint32_t kFewRing = kFewStages * kF8Tile, kFewX = kFewBlocks * kFewRows * 128;
+constexpr uint32_t kFewSmem = 1024 + kFewRing + kFewX + (kFewStages + kFewBlocks / 4 + 1) * kF8Scales + 256;
+
+struct FewArgs {
+    LinearArgs l;
+    const void* x;           // nullable: the blocks are in l.b
+    int x_type;
+    uint64_t x_stride;
+    uint32_t cols, wide;     // wide: rows are aligned for four values at a time
+    uint8_t *x8, *x8_scales;
+};
+struct FewSmem {
+    uint64_t full[kFewStages], empty[kFewStages], sum_full[2], sum_empty[2], ready, done;
+    uint32_t tmem, failed;
+};
+static_assert(sizeof(FewSmem) <= 256, "barriers");
+
+// Four neighbouring values, zeros beyond the row's end.
+template <typename T>
+__device__ __forceinline__ void load4(const T* p, uint32_t left, bool wide, float (&v)[4]) {
+    if (wide && left >= 4) {
+        if constexpr (sizeof(T) == 4) {
+            const float4 f = *reinterpret_cast<const float4*>(p);
+            v[0] = f.x; v[1] = f.y; v[2] = f.z; v[3] = f.w;
+        } else {
+            const uint2 raw = *reinterpret_cast<const uint2*>(p);
+            const T* e = reinterpret_cast<const T*>(&raw);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = to_float(e[i]);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = (uint32_t)i < left ? to_float(p[i]) : 0.0f;
+    }
+}
+__device__ __forceinline__ void load4_any(const FewArgs& a, uint32_t row, uint64_t col, float (&v)[4]) {
+    const uint32_t left = col < a.cols ? (uint32_t)(a.cols - col) : 0u;
+    const uint64_t at = row * a.x_stride + col;
+    if (a.x_type == CO3_F32) load4(static_cast<const float*>(a.x) + at, left, a.wide, v);
+    else if (a.x_type == CO3_F16) load4(static_cast<const __half*>(a.x) + at, left, a.wide, v);
+    else load4(static_cast<const __nv_bfloat16*>(a.x) + at, left, a.wide, v);
+}
+
+template <bool kTransposed>
+__global__ void __launch_bounds__(kF8Threads, 1) f8_few_kernel(const __grid_constant__ FewArgs few) {
+    extern __shared__ unsigned char smem_raw[];
+    const LinearArgs& a = few.l;
+    unsigned char* ring = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
+    unsigned char* xs = ring + kFewRing;                              // its blocks, 16 rows of 128 bytes each
+    unsigned char* scales = xs + kFewX;                               // the weights' for each stage, then x's for each group
+    unsigned char* x_scales = scales + kFewStages * kF8Scales;
+    FewSmem& sm = *reinterpret_cast<FewSmem*>(x_scales + (kFewBlocks / 4 + 1) * kF8Scales);
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
+    if (threadIdx.x == 0) {
+        for (uint32_t i = 0; i < kFewStages; ++i) { mbar_init(&sm.full[i], 1); mbar_init(&sm.empty[i], 1); }
+        for (uint32_t i = 0; i < 2; ++i) { mbar_init(&sm.sum_full[i], 1); mbar_init(&sm.sum_empty[i], 8); }
+        mbar_init(&sm.ready, 8);
+        mbar_init(&sm.done, 1);
+        sm.failed = 0;
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(&sm.tmem)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = sm.tmem;
+    volatile uint32_t* failed = &sm.failed;
+    wait_for_previous_kernel();
+
+    const uint32_t part = blockIdx.x % a.split, mt = blockIdx.x / a.split;
+    const uint32_t k0 = (uint32_t)((uint64_t)a.kb * part / a.split), k1 = (uint32_t)((uint64_t)a.kb * (part + 1) / a.split);
+    const bool issues = warp < 2 && elected();
+    if (warp == 0) {
+        uint32_t st = 0, turn = 0;
+        for (uint32_t q = k0; q < k1; ++q) {
+            if (turn > 0 && !f8_wait(&sm.empty[st], (turn - 1) & 1u)) { *failed = 1; break; }
+            if (issues) {
+                const bool with_scales = q == k0 || (q & 3u) == 0;
+                mbar_arrive_expect_tx(&sm.full[st], kF8Tile + (with_scales ? kF8Scales : 0u));
+                bulk_copy_g2s(ring + st * kF8Tile, a.a + q * a.a_block + mt * a.a_tile, kF8Tile, &sm.full[st]);
+                if (with_scales) bulk_copy_g2s(scales + st * kF8Scales, a.a_scales + (q >> 2) * a.a_group + (uint64_t)mt * kF8Scales, kF8Scales, &sm.full[st]);
+            }
+            if (++st == kFewStages) { st = 0; ++turn; }
+        }
+        // copies in flight end before the block does, whoever else has given up
+        for (uint32_t i = 0; i < kFewStages; ++i) {
+            const uint32_t begun = turn + (i < st ? 1u : 0u);
+            if (begun > 0) f8_wait(&sm.full[i], (begun - 1) & 1u);
+        }
+    } else if (warp == 1) {
+        uint32_t st = 0, turn = 0, sum = 0, sum_turn = 0, group = 0, left = 0;
+        bool ok = f8_wait(&sm.ready, 0);
+        for (uint32_t q = k0; q < k1 && ok; ++q) {
+            const bool fresh = left == 0;
+            if (fresh) {
+                left = min(a.blocks, k1 - q);
+                if (sum_turn > 0 && !f8_wait(&sm.sum_empty[sum], (sum_turn - 1) & 1u)) { ok = false; break; }
+            }
+            --left;
+            if (!f8_wait(&sm.full[st], turn & 1u)) { ok = false; break; }
+            tc_fence_after();
+            const bool with_scales = q == k0 || (q & 3u) == 0;
+            // the columns of eight groups ago are free: fewer than kFewStages blocks are under way
+            if (with_scales) group = (group + 1) % kScaleTurns;
+            if (issues) {
+                const uint32_t d = tmem + sum * kFewRows, sa = tmem + kTmemScales + group * kScaleCols, sb = sa + 4;
+                if (with_scales) {
+                    f8_scales_in(sa, smem_addr(scales + st * kF8Scales));
+                    f8_scales_in(sb, smem_addr(x_scales + ((q >> 2) - (k0 >> 2)) * kF8Scales));
+                }
+                const uint32_t at = smem_addr(ring + st * kF8Tile), bt = smem_addr(xs + (q - k0) * (kFewRows * 128u));
+                switch (q & 3u) {
+                    case 0: multiply_block<kTransposed, 0>(d, at, bt, kFewRows, sa, sb, !fresh); break;
+                    case 1: multiply_block<kTransposed, 1>(d, at, bt, kFewRows, sa, sb, !fresh); break;
+                    case 2: multiply_block<kTransposed, 2>(d, at, bt, kFewRows, sa, sb, !fresh); break;
+                    default: multiply_block<kTransposed, 3>(d, at, bt, kFewRows, sa, sb, !fresh); break;
+                }
+                tc_commit(&sm.empty[st]);
+                if (left == 0) tc_commit(&sm.sum_full[sum]);
+            }
+            if (left == 0 && ++sum == 2) { sum = 0; ++sum_turn; }
+            if (++st == kFewStages) { st = 0; ++turn; }
+        }
+        if (!ok) *failed = 1;
+        if (issues) tc_commit(&sm.done);
+        f8_wait(&sm.done, 0);
+    } else if (warp >= 4) {
+        // rows of a block by warps, four columns a lane; rows that are not there stay as they are: they reach no sum that counts
+        const uint32_t units = (k1 - k0) * a.rows;
+        constexpr uint32_t kAtOnce = 4;
+        for (uint32_t u0 = warp - 4u; u0 < units; u0 += 8 * kAtOnce) {
+            float v[kAtOnce][4];
+            uint32_t copied[kAtOnce], byte[kAtOnce];
+#pragma unroll
+            for (uint32_t i = 0; i < kAtOnce; ++i) {
+                const uint32_t u = u0 + 8 * i, q = k0 + u / a.rows, r = u % a.rows;
+                if (u >= units) continue;
+                if (few.x) {
+                    load4_any(few, r, q * 128ull + lane * 4u, v[i]);
+                } else {
+                    copied[i] = *reinterpret_cast<const uint32_t*>(a.b + q * a.b_block + r * 128u + lane * 4u);
+                    byte[i] = a.b_scales[(q >> 2) * a.b_group + f8_scale_at(r, q)];
+                }
+            }
+#pragma unroll
+            for (uint32_t i = 0; i < kAtOnce; ++i) {
+                const uint32_t u = u0 + 8 * i, q = k0 + u / a.rows, r = u % a.rows;
+                if (u >= units) continue;
+                const uint32_t piece = f8_piece(r, lane >> 2) + (lane & 3u) * 4u;
+                unsigned char* to = xs + (q - k0) * (kFewRows * 128u) + r * 128u;
+                if (few.x) {
+                    uint32_t m = max(max(f8_magnitude(v[i][0]), f8_magnitude(v[i][1])), max(f8_magnitude(v[i][2]), f8_magnitude(v[i][3])));
+                    m = __reduce_max_sync(0xffffffffu, m);
+                    int e = f8_exponent(m);
+                    if (m > kF8Rare) {
+                        m = 0;
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) m = max(m, f8_finite_magnitude(v[i][k]));
+                        e = f8_exponent(__reduce_max_sync(0xffffffffu, m));
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) v[i][k] = f8_rare(v[i][k], e);
+                    }
+                    const float inverse = power_of_two(-e);
+                    const uint32_t w = f8_from4(__fmul_rn(v[i][0], inverse), __fmul_rn(v[i][1], inverse), __fmul_rn(v[i][2], inverse), __fmul_rn(v[i][3], inverse));
+                    byte[i] = (uint32_t)(e + 127);
+                    *reinterpret_cast<uint32_t*>(to + piece) = w;
+                    if (mt == 0) {
+                        *reinterpret_cast<uint32_t*>(few.x8 + q * a.b_block + r * 128u + piece) = w;
+                        if (lane == 0) few.x8_scales[(q >> 2) * a.b_group + f8_scale_at(r, q)] = (uint8_t)byte[i];
+                    }
+                } else {
+                    *reinterpret_cast<uint32_t*>(to + lane * 4u) = copied[i];  // (swizzled already)
+                }
+                if (lane == 0) x_scales[((q >> 2) - (k0 >> 2)) * kF8Scales + f8_scale_at(r, q)] = (uint8_t)byte[i];
+            }
+        }
+        fence_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sm.ready);
+
+        const uint32_t quad = warp & 3u, half = (warp - 4u) >> 2, row = quad * 32u + lane;
+        constexpr int kHalf = kFewRows / 2;
+        uint32_t sum = 0, sum_turn = 0;
+        float acc[kHalf];
+        bool ok = true;
+        for (uint32_t q = k0; q < k1; q += a.blocks) {
+            ok = lane != 0 || f8_wait(&sm.sum_full[sum], sum_turn & 1u);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            tc_fence_after();
+            take_sums(tmem + ((quad * 32u) << 16) + sum * kFewRows + half * kHalf, q == k0, acc);
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sm.sum_empty[sum]);
+            if (++sum == 2) { sum = 0; ++sum_turn; }
+        }
+        if (!ok) {
+            *failed = 1;
+        } else {  // into the ring, of which no copy and no product is left
+            float* to = reinterpret_cast<float*>(ring) + half * kHalf * 128u + row;
+#pragma unroll
+            for (int i = 0; i < kHalf; ++i) to[i * 128] = acc[i];
+        }
+    }
+    __syncwarp();
+    __syncthreads();
+    cluster_sync();
+    // everybody's part is there; each block adds some of the entries in order
+    if (!*failed && warp >= 4) {
+        const uint32_t all = a.rows * 128u, i1 = all * (part + 1) / a.split;
+        for (uint32_t i = all * part / a.split + threadIdx.x - 128u; i < i1; i += 256u) {
+            const uint32_t r = i >> 7, feature = mt * 128u + (i & 127u);
+            float v = 0.0f;
+            for (uint32_t p = 0; p < a.split; ++p) v = __fadd_rn(v, load_peer(smem_addr(ring) + i * 4u, p));
+            if (feature < a.features) write_any<1>(a, feature, r, a.bias ? a.bias[feature] : 0.0f, &v);
+        }
+    }
+    tc_fence_before();
+    cluster_sync();  // nobody leaves while its part is read
+    tc_fence_after();
+    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+    if (threadIdx.x == 0 && *failed && a.res) atomicExch(&a.res->status, CO3_ERR_CUDA);
+}
+
 int device_sms(uint32_t* out) {
     static std::atomic<int> known[64];
     int dev = 0;
@@ -503,8 +736,8 @@ int device_sms(uint32_t* out) {
 }
 
 // Blocks of a cluster (1: none) work on kernel<smem>.
-template <auto* kKernel, uint32_t kSmem>
-int launch_clusters(const LinearArgs& a, uint32_t blocks, uint32_t cluster, cudaStream_t st) {
+template <auto* kKernel, uint32_t kSmem, typename Args>
+int launch_clusters(const Args& a, uint32_t blocks, uint32_t cluster, cudaStream_t st) {
     static std::atomic<bool> ready[64];
     int dev = 0;
     CO3_CUDA(cudaGetDevice(&dev));
@@ -541,12 +774,16 @@ int launch_pairs(LinearArgs a, bool transposed, uint32_t sms, cudaStream_t st) {
     return transposed ? launch_clusters<f8_pair_kernel<true>, kPairSmem>(a, blocks, 2, st) : launch_clusters<f8_pair_kernel<false>, kPairSmem>(a, blocks, 2, st);
 }
 
+// Blocks that divide a tile's sum: as many as leave none waiting, two blocks of columns each at least.
+uint32_t split_of(uint64_t tiles, uint32_t kb, uint32_t sms) {
+    uint32_t split = 1;
+    while (split < kMaxSplit && tiles * split * 2 <= sms && kb >= split * 4) split *= 2;
+    return split;
+}
 template <int kN>
 int launch_tile(LinearArgs a, bool transposed, uint32_t sms, cudaStream_t st) {
     a.n_tiles = (a.rows + kN - 1) / kN;
-    const uint64_t tiles = (uint64_t)a.m_tiles * a.n_tiles;
-    a.split = 1;
-    while (a.split < kMaxSplit && tiles * a.split * 2 <= sms && a.kb >= a.split * 4) a.split *= 2;
+    a.split = split_of((uint64_t)a.m_tiles * a.n_tiles, a.kb, sms);
     return transposed ? launch_linear<kN, true>(a, sms, st) : launch_linear<kN, false>(a, sms, st);
 }
 
@@ -574,10 +811,6 @@ int co3_f8_linear(const void* x, int x_type, uint64_t x_row_stride, void* x8, si
     uint32_t sms = 0;
     int e = device_sms(&sms);
     if (e != CO3_OK) return e;
-    if (x) {
-        e = co3_f8_pack(x, x_type, rows, from, x_row_stride, CO3_F8_ROWS, x8, x8_bytes, stream);
-        if (e != CO3_OK) return e;
-    }
     const uint8_t *w = static_cast<const uint8_t*>(w8), *b = static_cast<const uint8_t*>(x8);
     LinearArgs a = {};
     a.a = w;
@@ -599,7 +832,19 @@ int co3_f8_linear(const void* x, int x_type, uint64_t x_row_stride, void* x8, si
     a.blocks = y_type == CO3_F32 ? kBlocksF32 : kBlocks16;
     a.bias = bias;
     a.res = res;
-    if (rows <= 16) return launch_tile<16>(a, transposed != 0, sms, st);
+    if (rows <= kFewRows) {
+        a.split = split_of(a.m_tiles, a.kb, sms);
+        if ((a.kb + a.split - 1) / a.split <= kFewBlocks) {
+            FewArgs f = {a, x, x_type, x_row_stride, from, 0, static_cast<uint8_t*>(x8), static_cast<uint8_t*>(x8) + lx.scales};
+            f.wide = x && aligned(x, 4 * type_size(x_type)) && x_row_stride % 4 == 0;
+            return transposed ? launch_clusters<f8_few_kernel<true>, kFewSmem>(f, a.m_tiles * a.split, a.split, st)
+                              : launch_clusters<f8_few_kernel<false>, kFewSmem>(f, a.m_tiles * a.split, a.split, st);
+        }
+    }
+    if (x) {
+        e = co3_f8_pack(x, x_type, rows, from, x_row_stride, CO3_F8_ROWS, x8, x8_bytes, stream);
+        if (e != CO3_OK) return e;
+    }
     if (rows <= 64 || (uint64_t)a.m_tiles * ((rows + 127u) / 128u) * 2 <= sms) return launch_tile<64>(a, transposed != 0, sms, st);
     if (rows <= 128 || (uint64_t)a.m_tiles * ((rows + 255u) / 256u) <= sms) return launch_tile<128>(a, transposed != 0, sms, st);
     return launch_pairs(a, transposed != 0, sms, st);

@@ -428,30 +428,45 @@ struct JoinArgs {
     uint32_t clients, blocks0;  // blocks of the first sum
     int accumulate;
 };
+constexpr uint32_t kJoinEach = 4;  // entries of a thread
 __global__ void __launch_bounds__(256) f8_join_kernel(const __grid_constant__ JoinArgs a) {
     wait_for_previous_kernel();
     const bool second = blockIdx.x >= a.blocks0;
     const Join& j = a.j[second];
-    const uint64_t all = j.count * a.clients, step = (second ? gridDim.x - a.blocks0 : a.blocks0) * 256ull;
-    for (uint64_t i = (blockIdx.x - (second ? a.blocks0 : 0u)) * 256ull + threadIdx.x; i < all; i += step) {
-        const uint64_t u = a.clients == 1 ? 0 : i / j.count;
-        float* to = j.to + u * a.client_stride + (i - u * j.count);
-        float s = 0.0f;
-#pragma unroll 8
-        for (uint32_t p = 0; p < j.parts; ++p) s = __fadd_rn(s, j.from[p * all + i]);
-        *to = a.accumulate ? __fadd_rn(*to, s) : s;
-    }
+    const uint64_t all = j.count * a.clients, i0 = (blockIdx.x - (second ? a.blocks0 : 0u)) * (256ull * kJoinEach) + threadIdx.x;
+    float* to = j.to + blockIdx.y * a.client_stride;
+    const float* from = j.from + blockIdx.y * j.count;
+    float s[kJoinEach];
+#pragma unroll
+    for (uint32_t e = 0; e < kJoinEach; ++e) s[e] = 0.0f;
+#pragma unroll 4
+    for (uint32_t p = 0; p < j.parts; ++p)
+#pragma unroll
+        for (uint32_t e = 0; e < kJoinEach; ++e)
+            if (i0 + e * 256u < j.count) s[e] = __fadd_rn(s[e], __ldcs(from + p * all + i0 + e * 256u));
+#pragma unroll
+    for (uint32_t e = 0; e < kJoinEach; ++e)
+        if (i0 + e * 256u < j.count) to[i0 + e * 256u] = a.accumulate ? __fadd_rn(to[i0 + e * 256u], s[e]) : s[e];
 }
 int launch_join(const Join& first, const Join& second, uint32_t clients, uint64_t client_stride, int accumulate, cudaStream_t st) {
     JoinArgs a = {{first, second}, client_stride, clients, 0, accumulate};
     uint32_t blocks[2];
     for (int i = 0; i < 2; ++i) {
         if (!a.j[i].to) a.j[i].count = 0;
-        blocks[i] = (uint32_t)std::min<uint64_t>((a.j[i].count * clients + 255u) / 256u, 148 * 16);
+        blocks[i] = (uint32_t)((a.j[i].count + 256u * kJoinEach - 1) / (256u * kJoinEach));
     }
     if (blocks[0] + blocks[1] == 0) return CO3_OK;
     a.blocks0 = blocks[0];
-    CO3_CUDA(launch_behind(f8_join_kernel, dim3(blocks[0] + blocks[1]), dim3(256), 0, st, a));
+    // (a grid's second dimension ends at 65535)
+    for (uint32_t u0 = 0; u0 < clients; u0 += 65535u) {
+        const uint32_t n = std::min(clients - u0, 65535u);
+        CO3_CUDA(launch_behind(f8_join_kernel, dim3(blocks[0] + blocks[1], n), dim3(256), 0, st, a));
+        for (int i = 0; i < 2; ++i) {
+            if (!a.j[i].to) continue;
+            a.j[i].to += n * client_stride;
+            if (a.j[i].from) a.j[i].from += n * a.j[i].count;
+        }
+    }
     return CO3_OK;
 }
 

@@ -87,6 +87,14 @@ def test_large(rows, ins, outs, transposed, type_):
     run(rows, ins, outs, transposed, type_, bias=not transposed)
 
 
+@pytest.mark.parametrize("rows", [1, 7, 16])
+@pytest.mark.parametrize("ins,outs", [(9000, 130), (4300, 9600), (128 * 64, 9600), (40000, 130)])
+def test_few_rows_of_long_sums(ins, outs, rows):
+    """Sums divided among the blocks of a cluster, and ones too long for that."""
+    run(rows, ins, outs, False, ("f32", "f16", "bf16")[rows % 3], pad=rows % 2)
+    run(rows, outs, ins, True, ("f32", "f16", "bf16")[(rows + 1) % 3], bias=False)
+
+
 def test_small_sums_next_to_large_ones():
     """One row of x against all others far smaller: rows do not see each other's scales."""
     x = torch.full((200, 256), 1e-20, device="cuda")
