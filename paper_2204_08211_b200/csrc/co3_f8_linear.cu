@@ -119,12 +119,44 @@ __device__ __forceinline__ void take_sums(uint32_t from, bool first, float (&acc
     }
 }
 
-__device__ __forceinline__ float load_peer(uint32_t addr, uint32_t rank) {
-    uint32_t at;
-    float v;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(addr), "r"(rank));
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
-    return v;
+// The sums of four neighbouring entries over the cluster's blocks, in order, from the same place in each one's shared memory.
+__device__ __forceinline__ float4 add_parts(uint32_t addr, uint32_t split) {
+    float4 v[kMaxSplit];
+#pragma unroll
+    for (uint32_t p = 0; p < kMaxSplit; ++p) {
+        if (p >= split) break;
+        uint32_t at;
+        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(addr), "r"(p));
+        asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[p].x), "=f"(v[p].y), "=f"(v[p].z), "=f"(v[p].w) : "r"(at) : "memory");
+    }
+    float4 s = v[0];
+#pragma unroll
+    for (uint32_t p = 1; p < kMaxSplit; ++p) {
+        if (p >= split) break;
+        s = make_float4(__fadd_rn(s.x, v[p].x), __fadd_rn(s.y, v[p].y), __fadd_rn(s.z, v[p].z), __fadd_rn(s.w, v[p].w));
+    }
+    return s;
+}
+// This block's part of a tile whose parts lie in shared memory, 128 features for each row of x: `rows` of them from row n0 on, by 256
+// threads.
+template <typename T>
+__device__ __forceinline__ void join_parts(const LinearArgs& a, uint32_t sums, uint32_t part, uint32_t feature0, uint32_t n0, uint32_t rows, uint32_t tid) {
+    const uint32_t all = rows * 32u, i1 = all * (part + 1) / a.split, f = feature0 + (tid & 31u) * 4u;
+    for (uint32_t i = all * part / a.split / 32u * 32u + tid; i < i1; i += 256u) {
+        if (i < all * part / a.split) continue;
+        const uint32_t r = i >> 5;
+        const float4 v = add_parts(sums + i * 16u, a.split);
+        const float w[4] = {v.x, v.y, v.z, v.w};
+        T* p = static_cast<T*>(a.y) + (uint64_t)(n0 + r) * a.y_stride + f;
+#pragma unroll
+        for (uint32_t k = 0; k < 4; ++k)
+            if (f + k < a.features) p[k] = from_float<T>(a.bias ? __fadd_rn(w[k], a.bias[f + k]) : w[k]);
+    }
+}
+__device__ __forceinline__ void join_parts_any(const LinearArgs& a, uint32_t sums, uint32_t part, uint32_t feature0, uint32_t n0, uint32_t rows, uint32_t tid) {
+    if (a.y_type == CO3_F32) join_parts<float>(a, sums, part, feature0, n0, rows, tid);
+    else if (a.y_type == CO3_F16) join_parts<__half>(a, sums, part, feature0, n0, rows, tid);
+    else join_parts<__nv_bfloat16>(a, sums, part, feature0, n0, rows, tid);
 }
 
 // A lane's sums of kCount rows of x, from row `first` on.
@@ -282,15 +314,8 @@ __global__ void __launch_bounds__(kF8Threads, 1) f8_linear_kernel(const __grid_c
             // everybody's part is there; each block takes some of the columns
             __syncwarp();
             cluster_sync();
-            const uint32_t mt = first % a.m_tiles, n0 = first / a.m_tiles * kN, feature = mt * 128u + row;
-            const float bias = a.bias && feature < a.features ? a.bias[feature] : 0.0f;
-            const uint32_t c0 = kN * part / a.split, c1 = kN * (part + 1) / a.split;
-            for (uint32_t c = c0 + half; c < c1 && n0 + c < a.rows && !*failed; c += 2) {
-                const uint32_t at = smem_addr(ring) + (c * 128u + row) * 4u;
-                float v = 0.0f;
-                for (uint32_t p = 0; p < a.split; ++p) v = __fadd_rn(v, load_peer(at, p));
-                write_any<1>(a, feature, n0 + c, bias, &v);
-            }
+            const uint32_t n0 = first / a.m_tiles * kN;
+            if (!*failed) join_parts_any(a, smem_addr(ring), part, first % a.m_tiles * 128u, n0, min((uint32_t)kN, a.rows - n0), threadIdx.x - 128u);
         }
     }
     __syncwarp();
@@ -313,7 +338,7 @@ constexpr uint32_t kPairStageBytes = 2 * kF8Tile, kPairScaleBytes = 3 * kF8Scale
 constexpr uint32_t kPairSmem = 1024 + kPairStages * (kPairStageBytes + kPairScaleBytes) + 256;
 
 struct PairSmem {
-    uint64_t full[kPairStages], peer[kPairStages], empty[kPairStages], sum_full, sum_empty, done;
+    uint64_t full[kPairStages], empty[kPairStages], sum_full, sum_empty, done;
     uint32_t tmem, failed;
 };
 static_assert(sizeof(PairSmem) <= 256, "barriers");
@@ -347,7 +372,7 @@ __global__ void __launch_bounds__(kF8Threads, 1) f8_pair_kernel(const __grid_con
     PairSmem& sm = *reinterpret_cast<PairSmem*>(scales + kPairStages * kPairScaleBytes);
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u, rank = cluster_rank();
     if (threadIdx.x == 0) {
-        for (uint32_t i = 0; i < kPairStages; ++i) { mbar_init(&sm.full[i], 1); mbar_init(&sm.peer[i], 1); mbar_init(&sm.empty[i], 1); }
+        for (uint32_t i = 0; i < kPairStages; ++i) { mbar_init(&sm.full[i], rank == 0 ? 2 : 1); mbar_init(&sm.empty[i], 1); }
         mbar_init(&sm.sum_full, 1);
         mbar_init(&sm.sum_empty, 16);
         mbar_init(&sm.done, 1);
@@ -399,13 +424,13 @@ __global__ void __launch_bounds__(kF8Threads, 1) f8_pair_kernel(const __grid_con
                 if (begun > 0) f8_wait(&sm.full[i], (begun - 1) & 1u);
             }
         } else if (warp == 1 && rank == 1) {
-            // tells the first block what has arrived here
+            // tells the first block what has arrived here: its barrier waits for both
             uint32_t st = 0, turn = 0;
             bool ok = true;
             for (uint32_t t = first; t < tiles && ok; t += step)
                 for (uint32_t q = 0; q < a.kb; ++q) {
                     if (!f8_wait(&sm.full[st], turn & 1u)) { ok = false; break; }
-                    if (issues) mbar_arrive_at(&sm.peer[st], 0);
+                    if (issues) mbar_arrive_at(&sm.full[st], 0);
                     if (++st == kPairStages) { st = 0; ++turn; }
                 }
             if (!ok) *failed = 1;
@@ -423,7 +448,7 @@ __global__ void __launch_bounds__(kF8Threads, 1) f8_pair_kernel(const __grid_con
                         ++sums;
                     }
                     --left;
-                    if (!f8_wait(&sm.full[st], turn & 1u) || !f8_wait(&sm.peer[st], turn & 1u)) { ok = false; break; }
+                    if (!f8_wait(&sm.full[st], turn & 1u)) { ok = false; break; }
                     tc_fence_after();
                     if ((q & 3u) == 0) group = (group + 1) % kScaleTurns;
                     if (issues) {
@@ -706,15 +731,7 @@ __global__ void __launch_bounds__(kF8Threads, 1) f8_few_kernel(const __grid_cons
     __syncthreads();
     cluster_sync();
     // everybody's part is there; each block adds some of the entries in order
-    if (!*failed && warp >= 4) {
-        const uint32_t all = a.rows * 128u, i1 = all * (part + 1) / a.split;
-        for (uint32_t i = all * part / a.split + threadIdx.x - 128u; i < i1; i += 256u) {
-            const uint32_t r = i >> 7, feature = mt * 128u + (i & 127u);
-            float v = 0.0f;
-            for (uint32_t p = 0; p < a.split; ++p) v = __fadd_rn(v, load_peer(smem_addr(ring) + i * 4u, p));
-            if (feature < a.features) write_any<1>(a, feature, r, a.bias ? a.bias[feature] : 0.0f, &v);
-        }
-    }
+    if (!*failed && warp >= 4) join_parts_any(a, smem_addr(ring), part, mt * 128u, 0, a.rows, threadIdx.x - 128u);
     tc_fence_before();
     cluster_sync();  // nobody leaves while its part is read
     tc_fence_after();
@@ -845,9 +862,18 @@ int co3_f8_linear(const void* x, int x_type, uint64_t x_row_stride, void* x8, si
         e = co3_f8_pack(x, x_type, rows, from, x_row_stride, CO3_F8_ROWS, x8, x8_bytes, stream);
         if (e != CO3_OK) return e;
     }
-    if (rows <= 64 || (uint64_t)a.m_tiles * ((rows + 127u) / 128u) * 2 <= sms) return launch_tile<64>(a, transposed != 0, sms, st);
-    if (rows <= 128 || (uint64_t)a.m_tiles * ((rows + 255u) / 256u) <= sms) return launch_tile<128>(a, transposed != 0, sms, st);
-    return launch_pairs(a, transposed != 0, sms, st);
+    // The estimated time of each kind of tile, in ns: rounds of tiles, a stage of each kind, what a tile costs besides, and the join of a
+    // divided sum.  us measured, pairs / 128 / 64 rows: 512 x 4096 x 4096 22 / 25 / 37, 2048 x 2048 x 2048 19 / 28 / 39, 1501 x 1023 x
+    // 1001 15.5 / 13.3 / 15.5, 3000 x 128 x 1000 12.2 / 11.6 / 10.4.
+    auto single = [&](uint32_t n, uint32_t stage, uint32_t besides) {
+        const uint64_t tiles = (uint64_t)a.m_tiles * ((rows + n - 1) / n);
+        const uint32_t split = split_of(tiles, a.kb, sms);
+        return (tiles * split + sms - 1) / sms * ((uint64_t)(a.kb + split - 1) / split * stage + besides + (split > 1 ? 1500 : 0));
+    };
+    const uint64_t pairs = (uint64_t)((a.m_tiles + 1) / 2) * ((rows + kPairCols - 1) / kPairCols);
+    const uint64_t by_pairs = (pairs + sms / 2 - 1) / (sms / 2) * ((uint64_t)a.kb * 370 + 5500), by_128 = single(128, 470, 2500), by_64 = single(64, 430, 1500);
+    if (by_pairs <= by_128 && by_pairs <= by_64) return launch_pairs(a, transposed != 0, sms, st);
+    return by_128 < by_64 ? launch_tile<128>(a, transposed != 0, sms, st) : launch_tile<64>(a, transposed != 0, sms, st);
 }
 
 }  // extern "C"

@@ -207,7 +207,7 @@ __global__ void __launch_bounds__(256) f8_operands_kernel(const __grid_constant_
 // Products
 // ------------------------------------------------------------------------------------------------
 struct WeightSmem {
-    uint64_t full[kMaxStagesW], peer[kMaxStagesW], empty[kMaxStagesW], sum_full[2], sum_empty[2], done;
+    uint64_t full[kMaxStagesW], empty[kMaxStagesW], sum_full[2], sum_empty[2], done;
     uint32_t tmem, failed;
 };
 static_assert(sizeof(WeightSmem) <= 256, "barriers");
@@ -253,7 +253,7 @@ __global__ void __launch_bounds__(kF8Threads, 1) f8_weight_kernel(const __grid_c
     WeightSmem& sm = *reinterpret_cast<WeightSmem*>(ring + kRing);
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u, rank = cluster_rank();
     if (threadIdx.x == 0) {
-        for (uint32_t i = 0; i < kStages; ++i) { mbar_init(&sm.full[i], 1); mbar_init(&sm.peer[i], 1); mbar_init(&sm.empty[i], 1); }
+        for (uint32_t i = 0; i < kStages; ++i) { mbar_init(&sm.full[i], rank == 0 ? 2 : 1); mbar_init(&sm.empty[i], 1); }
         for (uint32_t i = 0; i < 2; ++i) { mbar_init(&sm.sum_full[i], 1); mbar_init(&sm.sum_empty[i], 16); }
         mbar_init(&sm.done, 1);
         sm.failed = 0;
@@ -304,14 +304,14 @@ __global__ void __launch_bounds__(kF8Threads, 1) f8_weight_kernel(const __grid_c
                 if (begun > 0) f8_wait(&sm.full[i], (begun - 1) & 1u);
             }
         } else if (warp == 1 && rank == 1) {
-            // tells the first block what has arrived here
+            // tells the first block what has arrived here: its barrier waits for both
             uint32_t st = 0, turn = 0;
             bool ok = true;
             for (uint32_t t = first; t < tiles && ok; t += step) {
                 const Place p = find_place(a, t);
                 for (uint32_t c = p.c0; c < p.c1; ++c) {
                     if (!f8_wait(&sm.full[st], turn & 1u)) { ok = false; break; }
-                    if (issues) mbar_arrive_at(&sm.peer[st], 0);
+                    if (issues) mbar_arrive_at(&sm.full[st], 0);
                     if (++st == kStages) { st = 0; ++turn; }
                 }
             }
@@ -325,7 +325,7 @@ __global__ void __launch_bounds__(kF8Threads, 1) f8_weight_kernel(const __grid_c
                 for (uint32_t c = p.c0; c < p.c1; ++c) {
                     const uint32_t in_sum = (c - p.c0) % kSumChunks;
                     if (in_sum == 0 && sum_turn > 0 && !f8_wait(&sm.sum_empty[sum], (sum_turn - 1) & 1u)) { ok = false; break; }
-                    if (!f8_wait(&sm.full[st], turn & 1u) || !f8_wait(&sm.peer[st], turn & 1u)) { ok = false; break; }
+                    if (!f8_wait(&sm.full[st], turn & 1u)) { ok = false; break; }
                     tc_fence_after();
                     const bool last = in_sum == kSumChunks - 1 || c + 1 == p.c1;
                     if (issues) {
@@ -414,7 +414,8 @@ __global__ void __launch_bounds__(kF8Threads, 1) f8_weight_kernel(const __grid_c
 }
 
 // ------------------------------------------------------------------------------------------------
-// to[u][i] (+)= sum over the parts of from[part][u][i], in order; with no parts: zeros.  Two such sums in one launch.
+// to[u][i] (+)= sum over the parts of from[part][u][i], in order; with no parts: zeros.  Two such sums in one launch: db, of few
+// columns and up to hundreds of parts, first (eight threads a column), then dw.
 // ------------------------------------------------------------------------------------------------
 struct Join {
     const float* from;
@@ -423,48 +424,59 @@ struct Join {
     uint32_t parts;
 };
 struct JoinArgs {
-    Join j[2];
+    Join db, dw;
     uint64_t client_stride;
-    uint32_t clients, blocks0;  // blocks of the first sum
+    uint32_t clients, db_blocks;
     int accumulate;
 };
 constexpr uint32_t kJoinEach = 4;  // entries of a thread
 __global__ void __launch_bounds__(256) f8_join_kernel(const __grid_constant__ JoinArgs a) {
+    __shared__ float sums[8][32];
     wait_for_previous_kernel();
-    const bool second = blockIdx.x >= a.blocks0;
-    const Join& j = a.j[second];
-    const uint64_t all = j.count * a.clients, i0 = (blockIdx.x - (second ? a.blocks0 : 0u)) * (256ull * kJoinEach) + threadIdx.x;
-    float* to = j.to + blockIdx.y * a.client_stride;
-    const float* from = j.from + blockIdx.y * j.count;
+    if (blockIdx.x < a.db_blocks) {
+        const uint64_t i = blockIdx.x * 32ull + (threadIdx.x & 31u), all = a.db.count * a.clients;
+        const float* from = a.db.from + blockIdx.y * a.db.count + i;
+        float s = 0.0f;
+        if (i < a.db.count)
+#pragma unroll 4
+            for (uint32_t p = threadIdx.x >> 5; p < a.db.parts; p += 8) s = __fadd_rn(s, __ldcs(from + p * all));
+        sums[threadIdx.x >> 5][threadIdx.x & 31u] = s;
+        __syncthreads();
+        if (threadIdx.x >= 32 || i >= a.db.count) return;
+        for (uint32_t w = 1; w < 8; ++w) s = __fadd_rn(s, sums[w][threadIdx.x]);
+        float* to = a.db.to + blockIdx.y * a.client_stride + i;
+        *to = a.accumulate ? __fadd_rn(*to, s) : s;
+        return;
+    }
+    const uint64_t all = a.dw.count * a.clients, i0 = (blockIdx.x - a.db_blocks) * (256ull * kJoinEach) + threadIdx.x;
+    float* to = a.dw.to + blockIdx.y * a.client_stride;
+    const float* from = a.dw.from + blockIdx.y * a.dw.count;
     float s[kJoinEach];
 #pragma unroll
     for (uint32_t e = 0; e < kJoinEach; ++e) s[e] = 0.0f;
 #pragma unroll 4
-    for (uint32_t p = 0; p < j.parts; ++p)
+    for (uint32_t p = 0; p < a.dw.parts; ++p)
 #pragma unroll
         for (uint32_t e = 0; e < kJoinEach; ++e)
-            if (i0 + e * 256u < j.count) s[e] = __fadd_rn(s[e], __ldcs(from + p * all + i0 + e * 256u));
+            if (i0 + e * 256u < a.dw.count) s[e] = __fadd_rn(s[e], __ldcs(from + p * all + i0 + e * 256u));
 #pragma unroll
     for (uint32_t e = 0; e < kJoinEach; ++e)
-        if (i0 + e * 256u < j.count) to[i0 + e * 256u] = a.accumulate ? __fadd_rn(to[i0 + e * 256u], s[e]) : s[e];
+        if (i0 + e * 256u < a.dw.count) to[i0 + e * 256u] = a.accumulate ? __fadd_rn(to[i0 + e * 256u], s[e]) : s[e];
 }
-int launch_join(const Join& first, const Join& second, uint32_t clients, uint64_t client_stride, int accumulate, cudaStream_t st) {
-    JoinArgs a = {{first, second}, client_stride, clients, 0, accumulate};
-    uint32_t blocks[2];
-    for (int i = 0; i < 2; ++i) {
-        if (!a.j[i].to) a.j[i].count = 0;
-        blocks[i] = (uint32_t)((a.j[i].count + 256u * kJoinEach - 1) / (256u * kJoinEach));
-    }
-    if (blocks[0] + blocks[1] == 0) return CO3_OK;
-    a.blocks0 = blocks[0];
+int launch_join(const Join& dw, const Join& db, uint32_t clients, uint64_t client_stride, int accumulate, cudaStream_t st) {
+    JoinArgs a = {db, dw, client_stride, clients, 0, accumulate};
+    if (!a.db.to) a.db.count = 0;
+    if (!a.dw.to) a.dw.count = 0;
+    a.db_blocks = (uint32_t)((a.db.count + 31u) / 32u);
+    const uint32_t blocks = a.db_blocks + (uint32_t)((a.dw.count + 256u * kJoinEach - 1) / (256u * kJoinEach));
+    if (blocks == 0) return CO3_OK;
     // (a grid's second dimension ends at 65535)
     for (uint32_t u0 = 0; u0 < clients; u0 += 65535u) {
         const uint32_t n = std::min(clients - u0, 65535u);
-        CO3_CUDA(launch_behind(f8_join_kernel, dim3(blocks[0] + blocks[1], n), dim3(256), 0, st, a));
-        for (int i = 0; i < 2; ++i) {
-            if (!a.j[i].to) continue;
-            a.j[i].to += n * client_stride;
-            if (a.j[i].from) a.j[i].from += n * a.j[i].count;
+        CO3_CUDA(launch_behind(f8_join_kernel, dim3(blocks, n), dim3(256), 0, st, a));
+        for (Join* j : {&a.db, &a.dw}) {
+            if (j->to) j->to += n * client_stride;
+            if (j->from) j->from += n * j->count;
         }
     }
     return CO3_OK;
@@ -487,9 +499,16 @@ bool weight_plan(uint64_t rows, uint32_t outs, uint32_t ins, uint32_t clients, u
     w->chunks = (uint32_t)((rows + kChunk - 1) / kChunk);
     const uint64_t all = (uint64_t)clients * w->chunks;
     if (all * std::max(w->k_tiles, w->groups) >= (1ull << 40) / kPlane16 / 4) return false;
-    // the tiles alone leave pairs of multiprocessors idle: the rows are divided, 128 at least for each part
+    // Rows are divided where that is estimated to save time, in ns: rounds of tiles, 280 a chunk and part of dy, 4000 a tile, and for
+    // the join a launch of 2500 and 5 bytes a ns.  (us, divided or not: 2 x 1501 x 1023 x 1001 fp16 36.4 and 31.8.)
     const uint64_t tiles = std::max<uint64_t>(1, (uint64_t)(w->k_tiles + 1) / 2 * w->n_tiles * clients);
-    w->parts = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(kPairsAssumed / tiles, w->chunks / 2));
+    const uint64_t size = (uint64_t)clients * outs * ins * 4, most = std::min<uint64_t>(kPairsAssumed, w->chunks / 2);
+    w->parts = 1;
+    uint64_t best = ~0ull;
+    for (uint32_t p = 1; p <= std::max<uint64_t>(1, most); ++p) {
+        const uint64_t ns = (tiles * p + kPairsAssumed - 1) / kPairsAssumed * ((uint64_t)((w->chunks + p - 1) / p) * 280 * pieces + 4000) + (p > 1 ? 2500 + (2ull * p + 1) * size / 5000 : 0);
+        if (ns < best) { best = ns; w->parts = p; }
+    }
     // the sums of dy: as many blocks as the device takes at once, about
     const uint64_t columns = std::max<uint64_t>(1, (uint64_t)w->groups * clients);
     w->db_parts = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>((4 * kSmsAssumed + columns - 1) / columns, w->chunks));
@@ -547,9 +566,13 @@ using namespace co3;
 extern "C" {
 
 int co3_f8_weight_gradient_workspace_bytes(uint64_t rows, uint32_t outs, uint32_t ins, uint32_t n_clients, size_t* out) {
-    WeightPlan w;
-    if (!out || !weight_plan(rows, outs, ins, n_clients, parts_of(CO3_F32), &w)) return CO3_ERR_INVALID_ARG;
-    *out = (size_t)w.bytes;
+    uint64_t most = 0;  // of the three types
+    for (int type : {CO3_F32, CO3_F16, CO3_BF16}) {
+        WeightPlan w;
+        if (!out || !weight_plan(rows, outs, ins, n_clients, parts_of(type), &w)) return CO3_ERR_INVALID_ARG;
+        most = std::max(most, w.bytes);
+    }
+    *out = (size_t)most;
     return CO3_OK;
 }
 
