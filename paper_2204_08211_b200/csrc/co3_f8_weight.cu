@@ -7,7 +7,7 @@
 //
 // A first kernel writes both operands, as the tensor cores read them, to the workspace (doing this inside the product costs every
 // tile the conversion of all its rows: 16384 x 4096 x 4096 bf16 2.02 ms), and sums dy.  The products are
-// tiles of 256 inputs (tensor memory's lanes, so that a warp writes neighbouring entries of dW) by 256 outputs, by pairs of
+// tiles of 256 inputs (tensor memory's lanes, so that a warp writes neighbouring entries of dW) by 256 or 128 outputs, by pairs of
 // blocks; a stage is 64 rows, a row of the batch per row of shared memory.  After every 256 rows the sums are taken out and
 // added up in registers (the tensor core cuts what it adds towards zero).  Few tiles: the rows are divided, and a last kernel adds
 // the parts in order.
@@ -24,7 +24,7 @@ namespace {
 
 constexpr uint32_t kChunk = 64;              // rows of a stage
 constexpr uint32_t kSumChunks = 4;           // chunks that tensor memory adds up
-constexpr uint32_t kOuts = 256;              // outputs of a tile; two groups of 128
+constexpr uint32_t kOuts = 256;              // outputs of a tile at most; two groups of 128
 constexpr uint32_t kAtom = kChunk * 128;     // bytes of 64 columns of a chunk
 constexpr uint32_t kPlane16 = 2 * kAtom;     // bytes of 128 columns of a chunk
 constexpr uint32_t kRing = 196608;           // bytes of the ring of stages
@@ -45,7 +45,8 @@ struct WeightArgs {
     uint64_t rows;                           // of a client
     uint32_t outs, ins, clients;
     uint32_t k_tiles, groups, chunks;        // blocks of 128 inputs, of 128 outputs, chunks of a client
-    uint32_t n_tiles, parts, db_parts;       // tiles of 256 outputs; row parts of the products, and of the sums of dy
+    uint32_t tile_outs, n_tiles;             // outputs of a tile (128 or 256), tiles of outputs
+    uint32_t parts, db_parts;                // row parts of the products, and of the sums of dy
     unsigned char *ws_x, *ws_dy;
     float *dw_parts, *db_parts_at;           // parts x clients x outs x ins; db_parts x clients x outs
     float *dw, *db;
@@ -233,8 +234,14 @@ __device__ __forceinline__ Place find_place(const WeightArgs& a, uint32_t t) {
     const uint32_t pairs = (a.k_tiles + 1) / 2;
     p.kp = t % pairs;
     t /= pairs;
-    p.n0 = t % a.n_tiles * kOuts;
+    p.n0 = t % a.n_tiles * a.tile_outs;
     t /= a.n_tiles;
+    if (a.parts == 1) {  // (the divisions would take as long as a stage)
+        p.part = p.c0 = 0;
+        p.u = t;
+        p.c1 = a.chunks;
+        return p;
+    }
     p.part = t % a.parts;
     p.u = t / a.parts;
     p.c0 = (uint32_t)((uint64_t)a.chunks * p.part / a.parts);
@@ -242,7 +249,7 @@ __device__ __forceinline__ Place find_place(const WeightArgs& a, uint32_t t) {
     return p;
 }
 // Outputs of a tile that are multiplied: 128, half of them in each block, or 256.
-__device__ __forceinline__ uint32_t tile_cols(const WeightArgs& a, uint32_t n0) { return a.outs - n0 > 128u ? 256u : 128u; }
+__device__ __forceinline__ uint32_t tile_cols(const WeightArgs& a, uint32_t n0) { return a.outs - n0 > 128u ? a.tile_outs : 128u; }
 
 template <int kParts>
 __global__ void __launch_bounds__(kF8Threads, 1) f8_weight_kernel(const __grid_constant__ WeightArgs a) {
@@ -356,26 +363,22 @@ __global__ void __launch_bounds__(kF8Threads, 1) f8_weight_kernel(const __grid_c
         bool ok = true;
         for (uint32_t t = first; t < tiles && ok; t += step) {
             const Place p = find_place(a, t);
-            const uint32_t o0 = p.n0 + half * (kOuts / 2);
+            const uint32_t cols = a.tile_outs / 2, o0 = p.n0 + half * cols;  // columns of a warp
             float acc[kOuts / 2];
             for (uint32_t c = p.c0; c < p.c1; c += kSumChunks) {
                 ok = lane != 0 || f8_wait(&sm.sum_full[sum], sum_turn & 1u);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 tc_fence_after();
-                const uint32_t from = tmem + ((quad * 32u) << 16) + sum * kOuts + half * (kOuts / 2);
+                const uint32_t from = tmem + ((quad * 32u) << 16) + sum * kOuts + half * cols;
                 if (o0 < a.outs) {
-                    if (c == p.c0) {
 #pragma unroll
-                        for (int h = 0; h < (int)kOuts / 2; h += 32) tc_load32(from + h, *reinterpret_cast<float(*)[32]>(acc + h));
-                    } else {
+                    for (int h = 0; h < (int)kOuts / 2; h += 64) {
+                        if ((uint32_t)h >= cols) break;
+                        float w[64];
+                        tc_load(from + h, w);
 #pragma unroll
-                        for (int h = 0; h < (int)kOuts / 2; h += 32) {
-                            float w[32];
-                            tc_load32(from + h, w);
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) acc[h + i] = __fadd_rn(acc[h + i], w[i]);
-                        }
+                        for (int i = 0; i < 64; ++i) acc[h + i] = c == p.c0 ? w[i] : __fadd_rn(acc[h + i], w[i]);
                     }
                 }
                 tc_fence_before();
@@ -386,11 +389,12 @@ __global__ void __launch_bounds__(kF8Threads, 1) f8_weight_kernel(const __grid_c
             if (!ok) break;
             const uint32_t k = (2 * p.kp + rank) * 128u + row;
             if (k < a.ins && o0 < a.outs) {
-                const uint32_t count = min(kOuts / 2, a.outs - o0);
+                const uint32_t count = min(cols, a.outs - o0);
                 const bool add = a.parts == 1 && a.accumulate;
                 float* to = (a.parts > 1 ? a.dw_parts + ((uint64_t)p.part * a.clients + p.u) * a.outs * a.ins : a.dw + p.u * a.client_stride) + (uint64_t)o0 * a.ins + k;
 #pragma unroll
                 for (int i0 = 0; i0 < (int)kOuts / 2; i0 += 16) {
+                    if ((uint32_t)i0 >= count) break;
                     if (add)
 #pragma unroll
                         for (int i = 0; i < 16; ++i)
@@ -486,7 +490,7 @@ int launch_join(const Join& dw, const Join& db, uint32_t clients, uint64_t clien
 // Sizes: they follow from the call's alone, so that the same call gives the same bits everywhere.
 // ------------------------------------------------------------------------------------------------
 struct WeightPlan {
-    uint32_t k_tiles, groups, n_tiles, chunks, parts, db_parts;
+    uint32_t k_tiles, groups, tile_outs, n_tiles, chunks, parts, db_parts;
     uint64_t x, dy, dw, db, bytes;  // offsets in the workspace
 };
 bool weight_plan(uint64_t rows, uint32_t outs, uint32_t ins, uint32_t clients, uint32_t pieces, WeightPlan* w) {
@@ -495,20 +499,27 @@ bool weight_plan(uint64_t rows, uint32_t outs, uint32_t ins, uint32_t clients, u
         return false;
     w->k_tiles = (ins + 127u) / 128u;
     w->groups = (outs + 127u) / 128u;
-    w->n_tiles = (outs + kOuts - 1) / kOuts;
     w->chunks = (uint32_t)((rows + kChunk - 1) / kChunk);
     const uint64_t all = (uint64_t)clients * w->chunks;
     if (all * std::max(w->k_tiles, w->groups) >= (1ull << 40) / kPlane16 / 4) return false;
-    // Rows are divided where that is estimated to save time, in ns: rounds of tiles, 280 a chunk and part of dy, 4000 a tile, and for
-    // the join a launch of 2500 and 5 bytes a ns.  (us, divided or not: 2 x 1501 x 1023 x 1001 fp16 36.4 and 31.8.)
-    const uint64_t tiles = std::max<uint64_t>(1, (uint64_t)(w->k_tiles + 1) / 2 * w->n_tiles * clients);
-    const uint64_t size = (uint64_t)clients * outs * ins * 4, most = std::min<uint64_t>(kPairsAssumed, w->chunks / 2);
-    w->parts = 1;
+    // Outputs of a tile, and how many parts the rows are divided into: the least estimated time, in ns.  Rounds of tiles; a chunk's
+    // products and handing over; what a tile costs besides, its sums written at 30 bytes a cycle above all; for the join a launch of 2500
+    // and 5 bytes a ns.  (us: 2 x 1501 x 1023 x 1001 fp16 divided 36.4, whole 31.8, of 128 outputs 25.7.)
+    const uint64_t pairs_k = (w->k_tiles + 1) / 2, size = (uint64_t)clients * outs * ins * 4, most = std::min<uint64_t>(kPairsAssumed, w->chunks / 2);
     uint64_t best = ~0ull;
-    for (uint32_t p = 1; p <= std::max<uint64_t>(1, most); ++p) {
-        const uint64_t ns = (tiles * p + kPairsAssumed - 1) / kPairsAssumed * ((uint64_t)((w->chunks + p - 1) / p) * 280 * pieces + 4000) + (p > 1 ? 2500 + (2ull * p + 1) * size / 5000 : 0);
-        if (ns < best) { best = ns; w->parts = p; }
-    }
+    for (uint32_t outs_of_tile : {256u, 128u})
+        for (uint32_t p = 1; p <= std::max<uint64_t>(1, most); ++p) {
+            const uint64_t n_tiles = (outs + outs_of_tile - 1) / outs_of_tile, rounds = (pairs_k * n_tiles * clients * p + kPairsAssumed - 1) / kPairsAssumed;
+            const uint64_t chunk = outs_of_tile == 256 ? 280 * pieces + 70 : 140 * pieces + 110;
+            const uint64_t ns = rounds * ((w->chunks + p - 1) / p * chunk + 600 + outs_of_tile * 10) + (p > 1 ? 2500 + (2ull * p + 1) * size / 5000 : 0);
+            if (ns < best) {
+                best = ns;
+                w->tile_outs = outs_of_tile;
+                w->n_tiles = (uint32_t)n_tiles;
+                w->parts = p;
+            }
+        }
+    const uint64_t tiles = pairs_k * w->n_tiles * clients;
     // the sums of dy: as many blocks as the device takes at once, about
     const uint64_t columns = std::max<uint64_t>(1, (uint64_t)w->groups * clients);
     w->db_parts = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>((4 * kSmsAssumed + columns - 1) / columns, w->chunks));
@@ -611,6 +622,7 @@ int co3_f8_weight_gradient(const void* dy, int type, uint64_t dy_row_stride, con
     a.k_tiles = w.k_tiles;
     a.groups = w.groups;
     a.chunks = w.chunks;
+    a.tile_outs = w.tile_outs;
     a.n_tiles = w.n_tiles;
     a.parts = w.parts;
     a.db_parts = w.db_parts;
