@@ -189,7 +189,7 @@ __device__ __forceinline__ void bring_dy(const WeightArgs& a, uint32_t u, uint32
 // Blocks for dy first (one for each client, 128 columns and part of the chunks), then for x (one for each client, block of columns
 // and chunk).
 template <typename T, bool kWide>
-__global__ void __launch_bounds__(256) f8_operands_kernel(const __grid_constant__ WeightArgs a) {
+__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 5 : 3) f8_operands_kernel(const __grid_constant__ WeightArgs a) {
     wait_for_previous_kernel();
     const uint32_t of_dy = a.clients * a.groups * a.db_parts;
     uint32_t b = blockIdx.x;
