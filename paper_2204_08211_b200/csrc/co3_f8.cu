@@ -1,7 +1,7 @@
 // Values to 8-bit blocks and back, and the activation between two layers with its backward pass from what was kept.
 //
 // All of it is bound by memory: one pass, each thread takes 16 bytes at a time where rows allow it.  A warp takes a row's 512
-// columns, four blocks, so that the four exponent bytes leave as one word; two rows at once keep enough loads in flight.  A
+// columns, four blocks, so that the four exponent bytes leave as one word.  A
 // square block is held in a thread block's registers until its largest magnitude is known.
 #include <math.h>
 
@@ -15,7 +15,13 @@ namespace co3 {
 namespace {
 
 constexpr int kWarps = 8;
-constexpr int kRowsAtOnce = 2;
+// Rows that a warp has under way, and blocks of threads that an SM holds at least: two and three, but for GELU, whose arithmetic
+// wants more warps (us: bf16 16384 x 8192 there and back 258 with four blocks, 274 with three; fp32 8192 x 8192 322, and 294 with one row
+// and four blocks; fp32 values alone 111, and 125 with one row; SILU bf16 224, and 231 with four blocks).
+template <typename T, int kAct>
+constexpr int kRowsAtOnce = sizeof(T) == 4 && kAct == CO3_ACT_GELU ? 1 : 2;
+template <int kAct>
+constexpr int kBlocks = kAct == CO3_ACT_GELU ? 4 : 3;
 enum Way { kWide, kSingle };  // 16 bytes at a time, or one element at a time
 
 // Four fp32 or eight 16-bit values as 16 bytes.
@@ -137,8 +143,10 @@ struct Lanes {
     static __device__ __forceinline__ void put(uint8_t* p, bool valid, const float (&v)[kVals], float inverse, uint32_t lane) {
         uint32_t w[kVals / 4];
 #pragma unroll
-        for (int i = 0; i < kVals / 4; ++i)
-            w[i] = f8_from4(__fmul_rn(v[4 * i], inverse), __fmul_rn(v[4 * i + 1], inverse), __fmul_rn(v[4 * i + 2], inverse), __fmul_rn(v[4 * i + 3], inverse));
+        for (int i = 0; i < kVals / 4; ++i) {
+            const F2 a = mul2({v[4 * i], v[4 * i + 1]}, f2_both(inverse)), b = mul2({v[4 * i + 2], v[4 * i + 3]}, f2_both(inverse));
+            w[i] = f8_from4(a.x, a.y, b.x, b.y);
+        }
         if constexpr (kWay == kSingle) w[0] = turn(w[0], lane);
         if (!valid) return;
         if constexpr (kPairs) *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
@@ -162,11 +170,12 @@ struct Lanes {
         if constexpr (kWay == kSingle) b.w[0] = turn(b.w[0], lane);
 #pragma unroll
         for (int i = 0; i < kVals / 4; ++i) {
-            const float2 x = f8_to2(b.w[i]), y = f8_to2(b.w[i] >> 16);
-            v[4 * i] = __fmul_rn(x.x, scale);
-            v[4 * i + 1] = __fmul_rn(x.y, scale);
-            v[4 * i + 2] = __fmul_rn(y.x, scale);
-            v[4 * i + 3] = __fmul_rn(y.y, scale);
+            const float2 lo = f8_to2(b.w[i]), hi = f8_to2(b.w[i] >> 16);
+            const F2 x = mul2({lo.x, lo.y}, f2_both(scale)), y = mul2({hi.x, hi.y}, f2_both(scale));
+            v[4 * i] = x.x;
+            v[4 * i + 1] = x.y;
+            v[4 * i + 2] = y.x;
+            v[4 * i + 3] = y.y;
         }
     }
 };
@@ -174,8 +183,8 @@ struct Lanes {
 // ------------------------------------------------------------------------------------------------
 // Activations
 // ------------------------------------------------------------------------------------------------
-// For 16-bit results kShort forms take the place of the library's functions, with which the kernels are bound by instructions
-// (16384 x 8192 bf16, GELU: forward 299, backward 338 us; with these FORWARD_US and BACKWARD_US).
+// For 16-bit results short forms take the place of the library's functions, two values at a time: with the library's, the kernels
+// are bound by instructions (16384 x 8192 bf16, GELU: forward 299 and backward 338 us).
 __device__ __forceinline__ float exp2_short(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -186,63 +195,82 @@ __device__ __forceinline__ float inverse_short(float x) {
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+__device__ __forceinline__ float min_nan(float a, float b) {  // NaN stays
+    float y;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+    return y;
+}
 // Phi(-|x|), Phi the normal distribution function, is 1/2 erfc(z) with z = |x| / sqrt(2), and erfc(z) exp(z^2) = t P(t), t = 1 / (1 + 0.375 z).
 // P is a polynomial of degree 6 fitted to the smallest relative error over 0 <= z <= 12 (1e-6); with the roundings 1.5e-6 for |x| <= 4
-// and 5e-6 for |x| <= 10, far below half a step of 16 bits.  e: exp(-x^2 / 2).
-__device__ __forceinline__ float normal_below_short(float x, float& e) {
-    const float ax = fabsf(x);
-    e = exp2_short(__fmul_rn(__fmul_rn(ax, ax), -0.72134752044448170f));
-    const float t = inverse_short(__fmaf_rn(ax, 0.26516504294495533f, 1.0f));
-    float p = __fmaf_rn(-0.0666150079f, t, 0.19073585385f);  // P / 2
-    p = __fmaf_rn(p, t, -0.06032206705f);
-    p = __fmaf_rn(p, t, 0.13837517965f);
-    p = __fmaf_rn(p, t, 0.0845211864f);
-    p = __fmaf_rn(p, t, 0.1076185385f);
-    p = __fmaf_rn(p, t, 0.1056866174f);
-    return __fmul_rn(e, __fmul_rn(t, p));
+// and 5e-6 for |x| <= 10, far below half a step of 16 bits.  ax: |x|, 64 at most (where exp(-x^2 / 2) is zero); e: exp(-x^2 / 2); the
+// result is t P(t) / 2.
+__device__ __forceinline__ F2 normal_short(F2 ax, F2& e) {
+    const F2 arg = mul2(mul2(ax, ax), f2_both(-0.72134752044448170f)), den = fma2(ax, f2_both(0.26516504294495533f), f2_both(1.0f));
+    e = {exp2_short(arg.x), exp2_short(arg.y)};
+    const F2 t = {inverse_short(den.x), inverse_short(den.y)};
+    F2 p = fma2(f2_both(-0.0666150079f), t, f2_both(0.19073585385f));
+    p = fma2(p, t, f2_both(-0.06032206705f));
+    p = fma2(p, t, f2_both(0.13837517965f));
+    p = fma2(p, t, f2_both(0.0845211864f));
+    p = fma2(p, t, f2_both(0.1076185385f));
+    p = fma2(p, t, f2_both(0.1056866174f));
+    return mul2(t, p);
 }
-template <bool kShort>
-__device__ __forceinline__ float logistic(float x) {
-    if constexpr (kShort) return inverse_short(__fadd_rn(1.0f, exp2_short(__fmul_rn(x, -1.4426950408889634f))));
-    return __fdiv_rn(1.0f, __fadd_rn(1.0f, expf(-x)));
+__device__ __forceinline__ F2 logistic_short(F2 x) {
+    const F2 arg = mul2(x, f2_both(-1.4426950408889634f)), den = add2({exp2_short(arg.x), exp2_short(arg.y)}, f2_both(1.0f));
+    return {inverse_short(den.x), inverse_short(den.y)};
 }
 
-// Infinities give the limits (the bounds below lie where the other factor is zero), NaN stays.
+// act(x), short forms if kShort.  Infinities give the limits (the bounds below lie where the other factor is zero), NaN stays.
 template <int kAct, bool kShort>
-__device__ __forceinline__ float act(float x) {
-    if constexpr (kAct == CO3_ACT_RELU) return x < 0.0f ? 0.0f : x;
+__device__ __forceinline__ F2 act(F2 x) {
     if constexpr (kAct == CO3_ACT_GELU && kShort) {
-        float e;
-        return __fmaf_rn(-fminf(fabsf(x), 64.0f), normal_below_short(x, e), x < 0.0f ? 0.0f : x);
+        F2 e;  // x > 0: x - x Phi(-x);  x < 0: x Phi(x)
+        const F2 ax = {min_nan(fabsf(x.x), 64.0f), min_nan(fabsf(x.y), 64.0f)}, q = normal_short(ax, e);
+        return fma2(mul2(ax, f2_both(-1.0f)), mul2(e, q), {fmaxf(x.x, 0.0f), fmaxf(x.y, 0.0f)});
+    } else if constexpr (kAct == CO3_ACT_SILU && kShort) {
+        return mul2({fmaxf(x.x, -200.0f), fmaxf(x.y, -200.0f)}, logistic_short(x));
+    } else {
+        auto one = [](float v) {
+            if constexpr (kAct == CO3_ACT_RELU) return v < 0.0f ? 0.0f : v;
+            if constexpr (kAct == CO3_ACT_GELU) return __fmul_rn(fmaxf(v, -64.0f), __fmul_rn(0.5f, erfcf(__fmul_rn(v, -0.70710678118654752f))));
+            if constexpr (kAct == CO3_ACT_SILU) return __fdiv_rn(fmaxf(v, -200.0f), __fadd_rn(1.0f, expf(-v)));
+            return v;
+        };
+        return {one(x.x), one(x.y)};
     }
-    if constexpr (kAct == CO3_ACT_GELU) return __fmul_rn(fmaxf(x, -64.0f), __fmul_rn(0.5f, erfcf(__fmul_rn(x, -0.70710678118654752f))));
-    if constexpr (kAct == CO3_ACT_SILU && kShort) return __fmul_rn(fmaxf(x, -200.0f), logistic<true>(x));
-    if constexpr (kAct == CO3_ACT_SILU) return __fdiv_rn(fmaxf(x, -200.0f), __fadd_rn(1.0f, expf(-x)));
-    return x;
 }
 template <int kAct, bool kShort>
-__device__ __forceinline__ float act_slope(float x) {
-    if constexpr (kAct == CO3_ACT_RELU) return x > 0.0f ? 1.0f : x <= 0.0f ? 0.0f : x;
-    if constexpr (kAct == CO3_ACT_GELU) {
-        float e, below;
-        if constexpr (kShort) {
-            const float q = normal_below_short(x, e);
-            below = x < 0.0f ? q : __fsub_rn(1.0f, q);
-        } else {
-            below = __fmul_rn(0.5f, erfcf(__fmul_rn(x, -0.70710678118654752f)));
-            e = expf(__fmul_rn(__fmul_rn(-0.5f, x), x));
-        }
-        return __fmaf_rn(x, __fmul_rn(0.39894228040143268f, e), below);
+__device__ __forceinline__ F2 act_slope(F2 x) {
+    if constexpr (kAct == CO3_ACT_GELU && kShort) {
+        F2 e;  // x < 0: g = Phi(x) + x phi(x);  x > 0: 1 - g(-x);  g(-|x|) = exp(-x^2 / 2) (t P / 2 - |x| / sqrt(2 pi))
+        const F2 ax = {min_nan(fabsf(x.x), 64.0f), min_nan(fabsf(x.y), 64.0f)}, q = normal_short(ax, e);
+        const F2 g = mul2(e, fma2(ax, f2_both(-0.39894228040143268f), q));
+        auto flip = [](float v, float by) { return __uint_as_float(__float_as_uint(v) ^ (~__float_as_uint(by) & 0x80000000u)); };
+        auto step = [](float v) { return (int)__float_as_uint(v) < 0 ? 0.0f : 1.0f; };
+        return add2({step(x.x), step(x.y)}, {flip(g.x, x.x), flip(g.y, x.y)});
+    } else if constexpr (kAct == CO3_ACT_SILU && kShort) {
+        const F2 p = logistic_short(x);  // p (1 + x (1 - p))
+        return mul2(p, fma2(x, fma2(p, f2_both(-1.0f), f2_both(1.0f)), f2_both(1.0f)));
+    } else {
+        auto one = [](float v) {
+            if constexpr (kAct == CO3_ACT_RELU) return v > 0.0f ? 1.0f : v <= 0.0f ? 0.0f : v;
+            if constexpr (kAct == CO3_ACT_GELU) {
+                const float below = __fmul_rn(0.5f, erfcf(__fmul_rn(v, -0.70710678118654752f)));
+                return __fmaf_rn(v, __fmul_rn(0.39894228040143268f, expf(__fmul_rn(__fmul_rn(-0.5f, v), v))), below);
+            }
+            if constexpr (kAct == CO3_ACT_SILU) {
+                const float p = __fdiv_rn(1.0f, __fadd_rn(1.0f, expf(-v)));
+                return __fmul_rn(p, __fmaf_rn(v, __fsub_rn(1.0f, p), 1.0f));
+            }
+            return 1.0f;
+        };
+        return {one(x.x), one(x.y)};
     }
-    if constexpr (kAct == CO3_ACT_SILU) {
-        const float p = logistic<kShort>(x);
-        return __fmul_rn(p, __fmaf_rn(x, __fsub_rn(1.0f, p), 1.0f));
-    }
-    return 1.0f;
 }
 
 // ------------------------------------------------------------------------------------------------
-// Rows: a warp takes unit_rows (2 or 8) rows of four blocks, two rows at a time.
+// Rows: a warp takes unit_rows (8 or 2) rows of four blocks.
 // ------------------------------------------------------------------------------------------------
 struct RowsArgs {
     const void* x;      // or dy
@@ -318,7 +346,7 @@ __device__ __forceinline__ void put_row(const Unit<T, kWay>& u, uint8_t* to, uin
 // x to x8 (if given), act(x) to y and to y8 (if given).  Rows up to a multiple of 16 are written, as zeros: the products read
 // so many.
 template <typename T, Way kWay, int kAct>
-__global__ void __launch_bounds__(kWarps * 32, 3) f8_rows_kernel(const __grid_constant__ RowsArgs a) {
+__global__ void __launch_bounds__(kWarps * 32, kBlocks<kAct>) f8_rows_kernel(const __grid_constant__ RowsArgs a) {
     using L = Lanes<T, kWay>;
     wait_for_previous_kernel();
     const uint32_t unit = blockIdx.x * kWarps + (threadIdx.x >> 5);
@@ -330,20 +358,20 @@ __global__ void __launch_bounds__(kWarps * 32, 3) f8_rows_kernel(const __grid_co
     int32_t left[L::kChunks];
 #pragma unroll
     for (int h = 0; h < L::kChunks; ++h) left[h] = u.left(a, h);
-    typename L::Raw raw[kRowsAtOnce][L::kChunks];
+    typename L::Raw raw[kRowsAtOnce<T, kAct>][L::kChunks];
     auto fetch = [&](uint32_t r0) {
 #pragma unroll
-        for (int r = 0; r < kRowsAtOnce; ++r) {
+        for (int r = 0; r < kRowsAtOnce<T, kAct>; ++r) {
 #pragma unroll
             for (int h = 0; h < L::kChunks; ++h) raw[r][h] = L::load(x + h * L::kChunkCols, r0 + r < rows ? left[h] : 0);
             x += a.x_stride;
         }
     };
 #pragma unroll 1
-    for (uint32_t r0 = 0; r0 < a.unit_rows; r0 += kRowsAtOnce) {
+    for (uint32_t r0 = 0; r0 < a.unit_rows; r0 += kRowsAtOnce<T, kAct>) {
         fetch(r0);
 #pragma unroll
-        for (int r = 0; r < kRowsAtOnce; ++r) {
+        for (int r = 0; r < kRowsAtOnce<T, kAct>; ++r) {
             float v[L::kChunks][L::kVals];
 #pragma unroll
             for (int h = 0; h < L::kChunks; ++h)
@@ -373,7 +401,11 @@ __global__ void __launch_bounds__(kWarps * 32, 3) f8_rows_kernel(const __grid_co
 #pragma unroll
                     for (int h = 0; h < L::kChunks; ++h)
 #pragma unroll
-                        for (int i = 0; i < L::kVals; ++i) v[h][i] = act<kAct, sizeof(T) == 2>(v[h][i]);
+                        for (int i = 0; i < L::kVals; i += 2) {
+                            const F2 t = act<kAct, sizeof(T) == 2>({v[h][i], v[h][i + 1]});
+                            v[h][i] = t.x;
+                            v[h][i + 1] = t.y;
+                        }
                 }
                 if (a.y)
 #pragma unroll
@@ -396,7 +428,7 @@ __global__ void __launch_bounds__(kWarps * 32, 3) f8_rows_kernel(const __grid_co
 
 // y <- the values of x8, or (kBackward) dx <- dy * act'(values of x8).
 template <typename T, Way kWay, int kAct, bool kBackward>
-__global__ void __launch_bounds__(kWarps * 32, 3) f8_values_kernel(const __grid_constant__ RowsArgs a) {
+__global__ void __launch_bounds__(kWarps * 32, kBlocks<kAct>) f8_values_kernel(const __grid_constant__ RowsArgs a) {
     using L = Lanes<T, kWay>;
     wait_for_previous_kernel();
     const uint32_t unit = blockIdx.x * kWarps + (threadIdx.x >> 5);
@@ -412,10 +444,10 @@ __global__ void __launch_bounds__(kWarps * 32, 3) f8_values_kernel(const __grid_
         uint32_t word;
         typename L::Bytes f8[L::kChunks];
         typename L::Raw dy[kBackward ? L::kChunks : 1];
-    } in[kRowsAtOnce];
+    } in[kRowsAtOnce<T, kAct>];
     auto fetch = [&](uint32_t r0) {
 #pragma unroll
-        for (int r = 0; r < kRowsAtOnce; ++r) {
+        for (int r = 0; r < kRowsAtOnce<T, kAct>; ++r) {
             const bool valid = r0 + r < rows;
             in[r].word = valid ? __ldg(reinterpret_cast<const uint32_t*>(a.x8 + u.word + (r0 + r) * 16u)) : 0x7f7f7f7fu;
 #pragma unroll
@@ -427,10 +459,10 @@ __global__ void __launch_bounds__(kWarps * 32, 3) f8_values_kernel(const __grid_
         }
     };
 #pragma unroll 1
-    for (uint32_t r0 = 0; r0 < rows; r0 += kRowsAtOnce) {
+    for (uint32_t r0 = 0; r0 < rows; r0 += kRowsAtOnce<T, kAct>) {
         fetch(r0);
 #pragma unroll
-        for (int r = 0; r < kRowsAtOnce; ++r) {
+        for (int r = 0; r < kRowsAtOnce<T, kAct>; ++r) {
             const auto& now = in[r];
             const uint32_t word = now.word >> (8u * L::block0(u.lane));
 #pragma unroll
@@ -439,7 +471,11 @@ __global__ void __launch_bounds__(kWarps * 32, 3) f8_values_kernel(const __grid_
                 L::values(now.f8[h], __uint_as_float(((word >> (8 * L::kBlocks * h)) & 0xffu) << 23), u.lane, v);
                 if constexpr (kBackward) {
 #pragma unroll
-                    for (int i = 0; i < L::kVals; ++i) v[i] = __fmul_rn(L::value(now.dy[h], i), act_slope<kAct, sizeof(T) == 2>(v[i]));
+                    for (int i = 0; i < L::kVals; i += 2) {
+                        const F2 d = mul2({L::value(now.dy[h], i), L::value(now.dy[h], i + 1)}, act_slope<kAct, sizeof(T) == 2>({v[i], v[i + 1]}));
+                        v[i] = d.x;
+                        v[i + 1] = d.y;
+                    }
                 }
                 L::store(y + h * L::kChunkCols, r0 + r < rows ? left[h] : 0, v);
             }
@@ -449,7 +485,8 @@ __global__ void __launch_bounds__(kWarps * 32, 3) f8_values_kernel(const __grid_
 }
 
 // ------------------------------------------------------------------------------------------------
-// Square blocks: a thread block of 256 each, 16 rows a warp.
+// Square blocks: a thread block of 256 each, 16 rows a warp.  Two blocks an SM, so that one stores while the other loads (4096 x 4096
+// fp32 there and back 29 us; one block of up to 217 registers a thread 34).
 // ------------------------------------------------------------------------------------------------
 struct SquareArgs {
     const void* x;
@@ -459,7 +496,7 @@ struct SquareArgs {
 };
 
 template <typename T, Way kWay>
-__global__ void __launch_bounds__(256) f8_square_kernel(const __grid_constant__ SquareArgs a) {
+__global__ void __launch_bounds__(256, kWay == kWide ? 2 : 3) f8_square_kernel(const __grid_constant__ SquareArgs a) {
     using L = Lanes<T, kWay>;
     constexpr int kRows = L::kPairs ? 2 : 1, kTurns = 16 / kRows;  // rows a warp's load covers
     __shared__ uint32_t part[kWarps];
@@ -528,7 +565,7 @@ void fill(RowsArgs& a, const F8Layout& l, uint64_t rows, uint32_t cols) {
     a.scales = l.scales;
     // eight rows a warp where that still gives every multiprocessor eight warps (148 of them), two otherwise
     const uint64_t padded = (rows + 15u) / 16u * 16u;
-    a.unit_rows = padded / 8u * a.groups >= 148u * 8u ? 8 : kRowsAtOnce;
+    a.unit_rows = padded / 8u * a.groups >= 148u * 8u ? 8 : 2;
     a.units = (uint32_t)(padded / a.unit_rows * a.groups);
 }
 

@@ -71,6 +71,29 @@ __device__ __forceinline__ int f8_exponent(uint32_t most) {
 }
 __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
 
+// Two fp32 operations in one instruction.
+struct F2 {
+    float x, y;
+};
+__device__ __forceinline__ unsigned long long f2_bits(F2 v) { return (unsigned long long)__float_as_uint(v.x) | ((unsigned long long)__float_as_uint(v.y) << 32); }
+__device__ __forceinline__ F2 f2_from(unsigned long long b) { return {__uint_as_float((uint32_t)b), __uint_as_float((uint32_t)(b >> 32))}; }
+__device__ __forceinline__ F2 f2_both(float v) { return {v, v}; }
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
+    unsigned long long r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(f2_bits(a)), "l"(f2_bits(b)), "l"(f2_bits(c)));
+    return f2_from(r);
+}
+__device__ __forceinline__ F2 mul2(F2 a, F2 b) {
+    unsigned long long r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(f2_bits(a)), "l"(f2_bits(b)));
+    return f2_from(r);
+}
+__device__ __forceinline__ F2 add2(F2 a, F2 b) {
+    unsigned long long r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(f2_bits(a)), "l"(f2_bits(b)));
+    return f2_from(r);
+}
+
 // Four values to e4m3, the first in the lowest byte.  NaN stays NaN.
 __device__ __forceinline__ uint32_t f8_from4(float a, float b, float c, float d) {
     uint16_t lo, hi;
