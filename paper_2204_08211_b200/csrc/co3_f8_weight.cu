@@ -6,11 +6,15 @@
 // bits, one for bf16, two for fp16, three for fp32, so that nothing of it is lost: the products are exact and the sums fp32.
 //
 // A first kernel writes both operands, as the tensor cores read them, to the workspace (doing this inside the product costs every
-// tile the conversion of all its rows: 16384 x 4096 x 4096 bf16 2.02 ms), and sums dy.  The products are
+// tile the conversion of all its rows: 16384 x 4096 x 4096 bf16 2.02 ms), and sums dy; bf16 gradients with rows on 16-byte boundaries
+// stay where they are, and the products' copies swizzle them (459 us with them rearranged, 442 so).  The products are
 // tiles of 256 inputs (tensor memory's lanes, so that a warp writes neighbouring entries of dW) by 256 or 128 outputs, by pairs of
 // blocks; a stage is 64 rows, a row of the batch per row of shared memory.  After every 256 rows the sums are taken out and
 // added up in registers (the tensor core cuts what it adds towards zero).  Few tiles: the rows are divided, and a last kernel adds
 // the parts in order.
+#include <cuda.h>
+#include <cudaTypedefs.h>
+
 #include <algorithm>
 #include <atomic>
 #include <type_traits>
@@ -52,6 +56,7 @@ struct WeightArgs {
     float *dw, *db;
     uint64_t client_stride;
     int accumulate;
+    int direct;                              // dy is read where it is
     co3_result* res;
 };
 
@@ -143,22 +148,24 @@ __device__ __forceinline__ void bring_dy(const WeightArgs& a, uint32_t u, uint32
                 for (int k = 0; k < 8; ++k) v[j][k] = 0.0f;
             }
         }
-        unsigned char* chunk = a.ws_dy + (((uint64_t)u * a.groups + g) * a.chunks + c) * (kParts * kPlane16) + (p >> 3) * kAtom;
+        if (!a.direct) {
+            unsigned char* chunk = a.ws_dy + (((uint64_t)u * a.groups + g) * a.chunks + c) * (kParts * kPlane16) + (p >> 3) * kAtom;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const uint32_t i = r0 + 16u * j;
-            uint32_t w[kParts][4];
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t i = r0 + 16u * j;
+                uint32_t w[kParts][4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                uint32_t lo[kParts], hi[kParts];
-                cut(v[j][2 * k], lo);
-                cut(v[j][2 * k + 1], hi);
+                for (int k = 0; k < 4; ++k) {
+                    uint32_t lo[kParts], hi[kParts];
+                    cut(v[j][2 * k], lo);
+                    cut(v[j][2 * k + 1], hi);
 #pragma unroll
-                for (int m = 0; m < kParts; ++m) w[m][k] = __byte_perm(lo[m], hi[m], 0x7632);
+                    for (int m = 0; m < kParts; ++m) w[m][k] = __byte_perm(lo[m], hi[m], 0x7632);
+                }
+#pragma unroll
+                for (int m = 0; m < kParts; ++m)
+                    *reinterpret_cast<uint4*>(chunk + m * kPlane16 + i * 128u + f8_piece(i, p & 7u)) = make_uint4(w[m][0], w[m][1], w[m][2], w[m][3]);
             }
-#pragma unroll
-            for (int m = 0; m < kParts; ++m)
-                *reinterpret_cast<uint4*>(chunk + m * kPlane16 + i * 128u + f8_piece(i, p & 7u)) = make_uint4(w[m][0], w[m][1], w[m][2], w[m][3]);
         }
         if (a.db) {
 #pragma unroll
@@ -191,7 +198,7 @@ __device__ __forceinline__ void bring_dy(const WeightArgs& a, uint32_t u, uint32
 template <typename T, bool kWide>
 __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 5 : 3) f8_operands_kernel(const __grid_constant__ WeightArgs a) {
     wait_for_previous_kernel();
-    const uint32_t of_dy = a.clients * a.groups * a.db_parts;
+    const uint32_t of_dy = a.direct && !a.db ? 0u : a.clients * a.groups * a.db_parts;
     uint32_t b = blockIdx.x;
     if (b < of_dy) {
         const uint32_t part = b / (a.clients * a.groups);
@@ -251,8 +258,15 @@ __device__ __forceinline__ Place find_place(const WeightArgs& a, uint32_t t) {
 // Outputs of a tile that are multiplied: 128, half of them in each block, or 256.
 __device__ __forceinline__ uint32_t tile_cols(const WeightArgs& a, uint32_t n0) { return a.outs - n0 > 128u ? a.tile_outs : 128u; }
 
-template <int kParts>
-__global__ void __launch_bounds__(kF8Threads, 1) f8_weight_kernel(const __grid_constant__ WeightArgs a) {
+// 64 columns of 64 rows of a client's dy, swizzled; zeros beyond the last column and row.
+__device__ __forceinline__ void copy_box(unsigned char* to, const CUtensorMap& map, uint32_t col, uint32_t row, uint32_t client, uint64_t* bar) {
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(smem_addr(to)), "l"(&map),
+                 "r"(col), "r"(row), "r"(client), "r"(smem_addr(bar))
+                 : "memory");
+}
+
+template <int kParts, bool kDirect>
+__global__ void __launch_bounds__(kF8Threads, 1) f8_weight_kernel(const __grid_constant__ WeightArgs a, const __grid_constant__ CUtensorMap dy_map) {
     extern __shared__ unsigned char smem_raw[];
     constexpr uint32_t kStageBytes = kPlane16 * (1 + kParts), kStages = kRing / kStageBytes;
     static_assert(kStages <= kMaxStagesW, "stages");
@@ -295,11 +309,17 @@ __global__ void __launch_bounds__(kF8Threads, 1) f8_weight_kernel(const __grid_c
                         unsigned char* to = ring + st * kStageBytes;
                         mbar_arrive_expect_tx(&sm.full[st], kPlane16 + kParts * (both ? kPlane16 : kAtom));
                         bulk_copy_g2s(to, x + (uint64_t)c * kPlane16, kPlane16, &sm.full[st]);
-                        const unsigned char* from = dy + (uint64_t)c * (kParts * kPlane16);
-                        if (both) {
-                            bulk_copy_g2s(to + kPlane16, from, kParts * kPlane16, &sm.full[st]);
+                        if constexpr (kDirect) {
+                            const uint32_t col = p.n0 + (both ? 128u : 64u) * rank;
+                            copy_box(to + kPlane16, dy_map, col, c * kChunk, p.u, &sm.full[st]);
+                            if (both) copy_box(to + kPlane16 + kAtom, dy_map, col + 64u, c * kChunk, p.u, &sm.full[st]);
                         } else {
-                            for (uint32_t m = 0; m < kParts; ++m) bulk_copy_g2s(to + kPlane16 * (1 + m), from + m * kPlane16 + rank * kAtom, kAtom, &sm.full[st]);
+                            const unsigned char* from = dy + (uint64_t)c * (kParts * kPlane16);
+                            if (both) {
+                                bulk_copy_g2s(to + kPlane16, from, kParts * kPlane16, &sm.full[st]);
+                            } else {
+                                for (uint32_t m = 0; m < kParts; ++m) bulk_copy_g2s(to + kPlane16 * (1 + m), from + m * kPlane16 + rank * kAtom, kAtom, &sm.full[st]);
+                            }
                         }
                     }
                     if (++st == kStages) { st = 0; ++turn; }
@@ -533,9 +553,33 @@ bool weight_plan(uint64_t rows, uint32_t outs, uint32_t ins, uint32_t clients, u
     return true;
 }
 
-template <int kParts>
-int launch_weight(const WeightArgs& a, cudaStream_t st) {
-    auto* kernel = f8_weight_kernel<kParts>;
+// The driver's call that describes a tensor to the copies, or null.
+PFN_cuTensorMapEncodeTiled_v12000 tensor_map_call() {
+    static std::atomic<void*> known{nullptr};
+    void* f = known.load(std::memory_order_relaxed);
+    if (!f) {
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess) {
+            (void)cudaGetLastError();
+            return nullptr;
+        }
+        known.store(f, std::memory_order_relaxed);
+    }
+    return reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(f);
+}
+// dy of bf16 as clients x rows x outputs; false: it has to be rearranged.
+bool describe(const WeightArgs& a, CUtensorMap* map) {
+    const cuuint64_t sizes[3] = {a.outs, a.rows, a.clients}, strides[2] = {a.dy_stride * 2, a.rows * a.dy_stride * 2};
+    const cuuint32_t box[3] = {64, kChunk, 1}, each[3] = {1, 1, 1};
+    if (strides[1] >= (1ull << 40)) return false;
+    const auto call = tensor_map_call();
+    return call && call(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(a.dy), sizes, strides, box, each, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                        CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int kParts, bool kDirect = false>
+int launch_weight(const WeightArgs& a, const CUtensorMap& map, cudaStream_t st) {
+    auto* kernel = f8_weight_kernel<kParts, kDirect>;
     static std::atomic<int> sms[64];
     int dev = 0;
     CO3_CUDA(cudaGetDevice(&dev));
@@ -559,12 +603,12 @@ int launch_weight(const WeightArgs& a, cudaStream_t st) {
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    CO3_CUDA(cudaLaunchKernelEx(&cfg, kernel, a));
+    CO3_CUDA(cudaLaunchKernelEx(&cfg, kernel, a, map));
     return CO3_OK;
 }
 template <typename T, bool kWide>
 int launch_operands(const WeightArgs& a, cudaStream_t st) {
-    const uint32_t blocks = a.clients * a.groups * a.db_parts + (a.dw ? a.clients * a.k_tiles * a.chunks : 0u);
+    const uint32_t blocks = (a.direct && !a.db ? 0u : a.clients * a.groups * a.db_parts) + (a.dw ? a.clients * a.k_tiles * a.chunks : 0u);
     CO3_CUDA(launch_behind(f8_operands_kernel<T, kWide>, dim3(blocks), dim3(256), 0, st, a));
     return CO3_OK;
 }
@@ -637,10 +681,16 @@ int co3_f8_weight_gradient(const void* dy, int type, uint64_t dy_row_stride, con
     a.res = res;
     const size_t s = type_size(type);
     const bool wide = aligned(dy, 16) && dy_row_stride * s % 16 == 0 && outs * s % 16 == 0;
+    CUtensorMap map = {};
+    a.direct = type == CO3_BF16 && wide && dw && describe(a, &map);
     int e = type == CO3_F32   ? (wide ? launch_operands<float, true>(a, st) : launch_operands<float, false>(a, st))
             : type == CO3_F16 ? (wide ? launch_operands<__half, true>(a, st) : launch_operands<__half, false>(a, st))
                               : (wide ? launch_operands<__nv_bfloat16, true>(a, st) : launch_operands<__nv_bfloat16, false>(a, st));
-    if (e == CO3_OK && dw) e = type == CO3_F32 ? launch_weight<3>(a, st) : type == CO3_F16 ? launch_weight<2>(a, st) : launch_weight<1>(a, st);
+    if (e == CO3_OK && dw)
+        e = type == CO3_F32   ? launch_weight<3>(a, map, st)
+            : type == CO3_F16 ? launch_weight<2>(a, map, st)
+            : a.direct        ? launch_weight<1, true>(a, map, st)
+                              : launch_weight<1>(a, map, st);
     if (e != CO3_OK) return e;
     return launch_join({a.dw_parts, w.parts > 1 ? dw : nullptr, (uint64_t)outs * ins, w.parts}, {a.db_parts_at, w.db_parts > 1 ? db : nullptr, outs, w.db_parts},
                        n_clients, client_stride_elems, accumulate, st);
