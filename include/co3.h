@@ -452,7 +452,8 @@ int co3_f8_linear(const void* x, int x_type, uint64_t x_row_stride, void* x8, si
                   uint32_t outs, uint32_t ins, int transposed, const float* bias, void* y, int y_type, uint64_t y_row_stride,
                   uint64_t rows, co3_result* res, void* stream);
 
-/* Device workspace of co3_f8_weight_gradient. */
+/* Device workspace of co3_f8_weight_gradient, whatever dy's type: bf16 forms of x8 (2 bytes a value) and of dy (6), and parts of sums where
+ * the rows are divided. */
 int co3_f8_weight_gradient_workspace_bytes(uint64_t rows, uint32_t outs, uint32_t ins, uint32_t n_clients, size_t* out /* [host] */);
 
 /*
@@ -465,7 +466,7 @@ int co3_f8_weight_gradient_workspace_bytes(uint64_t rows, uint32_t outs, uint32_
  *                    can be layers of the gradient vectors that co3_encode reads; added to what is there if `accumulate` is not
  *                    0.  No rows: zeros (or nothing, if accumulating)
  *   res              as above
- * dy is used to the last bit, products are exact, sums are fp32 in an order that depends on the sizes alone: the same call
+ * dy is used to the last bit (of fp32 values below 2^-102 the last bits may be lost), products are exact, sums are fp32 in an order that depends on the sizes alone: the same call
  * gives the same bits.
  */
 int co3_f8_weight_gradient(const void* dy, int type, uint64_t dy_row_stride, const void* x8, size_t x8_bytes, uint64_t rows,
@@ -543,7 +544,7 @@ int co3_muon_update(const float* grad, float* momentum, float* params, const co3
 
 /*
  * Diagnostics (no counterpart in the paper).  With profiling enabled every kernel launched by the
- * entry points above (layer norm, co3_orthogonalize and co3_muon_update excepted: they are not recorded) is bracketed by a CUDA event pair on the caller's stream; co3_profile_read
+ * entry points above (layer norm, co3_f8_*, co3_orthogonalize and co3_muon_update excepted: they are not recorded) is bracketed by a CUDA event pair on the caller's stream; co3_profile_read
  * waits for those events, adds up the elapsed time and the number of launches per kernel kind
  * (arrays of CO3_KERNEL_COUNT entries, [host]) and clears the records.  Off by default; at most
  * 16384 launches are recorded between reads.  Not thread-safe, and not to be left on inside a

@@ -107,6 +107,18 @@ def test_small_sums_next_to_large_ones():
     assert (y[7] > 1e22).all() and (y[8] < 1e-17).all()
 
 
+@pytest.mark.parametrize("rows", [3, 100, 2600])
+def test_scales_far_apart_on_both_sides(rows):
+    """Very small inputs times very large weights and the other way round: only the product has to be in range."""
+    ins, outs = 300, 2300
+    x, w, _ = inputs(rows, ins, outs, False, 2)
+    for up in (2.0 ** 90, 2.0 ** -90):
+        x8, w8, y = room(rows, ins), room(outs, ins, co3.F8_SQUARE), torch.empty(rows, outs, device="cuda")
+        assert co3.co3_f8_pack(w * up, w8, co3.F8_SQUARE) == co3.OK and co3.co3_f8_linear(x / up, x8, w8, None, y) == co3.OK
+        torch.cuda.synchronize()
+        check(x8, w8, None, y, rows, ins, outs, False, "f32")
+
+
 @pytest.mark.parametrize("rows", [5, 100, 2600])
 def test_nonfinite(rows):
     """A NaN or an infinity spoils its own row of x, or its own feature, and nothing else."""
