@@ -232,29 +232,45 @@ __device__ __forceinline__ void pair_mma(uint32_t d, uint64_t a, uint64_t b, uin
         : "memory");
 }
 
-// A pair's tile, and the chunks of rows that it sums.
-struct Place {
-    uint32_t u, part, n0, kp, c0, c1;
-};
-__device__ __forceinline__ Place find_place(const WeightArgs& a, uint32_t t) {
-    Place p;
-    const uint32_t pairs = (a.k_tiles + 1) / 2;
-    p.kp = t % pairs;
-    t /= pairs;
-    p.n0 = t % a.n_tiles * a.tile_outs;
-    t /= a.n_tiles;
-    if (a.parts == 1) {  // (the divisions would take as long as a stage)
-        p.part = p.c0 = 0;
-        p.u = t;
-        p.c1 = a.chunks;
-        return p;
+// A pair's tiles one after the other, and the chunks of rows that each sums.  Tiles are counted by blocks of inputs, outputs, parts of the
+// rows, clients; going on by so many tiles is adding these four digits with their carries (dividing anew for each tile took about 1000
+// cycles, a fifth of a small tile).
+struct Walk {
+    uint32_t t, tiles, step;
+    uint32_t kp, n, part, u;          // the tile
+    uint32_t d_kp, d_n, d_part, d_u;  // the step
+    __device__ __forceinline__ explicit Walk(const WeightArgs& a) {
+        const uint32_t pairs = (a.k_tiles + 1) / 2;
+        tiles = pairs * a.n_tiles * a.parts * a.clients;
+        t = blockIdx.x >> 1;
+        step = gridDim.x >> 1;
+        auto digits = [&](uint32_t v, uint32_t& k, uint32_t& nn, uint32_t& pp, uint32_t& uu) {
+            k = v % pairs;
+            v /= pairs;
+            nn = v % a.n_tiles;
+            v /= a.n_tiles;
+            pp = v % a.parts;
+            uu = v / a.parts;
+        };
+        digits(t, kp, n, part, u);
+        digits(step, d_kp, d_n, d_part, d_u);
     }
-    p.part = t % a.parts;
-    p.u = t / a.parts;
-    p.c0 = (uint32_t)((uint64_t)a.chunks * p.part / a.parts);
-    p.c1 = (uint32_t)((uint64_t)a.chunks * (p.part + 1) / a.parts);
-    return p;
-}
+    __device__ __forceinline__ bool more() const { return t < tiles; }
+    __device__ __forceinline__ void next(const WeightArgs& a) {
+        t += step;
+        const uint32_t pairs = (a.k_tiles + 1) / 2;
+        kp += d_kp;
+        n += d_n;
+        part += d_part;
+        u += d_u;
+        if (kp >= pairs) { kp -= pairs; ++n; }
+        if (n >= a.n_tiles) { n -= a.n_tiles; ++part; }
+        if (part >= a.parts) { part -= a.parts; ++u; }
+    }
+    __device__ __forceinline__ uint32_t n0(const WeightArgs& a) const { return n * a.tile_outs; }
+    __device__ __forceinline__ uint32_t c0(const WeightArgs& a) const { return a.parts == 1 ? 0u : (uint32_t)((uint64_t)a.chunks * part / a.parts); }
+    __device__ __forceinline__ uint32_t c1(const WeightArgs& a) const { return a.parts == 1 ? a.chunks : (uint32_t)((uint64_t)a.chunks * (part + 1) / a.parts); }
+};
 // Outputs of a tile that are multiplied: 128, half of them in each block, or 256.
 __device__ __forceinline__ uint32_t tile_cols(const WeightArgs& a, uint32_t n0) { return a.outs - n0 > 128u ? a.tile_outs : 128u; }
 
@@ -288,29 +304,27 @@ __global__ void __launch_bounds__(kF8Threads, 1) f8_weight_kernel(const __grid_c
     const uint32_t tmem = sm.tmem;
     volatile uint32_t* failed = &sm.failed;
     wait_for_previous_kernel();
-    const uint32_t tiles = (a.k_tiles + 1) / 2 * a.n_tiles * a.parts * a.clients;
-    const uint32_t first = blockIdx.x >> 1, step = gridDim.x >> 1;
 
     if (warp < 4) {
         few_registers();
         const bool issues = elected();
         if (warp == 0) {
             uint32_t st = 0, turn = 0;
-            for (uint32_t t = first; t < tiles && !*failed; t += step) {
-                const Place p = find_place(a, t);
+            for (Walk p(a); p.more() && !*failed; p.next(a)) {
+                const uint32_t n0 = p.n0(a), c1 = p.c1(a);
                 const uint32_t kt = min(2 * p.kp + rank, a.k_tiles - 1);  // (an odd last tile: the second block's sums go nowhere)
-                const bool both = tile_cols(a, p.n0) == 256u;
-                const uint32_t g = (p.n0 >> 7) + (both ? rank : 0u);
+                const bool both = tile_cols(a, n0) == 256u;
+                const uint32_t g = (n0 >> 7) + (both ? rank : 0u);
                 const unsigned char* x = a.ws_x + ((uint64_t)p.u * a.k_tiles + kt) * a.chunks * kPlane16;
                 const unsigned char* dy = a.ws_dy + ((uint64_t)p.u * a.groups + g) * a.chunks * (kParts * kPlane16);
-                for (uint32_t c = p.c0; c < p.c1; ++c) {
+                for (uint32_t c = p.c0(a); c < c1; ++c) {
                     if (turn > 0 && !f8_wait(&sm.empty[st], (turn - 1) & 1u)) { *failed = 1; break; }
                     if (issues) {
                         unsigned char* to = ring + st * kStageBytes;
                         mbar_arrive_expect_tx(&sm.full[st], kPlane16 + kParts * (both ? kPlane16 : kAtom));
                         bulk_copy_g2s(to, x + (uint64_t)c * kPlane16, kPlane16, &sm.full[st]);
                         if constexpr (kDirect) {
-                            const uint32_t col = p.n0 + (both ? 128u : 64u) * rank;
+                            const uint32_t col = n0 + (both ? 128u : 64u) * rank;
                             copy_box(to + kPlane16, dy_map, col, c * kChunk, p.u, &sm.full[st]);
                             if (both) copy_box(to + kPlane16 + kAtom, dy_map, col + 64u, c * kChunk, p.u, &sm.full[st]);
                         } else {
@@ -334,9 +348,9 @@ __global__ void __launch_bounds__(kF8Threads, 1) f8_weight_kernel(const __grid_c
             // tells the first block what has arrived here: its barrier waits for both
             uint32_t st = 0, turn = 0;
             bool ok = true;
-            for (uint32_t t = first; t < tiles && ok; t += step) {
-                const Place p = find_place(a, t);
-                for (uint32_t c = p.c0; c < p.c1; ++c) {
+            for (Walk p(a); p.more() && ok; p.next(a)) {
+                const uint32_t c1 = p.c1(a);
+                for (uint32_t c = p.c0(a); c < c1; ++c) {
                     if (!f8_wait(&sm.full[st], turn & 1u)) { ok = false; break; }
                     if (issues) mbar_arrive_at(&sm.full[st], 0);
                     if (++st == kStages) { st = 0; ++turn; }
@@ -346,15 +360,14 @@ __global__ void __launch_bounds__(kF8Threads, 1) f8_weight_kernel(const __grid_c
         } else if (warp == 1) {
             uint32_t st = 0, turn = 0, sum = 0, sum_turn = 0;
             bool ok = true;
-            for (uint32_t t = first; t < tiles && ok; t += step) {
-                const Place p = find_place(a, t);
-                const uint32_t instr = weight_instr(0) | ((tile_cols(a, p.n0) / 8u) << 17);
-                for (uint32_t c = p.c0; c < p.c1; ++c) {
-                    const uint32_t in_sum = (c - p.c0) % kSumChunks;
+            for (Walk p(a); p.more() && ok; p.next(a)) {
+                const uint32_t instr = weight_instr(0) | ((tile_cols(a, p.n0(a)) / 8u) << 17), c0 = p.c0(a), c1 = p.c1(a);
+                for (uint32_t c = c0; c < c1; ++c) {
+                    const uint32_t in_sum = (c - c0) % kSumChunks;
                     if (in_sum == 0 && sum_turn > 0 && !f8_wait(&sm.sum_empty[sum], (sum_turn - 1) & 1u)) { ok = false; break; }
                     if (!f8_wait(&sm.full[st], turn & 1u)) { ok = false; break; }
                     tc_fence_after();
-                    const bool last = in_sum == kSumChunks - 1 || c + 1 == p.c1;
+                    const bool last = in_sum == kSumChunks - 1 || c + 1 == c1;
                     if (issues) {
                         const uint32_t d = tmem + sum * kOuts, at = smem_addr(ring + st * kStageBytes);
                         const uint64_t dx = smem_desc(at, true, kAtom);
@@ -381,24 +394,27 @@ __global__ void __launch_bounds__(kF8Threads, 1) f8_weight_kernel(const __grid_c
         const uint32_t quad = warp & 3u, half = (warp - 4u) >> 2, row = quad * 32u + lane;
         uint32_t sum = 0, sum_turn = 0;
         bool ok = true;
-        for (uint32_t t = first; t < tiles && ok; t += step) {
-            const Place p = find_place(a, t);
-            const uint32_t cols = a.tile_outs / 2, o0 = p.n0 + half * cols;  // columns of a warp
+        const uint32_t cols = a.tile_outs / 2;  // of a warp
+        for (Walk p(a); p.more() && ok; p.next(a)) {
+            const uint32_t o0 = p.n0(a) + half * cols, c0 = p.c0(a), c1 = p.c1(a);
             float acc[kOuts / 2];
-            for (uint32_t c = p.c0; c < p.c1; c += kSumChunks) {
+            for (uint32_t c = c0; c < c1; c += kSumChunks) {
                 ok = lane != 0 || f8_wait(&sm.sum_full[sum], sum_turn & 1u);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 tc_fence_after();
                 const uint32_t from = tmem + ((quad * 32u) << 16) + sum * kOuts + half * cols;
-                if (o0 < a.outs) {
+                if (o0 < a.outs && c == c0) {
+                    if (cols == kOuts / 2) tc_load(from, acc);
+                    else tc_load(from, *reinterpret_cast<float(*)[kOuts / 4]>(acc));
+                } else if (o0 < a.outs) {
 #pragma unroll
                     for (int h = 0; h < (int)kOuts / 2; h += 64) {
                         if ((uint32_t)h >= cols) break;
                         float w[64];
                         tc_load(from + h, w);
 #pragma unroll
-                        for (int i = 0; i < 64; ++i) acc[h + i] = c == p.c0 ? w[i] : __fadd_rn(acc[h + i], w[i]);
+                        for (int i = 0; i < 64; ++i) acc[h + i] = __fadd_rn(acc[h + i], w[i]);
                     }
                 }
                 tc_fence_before();
