@@ -523,6 +523,98 @@ int launch_join(const Join& dw, const Join& db, uint32_t clients, uint64_t clien
 }
 
 // ------------------------------------------------------------------------------------------------
+// Small gradients in one launch, without the tensor cores: 32 outputs by 128 inputs a block, 4 x 4 entries a thread, 32 rows
+// at a time in shared memory as fp32, the next ones on their way.
+// ------------------------------------------------------------------------------------------------
+constexpr uint32_t kFewOuts = 32, kFewRowsW = 32;
+template <typename T>
+__global__ void __launch_bounds__(256) f8_weight_small_kernel(const __grid_constant__ WeightArgs a) {
+    __shared__ float xs[kFewRowsW][132];
+    __shared__ float ds[kFewRowsW][kFewOuts];
+    wait_for_previous_kernel();
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
+    const uint32_t o_tiles = (a.outs + kFewOuts - 1) / kFewOuts, i_tiles = a.dw ? a.k_tiles : 1u;
+    const uint32_t kt = blockIdx.x % i_tiles, ot = blockIdx.x / i_tiles % o_tiles, u = blockIdx.x / i_tiles / o_tiles;
+    const uint64_t row0 = u * a.rows;
+    const uint32_t xr = threadIdx.x >> 3, xp = threadIdx.x & 7u;   // this thread's row and piece of x, its column of dy
+    const uint32_t o = ot * kFewOuts + lane;
+    uint4 x;
+    float s, d[4];
+    auto fetch = [&](uint64_t r0) {
+        x = make_uint4(0, 0, 0, 0);
+        s = 1.0f;
+        const uint64_t row = row0 + r0 + xr;
+        if (a.dw && r0 + xr < a.rows) {
+            x = __ldg(reinterpret_cast<const uint4*>(a.x + f8_row(a.x_rows, kt, row) + f8_piece((uint32_t)row & 7u, xp)));
+            s = __uint_as_float((uint32_t)__ldg(a.x_scales + ((kt >> 2) * (a.x_rows >> 7) + (row >> 7)) * kF8Scales + f8_scale_at((uint32_t)row & 127u, kt)) << 23);
+        }
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j) {
+            const uint64_t r = r0 + warp + 8 * j;
+            d[j] = r < a.rows && o < a.outs ? to_float(static_cast<const T*>(a.dy)[(row0 + r) * a.dy_stride + o]) : 0.0f;
+        }
+    };
+    float acc[4][4], db = 0.0f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) acc[j][k] = 0.0f;
+    fetch(0);
+    for (uint64_t r0 = 0; r0 < a.rows; r0 += kFewRowsW) {
+        const uint32_t q[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float2 lo = f8_to2(q[k]), hi = f8_to2(q[k] >> 16);
+            *reinterpret_cast<float4*>(&xs[xr][xp * 16u + 4u * k]) = make_float4(__fmul_rn(lo.x, s), __fmul_rn(lo.y, s), __fmul_rn(hi.x, s), __fmul_rn(hi.y, s));
+        }
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j) ds[warp + 8 * j][lane] = d[j];
+        __syncthreads();
+        if (r0 + kFewRowsW < a.rows) fetch(r0 + kFewRowsW);
+        const uint32_t n = (uint32_t)min((uint64_t)kFewRowsW, a.rows - r0);
+        for (uint32_t r = 0; r < n; ++r) {
+            const float4 g = *reinterpret_cast<const float4*>(&ds[r][warp * 4u]);
+            const float gs[4] = {g.x, g.y, g.z, g.w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float v = xs[r][lane + 32u * k];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[j][k] = __fmaf_rn(gs[j], v, acc[j][k]);
+            }
+        }
+        if (kt == 0 && warp == 0)
+            for (uint32_t r = 0; r < n; ++r) db = __fadd_rn(db, ds[r][lane]);
+        __syncthreads();
+    }
+    if (a.dw)
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j) {
+            const uint32_t out = ot * kFewOuts + warp * 4u + j;
+            float* to = a.dw + u * a.client_stride + (uint64_t)out * a.ins + kt * 128u + lane;
+#pragma unroll
+            for (uint32_t k = 0; k < 4; ++k)
+                if (out < a.outs && kt * 128u + lane + 32u * k < a.ins) to[32u * k] = a.accumulate ? __fadd_rn(to[32u * k], acc[j][k]) : acc[j][k];
+        }
+    if (a.db && kt == 0 && warp == 0 && o < a.outs) {
+        float* to = a.db + u * a.client_stride + o;
+        *to = a.accumulate ? __fadd_rn(*to, db) : db;
+    }
+}
+// Whether that is the faster way: one launch against two or three, as long as the rows are few turns, the products below 2^26 (about
+// 8 us without the tensor cores) and the entries below 2^22 (us, a call with its arguments: 1 x 64 x 1024 x 1024 15.5 and 18.5, 30 x 200 x
+// 100 x 100 15.9 and 20.9; 1 x 1 x 8192 x 8192 66 and 55).
+bool small_gradient(uint64_t rows, uint32_t outs, uint32_t ins, uint32_t clients) {
+    const uint64_t entries = (uint64_t)outs * ins * clients;
+    return rows <= 256 && entries <= (1ull << 22) && rows * entries <= (1ull << 26);
+}
+template <typename T>
+int launch_small(const WeightArgs& a, cudaStream_t st) {
+    const uint32_t blocks = (a.dw ? a.k_tiles : 1u) * ((a.outs + kFewOuts - 1) / kFewOuts) * a.clients;
+    CO3_CUDA(launch_behind(f8_weight_small_kernel<T>, dim3(blocks), dim3(256), 0, st, a));
+    return CO3_OK;
+}
+
+// ------------------------------------------------------------------------------------------------
 // Sizes: they follow from the call's alone, so that the same call gives the same bits everywhere.
 // ------------------------------------------------------------------------------------------------
 struct WeightPlan {
@@ -695,6 +787,8 @@ int co3_f8_weight_gradient(const void* dy, int type, uint64_t dy_row_stride, con
     a.client_stride = client_stride_elems;
     a.accumulate = accumulate;
     a.res = res;
+    if (small_gradient(rows, outs, ins, n_clients))
+        return type == CO3_F32 ? launch_small<float>(a, st) : type == CO3_F16 ? launch_small<__half>(a, st) : launch_small<__nv_bfloat16>(a, st);
     const size_t s = type_size(type);
     const bool wide = aligned(dy, 16) && dy_row_stride * s % 16 == 0 && outs * s % 16 == 0;
     CUtensorMap map = {};

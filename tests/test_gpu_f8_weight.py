@@ -54,7 +54,8 @@ def check(dy, v, grads, at_w, at_b, clients, stride, before=None):
 @pytest.mark.parametrize("type_", list(TYPES))
 @pytest.mark.parametrize("clients,rows,ins,outs,pad", [
     (1, 1, 1, 1, 0), (1, 1, 128, 256, 0), (1, 64, 128, 128, 0), (1, 65, 129, 257, 0), (3, 101, 300, 200, 0), (2, 63, 100, 129, 1), (5, 64, 128, 384, 8),
-    (1, 300, 1000, 520, 0), (2, 1501, 1023, 1001, 17), (100, 8, 64, 40, 0), (300, 1, 40, 8, 3), (1, 3000, 257, 40, 0), (1, 5000, 512, 512, 0), (1, 700, 2100, 2050, 0)])
+    (1, 300, 1000, 520, 0), (2, 1501, 1023, 1001, 17), (100, 8, 64, 40, 0), (300, 1, 40, 8, 3), (1, 3000, 257, 40, 0), (1, 5000, 512, 512, 0), (1, 700, 2100, 2050, 0), (1, 256, 130, 70, 0), (1, 257, 130, 70, 1),
+    (40, 33, 130, 100, 2), (1, 3, 2200, 2000, 0), (400, 1, 3, 2, 0)])
 def test_sizes(clients, rows, ins, outs, pad, type_):
     """Dense and padded rows, one client and many, sizes around every tile; nothing is written beside the two layers."""
     total = clients * rows
@@ -102,9 +103,10 @@ def test_accumulates_and_leaves_out(clients, rows, ins, outs, type_):
             assert torch.equal(rows_of(g)[part], rows_of(both if wanted else before)[part])
 
 
-def test_every_bit_of_fp32_counts():
+@pytest.mark.parametrize("rows", [64, 512])
+def test_every_bit_of_fp32_counts(rows):
     """dy whose parts of eight bits cancel in the sums but for the lowest."""
-    rows, ins, outs = 64, 128, 128
+    ins, outs = 128, 128
     x8, v = room(rows, ins), torch.ones(rows, ins, device="cuda")
     assert co3.co3_f8_pack(v, x8) == co3.OK
     dy = torch.full((rows, outs), 1.0, device="cuda")
@@ -113,13 +115,14 @@ def test_every_bit_of_fp32_counts():
     assert co3.co3_f8_weight_gradient(dy, x8, ins, grads, None, 1, outs * ins, workspace(rows, outs, ins, 1)) == co3.OK
     torch.cuda.synchronize()
     # the tensor core adds up the lowest parts first: they are all of one sign; the others cancel exactly
-    assert torch.equal(grads, torch.full_like(grads, -32 * 2.0 ** -23))
+    assert torch.equal(grads, torch.full_like(grads, -rows / 2 * 2.0 ** -23))
 
 
+@pytest.mark.parametrize("rows", [130, 700])
 @pytest.mark.parametrize("type_", list(TYPES))
-def test_nonfinite(type_):
+def test_nonfinite(type_, rows):
     """An infinity of dy times inputs that are not zero, a NaN of dy, a NaN among the kept inputs: each where it belongs."""
-    rows, ins, outs = 130, 200, 300
+    ins, outs = 200, 304
     x = torch.rand(rows, ins, device="cuda") + 0.5
     x[100, 7] = float("nan")
     x8 = room(rows, ins)
