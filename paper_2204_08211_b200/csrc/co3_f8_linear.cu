@@ -3,10 +3,10 @@
 // The weights are the first operand, 128 of their rows (or, transposed, of their columns) per tile, and the rows of x the second,
 // 16 to 256 of them: tensor memory then holds an output feature per lane and a row of x per column, so that a warp's 32 lanes
 // write neighbouring entries of y, and few rows of x cost little.  The tensor core applies both operands' scales while it multiplies
-// (kind::mxf8f6f4, an exponent byte for each 32 columns of the sum: the same four times); sums are fp32 in tensor memory over the
-// whole length.
+// (kind::mxf8f6f4, an exponent byte for each 32 columns of the sum: the same four times); sums are fp32 in tensor memory, and in
+// registers every so many columns.
 //
-// A block of threads: one thread issues bulk copies, one the products, eight warps take the sums out.  A stage of the ring is a
+// A block of threads: one warp issues bulk copies, one the products, eight warps take the sums out.  A stage of the ring is a
 // block of 128 columns of the sum; exponent bytes come with every fourth.  Few tiles: the blocks of a cluster divide the
 // sum's length, and add their parts through shared memory in order.
 #include <algorithm>
@@ -739,16 +739,39 @@ __global__ void __launch_bounds__(kF8Threads, 1) f8_few_kernel(const __grid_cons
     if (threadIdx.x == 0 && *failed && a.res) atomicExch(&a.res->status, CO3_ERR_CUDA);
 }
 
-int device_sms(uint32_t* out) {
-    static std::atomic<int> known[64];
+// Multiprocessors, and how many clusters of 2, 4 and 8 blocks run at once, a block on each multiprocessor (74, 33 and 15 here: clusters
+// stay within a group of 16 to 20 multiprocessors).
+struct Device {
+    uint32_t at_once[4];  // clusters of 1, 2, 4, 8
+};
+int this_device(Device* out) {
+    static std::atomic<uint64_t> known[64];  // four times 16 bits
     int dev = 0;
     CO3_CUDA(cudaGetDevice(&dev));
-    int n = dev < 64 ? known[dev].load(std::memory_order_relaxed) : 0;
-    if (n == 0) {
+    uint64_t v = dev < 64 ? known[dev].load(std::memory_order_relaxed) : 0;
+    if (v == 0) {
+        int n = 0;
         CO3_CUDA(cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev));
-        if (dev < 64) known[dev].store(n, std::memory_order_relaxed);
+        v = (uint64_t)(uint16_t)n;
+        auto* kernel = f8_linear_kernel<64, false, true>;
+        CO3_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Shape<64>::kSmem));
+        for (uint32_t i = 1; i < 4; ++i) {
+            cudaLaunchConfig_t cfg = {};
+            cfg.gridDim = dim3(1u << i);
+            cfg.blockDim = dim3(kF8Threads);
+            cfg.dynamicSmemBytes = Shape<64>::kSmem;
+            cudaLaunchAttribute attr[1];
+            attr[0].id = cudaLaunchAttributeClusterDimension;
+            attr[0].val.clusterDim.x = 1u << i;
+            attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+            cfg.attrs = attr;
+            cfg.numAttrs = 1;
+            CO3_CUDA(cudaOccupancyMaxActiveClusters(&n, kernel, &cfg));
+            v |= (uint64_t)(uint16_t)n << (16 * i);
+        }
+        if (dev < 64) known[dev].store(v, std::memory_order_relaxed);
     }
-    *out = (uint32_t)n;
+    for (uint32_t i = 0; i < 4; ++i) out->at_once[i] = (uint32_t)(v >> (16 * i)) & 0xffffu;
     return CO3_OK;
 }
 
@@ -779,29 +802,29 @@ int launch_clusters(const Args& a, uint32_t blocks, uint32_t cluster, cudaStream
     return CO3_OK;
 }
 template <int kN, bool kTransposed>
-int launch_linear(const LinearArgs& a, uint32_t sms, cudaStream_t st) {
+int launch_linear(const LinearArgs& a, const Device& d, cudaStream_t st) {
     const uint32_t tiles = a.m_tiles * a.n_tiles;
     if (a.split > 1) return launch_clusters<f8_linear_kernel<kN, kTransposed, true>, Shape<kN>::kSmem>(a, tiles * a.split, a.split, st);
-    return launch_clusters<f8_linear_kernel<kN, kTransposed, false>, Shape<kN>::kSmem>(a, std::min(tiles, sms), 1, st);
+    return launch_clusters<f8_linear_kernel<kN, kTransposed, false>, Shape<kN>::kSmem>(a, std::min(tiles, d.at_once[0]), 1, st);
 }
-int launch_pairs(LinearArgs a, bool transposed, uint32_t sms, cudaStream_t st) {
+int launch_pairs(LinearArgs a, bool transposed, const Device& d, cudaStream_t st) {
     a.n_tiles = (a.rows + kPairCols - 1) / kPairCols;
     const uint64_t tiles = (uint64_t)((a.m_tiles + 1) / 2) * a.n_tiles;
-    const uint32_t blocks = 2 * (uint32_t)std::min<uint64_t>(tiles, sms / 2);
+    const uint32_t blocks = 2 * (uint32_t)std::min<uint64_t>(tiles, std::max(1u, d.at_once[1]));
     return transposed ? launch_clusters<f8_pair_kernel<true>, kPairSmem>(a, blocks, 2, st) : launch_clusters<f8_pair_kernel<false>, kPairSmem>(a, blocks, 2, st);
 }
-
-// Blocks that divide a tile's sum: as many as leave none waiting, two blocks of columns each at least.
-uint32_t split_of(uint64_t tiles, uint32_t kb, uint32_t sms) {
+// Blocks that divide a tile's sum: as many as leave no cluster waiting (16 x 8192 x 4608: 51 us in two rounds of clusters, 21 in one), two
+// blocks of columns each at least.
+uint32_t split_of(uint64_t tiles, uint32_t kb, const Device& d) {
     uint32_t split = 1;
-    while (split < kMaxSplit && tiles * split * 2 <= sms && kb >= split * 4) split *= 2;
+    for (uint32_t i = 1; i < 4 && tiles <= d.at_once[i] && kb >= (2u << i); ++i) split = 1u << i;
     return split;
 }
 template <int kN>
-int launch_tile(LinearArgs a, bool transposed, uint32_t sms, cudaStream_t st) {
+int launch_tile(LinearArgs a, bool transposed, const Device& d, cudaStream_t st) {
     a.n_tiles = (a.rows + kN - 1) / kN;
-    a.split = split_of((uint64_t)a.m_tiles * a.n_tiles, a.kb, sms);
-    return transposed ? launch_linear<kN, true>(a, sms, st) : launch_linear<kN, false>(a, sms, st);
+    a.split = split_of((uint64_t)a.m_tiles * a.n_tiles, a.kb, d);
+    return transposed ? launch_linear<kN, true>(a, d, st) : launch_linear<kN, false>(a, d, st);
 }
 
 }  // namespace
@@ -825,8 +848,8 @@ int co3_f8_linear(const void* x, int x_type, uint64_t x_row_stride, void* x8, si
         return CO3_ERR_INVALID_ARG;
     if (x8_bytes < lx.bytes || w8_bytes < lw.bytes) return CO3_ERR_CAPACITY;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
-    uint32_t sms = 0;
-    int e = device_sms(&sms);
+    Device d = {};
+    int e = this_device(&d);
     if (e != CO3_OK) return e;
     const uint8_t *w = static_cast<const uint8_t*>(w8), *b = static_cast<const uint8_t*>(x8);
     LinearArgs a = {};
@@ -850,8 +873,10 @@ int co3_f8_linear(const void* x, int x_type, uint64_t x_row_stride, void* x8, si
     a.bias = bias;
     a.res = res;
     if (rows <= kFewRows) {
-        a.split = split_of(a.m_tiles, a.kb, sms);
-        if ((a.kb + a.split - 1) / a.split <= kFewBlocks) {
+        // while a warp packs two rounds of rows at most; beyond, packing apart and the kernel below are faster (16 x 8192 x 2048: 30 and 20 us)
+        a.split = split_of(a.m_tiles, a.kb, d);
+        const uint64_t own = (a.kb + a.split - 1) / a.split;
+        if (own <= kFewBlocks && own * rows <= 64) {
             FewArgs f = {a, x, x_type, x_row_stride, from, 0, static_cast<uint8_t*>(x8), static_cast<uint8_t*>(x8) + lx.scales};
             f.wide = x && aligned(x, 4 * type_size(x_type)) && x_row_stride % 4 == 0;
             return transposed ? launch_clusters<f8_few_kernel<true>, kFewSmem>(f, a.m_tiles * a.split, a.split, st)
@@ -867,13 +892,14 @@ int co3_f8_linear(const void* x, int x_type, uint64_t x_row_stride, void* x8, si
     // 1001 15.5 / 13.3 / 15.5, 3000 x 128 x 1000 12.2 / 11.6 / 10.4.
     auto single = [&](uint32_t n, uint32_t stage, uint32_t besides) {
         const uint64_t tiles = (uint64_t)a.m_tiles * ((rows + n - 1) / n);
-        const uint32_t split = split_of(tiles, a.kb, sms);
-        return (tiles * split + sms - 1) / sms * ((uint64_t)(a.kb + split - 1) / split * stage + besides + (split > 1 ? 1500 : 0));
+        const uint32_t split = split_of(tiles, a.kb, d);
+        return (split > 1 ? 1 : (tiles + d.at_once[0] - 1) / d.at_once[0]) * ((uint64_t)(a.kb + split - 1) / split * stage + besides + (split > 1 ? 1500 : 0));
     };
     const uint64_t pairs = (uint64_t)((a.m_tiles + 1) / 2) * ((rows + kPairCols - 1) / kPairCols);
-    const uint64_t by_pairs = (pairs + sms / 2 - 1) / (sms / 2) * ((uint64_t)a.kb * 370 + 5500), by_128 = single(128, 470, 2500), by_64 = single(64, 430, 1500);
-    if (by_pairs <= by_128 && by_pairs <= by_64) return launch_pairs(a, transposed != 0, sms, st);
-    return by_128 < by_64 ? launch_tile<128>(a, transposed != 0, sms, st) : launch_tile<64>(a, transposed != 0, sms, st);
+    const uint64_t pairs_at_once = std::max(1u, d.at_once[1]);
+    const uint64_t by_pairs = (pairs + pairs_at_once - 1) / pairs_at_once * ((uint64_t)a.kb * 370 + 5500), by_128 = single(128, 470, 2500), by_64 = single(64, 430, 1500);
+    if (by_pairs <= by_128 && by_pairs <= by_64) return launch_pairs(a, transposed != 0, d, st);
+    return by_128 < by_64 ? launch_tile<128>(a, transposed != 0, d, st) : launch_tile<64>(a, transposed != 0, d, st);
 }
 
 }  // extern "C"
