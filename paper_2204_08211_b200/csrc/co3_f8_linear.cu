@@ -531,8 +531,12 @@ struct FewArgs {
     uint32_t cols, wide;     // wide: rows are aligned for four values at a time
     uint8_t *x8, *x8_scales;
 };
+// Two warps issue products, for every other group of four blocks, each into sums of its own that are added up at the end: one alone takes
+// 0.35 us for the 16 KB of a stage (1 x 8192 x 8192 22.4 us, with two 17.6; the weights' bytes 10).
+constexpr uint32_t kFewSums = 4;
+static_assert(kFewStages == 8 && (kFewBlocks / 4 + 2) / 2 * 4 <= kFewSums * kBlocksF32 && kFewBlocks <= kBlocks16, "a warp's sums");
 struct FewSmem {
-    uint64_t full[kFewStages], empty[kFewStages], sum_full[2], sum_empty[2], ready, done;
+    uint64_t full[kFewStages], empty[kFewStages], sum_full[2], ready, done[2];
     uint32_t tmem, failed;
 };
 static_assert(sizeof(FewSmem) <= 256, "barriers");
@@ -575,9 +579,8 @@ __global__ void __launch_bounds__(kF8Threads, 1) f8_few_kernel(const __grid_cons
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
     if (threadIdx.x == 0) {
         for (uint32_t i = 0; i < kFewStages; ++i) { mbar_init(&sm.full[i], 1); mbar_init(&sm.empty[i], 1); }
-        for (uint32_t i = 0; i < 2; ++i) { mbar_init(&sm.sum_full[i], 1); mbar_init(&sm.sum_empty[i], 8); }
+        for (uint32_t i = 0; i < 2; ++i) { mbar_init(&sm.sum_full[i], 1); mbar_init(&sm.done[i], 1); }
         mbar_init(&sm.ready, 8);
-        mbar_init(&sm.done, 1);
         sm.failed = 0;
     }
     if (warp == 1) {
@@ -594,7 +597,7 @@ __global__ void __launch_bounds__(kF8Threads, 1) f8_few_kernel(const __grid_cons
 
     const uint32_t part = blockIdx.x % a.split, mt = blockIdx.x / a.split;
     const uint32_t k0 = (uint32_t)((uint64_t)a.kb * part / a.split), k1 = (uint32_t)((uint64_t)a.kb * (part + 1) / a.split);
-    const bool issues = warp < 2 && elected();
+    const bool issues = warp < 3 && elected();
     if (warp == 0) {
         uint32_t st = 0, turn = 0;
         for (uint32_t q = k0; q < k1; ++q) {
@@ -612,23 +615,21 @@ __global__ void __launch_bounds__(kF8Threads, 1) f8_few_kernel(const __grid_cons
             const uint32_t begun = turn + (i < st ? 1u : 0u);
             if (begun > 0) f8_wait(&sm.full[i], (begun - 1) & 1u);
         }
-    } else if (warp == 1) {
-        uint32_t st = 0, turn = 0, sum = 0, sum_turn = 0, group = 0, left = 0;
+    } else if (warp < 3) {
+        const uint32_t which = warp - 1u;
+        uint32_t mine = 0, group = 0;  // blocks and groups of this warp
         bool ok = f8_wait(&sm.ready, 0);
         for (uint32_t q = k0; q < k1 && ok; ++q) {
-            const bool fresh = left == 0;
-            if (fresh) {
-                left = min(a.blocks, k1 - q);
-                if (sum_turn > 0 && !f8_wait(&sm.sum_empty[sum], (sum_turn - 1) & 1u)) { ok = false; break; }
-            }
-            --left;
+            if ((((q >> 2) - (k0 >> 2)) & 1u) != which) continue;
+            const uint32_t st = (q - k0) % kFewStages, turn = (q - k0) / kFewStages;
             if (!f8_wait(&sm.full[st], turn & 1u)) { ok = false; break; }
             tc_fence_after();
             const bool with_scales = q == k0 || (q & 3u) == 0;
-            // the columns of eight groups ago are free: fewer than kFewStages blocks are under way
-            if (with_scales) group = (group + 1) % kScaleTurns;
+            // the columns of four groups of this warp ago are free: only two groups are under way
+            if (with_scales) group = (group + 1) % (kScaleTurns / 2);
             if (issues) {
-                const uint32_t d = tmem + sum * kFewRows, sa = tmem + kTmemScales + group * kScaleCols, sb = sa + 4;
+                const uint32_t d = tmem + (which * kFewSums + mine / a.blocks) * kFewRows, sa = tmem + kTmemScales + (which * (kScaleTurns / 2) + group) * kScaleCols, sb = sa + 4;
+                const bool fresh = mine % a.blocks == 0;
                 if (with_scales) {
                     f8_scales_in(sa, smem_addr(scales + st * kF8Scales));
                     f8_scales_in(sb, smem_addr(x_scales + ((q >> 2) - (k0 >> 2)) * kF8Scales));
@@ -641,14 +642,15 @@ __global__ void __launch_bounds__(kF8Threads, 1) f8_few_kernel(const __grid_cons
                     default: multiply_block<kTransposed, 3>(d, at, bt, kFewRows, sa, sb, !fresh); break;
                 }
                 tc_commit(&sm.empty[st]);
-                if (left == 0) tc_commit(&sm.sum_full[sum]);
             }
-            if (left == 0 && ++sum == 2) { sum = 0; ++sum_turn; }
-            if (++st == kFewStages) { st = 0; ++turn; }
+            ++mine;
         }
         if (!ok) *failed = 1;
-        if (issues) tc_commit(&sm.done);
-        f8_wait(&sm.done, 0);
+        if (issues) {
+            tc_commit(&sm.sum_full[which]);
+            tc_commit(&sm.done[which]);
+        }
+        f8_wait(&sm.done[which], 0);
     } else if (warp >= 4) {
         // rows of a block by warps, four columns a lane; rows that are not there stay as they are: they reach no sum that counts
         const uint32_t units = (k1 - k0) * a.rows;
@@ -705,19 +707,17 @@ __global__ void __launch_bounds__(kF8Threads, 1) f8_few_kernel(const __grid_cons
 
         const uint32_t quad = warp & 3u, half = (warp - 4u) >> 2, row = quad * 32u + lane;
         constexpr int kHalf = kFewRows / 2;
-        uint32_t sum = 0, sum_turn = 0;
+        uint32_t blocks[2] = {0, 0};  // of the two warps
+        for (uint32_t q = k0; q < k1; ++q) ++blocks[((q >> 2) - (k0 >> 2)) & 1u];
         float acc[kHalf];
-        bool ok = true;
-        for (uint32_t q = k0; q < k1; q += a.blocks) {
-            ok = lane != 0 || f8_wait(&sm.sum_full[sum], sum_turn & 1u);
-            ok = __all_sync(0xffffffffu, ok);
-            if (!ok) break;
+        bool ok = lane != 0 || (f8_wait(&sm.sum_full[0], 0) && f8_wait(&sm.sum_full[1], 0));
+        ok = __all_sync(0xffffffffu, ok);
+        if (ok) {
             tc_fence_after();
-            take_sums(tmem + ((quad * 32u) << 16) + sum * kFewRows + half * kHalf, q == k0, acc);
+            for (uint32_t w = 0; w < 2; ++w)
+                for (uint32_t i = 0; i * a.blocks < blocks[w]; ++i)
+                    take_sums(tmem + ((quad * 32u) << 16) + (w * kFewSums + i) * kFewRows + half * kHalf, w == 0 && i == 0, acc);
             tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&sm.sum_empty[sum]);
-            if (++sum == 2) { sum = 0; ++sum_turn; }
         }
         if (!ok) {
             *failed = 1;
