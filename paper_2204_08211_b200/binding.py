@@ -449,8 +449,16 @@ def co3_muon_update(grad, momentum, params, mats, mu, nesterov, lr, weight_decay
                                    workspace.numel() * workspace.element_size(), _stream(stream))
 
 
+def _f8_sizes(*sizes) -> None:
+    """The library's integers would keep the lower bits of larger sizes."""
+    for n in sizes:
+        if not 0 <= n < 1 << 31:
+            raise ValueError("8-bit blocks: rows and columns from 0 to 2^31 - 1")
+
+
 def co3_f8_bytes(rows: int, cols: int, kind: int = F8_ROWS) -> int:
     """Size of the buffer that holds a rows x cols matrix in 8-bit blocks."""
+    _f8_sizes(rows, cols)
     out = C.c_size_t(0)
     st = _load().co3_f8_bytes(rows, cols, kind, C.byref(out))
     if st != OK:
@@ -479,6 +487,7 @@ def _res(t):
 def co3_f8_pack(x, out, kind: int = F8_ROWS, stream=None) -> int:
     """out (uint8, co3_f8_bytes of x's rows and columns) <- x in 8-bit blocks."""
     p, rows, cols, xs = _rows(x)
+    _f8_sizes(rows, cols)
     q, n = _f8(out)
     return (_lib or _load()).co3_f8_pack(p, _TYPES[x.dtype], rows, cols, xs, kind, q, n, _stream_of(x, stream))
 
@@ -486,6 +495,7 @@ def co3_f8_pack(x, out, kind: int = F8_ROWS, stream=None) -> int:
 def co3_f8_unpack(f8, y, kind: int = F8_ROWS, stream=None) -> int:
     """y <- the values of a buffer of 8-bit blocks that holds a matrix of y's shape."""
     p, rows, cols, ys = _rows(y)
+    _f8_sizes(rows, cols)
     q, n = _f8(f8)
     return (_lib or _load()).co3_f8_unpack(q, n, kind, p, _TYPES[y.dtype], rows, cols, ys, _stream_of(y, stream))
 
@@ -493,6 +503,7 @@ def co3_f8_unpack(f8, y, kind: int = F8_ROWS, stream=None) -> int:
 def co3_f8_activation(x, act: int, y=None, y8=None, x8=None, stream=None) -> int:
     """y <- act(x), y8 <- act(x) in 8-bit blocks, x8 <- x in 8-bit blocks; each of the three may be None."""
     p, rows, cols, xs = _rows(x)
+    _f8_sizes(rows, cols)
     py, ys = (None, 0) if y is None else _rows(y, x)[::3]
     q, n = _f8(y8)
     k, m = _f8(x8)
@@ -503,6 +514,7 @@ def co3_f8_activation(x, act: int, y=None, y8=None, x8=None, stream=None) -> int
 def co3_f8_activation_backward(dy, x8, act: int, dx, stream=None) -> int:
     """dx <- dy * act'(x) with the values of x that co3_f8_activation left in x8; dx may be dy."""
     p, rows, cols, ds = _rows(dy)
+    _f8_sizes(rows, cols)
     po, _, _, os_ = _rows(dx, dy)
     k, n = _f8(x8)
     return (_lib or _load()).co3_f8_activation_backward(p, _TYPES[dy.dtype], rows, cols, ds, k, n, act, po, os_, _stream_of(dy, stream))
@@ -524,6 +536,7 @@ def co3_f8_linear(x, x8, w8, bias, y, transposed: bool = False, cols: int | None
         cols = width
     if rx != rows:
         raise ValueError("co3_f8_linear: x and y have different rows")
+    _f8_sizes(rows, to, cols)
     q, n = _f8(x8)
     w, m = _f8(w8)
     outs, ins = (cols, to) if transposed else (to, cols)
@@ -533,6 +546,7 @@ def co3_f8_linear(x, x8, w8, bias, y, transposed: bool = False, cols: int | None
 
 def co3_f8_weight_gradient_workspace_bytes(rows: int, outs: int, ins: int, n_clients: int = 1) -> int:
     """Device workspace of co3_f8_weight_gradient for n_clients batches of `rows` rows each."""
+    _f8_sizes(rows, outs, ins, n_clients)
     out = C.c_size_t(0)
     st = _load().co3_f8_weight_gradient_workspace_bytes(rows, outs, ins, n_clients, C.byref(out))
     if st != OK:
@@ -547,8 +561,9 @@ def co3_f8_weight_gradient(dy, x8, ins: int, dw, db, n_clients: int, client_stri
     p, rows, outs, ds = _rows(dy)
     if n_clients < 1 or rows % n_clients:
         raise ValueError("co3_f8_weight_gradient: the rows do not divide into n_clients batches")
-    if client_stride_elems < 0 or ins < 0:  # the library takes them as unsigned
-        raise ValueError("co3_f8_weight_gradient: negative sizes")
+    if client_stride_elems < 0:  # the library takes it as unsigned
+        raise ValueError("co3_f8_weight_gradient: clients' vectors that lie backwards")
+    _f8_sizes(rows, outs, ins, n_clients)
     q, n = _f8(x8)
     before = (n_clients - 1) * client_stride_elems
     return (_lib or _load()).co3_f8_weight_gradient(

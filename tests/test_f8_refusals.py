@@ -49,6 +49,16 @@ def test_bytes_refusals(lib):
         assert lib.co3_f8_weight_gradient_workspace_bytes(rows, outs, ins, clients, ctypes.byref(out)) == co3.ERR_INVALID_ARG
 
 
+def test_sizes_that_would_be_cut_to_32_bits():
+    for rows, cols in ((1, 2 ** 32 + 5), (2 ** 32 + 5, 1), (-1, 4), (4, -1), (2 ** 31, 1)):
+        with pytest.raises(ValueError):
+            co3.co3_f8_bytes(rows, cols)
+        with pytest.raises(ValueError):
+            co3.co3_f8_weight_gradient_workspace_bytes(rows, cols, 8)
+    with pytest.raises(ValueError):
+        co3.co3_f8_weight_gradient_workspace_bytes(8, 8, 2 ** 32 + 8)
+
+
 def test_pack_and_activation_refusals(lib):
     big = 1 << 40
     pack = lambda x=AT, t=0, rows=8, cols=8, stride=8, kind=0, out=AT, n=big: lib.co3_f8_pack(x, t, rows, cols, stride, kind, out, n, None)
