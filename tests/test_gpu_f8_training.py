@@ -3,6 +3,8 @@ example run them: every gradient against the formula in 64 bits on what the call
 graph, and the session's refusals."""
 import importlib.util
 import os
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -178,3 +180,47 @@ def test_session_refuses_layers_of_another_shape():
     for weight, bias, shape in ((1, None, (3, 4)), (0, 0, (3, 4)), (0, 1, (4, 3)), (0, 1, (2, 6))):
         with pytest.raises(ValueError):
             sess.linear_backward(dy, None, x8, w8, weight, bias, shape, None, grads, ws)
+
+
+FIRST_CALLS = """
+import sys
+sys.path.insert(0, sys.argv[1])
+import torch
+import paper_2204_08211_b200 as co3
+room = lambda r, c, k=co3.F8_ROWS: torch.empty(co3.co3_f8_bytes(r, c, k), dtype=torch.uint8, device="cuda")
+cases = []
+for rows, ins, outs in ((3, 300, 500), (200, 300, 500), (3000, 512, 2304)):
+    x, dy, w = torch.randn(rows, ins, device="cuda"), torch.randn(rows, outs, device="cuda").bfloat16(), torch.randn(outs, ins, device="cuda")
+    t = dict(x=x, dy=dy, w=w, x8=room(rows, ins), d8=room(rows, outs), w8=room(outs, ins, co3.F8_SQUARE), y=torch.empty(rows, outs, device="cuda"),
+             dx=torch.empty(rows, ins, device="cuda"), g=torch.empty(outs * ins + outs, device="cuda"),
+             ws=torch.empty(co3.co3_f8_weight_gradient_workspace_bytes(rows, outs, ins), dtype=torch.uint8, device="cuda"))
+    cases.append((ins, outs, t))
+
+def run():
+    for ins, outs, t in cases:
+        assert co3.co3_f8_pack(t["w"], t["w8"], co3.F8_SQUARE) == co3.OK
+        assert co3.co3_f8_linear(t["x"], t["x8"], t["w8"], None, t["y"]) == co3.OK
+        assert co3.co3_f8_linear(t["dy"], t["d8"], t["w8"], None, t["dx"], True) == co3.OK
+        assert co3.co3_f8_weight_gradient(t["dy"], t["x8"], ins, t["g"], t["g"][outs * ins:], 1, outs * ins + outs, t["ws"]) == co3.OK
+
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    run()
+graph.replay()
+torch.cuda.synchronize()
+kept = [[t[k].clone() for k in ("y", "dx", "g")] for _, _, t in cases]
+run()
+torch.cuda.synchronize()
+for (_, _, t), want in zip(cases, kept):
+    for k, v in zip(("y", "dx", "g"), want):
+        assert torch.isfinite(v).all() and torch.equal(t[k], v), k
+print("captured")
+"""
+
+
+def test_first_calls_of_a_process_can_be_captured():
+    """What the calls ask the device for once (attributes, clusters at once, the driver's tensor maps) is allowed while a stream is captured."""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    p = subprocess.run([sys.executable, "-c", FIRST_CALLS, root], capture_output=True, text=True, timeout=120)
+    assert p.returncode == 0 and "captured" in p.stdout, p.stderr[-2000:]

@@ -163,6 +163,20 @@ def test_against_differences():
         assert (grads.view(outs, ins)[o, i].double() - d).abs() <= (rows / 16 + 3) * 2.0 ** -20.8 * size + 1e-9 * f(w.abs()).abs()
 
 
+def test_bias_alone():
+    """Without weights: no inputs are needed; a layer without inputs has a bias all the same."""
+    for rows, outs in ((40, 24), (3000, 136)):
+        dy = gradients(2 * rows, outs, rows)
+        for ins in (0, 16):
+            grads = torch.full((2 * (outs + 3),), 7.0, device="cuda")
+            assert co3.co3_f8_weight_gradient(dy, None, ins, None, grads, 2, outs + 3, workspace(rows, outs, ins, 2)) == co3.OK
+            torch.cuda.synchronize()
+            for u in range(2):
+                d = dy[u * rows:(u + 1) * rows].double()
+                got = grads[u * (outs + 3):(u + 1) * (outs + 3)]
+                assert ((got[:outs].double() - d.sum(0)).abs() <= (rows + 3) * 2.0 ** -24 * d.abs().sum(0)).all() and (got[outs:] == 7.0).all()
+
+
 def test_no_rows():
     grads = torch.full((2 * 40,), 7.0, device="cuda")
     dy, x8, ws = torch.zeros(0, 8, device="cuda"), room(0, 4), workspace(0, 8, 4, 2)
