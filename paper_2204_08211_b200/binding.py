@@ -449,10 +449,13 @@ def co3_muon_update(grad, momentum, params, mats, mu, nesterov, lr, weight_decay
                                    workspace.numel() * workspace.element_size(), _stream(stream))
 
 
+_F8_MOST = (1 << 31) - 1
+
+
 def _f8_sizes(*sizes) -> None:
     """The library's integers would keep the lower bits of larger sizes."""
     for n in sizes:
-        if not 0 <= n < 1 << 31:
+        if not 0 <= n <= _F8_MOST:
             raise ValueError("8-bit blocks: rows and columns from 0 to 2^31 - 1")
 
 
@@ -487,7 +490,8 @@ def _res(t):
 def co3_f8_pack(x, out, kind: int = F8_ROWS, stream=None) -> int:
     """out (uint8, co3_f8_bytes of x's rows and columns) <- x in 8-bit blocks."""
     p, rows, cols, xs = _rows(x)
-    _f8_sizes(rows, cols)
+    if rows > _F8_MOST or cols > _F8_MOST:
+        _f8_sizes(rows, cols)
     q, n = _f8(out)
     return (_lib or _load()).co3_f8_pack(p, _TYPES[x.dtype], rows, cols, xs, kind, q, n, _stream_of(x, stream))
 
@@ -495,7 +499,8 @@ def co3_f8_pack(x, out, kind: int = F8_ROWS, stream=None) -> int:
 def co3_f8_unpack(f8, y, kind: int = F8_ROWS, stream=None) -> int:
     """y <- the values of a buffer of 8-bit blocks that holds a matrix of y's shape."""
     p, rows, cols, ys = _rows(y)
-    _f8_sizes(rows, cols)
+    if rows > _F8_MOST or cols > _F8_MOST:
+        _f8_sizes(rows, cols)
     q, n = _f8(f8)
     return (_lib or _load()).co3_f8_unpack(q, n, kind, p, _TYPES[y.dtype], rows, cols, ys, _stream_of(y, stream))
 
@@ -503,7 +508,8 @@ def co3_f8_unpack(f8, y, kind: int = F8_ROWS, stream=None) -> int:
 def co3_f8_activation(x, act: int, y=None, y8=None, x8=None, stream=None) -> int:
     """y <- act(x), y8 <- act(x) in 8-bit blocks, x8 <- x in 8-bit blocks; each of the three may be None."""
     p, rows, cols, xs = _rows(x)
-    _f8_sizes(rows, cols)
+    if rows > _F8_MOST or cols > _F8_MOST:
+        _f8_sizes(rows, cols)
     py, ys = (None, 0) if y is None else _rows(y, x)[::3]
     q, n = _f8(y8)
     k, m = _f8(x8)
@@ -514,7 +520,8 @@ def co3_f8_activation(x, act: int, y=None, y8=None, x8=None, stream=None) -> int
 def co3_f8_activation_backward(dy, x8, act: int, dx, stream=None) -> int:
     """dx <- dy * act'(x) with the values of x that co3_f8_activation left in x8; dx may be dy."""
     p, rows, cols, ds = _rows(dy)
-    _f8_sizes(rows, cols)
+    if rows > _F8_MOST or cols > _F8_MOST:
+        _f8_sizes(rows, cols)
     po, _, _, os_ = _rows(dx, dy)
     k, n = _f8(x8)
     return (_lib or _load()).co3_f8_activation_backward(p, _TYPES[dy.dtype], rows, cols, ds, k, n, act, po, os_, _stream_of(dy, stream))
@@ -536,7 +543,8 @@ def co3_f8_linear(x, x8, w8, bias, y, transposed: bool = False, cols: int | None
         cols = width
     if rx != rows:
         raise ValueError("co3_f8_linear: x and y have different rows")
-    _f8_sizes(rows, to, cols)
+    if rows > _F8_MOST or to > _F8_MOST or not 0 <= cols <= _F8_MOST:
+        _f8_sizes(rows, to, cols)
     q, n = _f8(x8)
     w, m = _f8(w8)
     outs, ins = (cols, to) if transposed else (to, cols)
