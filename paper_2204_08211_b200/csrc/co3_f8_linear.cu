@@ -36,6 +36,7 @@ struct LinearArgs {
     uint32_t features, rows;
     uint32_t m_tiles, n_tiles;
     uint32_t split;
+    uint32_t pair_rows;                      // rows of x in a pair's tile, 128 or 256
     uint32_t blocks;                         // blocks that tensor memory adds up
     void* y;
     uint64_t y_stride;
@@ -331,7 +332,7 @@ __global__ void __launch_bounds__(kF8Threads, 1) f8_linear_kernel(const __grid_c
 }
 
 // ------------------------------------------------------------------------------------------------
-// Tiles of 256 features by 256 rows of x, by pairs of blocks.
+// Tiles of 256 features by 256 (or 128) rows of x, by pairs of blocks.
 // ------------------------------------------------------------------------------------------------
 constexpr uint32_t kPairCols = 256, kPairStages = 6;
 constexpr uint32_t kPairStageBytes = 2 * kF8Tile, kPairScaleBytes = 3 * kF8Scales;  // the second operand's scales for all 256 rows
@@ -396,7 +397,7 @@ __global__ void __launch_bounds__(kF8Threads, 1) f8_pair_kernel(const __grid_con
             uint32_t st = 0, turn = 0;
             for (uint32_t t = first; t < tiles && !*failed; t += step) {
                 const uint32_t mt = min(2 * (t % m_pairs) + rank, a.m_tiles - 1);  // (an odd last tile: the second block's sums go nowhere)
-                const uint32_t n0 = t / m_pairs * kPairCols, n = min(kPairCols, (a.rows - n0 + 15u) & ~15u);
+                const uint32_t n0 = t / m_pairs * a.pair_rows, n = min(a.pair_rows, (a.rows - n0 + 15u) & ~15u);
                 const uint32_t b_scales = n > 128 ? 2 * kF8Scales : kF8Scales, half = n / 2;
                 const uint8_t *from_a = a.a + mt * a.a_tile, *from_b = a.b + (n0 + rank * half) * 128ull;
                 for (uint32_t q = 0; q < a.kb; ++q) {
@@ -438,7 +439,7 @@ __global__ void __launch_bounds__(kF8Threads, 1) f8_pair_kernel(const __grid_con
             uint32_t st = 0, turn = 0, sums = 0, group = 0;  // sums: begun
             bool ok = true;
             for (uint32_t t = first; t < tiles && ok; t += step) {
-                const uint32_t n = min(kPairCols, (a.rows - t / m_pairs * kPairCols + 15u) & ~15u);
+                const uint32_t n = min(a.pair_rows, (a.rows - t / m_pairs * a.pair_rows + 15u) & ~15u);
                 uint32_t left = 0;  // blocks that the present sum still takes
                 for (uint32_t q = 0; q < a.kb; ++q) {
                     const bool fresh = left == 0;
@@ -484,24 +485,28 @@ __global__ void __launch_bounds__(kF8Threads, 1) f8_pair_kernel(const __grid_con
         many_registers();
         constexpr int kHalf = kPairCols / 2;
         const uint32_t quad = warp & 3u, half = (warp - 4u) >> 2, row = quad * 32u + lane;
+        const uint32_t cols = a.pair_rows / 2;  // of a warp
         uint32_t sums = 0;
         bool ok = true;
         for (uint32_t t = first; t < tiles && ok; t += step) {
-            const uint32_t n0 = t / m_pairs * kPairCols, feature = (2 * (t % m_pairs) + rank) * 128u + row;
+            const uint32_t n0 = t / m_pairs * a.pair_rows, feature = (2 * (t % m_pairs) + rank) * 128u + row;
             float acc[kHalf];
             for (uint32_t q = 0; q < a.kb; q += a.blocks, ++sums) {
                 ok = lane != 0 || f8_wait(&sm.sum_full, sums & 1u);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 tc_fence_after();
-                take_sums(tmem + ((quad * 32u) << 16) + half * kHalf, q == 0, acc);
+                const uint32_t from = tmem + ((quad * 32u) << 16) + half * cols;
+                if (cols == kHalf) take_sums(from, q == 0, acc);
+                else take_sums(from, q == 0, *reinterpret_cast<float(*)[kHalf / 2]>(acc));
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive_at(&sm.sum_empty, 0);
             }
             if (!ok) break;
             const float bias = a.bias && feature < a.features ? a.bias[feature] : 0.0f;
-            write_any<kHalf>(a, feature, n0 + half * kHalf, bias, acc);
+            if (cols == kHalf) write_any<kHalf>(a, feature, n0 + half * cols, bias, acc);
+            else write_any<kHalf / 2>(a, feature, n0 + half * cols, bias, acc);
         }
         if (!ok) *failed = 1;
     }
@@ -807,8 +812,9 @@ int launch_linear(const LinearArgs& a, const Device& d, cudaStream_t st) {
     if (a.split > 1) return launch_clusters<f8_linear_kernel<kN, kTransposed, true>, Shape<kN>::kSmem>(a, tiles * a.split, a.split, st);
     return launch_clusters<f8_linear_kernel<kN, kTransposed, false>, Shape<kN>::kSmem>(a, std::min(tiles, d.at_once[0]), 1, st);
 }
-int launch_pairs(LinearArgs a, bool transposed, const Device& d, cudaStream_t st) {
-    a.n_tiles = (a.rows + kPairCols - 1) / kPairCols;
+int launch_pairs(LinearArgs a, uint32_t rows_of_tile, bool transposed, const Device& d, cudaStream_t st) {
+    a.pair_rows = rows_of_tile;
+    a.n_tiles = (a.rows + rows_of_tile - 1) / rows_of_tile;
     const uint64_t tiles = (uint64_t)((a.m_tiles + 1) / 2) * a.n_tiles;
     const uint32_t blocks = 2 * (uint32_t)std::min<uint64_t>(tiles, std::max(1u, d.at_once[1]));
     return transposed ? launch_clusters<f8_pair_kernel<true>, kPairSmem>(a, blocks, 2, st) : launch_clusters<f8_pair_kernel<false>, kPairSmem>(a, blocks, 2, st);
@@ -888,18 +894,21 @@ int co3_f8_linear(const void* x, int x_type, uint64_t x_row_stride, void* x8, si
         if (e != CO3_OK) return e;
     }
     // The estimated time of each kind of tile, in ns: rounds of tiles, a stage of each kind, what a tile costs besides, and the join of a
-    // divided sum.  us measured, pairs / 128 / 64 rows: 512 x 4096 x 4096 22 / 25 / 37, 2048 x 2048 x 2048 19 / 28 / 39, 1501 x 1023 x
-    // 1001 15.5 / 13.3 / 15.5, 3000 x 128 x 1000 12.2 / 11.6 / 10.4.
+    // divided sum.  us measured, pairs with 256 and 128 rows / one block with 128 and 64: 512 x 4096 x 4096 21.6 and 19.3 / 25 and 37, 2048 x
+    // 2048 x 2048 19.2 and 21.5 / 28 and 39, 1501 x 1023 x 1001 15.5 and 12.5 / 13.2 and 15.5, 3000 x 128 x 1000 12.2 and 12.5 / 11.6 and 10.4.
     auto single = [&](uint32_t n, uint32_t stage, uint32_t besides) {
         const uint64_t tiles = (uint64_t)a.m_tiles * ((rows + n - 1) / n);
         const uint32_t split = split_of(tiles, a.kb, d);
         return (split > 1 ? 1 : (tiles + d.at_once[0] - 1) / d.at_once[0]) * ((uint64_t)(a.kb + split - 1) / split * stage + besides + (split > 1 ? 1500 : 0));
     };
-    const uint64_t pairs = (uint64_t)((a.m_tiles + 1) / 2) * ((rows + kPairCols - 1) / kPairCols);
-    const uint64_t pairs_at_once = std::max(1u, d.at_once[1]);
-    const uint64_t by_pairs = (pairs + pairs_at_once - 1) / pairs_at_once * ((uint64_t)a.kb * 370 + 5500), by_128 = single(128, 470, 2500), by_64 = single(64, 430, 1500);
-    if (by_pairs <= by_128 && by_pairs <= by_64) return launch_pairs(a, transposed != 0, d, st);
-    return by_128 < by_64 ? launch_tile<128>(a, transposed != 0, d, st) : launch_tile<64>(a, transposed != 0, d, st);
+    auto by_pairs = [&](uint32_t n, uint32_t stage, uint32_t besides) {
+        const uint64_t pairs = (uint64_t)((a.m_tiles + 1) / 2) * ((rows + n - 1) / n), at_once = std::max(1u, d.at_once[1]);
+        return (pairs + at_once - 1) / at_once * ((uint64_t)a.kb * stage + besides);
+    };
+    const uint64_t ns[4] = {by_pairs(256, 370, 5500), by_pairs(128, 300, 3500), single(128, 470, 2500), single(64, 430, 1500)};
+    const int best = (int)(std::min_element(ns, ns + 4) - ns);
+    if (best < 2) return launch_pairs(a, best == 0 ? 256 : 128, transposed != 0, d, st);
+    return best == 2 ? launch_tile<128>(a, transposed != 0, d, st) : launch_tile<64>(a, transposed != 0, d, st);
 }
 
 }  // extern "C"
