@@ -201,24 +201,27 @@ __device__ __forceinline__ float min_nan(float a, float b) {  // NaN stays
     return y;
 }
 // Phi(-|x|), Phi the normal distribution function, is 1/2 erfc(z) with z = |x| / sqrt(2), and erfc(z) exp(z^2) = t P(t), t = 1 / (1 + 0.375 z).
-// P is a polynomial of degree 6 fitted to the smallest relative error over 0 <= z <= 12 (1e-6); with the roundings 1.5e-6 for |x| <= 4
-// and 5e-6 for |x| <= 10, far below half a step of 16 bits.  ax: |x|, 64 at most (where exp(-x^2 / 2) is zero); e: exp(-x^2 / 2); the
-// result is t P(t) / 2.
+// P is a polynomial of degree 6 fitted to the smallest relative error over 0 <= z <= 12 (1e-6); with the roundings 2e-6 for |x| <= 4
+// and 6e-6 for |x| <= 10, far below half a step of 16 bits.  ax: |x|, 64 at most (where exp(-x^2 / 2) is zero); e: 2^16 exp(-x^2 / 2),
+// so that the instruction, which takes what is below 2^-126 for zero, loses nothing that bf16 holds; the result is 2^-16 t P(t) / 2.
+constexpr float kDown16 = 1.0f / 65536.0f;
 __device__ __forceinline__ F2 normal_short(F2 ax, F2& e) {
-    const F2 arg = mul2(mul2(ax, ax), f2_both(-0.72134752044448170f)), den = fma2(ax, f2_both(0.26516504294495533f), f2_both(1.0f));
+    const F2 arg = fma2(mul2(ax, ax), f2_both(-0.72134752044448170f), f2_both(16.0f)), den = fma2(ax, f2_both(0.26516504294495533f), f2_both(1.0f));
     e = {exp2_short(arg.x), exp2_short(arg.y)};
     const F2 t = {inverse_short(den.x), inverse_short(den.y)};
-    F2 p = fma2(f2_both(-0.0666150079f), t, f2_both(0.19073585385f));
-    p = fma2(p, t, f2_both(-0.06032206705f));
-    p = fma2(p, t, f2_both(0.13837517965f));
-    p = fma2(p, t, f2_both(0.0845211864f));
-    p = fma2(p, t, f2_both(0.1076185385f));
-    p = fma2(p, t, f2_both(0.1056866174f));
+    F2 p = fma2(f2_both(-0.0666150079f * kDown16), t, f2_both(0.19073585385f * kDown16));
+    p = fma2(p, t, f2_both(-0.06032206705f * kDown16));
+    p = fma2(p, t, f2_both(0.13837517965f * kDown16));
+    p = fma2(p, t, f2_both(0.0845211864f * kDown16));
+    p = fma2(p, t, f2_both(0.1076185385f * kDown16));
+    p = fma2(p, t, f2_both(0.1056866174f * kDown16));
     return mul2(t, p);
 }
+// 1 / (1 + exp(-x)) as 2^-24 / (2^-24 + 2^-24 exp(-x)): the sum and its inverse are normal numbers down to x = -104.
+constexpr float kDown24 = 1.0f / 16777216.0f;
 __device__ __forceinline__ F2 logistic_short(F2 x) {
-    const F2 arg = mul2(x, f2_both(-1.4426950408889634f)), den = add2({exp2_short(arg.x), exp2_short(arg.y)}, f2_both(1.0f));
-    return {inverse_short(den.x), inverse_short(den.y)};
+    const F2 arg = fma2(x, f2_both(-1.4426950408889634f), f2_both(-24.0f)), den = add2({exp2_short(arg.x), exp2_short(arg.y)}, f2_both(kDown24));
+    return mul2({inverse_short(den.x), inverse_short(den.y)}, f2_both(kDown24));
 }
 
 // act(x), short forms if kShort.  Infinities give the limits (the bounds below lie where the other factor is zero), NaN stays.
@@ -234,7 +237,10 @@ __device__ __forceinline__ F2 act(F2 x) {
         auto one = [](float v) {
             if constexpr (kAct == CO3_ACT_RELU) return v < 0.0f ? 0.0f : v;
             if constexpr (kAct == CO3_ACT_GELU) return __fmul_rn(fmaxf(v, -64.0f), __fmul_rn(0.5f, erfcf(__fmul_rn(v, -0.70710678118654752f))));
-            if constexpr (kAct == CO3_ACT_SILU) return __fdiv_rn(fmaxf(v, -200.0f), __fadd_rn(1.0f, expf(-v)));
+            if constexpr (kAct == CO3_ACT_SILU) {  // exp(-|x|), which stays in range
+                const float e = expf(-fabsf(v));
+                return __fdiv_rn(v < 0.0f ? __fmul_rn(fmaxf(v, -200.0f), e) : v, __fadd_rn(1.0f, e));
+            }
             return v;
         };
         return {one(x.x), one(x.y)};
@@ -243,9 +249,9 @@ __device__ __forceinline__ F2 act(F2 x) {
 template <int kAct, bool kShort>
 __device__ __forceinline__ F2 act_slope(F2 x) {
     if constexpr (kAct == CO3_ACT_GELU && kShort) {
-        F2 e;  // x < 0: g = Phi(x) + x phi(x);  x > 0: 1 - g(-x);  g(-|x|) = exp(-x^2 / 2) (t P / 2 - |x| / sqrt(2 pi))
+        F2 e;  // x < 0: g = Phi(x) + x phi(x);  x > 0: 1 - g(-x);  g(-|x|) = exp(-x^2 / 2) (t P / 2 - |x| / sqrt(2 pi)), the bracket times 2^-16
         const F2 ax = {min_nan(fabsf(x.x), 64.0f), min_nan(fabsf(x.y), 64.0f)}, q = normal_short(ax, e);
-        const F2 g = mul2(e, fma2(ax, f2_both(-0.39894228040143268f), q));
+        const F2 g = mul2(e, fma2(ax, f2_both(-0.39894228040143268f * kDown16), q));
         auto flip = [](float v, float by) { return __uint_as_float(__float_as_uint(v) ^ (~__float_as_uint(by) & 0x80000000u)); };
         auto step = [](float v) { return (int)__float_as_uint(v) < 0 ? 0.0f : 1.0f; };
         return add2({step(x.x), step(x.y)}, {flip(g.x, x.x), flip(g.y, x.y)});
@@ -260,7 +266,7 @@ __device__ __forceinline__ F2 act_slope(F2 x) {
                 return __fmaf_rn(v, __fmul_rn(0.39894228040143268f, expf(__fmul_rn(__fmul_rn(-0.5f, v), v))), below);
             }
             if constexpr (kAct == CO3_ACT_SILU) {
-                const float p = __fdiv_rn(1.0f, __fadd_rn(1.0f, expf(-v)));
+                const float e = expf(-fabsf(v)), p = __fdiv_rn(v < 0.0f ? e : 1.0f, __fadd_rn(1.0f, e));
                 return __fmul_rn(p, __fmaf_rn(v, __fsub_rn(1.0f, p), 1.0f));
             }
             return 1.0f;
