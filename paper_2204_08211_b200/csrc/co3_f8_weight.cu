@@ -14,6 +14,7 @@
 // the parts in order.
 #include <cuda.h>
 #include <cudaTypedefs.h>
+#include <stddef.h>
 
 #include <algorithm>
 #include <atomic>
@@ -527,10 +528,16 @@ int launch_join(const Join& dw, const Join& db, uint32_t clients, uint64_t clien
 // at a time in shared memory as fp32, the next ones on their way.
 // ------------------------------------------------------------------------------------------------
 constexpr uint32_t kFewOuts = 32, kFewRowsW = 32;
+struct alignas(16) SmallSmem {  // rows are written and read 16 bytes at a time
+    float x[kFewRowsW][132];
+    float dy[kFewRowsW][kFewOuts];
+};
+static_assert(alignof(SmallSmem) % 16 == 0 && sizeof(SmallSmem::x[0]) % 16 == 0 && offsetof(SmallSmem, dy) % 16 == 0 && sizeof(SmallSmem::dy[0]) % 16 == 0, "16-byte accesses");
 template <typename T>
 __global__ void __launch_bounds__(256) f8_weight_small_kernel(const __grid_constant__ WeightArgs a) {
-    __shared__ float xs[kFewRowsW][132];
-    __shared__ float ds[kFewRowsW][kFewOuts];
+    __shared__ SmallSmem sm;
+    auto &xs = sm.x;
+    auto &ds = sm.dy;
     wait_for_previous_kernel();
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
     const uint32_t o_tiles = (a.outs + kFewOuts - 1) / kFewOuts, i_tiles = a.dw ? a.k_tiles : 1u;
