@@ -149,7 +149,7 @@ __device__ __forceinline__ void bring_dy(const WeightArgs& a, uint32_t u, uint32
                 for (int k = 0; k < 8; ++k) v[j][k] = 0.0f;
             }
         }
-        if (!a.direct) {
+        if (a.dw && !a.direct) {
             unsigned char* chunk = a.ws_dy + (((uint64_t)u * a.groups + g) * a.chunks + c) * (kParts * kPlane16) + (p >> 3) * kAtom;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
