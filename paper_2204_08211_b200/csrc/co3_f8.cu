@@ -601,6 +601,13 @@ int launch_square(const SquareArgs& a, cudaStream_t st) {
     return CO3_OK;
 }
 
+// Rows over themselves under another stride: some would be written before they are read.
+bool crossed(const void* x, uint64_t x_stride, const void* y, uint64_t y_stride, uint64_t rows) { return x == y && x_stride != y_stride && rows > 1; }
+bool overlapping(const void* a, const void* b, uint64_t bytes) {
+    const uintptr_t p = reinterpret_cast<uintptr_t>(a), q = reinterpret_cast<uintptr_t>(b);
+    return a && b && (p < q ? q - p : p - q) < bytes;
+}
+
 // f<T, kWay>() for the buffers' type and way
 #define CO3_BY_TYPE(type, w, f, ...)                                                                        \
     ((type) == CO3_F32   ? ((w) ? f<float, kWide>(__VA_ARGS__) : f<float, kSingle>(__VA_ARGS__))            \
@@ -639,7 +646,7 @@ int co3_f8_activation(const void* x, int type, uint64_t rows, uint32_t cols, uin
     if (type < CO3_F32 || type > CO3_BF16 || act < CO3_ACT_NONE || act > CO3_ACT_SILU || !f8_layout(rows, cols, CO3_F8_ROWS, &l)) return CO3_ERR_INVALID_ARG;
     if (rows == 0 || cols == 0) return CO3_OK;
     if (!f8_valid_rows(type, x, x_row_stride, cols) || (y && !f8_valid_rows(type, y, y_row_stride, cols)) || (y8 && !f8_valid(y8)) || (x8 && !f8_valid(x8)) ||
-        (!y && !y8 && !x8) || (y8 && y8 == x8))
+        (!y && !y8 && !x8) || overlapping(x8, y8, l.bytes) || crossed(x, x_row_stride, y, y_row_stride, rows))
         return CO3_ERR_INVALID_ARG;
     if ((y8 || x8) && f8_bytes < l.bytes) return CO3_ERR_CAPACITY;
     RowsArgs a = {};
@@ -656,7 +663,9 @@ static int values(const void* dy, uint64_t dy_row_stride, const void* x8, size_t
     F8Layout l;
     if (type < CO3_F32 || type > CO3_BF16 || act > CO3_ACT_SILU || !f8_layout(rows, cols, kind, &l)) return CO3_ERR_INVALID_ARG;
     if (rows == 0 || cols == 0) return CO3_OK;
-    if (!f8_valid_rows(type, out, out_row_stride, cols) || !f8_valid(x8) || (act >= 0 && !f8_valid_rows(type, dy, dy_row_stride, cols))) return CO3_ERR_INVALID_ARG;
+    if (!f8_valid_rows(type, out, out_row_stride, cols) || !f8_valid(x8) ||
+        (act >= 0 && (!f8_valid_rows(type, dy, dy_row_stride, cols) || crossed(dy, dy_row_stride, out, out_row_stride, rows))))
+        return CO3_ERR_INVALID_ARG;
     if (x8_bytes < l.bytes) return CO3_ERR_CAPACITY;
     RowsArgs a = {};
     a.x = dy; a.y = out;
