@@ -445,8 +445,8 @@ int co3_f8_activation_backward(const void* dy, int type, uint64_t rows, uint32_t
  *   y [device]       y_type elements, rows x outs (transposed: rows x ins), aligned to their size; must not overlap x, x8 or w8
  *   res [device]     nullable: one co3_result that the caller has cleared; its status becomes CO3_ERR_CUDA if a copy inside the
  *                    kernel never completed (y is undefined then), and is left alone otherwise
- * Products are exact and sums fp32; y is rounded once.  The same call gives the same bits.  ins == 0 (transposed: outs == 0)
- * is refused; rows == 0 or an empty y: nothing is done.
+ * Products are exact and sums fp32, in an order that depends on the sizes and y's type alone: the same call gives the same
+ * bits.  y is rounded once.  ins == 0 (transposed: outs == 0) is refused; rows == 0 or an empty y: nothing is done.
  */
 int co3_f8_linear(const void* x, int x_type, uint64_t x_row_stride, void* x8, size_t x8_bytes, const void* w8, size_t w8_bytes,
                   uint32_t outs, uint32_t ins, int transposed, const float* bias, void* y, int y_type, uint64_t y_row_stride,

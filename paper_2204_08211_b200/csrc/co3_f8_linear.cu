@@ -744,39 +744,21 @@ __global__ void __launch_bounds__(kF8Threads, 1) f8_few_kernel(const __grid_cons
     if (threadIdx.x == 0 && *failed && a.res) atomicExch(&a.res->status, CO3_ERR_CUDA);
 }
 
-// Multiprocessors, and how many clusters of 2, 4 and 8 blocks run at once, a block on each multiprocessor (74, 33 and 15 here: clusters
-// stay within a group of 16 to 20 multiprocessors).
-struct Device {
-    uint32_t at_once[4];  // clusters of 1, 2, 4, 8
-};
-int this_device(Device* out) {
-    static std::atomic<uint64_t> known[64];  // four times 16 bits
+// Clusters of 1, 2, 4 and 8 blocks that run at once, a block on each of 148 multiprocessors (clusters stay within a group of 16 to 20 of them).
+// What is chosen for a call follows from these numbers and its sizes, never from what a device or a part of one reports: the same call
+// gives the same bits everywhere.
+constexpr uint32_t kAtOnce[4] = {148, 74, 33, 15};
+
+int multiprocessors(uint32_t* out) {
+    static std::atomic<int> known[64];
     int dev = 0;
     CO3_CUDA(cudaGetDevice(&dev));
-    uint64_t v = dev < 64 ? known[dev].load(std::memory_order_relaxed) : 0;
-    if (v == 0) {
-        int n = 0;
+    int n = dev < 64 ? known[dev].load(std::memory_order_relaxed) : 0;
+    if (n == 0) {
         CO3_CUDA(cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev));
-        v = (uint64_t)(uint16_t)n;
-        auto* kernel = f8_linear_kernel<64, false, true>;
-        CO3_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Shape<64>::kSmem));
-        for (uint32_t i = 1; i < 4; ++i) {
-            cudaLaunchConfig_t cfg = {};
-            cfg.gridDim = dim3(1u << i);
-            cfg.blockDim = dim3(kF8Threads);
-            cfg.dynamicSmemBytes = Shape<64>::kSmem;
-            cudaLaunchAttribute attr[1];
-            attr[0].id = cudaLaunchAttributeClusterDimension;
-            attr[0].val.clusterDim.x = 1u << i;
-            attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-            cfg.attrs = attr;
-            cfg.numAttrs = 1;
-            CO3_CUDA(cudaOccupancyMaxActiveClusters(&n, kernel, &cfg));
-            v |= (uint64_t)(uint16_t)n << (16 * i);
-        }
-        if (dev < 64) known[dev].store(v, std::memory_order_relaxed);
+        if (dev < 64) known[dev].store(n, std::memory_order_relaxed);
     }
-    for (uint32_t i = 0; i < 4; ++i) out->at_once[i] = (uint32_t)(v >> (16 * i)) & 0xffffu;
+    *out = (uint32_t)n;
     return CO3_OK;
 }
 
@@ -807,30 +789,30 @@ int launch_clusters(const Args& a, uint32_t blocks, uint32_t cluster, cudaStream
     return CO3_OK;
 }
 template <int kN, bool kTransposed>
-int launch_linear(const LinearArgs& a, const Device& d, cudaStream_t st) {
+int launch_linear(const LinearArgs& a, uint32_t sms, cudaStream_t st) {
     const uint32_t tiles = a.m_tiles * a.n_tiles;
     if (a.split > 1) return launch_clusters<f8_linear_kernel<kN, kTransposed, true>, Shape<kN>::kSmem>(a, tiles * a.split, a.split, st);
-    return launch_clusters<f8_linear_kernel<kN, kTransposed, false>, Shape<kN>::kSmem>(a, std::min(tiles, d.at_once[0]), 1, st);
+    return launch_clusters<f8_linear_kernel<kN, kTransposed, false>, Shape<kN>::kSmem>(a, std::min(tiles, sms), 1, st);
 }
-int launch_pairs(LinearArgs a, uint32_t rows_of_tile, bool transposed, const Device& d, cudaStream_t st) {
+int launch_pairs(LinearArgs a, uint32_t rows_of_tile, bool transposed, uint32_t sms, cudaStream_t st) {
     a.pair_rows = rows_of_tile;
     a.n_tiles = (a.rows + rows_of_tile - 1) / rows_of_tile;
     const uint64_t tiles = (uint64_t)((a.m_tiles + 1) / 2) * a.n_tiles;
-    const uint32_t blocks = 2 * (uint32_t)std::min<uint64_t>(tiles, std::max(1u, d.at_once[1]));
+    const uint32_t blocks = 2 * (uint32_t)std::min<uint64_t>(tiles, std::max(1u, sms / 2));
     return transposed ? launch_clusters<f8_pair_kernel<true>, kPairSmem>(a, blocks, 2, st) : launch_clusters<f8_pair_kernel<false>, kPairSmem>(a, blocks, 2, st);
 }
 // Blocks that divide a tile's sum: as many as leave no cluster waiting (16 x 8192 x 4608: 51 us in two rounds of clusters, 21 in one), two
 // blocks of columns each at least.
-uint32_t split_of(uint64_t tiles, uint32_t kb, const Device& d) {
+uint32_t split_of(uint64_t tiles, uint32_t kb) {
     uint32_t split = 1;
-    for (uint32_t i = 1; i < 4 && tiles <= d.at_once[i] && kb >= (2u << i); ++i) split = 1u << i;
+    for (uint32_t i = 1; i < 4 && tiles <= kAtOnce[i] && kb >= (2u << i); ++i) split = 1u << i;
     return split;
 }
 template <int kN>
-int launch_tile(LinearArgs a, bool transposed, const Device& d, cudaStream_t st) {
+int launch_tile(LinearArgs a, bool transposed, uint32_t sms, cudaStream_t st) {
     a.n_tiles = (a.rows + kN - 1) / kN;
-    a.split = split_of((uint64_t)a.m_tiles * a.n_tiles, a.kb, d);
-    return transposed ? launch_linear<kN, true>(a, d, st) : launch_linear<kN, false>(a, d, st);
+    a.split = split_of((uint64_t)a.m_tiles * a.n_tiles, a.kb);
+    return transposed ? launch_linear<kN, true>(a, sms, st) : launch_linear<kN, false>(a, sms, st);
 }
 
 }  // namespace
@@ -854,8 +836,8 @@ int co3_f8_linear(const void* x, int x_type, uint64_t x_row_stride, void* x8, si
         return CO3_ERR_INVALID_ARG;
     if (x8_bytes < lx.bytes || w8_bytes < lw.bytes) return CO3_ERR_CAPACITY;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
-    Device d = {};
-    int e = this_device(&d);
+    uint32_t sms = 0;
+    int e = multiprocessors(&sms);
     if (e != CO3_OK) return e;
     const uint8_t *w = static_cast<const uint8_t*>(w8), *b = static_cast<const uint8_t*>(x8);
     LinearArgs a = {};
@@ -880,7 +862,7 @@ int co3_f8_linear(const void* x, int x_type, uint64_t x_row_stride, void* x8, si
     a.res = res;
     if (rows <= kFewRows) {
         // while a warp packs two rounds of rows at most; beyond, packing apart and the kernel below are faster (16 x 8192 x 2048: 30 and 20 us)
-        a.split = split_of(a.m_tiles, a.kb, d);
+        a.split = split_of(a.m_tiles, a.kb);
         const uint64_t own = (a.kb + a.split - 1) / a.split;
         if (own <= kFewBlocks && own * rows <= 64) {
             FewArgs f = {a, x, x_type, x_row_stride, from, 0, static_cast<uint8_t*>(x8), static_cast<uint8_t*>(x8) + lx.scales};
@@ -898,17 +880,17 @@ int co3_f8_linear(const void* x, int x_type, uint64_t x_row_stride, void* x8, si
     // 2048 x 2048 19.2 and 21.5 / 28 and 39, 1501 x 1023 x 1001 15.5 and 12.5 / 13.2 and 15.5, 3000 x 128 x 1000 12.2 and 12.5 / 11.6 and 10.4.
     auto single = [&](uint32_t n, uint32_t stage, uint32_t besides) {
         const uint64_t tiles = (uint64_t)a.m_tiles * ((rows + n - 1) / n);
-        const uint32_t split = split_of(tiles, a.kb, d);
-        return (split > 1 ? 1 : (tiles + d.at_once[0] - 1) / d.at_once[0]) * ((uint64_t)(a.kb + split - 1) / split * stage + besides + (split > 1 ? 1500 : 0));
+        const uint32_t split = split_of(tiles, a.kb);
+        return (split > 1 ? 1 : (tiles + kAtOnce[0] - 1) / kAtOnce[0]) * ((uint64_t)(a.kb + split - 1) / split * stage + besides + (split > 1 ? 1500 : 0));
     };
     auto by_pairs = [&](uint32_t n, uint32_t stage, uint32_t besides) {
-        const uint64_t pairs = (uint64_t)((a.m_tiles + 1) / 2) * ((rows + n - 1) / n), at_once = std::max(1u, d.at_once[1]);
-        return (pairs + at_once - 1) / at_once * ((uint64_t)a.kb * stage + besides);
+        const uint64_t pairs = (uint64_t)((a.m_tiles + 1) / 2) * ((rows + n - 1) / n);
+        return (pairs + kAtOnce[1] - 1) / kAtOnce[1] * ((uint64_t)a.kb * stage + besides);
     };
     const uint64_t ns[4] = {by_pairs(256, 370, 5500), by_pairs(128, 300, 3500), single(128, 470, 2500), single(64, 430, 1500)};
     const int best = (int)(std::min_element(ns, ns + 4) - ns);
-    if (best < 2) return launch_pairs(a, best == 0 ? 256 : 128, transposed != 0, d, st);
-    return best == 2 ? launch_tile<128>(a, transposed != 0, d, st) : launch_tile<64>(a, transposed != 0, d, st);
+    if (best < 2) return launch_pairs(a, best == 0 ? 256 : 128, transposed != 0, sms, st);
+    return best == 2 ? launch_tile<128>(a, transposed != 0, sms, st) : launch_tile<64>(a, transposed != 0, sms, st);
 }
 
 }  // extern "C"
