@@ -36,6 +36,8 @@ _lib = None
 _F32 = torch.float32
 _current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
     lambda device: torch.cuda.current_stream(device).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+_several_devices = True  # found out when the library is loaded: with one device, the current one needs no asking (0.1 us)
 
 
 def library_path() -> str:
@@ -43,7 +45,7 @@ def library_path() -> str:
 
 
 def _load():
-    global _lib
+    global _lib, _several_devices
     if _lib is not None:
         return _lib
     if not os.path.exists(_LIB_PATH):
@@ -93,6 +95,7 @@ def _load():
                  "co3_f8_weight_gradient_workspace_bytes", "co3_f8_weight_gradient", "co3_layer_norm", "co3_layer_norm_workspace_bytes", "co3_layer_norm_backward", "co3_ns_default", "co3_orthogonalize_workspace_bytes", "co3_orthogonalize", "co3_muon_update", "co3_histogram", "co3_convert_dither", "co3_histogram_dither", "co3_encode_dither", "co3_error_magnitude", "co3_model_weights", "co3_fit_scale", "co3_profile_enable", "co3_profile_read", "co3_convert_static", "co3_workspace_bytes", "co3_stream_capacity_bytes", "co3_convert", "co3_code_build", "co3_code_build_device", "co3_encode",
                  "co3_encode_symbols", "co3_decode_aggregate", "co3_decode_aggregate_update", "co3_decode"):
         getattr(L, name).restype = C.c_int
+    _several_devices = torch.cuda.device_count() > 1
     _lib = L
     return L
 
@@ -322,12 +325,16 @@ def co3_decode(stream_in, stream_bytes, fmts, codes, segs, n_seg, n_elem, ghat_o
 
 
 def _rows(t, like=None):
-    """(pointer, rows, cols, row stride) of a 2-D CUDA tensor whose rows are contiguous, of the shape and type of `like`."""
+    """(pointer, rows, cols, row stride) of a 2-D tensor of the current device whose rows are contiguous, of the shape and type of
+    `like`.  (Kernels run on the current device, and the default stream's handle is the same on all: nothing else would notice.)"""
     shape = t.shape
+    device = t.get_device()
+    if device < 0 or (_several_devices and device != _current_device()):
+        raise ValueError("expected a CUDA tensor of the current device")
     if like is None:
-        if not t.is_cuda or len(shape) != 2 or t.dtype not in _TYPES:
+        if len(shape) != 2 or t.dtype not in _TYPES:
             raise ValueError("expected a 2-D CUDA tensor of fp32, fp16 or bf16")
-    elif shape != like.shape or t.dtype is not like.dtype or not t.is_cuda:
+    elif shape != like.shape or t.dtype is not like.dtype:
         raise ValueError("expected tensors of one shape and type")
     rows, cols = shape
     rs, cs = t.stride()
@@ -341,12 +348,12 @@ def _stream_of(t, stream):
     return _current_stream(t.get_device()) if stream is None else _stream(stream)
 
 
-def _vec(t, n):
-    """Device pointer of n fp32 values (or None)."""
+def _vec(t, n, device=None):
+    """Device pointer of n fp32 values (or None), of this device if one is given."""
     if t is None:
         return None
-    if t.dtype is not _F32 or not t.is_cuda or t.numel() < n or not t.is_contiguous():
-        raise ValueError("expected a contiguous fp32 CUDA tensor of at least %d elements" % n)
+    if t.dtype is not _F32 or (not t.is_cuda if device is None else t.get_device() != device) or t.numel() < n or not t.is_contiguous():
+        raise ValueError("expected a contiguous fp32 CUDA tensor of at least %d elements%s" % (n, "" if device is None else ", of the same device"))
     return t.data_ptr()
 
 
@@ -469,21 +476,21 @@ def co3_f8_bytes(rows: int, cols: int, kind: int = F8_ROWS) -> int:
     return out.value
 
 
-def _f8(t):
+def _f8(t, device):
     """(pointer, bytes) of a buffer of 8-bit blocks."""
     if t is None:
         return None, 0
-    if t.dtype is not torch.uint8 or not t.is_cuda or not t.is_contiguous():
-        raise ValueError("expected a contiguous uint8 CUDA tensor of co3_f8_bytes bytes")
+    if t.dtype is not torch.uint8 or t.get_device() != device or not t.is_contiguous():
+        raise ValueError("expected a contiguous uint8 CUDA tensor of co3_f8_bytes bytes, of the same device")
     return t.data_ptr(), t.numel()
 
 
-def _res(t):
+def _res(t, device):
     """Device pointer of a co3_result (or None)."""
     if t is None:
         return None
-    if not t.is_cuda or not t.is_contiguous() or t.numel() * t.element_size() < RESULT_DTYPE.itemsize:
-        raise ValueError("expected a CUDA tensor that holds a co3_result")
+    if t.get_device() != device or not t.is_contiguous() or t.numel() * t.element_size() < RESULT_DTYPE.itemsize:
+        raise ValueError("expected a CUDA tensor that holds a co3_result, of the same device")
     return t.data_ptr()
 
 
@@ -492,8 +499,9 @@ def co3_f8_pack(x, out, kind: int = F8_ROWS, stream=None) -> int:
     p, rows, cols, xs = _rows(x)
     if rows > _F8_MOST or cols > _F8_MOST:
         _f8_sizes(rows, cols)
-    q, n = _f8(out)
-    return (_lib or _load()).co3_f8_pack(p, _TYPES[x.dtype], rows, cols, xs, kind, q, n, _stream_of(x, stream))
+    device = x.get_device()
+    q, n = _f8(out, device)
+    return (_lib or _load()).co3_f8_pack(p, _TYPES[x.dtype], rows, cols, xs, kind, q, n, _current_stream(device) if stream is None else _stream(stream))
 
 
 def co3_f8_unpack(f8, y, kind: int = F8_ROWS, stream=None) -> int:
@@ -501,8 +509,9 @@ def co3_f8_unpack(f8, y, kind: int = F8_ROWS, stream=None) -> int:
     p, rows, cols, ys = _rows(y)
     if rows > _F8_MOST or cols > _F8_MOST:
         _f8_sizes(rows, cols)
-    q, n = _f8(f8)
-    return (_lib or _load()).co3_f8_unpack(q, n, kind, p, _TYPES[y.dtype], rows, cols, ys, _stream_of(y, stream))
+    device = y.get_device()
+    q, n = _f8(f8, device)
+    return (_lib or _load()).co3_f8_unpack(q, n, kind, p, _TYPES[y.dtype], rows, cols, ys, _current_stream(device) if stream is None else _stream(stream))
 
 
 def co3_f8_activation(x, act: int, y=None, y8=None, x8=None, stream=None) -> int:
@@ -511,10 +520,12 @@ def co3_f8_activation(x, act: int, y=None, y8=None, x8=None, stream=None) -> int
     if rows > _F8_MOST or cols > _F8_MOST:
         _f8_sizes(rows, cols)
     py, ys = (None, 0) if y is None else _rows(y, x)[::3]
-    q, n = _f8(y8)
-    k, m = _f8(x8)
+    device = x.get_device()
+    q, n = _f8(y8, device)
+    k, m = _f8(x8, device)
     size = n if k is None else m if q is None else min(n, m)
-    return (_lib or _load()).co3_f8_activation(p, _TYPES[x.dtype], rows, cols, xs, act, py, ys, q, k, size, _stream_of(x, stream))
+    return (_lib or _load()).co3_f8_activation(p, _TYPES[x.dtype], rows, cols, xs, act, py, ys, q, k, size,
+                                               _current_stream(device) if stream is None else _stream(stream))
 
 
 def co3_f8_activation_backward(dy, x8, act: int, dx, stream=None) -> int:
@@ -523,8 +534,10 @@ def co3_f8_activation_backward(dy, x8, act: int, dx, stream=None) -> int:
     if rows > _F8_MOST or cols > _F8_MOST:
         _f8_sizes(rows, cols)
     po, _, _, os_ = _rows(dx, dy)
-    k, n = _f8(x8)
-    return (_lib or _load()).co3_f8_activation_backward(p, _TYPES[dy.dtype], rows, cols, ds, k, n, act, po, os_, _stream_of(dy, stream))
+    device = dy.get_device()
+    k, n = _f8(x8, device)
+    return (_lib or _load()).co3_f8_activation_backward(p, _TYPES[dy.dtype], rows, cols, ds, k, n, act, po, os_,
+                                                        _current_stream(device) if stream is None else _stream(stream))
 
 
 def co3_f8_linear(x, x8, w8, bias, y, transposed: bool = False, cols: int | None = None, res=None, stream=None) -> int:
@@ -545,11 +558,12 @@ def co3_f8_linear(x, x8, w8, bias, y, transposed: bool = False, cols: int | None
         raise ValueError("co3_f8_linear: x and y have different rows")
     if rows > _F8_MOST or to > _F8_MOST or not 0 <= cols <= _F8_MOST:
         _f8_sizes(rows, to, cols)
-    q, n = _f8(x8)
-    w, m = _f8(w8)
+    device = y.get_device()
+    q, n = _f8(x8, device)
+    w, m = _f8(w8, device)
     outs, ins = (cols, to) if transposed else (to, cols)
-    return (_lib or _load()).co3_f8_linear(px, type_, xs, q, n, w, m, outs, ins, 1 if transposed else 0, _vec(bias, to), py, _TYPES[y.dtype], ys,
-                                           rows, _res(res), _stream_of(y, stream))
+    return (_lib or _load()).co3_f8_linear(px, type_, xs, q, n, w, m, outs, ins, 1 if transposed else 0, _vec(bias, to, device), py, _TYPES[y.dtype], ys,
+                                           rows, _res(res, device), _current_stream(device) if stream is None else _stream(stream))
 
 
 def co3_f8_weight_gradient_workspace_bytes(rows: int, outs: int, ins: int, n_clients: int = 1) -> int:
@@ -572,12 +586,15 @@ def co3_f8_weight_gradient(dy, x8, ins: int, dw, db, n_clients: int, client_stri
     if client_stride_elems < 0:  # the library takes it as unsigned
         raise ValueError("co3_f8_weight_gradient: clients' vectors that lie backwards")
     _f8_sizes(rows, outs, ins, n_clients)
-    q, n = _f8(x8)
+    device = dy.get_device()
+    q, n = _f8(x8, device)
+    if workspace.get_device() != device or not workspace.is_contiguous():
+        raise ValueError("co3_f8_weight_gradient: expected a contiguous workspace on the same device")
     before = (n_clients - 1) * client_stride_elems
     return (_lib or _load()).co3_f8_weight_gradient(
-        p, _TYPES[dy.dtype], ds, q, n, rows // n_clients, outs, ins, _vec(dw, before + outs * ins), _vec(db, before + outs), n_clients,
-        client_stride_elems, 1 if accumulate else 0, _dev(workspace), workspace.numel() * workspace.element_size(), _res(res),
-        _stream_of(dy, stream))
+        p, _TYPES[dy.dtype], ds, q, n, rows // n_clients, outs, ins, _vec(dw, before + outs * ins, device), _vec(db, before + outs, device), n_clients,
+        client_stride_elems, 1 if accumulate else 0, workspace.data_ptr(), workspace.numel() * workspace.element_size(), _res(res, device),
+        _current_stream(device) if stream is None else _stream(stream))
 
 
 KERNEL_NAMES = ("prepare", "convert", "pack", "scan", "compact", "code_build", "decode", "fit", "clear")
