@@ -455,7 +455,7 @@ __global__ void __launch_bounds__(kWarps * 32, kBlocks<kAct>) f8_values_kernel(c
 #pragma unroll
         for (int r = 0; r < kRowsAtOnce<T, kAct>; ++r) {
             const bool valid = r0 + r < rows;
-            in[r].word = valid ? __ldg(reinterpret_cast<const uint32_t*>(a.x8 + u.word + (r0 + r) * 16u)) : 0x7f7f7f7fu;
+            in[r].word = valid ? *reinterpret_cast<const uint32_t*>(a.x8 + u.word + (r0 + r) * 16u) : 0x7f7f7f7fu;
 #pragma unroll
             for (int h = 0; h < L::kChunks; ++h) {
                 in[r].f8[h] = L::get(a.x8 + u.bytes(r0 + r, h), valid && u.has(h));

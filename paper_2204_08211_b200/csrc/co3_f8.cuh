@@ -22,6 +22,8 @@
 
 namespace co3 {
 
+// All of these kernels are launched behind the one before them, which may still be writing what they will read once it has completed: they
+// use ordinary loads, not those for what is never written while a kernel runs.
 constexpr uint32_t kF8Block = 128;
 constexpr uint32_t kF8Tile = 128 * 128;        // bytes of 128 rows of a block of columns
 constexpr uint32_t kF8Scales = 512;            // bytes of a tile of exponent bytes

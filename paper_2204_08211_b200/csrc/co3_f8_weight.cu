@@ -89,7 +89,7 @@ __device__ __forceinline__ void bring_x(const WeightArgs& a, uint32_t u, uint32_
         const uint64_t row = row0 + i;
         if (i < rows) {
             x = __ldcs(reinterpret_cast<const uint4*>(a.x + f8_row(a.x_rows, kt, row) + ((threadIdx.x & 7u) << 4)));
-            s = __uint_as_float((uint32_t)__ldg(a.x_scales + ((kt >> 2) * (a.x_rows >> 7) + (row >> 7)) * kF8Scales + f8_scale_at((uint32_t)row & 127u, kt)) << 23);
+            s = __uint_as_float((uint32_t)a.x_scales[((kt >> 2) * (a.x_rows >> 7) + (row >> 7)) * kF8Scales + f8_scale_at((uint32_t)row & 127u, kt)] << 23);
         }
         const uint32_t piece = (threadIdx.x & 7u) ^ ((uint32_t)row & 7u);  // columns 16 piece ..
         const uint32_t q[4] = {x.x, x.y, x.z, x.w};
@@ -552,8 +552,8 @@ __global__ void __launch_bounds__(256) f8_weight_small_kernel(const __grid_const
         s = 1.0f;
         const uint64_t row = row0 + r0 + xr;
         if (a.dw && r0 + xr < a.rows) {
-            x = __ldg(reinterpret_cast<const uint4*>(a.x + f8_row(a.x_rows, kt, row) + f8_piece((uint32_t)row & 7u, xp)));
-            s = __uint_as_float((uint32_t)__ldg(a.x_scales + ((kt >> 2) * (a.x_rows >> 7) + (row >> 7)) * kF8Scales + f8_scale_at((uint32_t)row & 127u, kt)) << 23);
+            x = *reinterpret_cast<const uint4*>(a.x + f8_row(a.x_rows, kt, row) + f8_piece((uint32_t)row & 7u, xp));
+            s = __uint_as_float((uint32_t)a.x_scales[((kt >> 2) * (a.x_rows >> 7) + (row >> 7)) * kF8Scales + f8_scale_at((uint32_t)row & 127u, kt)] << 23);
         }
 #pragma unroll
         for (uint32_t j = 0; j < 4; ++j) {
