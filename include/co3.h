@@ -422,8 +422,9 @@ int co3_f8_unpack(const void* in, size_t in_bytes, int kind, void* y, int type, 
  *     y = act(x);   y8 = y in blocks (the next layer's operand);   x8 = x in blocks;   dx = dy * act'(values of x8)
  *   act              CO3_ACT_NONE (x), CO3_ACT_RELU (max(x, 0), slope 0 at 0), CO3_ACT_GELU (x Phi(x), Phi the normal distribution
  *                    function), CO3_ACT_SILU (x / (1 + exp(-x)))
- *   y, y8, x8        each nullable, not all; y may be x (another stride is refused); y8 holds act(x) as fp32 arithmetic gives
- *                    it, before it is rounded to `type`; both of CO3_F8_ROWS and of at least f8_bytes bytes, apart from one another
+ *   y, y8, x8        each nullable, not all; y may be x (another stride is refused); y8 holds act(x) before it is rounded to
+ *                    `type`, GELU and SiLU within 2^-15 of it where |x| <= 10 (for 16-bit x shorter forms are used, good to the
+ *                    rounding of y); both of CO3_F8_ROWS and of at least f8_bytes bytes, apart from one another
  *   dx               may be dy (another stride is refused)
  */
 #define CO3_ACT_NONE 0
