@@ -448,6 +448,7 @@ int co3_f8_activation_backward(const void* dy, int type, uint64_t rows, uint32_t
  *                    kernel never completed (y is undefined then), and is left alone otherwise
  * Products are exact and sums fp32, in an order that depends on the sizes and y's type alone: the same call gives the same
  * bits.  y is rounded once.  ins == 0 (transposed: outs == 0) is refused; rows == 0 or an empty y: nothing is done.
+ * ceil(columns of y / 128) * ceil(rows / 16) is below 2^30.
  */
 int co3_f8_linear(const void* x, int x_type, uint64_t x_row_stride, void* x8, size_t x8_bytes, const void* w8, size_t w8_bytes,
                   uint32_t outs, uint32_t ins, int transposed, const float* bias, void* y, int y_type, uint64_t y_row_stride,
@@ -467,8 +468,9 @@ int co3_f8_weight_gradient_workspace_bytes(uint64_t rows, uint32_t outs, uint32_
  *                    can be layers of the gradient vectors that co3_encode reads; added to what is there if `accumulate` is not
  *                    0.  No rows: zeros (or nothing, if accumulating)
  *   res              as above
- * dy is used to the last bit (of fp32 values below 2^-102 the last bits may be lost), products are exact, sums are fp32 in an order that depends on the sizes alone: the same call
- * gives the same bits.
+ * dy is used to the last bit (of fp32 values below 2^-102 the last bits may be lost), products are exact, sums are fp32 in an
+ * order that depends on the sizes and dy's type alone: the same call gives the same bits.  n_clients * rows, outs and ins
+ * are below 2^31, n_clients * outs * ins below 2^40, n_clients * ceil(rows / 64) * ceil(max(outs, ins) / 128) below 2^24.
  */
 int co3_f8_weight_gradient(const void* dy, int type, uint64_t dy_row_stride, const void* x8, size_t x8_bytes, uint64_t rows,
                            uint32_t outs, uint32_t ins, float* dw, float* db, uint32_t n_clients, uint64_t client_stride_elems,

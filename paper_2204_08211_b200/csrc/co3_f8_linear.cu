@@ -24,7 +24,10 @@ constexpr uint32_t kMaxSplit = 8;
 constexpr uint32_t kTmemScales = 256;        // first column of the exponent bytes; eight turns of 16 columns
 constexpr uint32_t kScaleTurns = 8, kScaleCols = 16;
 // The tensor core cuts what it adds towards zero, about 2^-25 of the sum each time: a sum is taken out and added up in registers,
-// to nearest, after so many blocks.  Results of 16 bits round by 2^-12 and more.
+// to nearest, after so many blocks.  Results of 16 bits round by 2^-12 and more.  For fp32 results, us and error relative to the
+// result's norm after 8, 4 and 2 blocks (fp32 products in PyTorch): 6400 x 512 x 512 14.3, 14.2, 15.0 and 3.3, 3.3, 2.5e-8 (2.6);
+// 2048 x 2048 x 2048 23.7, 25.2, 28.3 and 6.5, 5.0, 4.8e-8 (5.9); 16384 x 4096 x 4096 291, 324, 401 and 7.2, 6.2, 6.5e-8 (8.5).  Beside
+// the 2^-4 by which operands of 8 bits are off none of it counts: 8.
 constexpr uint32_t kBlocksF32 = 8, kBlocks16 = 32;
 
 struct LinearArgs {
