@@ -1,4 +1,4 @@
-"""Replays of a captured product one by one, and values of the activation beyond 32-bit offsets."""
+"""Replays of a captured product one by one, forks and joins of streams, and values of the activation beyond 32-bit offsets."""
 import math
 
 import pytest
@@ -67,3 +67,46 @@ def test_activation_beyond_32_bit_offsets():
         assert torch.equal(x[e], torch.where(v > 0, k, torch.zeros_like(k))) and torch.equal(x[e], dx)
         assert (x[e] > 0).float().mean() > 0.4
     assert (y[tail:-tail] == 0).all() and (x[tail:-tail] == 0).all()
+
+
+@pytest.mark.parametrize("rows", [4, 300, 3000])
+def test_forks_and_joins(rows):
+    """Weights packed on one stream, the product on another that waits for it, the weight gradient on the first again: plain and captured."""
+    ins, outs = 512, 1024
+    gen = torch.Generator(device="cuda").manual_seed(rows)
+    x, w, dy = (torch.randn(*s, generator=gen, device="cuda") for s in ((rows, ins), (outs, ins), (rows, outs)))
+    x2, w2, dy2 = (torch.empty_like(t) for t in (x, w, dy))
+    x8, w8 = (torch.empty(co3.co3_f8_bytes(*s), dtype=torch.uint8, device="cuda") for s in ((rows, ins), (outs, ins, co3.F8_SQUARE)))
+    y, g = torch.empty(rows, outs, device="cuda"), torch.zeros(outs * ins + outs, device="cuda")
+    ws = torch.empty(co3.co3_f8_weight_gradient_workspace_bytes(rows, outs, ins), dtype=torch.uint8, device="cuda")
+    side = torch.cuda.Stream()
+
+    def step():
+        main = torch.cuda.current_stream()
+        side.wait_stream(main)
+        with torch.cuda.stream(side):
+            w2.copy_(w * 2)
+            assert co3.co3_f8_pack(w2, w8, co3.F8_SQUARE) == co3.OK
+            dy2.copy_(dy)
+        x2.copy_(x)
+        main.wait_stream(side)
+        assert co3.co3_f8_linear(x2, x8, w8, None, y) == co3.OK
+        side.wait_stream(main)
+        with torch.cuda.stream(side):
+            assert co3.co3_f8_weight_gradient(dy2, x8, ins, g, g[outs * ins:], 1, 0, ws) == co3.OK
+        main.wait_stream(side)
+
+    # one after the other on one stream
+    assert co3.co3_f8_pack(w * 2, w8, co3.F8_SQUARE) == co3.OK and co3.co3_f8_linear(x, x8, w8, None, y) == co3.OK
+    assert co3.co3_f8_weight_gradient(dy, x8, ins, g, g[outs * ins:], 1, 0, ws) == co3.OK
+    torch.cuda.synchronize()
+    want = [t.clone() for t in (y, g)]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for run in (graph.replay, step) * 10:
+        for t in (y, g, w8, x8):
+            t.zero_()
+        run()
+        torch.cuda.synchronize()
+        assert torch.equal(y, want[0]) and torch.equal(g, want[1])
